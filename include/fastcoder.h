@@ -502,6 +502,147 @@ fc_status fc_tree_attention_ws(const uint16_t* q, const uint16_t* k_tree, const 
                                void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Paged cache                                                               */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The target model's key/value cache between two verified drafts (Section
+ * IV-D), for many sequences of any length: pages of FC_PAGE_TOKENS tokens from
+ * one pool, keys and values held in 4 bits.
+ *
+ * pool [n_pages][Hkv][FC_PAGE_HEAD_BYTES] bytes (one per layer), 16-byte
+ * aligned.  The 8,704 bytes of a (page, key head) are 64 x 64 bytes of key
+ * codes (token by token, two dims a byte, the even one in the low half), as
+ * many of value codes, 256 bytes of key scales and 256 of value scales.  A code
+ * is a sign (8) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6; each 32 dims of a token
+ * share the scale 2^(byte - 127), the smallest power of two of which no
+ * magnitude exceeds seven, within [2^-125, 2^125].  Codes are the nearest ones,
+ * ties to the even code.  Larger magnitudes saturate.  A group that held an
+ * infinity or a NaN has the byte 255 and reads as NaN.  Group g of token t has
+ * its key scale at (g * 16 + t % 16) * 4 + t / 16 of the key scales and its
+ * value scale at ((t % 16) * 4 + g) * 4 + t / 16 of the value scales.  Keys are
+ * held rotated by their positions.  A pool's bytes before the first write do
+ * not matter.
+ *
+ * Token t of sequence b lies at row t % 64 of page table[b][t / 64]; its slot
+ * is page * 64 + t % 64.  The same table, slots and positions serve every
+ * layer's pool.  1 <= n_pages <= 2^25 - 1.
+ */
+#define FC_PAGE_TOKENS 64
+#define FC_PAGE_HEAD_BYTES 8704
+
+/* Bytes of one layer's pool (0 for sizes out of range). */
+size_t fc_paged_pool_bytes(int32_t n_pages, int32_t Hkv);
+
+/*
+ * Block tables, free pages and slot maps of a step, from lengths that may
+ * themselves be results on the device (add = accept_len of fc_verify_accept).
+ *
+ * len, add [B]      : cached tokens, and how many each sequence gains.  Below 0
+ *                     it loses as many of its last ones (all of them: it ends).
+ * table [B][max_pages] : page of each 64 tokens; the entries of new pages are
+ *                     written, no others.
+ * queue [n_pages], ends [2] : the free pages, a ring: entries ends[0] ..
+ *                     ends[1] - 1, each at its number modulo n_pages (0 <=
+ *                     ends[0] <= ends[1]).  New pages are taken at ends[0] in
+ *                     the order of the sequences; pages given back are written
+ *                     at ends[1], in the same order.  ends_out receives the
+ *                     new ends.
+ * len_out [B]       : the new lengths.
+ * cu [B + 1]        : first token of each sequence among the step's tokens
+ *                     (exclusive sums of max(add, 0)), and their total.
+ * slot, pos, src [n_slots] : of each token its slot, its position and the row
+ *                     it comes from; -1 behind the last token.
+ * src is the token's own number or, with mask [B][R][R] and last_node [B] (a
+ * step of draft trees: both or neither; R is not read otherwise), row b * R + j
+ * with j the t-th row that row last_node[b] may see (its path from the root, as
+ * parents come before children); -1 past the last such row.
+ *
+ * A sequence is refused - it keeps its length, its tokens' slots are -1 - if
+ * its new length needs more than max_pages pages, if its tokens end past
+ * n_slots, or if the new pages of the sequences up to it (refused ones of this
+ * last kind included) are more than the ring holds: so with too few pages the
+ * first sequences are served and len_out tells which.  Pages given back in a
+ * call are free from the next one on.
+ *
+ * len is clamped to [0, 64 max_pages].  A slot whose table entry lies outside
+ * the pool is -1.  The same inputs give the same results however often the
+ * call is repeated: nothing that it reads is written, so len_out and ends_out
+ * must not be len and ends (FC_ERR_INVALID).  0 <= B <= 65536, 1 <= R <=
+ * FC_MAX_TREE_ROWS, 0 <= n_slots < 2^30, max_pages >= 1, 64 max_pages < 2^31.
+ */
+fc_status fc_paged_plan(const int32_t* len, const int32_t* add, const int32_t* mask, const int32_t* last_node,
+                        int32_t B, int32_t R, int32_t n_slots, int32_t* table, int32_t max_pages, int32_t* queue,
+                        int32_t n_pages, const int64_t* ends, int32_t* len_out, int32_t* cu, int32_t* slot,
+                        int32_t* pos, int32_t* src, int64_t* ends_out, hipStream_t stream);
+
+/*
+ * Rounds rows of keys and values to 4 bits and places them: row src[i] of k and
+ * v (row i without src) goes to slot[i] of the pool, its keys rotated by
+ * position pos[i] first (rotate-half form, as fc_tree_attention rotates; in
+ * double precision, then rounded to fp32).  rope_base 0: the keys are rotated
+ * already and pos is not read.  k, v: bf16 [n_src][Hkv][D], rows k_stride and
+ * v_stride elements apart (multiples of 8, at least Hkv * D; slices of a fused
+ * projection need no copy), 16-byte aligned.  An entry with a slot outside the
+ * pool or a row outside [0, n_src) is skipped.  The slots of one call must
+ * differ from each other.  D must be FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED
+ * otherwise); rope_base is 0 or above 1; Hkv <= 1024.
+ */
+fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k, int64_t k_stride,
+                         const uint16_t* v, int64_t v_stride, int32_t n_src, const int32_t* slot, const int32_t* pos,
+                         const int32_t* src, int32_t n, float rope_base, hipStream_t stream);
+
+/*
+ * Rows of the pool as bf16 (exact: every held value is one): k and v
+ * [n][Hkv][D], 16-byte aligned, receive the keys (rotated, as held) and values
+ * of slot[i].  Rows of entries with a slot outside the pool are left as they
+ * were.
+ */
+fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot, int32_t n,
+                        uint16_t* k, uint16_t* v, hipStream_t stream);
+
+/*
+ * fc_tree_attention over the paged cache: row i of tree b sits at position
+ * prefix_len[b] + pos_ids[b][i] and attends to the prefix_len[b] cached tokens
+ * of its table row and to the tree rows j < num_nodes[b] with mask[b][i][j] =
+ * 1, whose keys and values are given in bf16.  One row per tree is the decoding
+ * step of a single token.
+ *
+ * q [B * R][H][D], k_tree, v_tree [B * R][Hkv][D] bf16, rows q_stride,
+ * k_stride and v_stride elements apart (multiples of 8, at least the row's
+ * length), 16-byte aligned; query head h reads key head h / (H / Hkv).
+ * num_nodes [B] (NULL: R), pos_ids [B][R] (NULL: row i has i), mask [B][R][R]
+ * (NULL: row i sees the rows up to i).  prefix_len and num_nodes are clamped to
+ * [0, max_len] and [0, R]; max_len <= 64 max_pages is what the host knows of
+ * the longest prefix, and sizes the launch and the workspace.  Table entries of
+ * a prefix that lie outside the pool count as absent keys.  rope_base 0:
+ * queries and keys are rotated already.  out [B][R][H][D] bf16, 16-byte
+ * aligned; rows at or past num_nodes[b], and rows that may attend to nothing,
+ * are 0.
+ *
+ * Rotated and scaled queries meet the cached keys as the sum of three 6-bit
+ * parts (together within 2^-13 of the largest of each 32 dims), and the tree's
+ * rotated keys, rounded to bf16, as the sum of two bf16 ones; softmax weights
+ * are rounded to bf16, sums are fp32.  What is not finite among the keys and
+ * values that a row attends to, or in its query, shows in its result (a NaN, an
+ * infinity among values too); absent, masked and later tokens do not count,
+ * whatever they hold.
+ *
+ * ws holds fc_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (may
+ * be NULL where that is 0); its contents on entry do not matter.  How a prefix
+ * is cut into parts depends on the sizes and its own length; the same call gives
+ * the same bits every time.  1 <= R <= FC_MAX_TREE_ROWS, H % Hkv == 0, D =
+ * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
+ */
+size_t fc_paged_attention_workspace_bytes(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len);
+fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,
+                             const uint16_t* v_tree, int64_t v_stride, const uint8_t* pool, int32_t n_pages,
+                             const int32_t* table, int32_t max_pages, const int32_t* prefix_len,
+                             const int32_t* num_nodes, const int32_t* mask, const int32_t* pos_ids, int32_t B,
+                             int32_t R, int32_t H, int32_t Hkv, int32_t D, int32_t max_len, float rope_base,
+                             uint16_t* out, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Decode-trace replay                                                       */
 /* ------------------------------------------------------------------------ */
 

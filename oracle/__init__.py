@@ -434,3 +434,187 @@ def tree_attention(q, k_tree, v_tree, k_cache, v_cache, prefix_len, num_nodes, m
                 w = np.exp(s - s.max())
                 out[b, i, h] = (w / w.sum()) @ vals[allowed]
     return out
+
+
+# ------------------------------------------------------------ paged cache --
+
+PAGE_TOKENS, PAGE_BYTES = 64, 8704
+_E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6], np.float64)
+
+
+def fp4_round(x: np.ndarray):
+    """Codes (uint8, 0..15) and scale bytes of rows [..., D] in groups of 32:
+    the scale 2^(byte - 127) is the smallest power of two in [2^-125, 2^125] of
+    which no magnitude of the group exceeds seven; a code is the nearest value
+    of {0, 0.5, 1, 1.5, 2, 3, 4, 6} with the sign in bit 3, ties to the even
+    code; a group with something not finite has the byte 255 and code 0."""
+    x = np.asarray(x, np.float64)
+    y = x.reshape(x.shape[:-1] + (-1, 32))
+    finite = np.isfinite(y).all(-1)
+    top = np.where(finite, np.abs(np.where(np.isfinite(y), y, 0)).max(-1), 0.0)
+    e = np.full(top.shape, -125)
+    for k in range(-125, 125):  # one more while seven times the power is too small
+        e = np.where(top > 7 * 2.0 ** k, k + 1, e)
+    a = np.where(finite[..., None], np.abs(y), 0) / 2.0 ** e[..., None]
+    far = np.abs(a[..., None] - _E2M1)
+    best = far.min(-1)
+    code = np.full(a.shape, 255, np.int64)
+    for c in (1, 3, 5, 7, 0, 2, 4, 6):  # even codes last: they win ties
+        code = np.where(far[..., c] == best, c, code)
+    code = np.where(finite[..., None], code + 8 * np.signbit(y), 0).astype(np.uint8)
+    return code.reshape(x.shape), np.where(finite, e + 127, 255).astype(np.uint8)
+
+
+def fp4_value(code: np.ndarray, scale: np.ndarray) -> np.ndarray:
+    """What codes [..., D] with scale bytes [..., D / 32] stand for (float64)."""
+    v = np.where(code & 8, -1.0, 1.0) * _E2M1[code & 7]
+    s = np.where(scale == 255, np.nan, 2.0 ** (scale.astype(np.float64) - 127))
+    return v * np.repeat(s, 32, axis=-1)
+
+
+def page_of(k_code, k_scale, v_code, v_scale) -> np.ndarray:
+    """The bytes of a page: codes [64][128] and scale bytes [64][4] of keys and values."""
+    page = np.zeros(PAGE_BYTES, np.uint8)
+    for i, (c, s) in enumerate(((k_code, k_scale), (v_code, v_scale))):
+        page[4096 * i:4096 * (i + 1)] = (c[:, 0::2] | (c[:, 1::2] << 4)).reshape(-1)
+        for t in range(64):
+            for g in range(4):
+                at = (g * 16 + t % 16) * 4 + t // 16 if i == 0 else (t % 16 * 4 + g) * 4 + t // 16
+                page[8192 + 256 * i + at] = s[t, g]
+    return page
+
+
+def page_parts(page: np.ndarray):
+    """k_code, k_scale, v_code, v_scale of a page's bytes: page_of backwards."""
+    out = []
+    for i in (0, 1):
+        b = page[4096 * i:4096 * (i + 1)].reshape(64, 64)
+        code = np.stack([b & 15, b >> 4], -1).reshape(64, 128)
+        s = page[8192 + 256 * i:8192 + 256 * (i + 1)]
+        t, g = np.arange(64)[:, None], np.arange(4)[None]
+        out += [code, s[(g * 16 + t % 16) * 4 + t // 16 if i == 0 else (t % 16 * 4 + g) * 4 + t // 16]]
+    return out
+
+
+def paged_write(pool: np.ndarray, k, v, slot, pos=None, src=None, rope_base: float = 10000.0) -> np.ndarray:
+    """The pool [n_pages][Hkv][8704] after rows of k and v [n_src][Hkv][128] are
+    rotated (rope_base 0: not), rounded to float32, then to 4 bits, and placed."""
+    pool = pool.copy()
+    n_pages, Hkv = pool.shape[:2]
+    for i, sl in enumerate(np.asarray(slot)):
+        r = i if src is None else int(src[i])
+        if sl < 0 or sl >= 64 * n_pages or r < 0 or r >= len(k):
+            continue
+        kk = np.asarray(k[r], np.float64)
+        if rope_base:
+            kk = rope(kk, np.full(Hkv, pos[i]), rope_base).astype(np.float32).astype(np.float64)
+        kc, ks = fp4_round(kk)
+        vc, vs = fp4_round(v[r])
+        for h in range(Hkv):
+            parts = page_parts(pool[sl // 64, h])
+            for part, row in zip(parts, (kc[h], ks[h], vc[h], vs[h])):
+                part[sl % 64] = row
+            pool[sl // 64, h] = page_of(*parts)
+    return pool
+
+
+def paged_rows(pool: np.ndarray, table, n: int):
+    """Keys and values (float64 [n][Hkv][128]) of the first n tokens of a table
+    row, and which of them are there (a page outside the pool holds none)."""
+    n_pages, Hkv = pool.shape[:2]
+    k, v = np.zeros((n, Hkv, 128)), np.zeros((n, Hkv, 128))
+    there = np.zeros(n, bool)
+    for p in range((n + 63) // 64):
+        a, b = 64 * p, min(64 * p + 64, n)
+        if not 0 <= table[p] < n_pages:
+            continue
+        there[a:b] = True
+        for h in range(Hkv):
+            kc, ks, vc, vs = page_parts(pool[table[p], h])
+            k[a:b, h], v[a:b, h] = fp4_value(kc, ks)[:b - a], fp4_value(vc, vs)[:b - a]
+    return k, v, there
+
+
+def paged_plan(length, add, table, queue, ends, n_slots: int, mask=None, last_node=None) -> dict:
+    """A step's plan, one sequence after another: see fc_paged_plan."""
+    table, queue = table.copy(), queue.copy()
+    B, max_pages = table.shape
+    n_pages = len(queue)
+    head, tail = int(ends[0]), int(ends[1])
+    avail = tail - head
+    out = dict(len=np.zeros(B, np.int32), cu=np.zeros(B + 1, np.int32), slot=np.full(n_slots, -1, np.int32),
+               pos=np.full(n_slots, -1, np.int32), src=np.full(n_slots, -1, np.int32))
+    asked = given = back = at = 0
+    pages_of = lambda n: -(-n // 64)  # noqa: E731
+    for b in range(B):
+        n = min(max(int(length[b]), 0), 64 * max_pages)
+        want = max(int(add[b]), 0)
+        new = max(n + int(add[b]), 0)
+        out["cu"][b] = at
+        if add[b] < 0:
+            for p in range(pages_of(new), pages_of(n)):
+                queue[(tail + back) % n_pages] = table[b, p]
+                back += 1
+        ok = True
+        if want:
+            need = pages_of(new) - pages_of(n)
+            ok = pages_of(new) <= max_pages and at + want <= n_slots
+            if ok and need:
+                ok = asked + need <= avail
+                first = asked
+                asked += need
+                if ok:
+                    given = asked
+                    for p in range(need):
+                        table[b, pages_of(n) + p] = queue[(head + first + p) % n_pages]
+            if ok:
+                rows = None if mask is None else (
+                    np.flatnonzero(mask[b, last_node[b]] == 1) if 0 <= last_node[b] < mask.shape[1] else [])
+                for t in range(want):
+                    page = int(table[b, (n + t) // 64])
+                    out["slot"][at + t] = page * 64 + (n + t) % 64 if 0 <= page < n_pages else -1
+                    out["pos"][at + t] = n + t
+                    out["src"][at + t] = at + t if rows is None else (
+                        b * mask.shape[1] + rows[t] if t < len(rows) else -1)
+        out["len"][b] = new if ok else n
+        at += want
+    out["cu"][B] = min(at, 2 ** 31 - 1)
+    return dict(out, ends=np.array([head + given, tail + back], np.int64), table=table, queue=queue)
+
+
+def paged_attention(q, k_tree, v_tree, pool, table, prefix_len, num_nodes=None, mask=None, pos_ids=None,
+                    max_len=None, rope_base: float = 10000.0):
+    """tree_attention over the paged cache (float64).  Returns the result, the
+    weighted mean of |v| and, per row and head, the sums of |q_d k_d| / sqrt(D)
+    that bound a score's rounding: over each 32 cached dims with q's largest in
+    place of q_d, and over the tree's keys."""
+    q, k_tree, v_tree = (np.asarray(x, np.float64) for x in (q, k_tree, v_tree))
+    B, R, H, D = q.shape
+    Hkv = k_tree.shape[2]
+    out, mean = np.zeros((B, R, H, D)), np.zeros((B, R, H, D))
+    far = np.zeros((2, B, R, H))
+    for b in range(B):
+        P = min(max(int(prefix_len[b]), 0), 64 * np.shape(table)[1] if max_len is None else max_len)
+        n = R if num_nodes is None else min(max(int(num_nodes[b]), 0), R)
+        pos = P + (np.arange(R) if pos_ids is None else np.asarray(pos_ids[b]).astype(np.int64))
+        kc, vc, there = paged_rows(pool, table[b], P)
+        for h in range(H):
+            g = h // (H // Hkv)
+            qh = rope(q[b, :, h], pos, rope_base) if rope_base else q[b, :, h]
+            kt = rope(k_tree[b, :, g], pos, rope_base) if rope_base else k_tree[b, :, g]
+            top = np.repeat(np.abs(qh).reshape(R, 4, 32).max(-1), 32, axis=-1)
+            for i in range(n):
+                own = np.arange(R) <= i if mask is None else np.asarray(mask[b][i]) == 1
+                own = own & (np.arange(R) < n)
+                keys = np.concatenate([kc[there, g], kt[own]])
+                vals = np.concatenate([vc[there, g], v_tree[b, own, g]])
+                if not len(keys):
+                    continue
+                with np.errstate(invalid="ignore", over="ignore"):
+                    s = keys @ qh[i] / np.sqrt(D)
+                    w = np.exp(s - s.max())
+                    w /= w.sum()
+                    out[b, i, h], mean[b, i, h] = w @ vals, w @ np.abs(vals)
+                far[0, b, i, h] = (np.abs(kc[there, g]) @ top[i] / np.sqrt(D)).max(initial=0.0)
+                far[1, b, i, h] = (np.abs(kt[own]) @ np.abs(qh[i]) / np.sqrt(D)).max(initial=0.0)
+    return out, mean, far

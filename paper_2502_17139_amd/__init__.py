@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 
 import numpy as np
@@ -26,6 +27,8 @@ FC_MAX_TREE_ROWS = 256
 FC_BUCKETS = 65537
 FC_MAX_CACHE_TOKENS = 16384
 FC_TREE_ATTN_HEAD_DIM = 128
+FC_PAGE_TOKENS = 64
+FC_PAGE_HEAD_BYTES = 8704
 
 FC_ERR_WORKSPACE = 2
 STATUS = {0: "FC_OK", 1: "FC_ERR_INVALID", 2: "FC_ERR_WORKSPACE", 3: "FC_ERR_DEVICE", 4: "FC_ERR_UNSUPPORTED"}
@@ -41,6 +44,8 @@ EXPORTS = (
     "fc_verify_accept", "fc_targets_from_truth", "fc_cache_lds_bytes", "fc_cache_retrieve", "fc_cache_write",
     "fc_tree_attention", "fc_tree_attention_workspace_bytes", "fc_tree_attention_ws", "fc_replay_init",
     "fc_replay_run", "fc_retrieve_noalloc_max_bytes", "fc_retrieve_noalloc", "fc_datastore_build_stats",
+    "fc_paged_pool_bytes", "fc_paged_plan", "fc_paged_write", "fc_paged_read", "fc_paged_attention_workspace_bytes",
+    "fc_paged_attention",
 )
 
 
@@ -166,6 +171,19 @@ def lib() -> ctypes.CDLL:
     L.fc_tree_attention_workspace_bytes.argtypes = [i32] * 4
     L.fc_tree_attention_ws.restype = ctypes.c_int
     L.fc_tree_attention_ws.argtypes = [vp] * 9 + [i32] * 6 + [ctypes.c_float, vp, vp, sz, vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    L.fc_paged_pool_bytes.restype = sz
+    L.fc_paged_pool_bytes.argtypes = [i32] * 2
+    L.fc_paged_plan.restype = ctypes.c_int
+    L.fc_paged_plan.argtypes = [vp] * 4 + [i32] * 3 + [vp, i32, vp, i32] + [vp] * 8
+    L.fc_paged_write.restype = ctypes.c_int
+    L.fc_paged_write.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, i32, vp, vp, vp, i32, f32, vp]
+    L.fc_paged_read.restype = ctypes.c_int
+    L.fc_paged_read.argtypes = [vp, i32, i32, i32, vp, i32, vp, vp, vp]
+    L.fc_paged_attention_workspace_bytes.restype = sz
+    L.fc_paged_attention_workspace_bytes.argtypes = [i32] * 5
+    L.fc_paged_attention.restype = ctypes.c_int
+    L.fc_paged_attention.argtypes = ([vp, i64] * 3 + [vp, i32, vp, i32] + [vp] * 4 + [i32] * 6 + [f32, vp, vp, sz, vp])
     L.fc_build_tree_workspace_bytes.restype = sz
     L.fc_build_tree_workspace_bytes.argtypes = [i32]
     L.fc_build_tree.restype = ctypes.c_int
@@ -621,6 +639,214 @@ def fc_tree_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tenso
     _check("fc_tree_attention", lib().fc_tree_attention_ws(
         *_ptrs((q, k_tree, v_tree, k_cache, v_cache, prefix_len, tree["num_nodes"], tree["mask"], tree["pos_ids"])),
         B, R, H, Hkv, D, Pmax, rope_base, _ptr(out), _ptr(workspace), size, _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------- paged cache ----
+
+PLAN_FIELDS = ("len", "cu", "slot", "pos", "src", "ends")
+_PLAN_DTYPES = (torch.int32,) * 5 + (torch.int64,)
+
+
+class _Launch:
+    """A call's device and stream: every tensor has to be on one device, which
+    is made the current one for the call where it is not.  The call's own
+    tensors come from the pool of the stream that it runs on."""
+
+    def __init__(self, stream, tensors):
+        self.device = next(t for t in tensors if t is not None).device
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"tensors on {self.device} and {t.device}: one device expected")
+        if self.device.type != "cuda":
+            raise ValueError("device tensor expected")
+        if isinstance(stream, torch.cuda.Stream) and stream.device != self.device:
+            raise ValueError(f"a stream of {self.device} expected, not of {stream.device}")
+        self.stream = stream
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return self
+
+    def __exit__(self, *_):
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.before)
+
+    def raw(self) -> int:
+        return _stream(self.stream)
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        if self.stream is None:
+            return _empty(shape, dtype, self.device)
+        size = math.prod(shape) * dtype.itemsize
+        return _scratch(size, self.device, self.stream).view(dtype).view(shape)
+
+
+def _rows(name: str, t: torch.Tensor, heads: int | None = None) -> int:
+    """Elements between the rows of [rows][heads][D] or [B][R][heads][D]: whole
+    rows, the rows of a batch one after another, at any distance (slices of a
+    fused projection)."""
+    if t.dtype != torch.bfloat16 or t.dim() not in (3, 4):
+        raise ValueError(f"{name} must be a 3-D or 4-D bfloat16 tensor")
+    D = FC_TREE_ATTN_HEAD_DIM
+    if t.shape[-1] != D or (heads is not None and t.shape[-2] != heads):
+        raise ValueError(f"{name} must have rows of [{'heads' if heads is None else heads}][{D}]")
+    row = t.stride(-3) if t.shape[-3] > 1 else (t.stride(0) if t.dim() == 4 and t.shape[0] > 1 else t.shape[-2] * D)
+    if t.numel() and (t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != D) or
+                      (t.dim() == 4 and t.shape[0] > 1 and t.stride(0) != t.shape[1] * row)):
+        raise ValueError(f"{name} must have contiguous heads and evenly spaced rows")
+    return row
+
+
+def _pool(pool: torch.Tensor) -> tuple:
+    if pool.dtype != torch.uint8 or pool.dim() != 3 or pool.shape[2] != FC_PAGE_HEAD_BYTES:
+        raise ValueError(f"pool must be uint8 [n_pages][Hkv][{FC_PAGE_HEAD_BYTES}]")
+    return int(pool.shape[0]), int(pool.shape[1])
+
+
+def paged_pool(n_pages: int, Hkv: int, device) -> torch.Tensor:
+    """One layer's pool of pages."""
+    return _empty((n_pages, Hkv, FC_PAGE_HEAD_BYTES), torch.uint8, device)
+
+
+def paged_state(B: int, max_pages: int, n_pages: int, device) -> dict:
+    """The bookkeeping of an empty cache: lengths, tables, and every page free."""
+    i32 = torch.int32
+    return dict(len=torch.zeros(B, dtype=i32, device=device),
+                table=torch.full((B, max_pages), -1, dtype=i32, device=device),
+                queue=torch.arange(n_pages, dtype=i32, device=device),
+                ends=torch.tensor([0, n_pages], dtype=torch.int64, device=device))
+
+
+def fc_paged_pool_bytes(n_pages: int, Hkv: int) -> int:
+    return int(lib().fc_paged_pool_bytes(n_pages, Hkv))
+
+
+def fc_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, queue: torch.Tensor,
+                  ends: torch.Tensor, n_slots: int, tree: dict | None = None, last_node: torch.Tensor | None = None,
+                  out: dict | None = None, stream=None) -> dict:
+    """Pages, block tables and slot maps of a step (see include/fastcoder.h):
+    length, add [B], table [B][max_pages], queue [n_pages] int32, ends [2]
+    int64; with a tree and the last_node of fc_verify_accept the step's tokens
+    are the accepted rows.  Writes new entries of table and queue, returns len,
+    cu, slot, pos, src and ends, which are inputs of the next step."""
+    if table.dim() != 2 or queue.dim() != 1:
+        raise ValueError("table [B][max_pages] and queue [n_pages] expected")
+    B, max_pages = table.shape
+    i32 = torch.int32
+    for name, t, dt, shape in (("length", length, i32, (B,)), ("add", add, i32, (B,)), ("table", table, i32, None),
+                               ("queue", queue, i32, None), ("ends", ends, torch.int64, (2,))):
+        _expect(name, t, dt, shape)
+    if (tree is None) != (last_node is None):
+        raise ValueError("a tree and its last_node go together")
+    mask, R = None, 0
+    if tree is not None:
+        mask = tree["mask"]
+        R = mask.shape[-1]
+        _expect("mask", mask, i32, (B, R, R))
+        _expect("last_node", last_node, i32, (B,))
+    shapes = ((B,), (B + 1,), (n_slots,), (n_slots,), (n_slots,), (2,))
+    if out is not None:
+        _expect_all(PLAN_FIELDS, [out.get(f) for f in PLAN_FIELDS], _PLAN_DTYPES, shapes)
+    given = [] if out is None else [out[f] for f in PLAN_FIELDS]
+    ins = (length, add, mask, last_node, table, queue, ends)
+    with _Launch(stream, (*ins, *given)) as on:
+        if out is None:
+            out = {f: on.empty(shape, dt) for f, shape, dt in zip(PLAN_FIELDS, shapes, _PLAN_DTYPES)}
+        o = [_ptr(out[f]) for f in PLAN_FIELDS]
+        _check("fc_paged_plan", lib().fc_paged_plan(
+            _ptr(length), _ptr(add), _ptr(mask), _ptr(last_node), B, R, n_slots, _ptr(table), max_pages, _ptr(queue),
+            queue.numel(), _ptr(ends), *o, on.raw()))
+    return out
+
+
+def fc_paged_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor,
+                   pos: torch.Tensor | None = None, src: torch.Tensor | None = None, rope_base: float = 10000.0,
+                   stream=None) -> None:
+    """Rounds rows of k and v (bf16 [rows][Hkv][D] or [B][R][Hkv][D], rows at
+    any even distance) to 4 bits into the pool: row src[i] (or i), its keys
+    rotated by pos[i], to slot[i].  rope_base 0: rotated already."""
+    n_pages, Hkv = _pool(pool)
+    ks, vs = _rows("k", k, Hkv), _rows("v", v, Hkv)
+    if k.shape != v.shape:
+        raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
+    n_src = k.numel() // (Hkv * FC_TREE_ATTN_HEAD_DIM)
+    n = slot.numel()
+    _expect("slot", slot, torch.int32, (n,))
+    _expect("pos", pos, torch.int32, (n,), optional=rope_base == 0)
+    _expect("src", src, torch.int32, (n,), optional=True)
+    with _Launch(stream, (pool, k, v, slot, pos, src)) as on:
+        _check("fc_paged_write", lib().fc_paged_write(
+            _ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, k.data_ptr(), ks, v.data_ptr(), vs, n_src, _ptr(slot),
+            _ptr(pos), _ptr(src), n, rope_base, on.raw()))
+
+
+def fc_paged_read(pool: torch.Tensor, slot: torch.Tensor, out=None, stream=None) -> tuple:
+    """Keys (as held: rotated) and values of slots, bf16 [n][Hkv][D] each; rows
+    of slots outside the pool are left as they were."""
+    n_pages, Hkv = _pool(pool)
+    n = slot.numel()
+    _expect("slot", slot, torch.int32, (n,))
+    shape = (n, Hkv, FC_TREE_ATTN_HEAD_DIM)
+    if out is not None:
+        for name, t in zip(("k", "v"), out):
+            _expect(name, t, torch.bfloat16, shape)
+    with _Launch(stream, (pool, slot, *(out or ()))) as on:
+        if out is None:
+            out = on.empty(shape, torch.bfloat16), on.empty(shape, torch.bfloat16)
+        k, v = out
+        _check("fc_paged_read", lib().fc_paged_read(_ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, _ptr(slot), n,
+                                                    _ptr(k), _ptr(v), on.raw()))
+    return k, v
+
+
+def fc_paged_attention_workspace_bytes(B: int, R: int, H: int, Hkv: int, max_len: int) -> int:
+    return int(lib().fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len))
+
+
+def fc_paged_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pool: torch.Tensor,
+                       table: torch.Tensor, prefix_len: torch.Tensor, tree: dict | None = None,
+                       max_len: int | None = None, rope_base: float = 10000.0, out: torch.Tensor | None = None,
+                       stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """fc_tree_attention over the paged 4-bit cache: bf16 q [B][R][H][D],
+    k/v_tree [B][R][Hkv][D] (rows at any even distance), the pool and the table
+    [B][max_pages] of the cached prefixes; returns bf16 [B][R][H][D].  Without
+    a tree each row sees the rows before it (R = 1: one decoded token).
+    max_len bounds prefix_len (longer prefixes are cut off there) and is the
+    tables' width unless the caller knows better; shorter bounds launch less.
+    Scratch memory as in fc_tree_attention."""
+    if q.dim() != 4 or table.dim() != 2:
+        raise ValueError("q [B][R][H][D] and table [B][max_pages] expected")
+    n_pages, Hkv = _pool(pool)
+    B, R, H, D = q.shape
+    qs, ks, vs = _rows("q", q), _rows("k_tree", k_tree, Hkv), _rows("v_tree", v_tree, Hkv)
+    for name, t in (("k_tree", k_tree), ("v_tree", v_tree)):
+        _expect(name, t, torch.bfloat16, (B, R, Hkv, D))
+    max_pages = table.shape[1]
+    _expect("table", table, torch.int32, (B, max_pages))
+    _expect("prefix_len", prefix_len, torch.int32, (B,))
+    nodes = mask = pos_ids = None
+    if tree is not None:
+        nodes, mask, pos_ids = tree["num_nodes"], tree["mask"], tree["pos_ids"]
+        _expect("num_nodes", nodes, torch.int32, (B,))
+        _expect("mask", mask, torch.int32, (B, R, R))
+        _expect("pos_ids", pos_ids, torch.int32, (B, R))
+    _expect("out", out, torch.bfloat16, (B, R, H, D), optional=True)
+    _expect("workspace", workspace, torch.uint8, optional=True)
+    if max_len is None:
+        max_len = max_pages * FC_PAGE_TOKENS
+    need = fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len)
+    with _Launch(stream, (q, k_tree, v_tree, pool, table, prefix_len, nodes, mask, pos_ids, out, workspace)) as on:
+        if out is None:
+            out = on.empty((B, R, H, D), torch.bfloat16)
+        if workspace is None and need > 0:
+            workspace = on.empty((need,), torch.uint8)
+        _check("fc_paged_attention", lib().fc_paged_attention(
+            q.data_ptr(), qs, k_tree.data_ptr(), ks, v_tree.data_ptr(), vs, _ptr(pool), n_pages, _ptr(table),
+            max_pages, _ptr(prefix_len), _ptr(nodes), _ptr(mask), _ptr(pos_ids), B, R, H, Hkv, D, max_len, rope_base,
+            _ptr(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), on.raw()))
     return out
 
 

@@ -1,0 +1,380 @@
+// The paged 4-bit cache on gfx950: its plan, writes and reads (fc_paged_plan,
+// fc_paged_write, fc_paged_read).
+//
+// All three move little arithmetic and are bound by launches (a decoding
+// step's few hundred tokens) or by memory (prompts).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fastcoder.h"
+#include "fc_device.h"
+#include "fc_host.h"
+#include "fc_page.h"
+
+namespace {
+
+using fc::kHeadDim;
+using fc::kPage;
+using fc::kPageBytes;
+
+// ------------------------------------------------------------------- plan --
+
+constexpr int kPlanThreads = 256;
+constexpr int kPlanTokens = 1024;  // tokens of the slot map that a workgroup writes
+
+// Every workgroup scans all sequences (three prefix sums: tokens, new pages,
+// pages given back) and keeps, in LDS, those whose tokens fall into its own
+// window of the slot map; so no workgroup waits for another and one launch does
+// it all.  A window position that starts a sequence carries that sequence's
+// data; a running maximum over the positions takes each token to its start.
+// The scan is 8 bytes a sequence from L2: at the 65,536 sequences allowed it is
+// what costs, at the thousands of a serving batch it is not.
+__global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
+    const int32_t* __restrict__ len, const int32_t* __restrict__ add, const int32_t* __restrict__ mask,
+    const int32_t* __restrict__ last_node, int B, int R, int n_slots, int32_t* table, int max_pages, int32_t* queue,
+    int n_pages, const int64_t* __restrict__ ends, int32_t* __restrict__ len_out, int32_t* __restrict__ cu,
+    int32_t* __restrict__ slot, int32_t* __restrict__ pos, int32_t* __restrict__ src,
+    int64_t* __restrict__ ends_out) {
+  struct Seq {  // of a window position that starts a sequence
+    int64_t pos0;       // position of the token at window position 0, were it this sequence's
+    int32_t b;
+    int32_t held;       // pages it had
+    uint32_t page0;     // new pages taken before its own
+    uint32_t count;     // tokens
+    int32_t first;      // its token number at this window position
+    int32_t ok;
+  };
+  struct Back {  // pages that a sequence gives back
+    uint64_t to;
+    int32_t b, from, count;
+  };
+  __shared__ uint64_t s_scan[kPlanThreads / fc::kWave + 1];
+  __shared__ int s_scan_max[kPlanThreads / fc::kWave + 1];
+  __shared__ Seq s_seq[kPlanTokens];
+  __shared__ int s_start[kPlanTokens];  // window position + 1 where a sequence starts, else 0
+  __shared__ int32_t s_src[kPlanTokens];
+  __shared__ int s_list[kPlanTokens];
+  __shared__ Back s_back[kPlanThreads];
+  __shared__ int s_listed, s_backs;
+  __shared__ unsigned long long s_given;
+
+  const int tid = (int)threadIdx.x;
+  const int64_t w0 = (int64_t)blockIdx.x * kPlanTokens;
+  const int64_t head = ends[0], tail = ends[1];
+  const uint64_t held_free = tail > head ? (uint64_t)(tail - head) : 0;
+  const uint64_t avail = held_free < (uint64_t)n_pages ? held_free : (uint64_t)n_pages;
+  const uint64_t head_at = (uint64_t)head % (uint32_t)n_pages, tail_at = (uint64_t)tail % (uint32_t)n_pages;
+  for (int x = tid; x < kPlanTokens; x += kPlanThreads) s_start[x] = 0, s_src[x] = -1;
+  if (tid == 0) s_listed = 0, s_given = 0;
+  __syncthreads();
+
+  uint64_t tokens = 0, taken = 0, given_back = 0;  // of the sequences before this chunk
+  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    const bool in = b < B;
+    const int64_t cap = (int64_t)max_pages * kPage;
+    int64_t n = in ? len[b] : 0;
+    n = n < 0 ? 0 : n > cap ? cap : n;
+    const int64_t a = in ? add[b] : 0;
+    const uint64_t want = a > 0 ? (uint64_t)a : 0;
+    int64_t now = n + a < 0 ? 0 : n + a;
+    const int64_t held = (n + kPage - 1) / kPage, pages = (now + kPage - 1) / kPage;
+    uint64_t sum;
+    if (tid == 0) s_backs = 0;
+    const uint64_t first = tokens + fc::block_excl_sum<uint64_t>(want, s_scan, &sum);
+    tokens += sum;
+    const bool fits = a <= 0 || (pages <= max_pages && first + want <= (uint64_t)n_slots);
+    const uint64_t need = fits && a > 0 ? (uint64_t)(pages - held) : 0;
+    const uint64_t page0 = taken + fc::block_excl_sum<uint64_t>(need, s_scan, &sum);
+    taken += sum;
+    const bool ok = fits && (need == 0 || page0 + need <= avail);
+    if (ok && need > 0) atomicMax(&s_given, (unsigned long long)(page0 + need));  // the sums only grow
+    if (!ok) now = n;
+    const uint64_t back = a < 0 ? (uint64_t)(held - pages) : 0;
+    const uint64_t to = given_back + fc::block_excl_sum<uint64_t>(back, s_scan, &sum);
+    given_back += sum;
+    if (in && blockIdx.x == 0) {
+      len_out[b] = (int32_t)now;
+      const uint64_t end = first + want;
+      cu[b + 1] = (int32_t)(end < 0x7FFFFFFFu ? end : 0x7FFFFFFFu);
+    }
+    if (back > 0 && (uint32_t)b % gridDim.x == blockIdx.x)
+      s_back[atomicAdd(&s_backs, 1)] = Back{tail_at + to, b, (int32_t)pages, (int32_t)back};
+    if (want > 0 && (int64_t)first < w0 + kPlanTokens && (int64_t)(first + want) > w0) {
+      const int x = (int64_t)first > w0 ? (int)((int64_t)first - w0) : 0;
+      s_seq[x] = Seq{n - ((int64_t)first - w0), b, (int32_t)held, (uint32_t)page0,
+                     (uint32_t)want, (int32_t)(w0 + x - (int64_t)first), ok ? 1 : 0};
+      s_start[x] = x + 1;
+      s_list[atomicAdd(&s_listed, 1)] = x;  // any order: each writes its own places
+    }
+    __syncthreads();
+    for (int i = 0; i < s_backs; ++i) {
+      const Back r = s_back[i];
+      for (int j = tid; j < r.count; j += kPlanThreads)
+        queue[(r.to + (uint32_t)j) % (uint32_t)n_pages] = table[(int64_t)r.b * max_pages + r.from + j];
+    }
+    __syncthreads();
+  }
+  if (tid == 0 && blockIdx.x == 0) {
+    cu[0] = 0;
+    ends_out[0] = head + (int64_t)s_given;
+    ends_out[1] = tail + (int64_t)given_back;
+  }
+
+  // a tree step's source rows: a wave per sequence takes the rows that the
+  // accepted row may see, in order
+  if (mask) {
+    const int lane = fc::lane_id();
+    for (int i = tid / fc::kWave; i < s_listed; i += kPlanThreads / fc::kWave) {
+      const int x = s_list[i];
+      const Seq q = s_seq[x];
+      const int last = last_node[q.b];
+      if (last < 0 || last >= R) continue;
+      const int32_t* row = mask + ((int64_t)q.b * R + last) * R;
+      int before = 0;
+      for (int j0 = 0; j0 < R; j0 += fc::kWave) {
+        const int j = j0 + lane;
+        const bool on = j < R && row[j] == 1;
+        const uint64_t all = fc::ballot(on);
+        const int t = before + (int)__builtin_popcountll(all & fc::lanemask_lt());
+        const int at = x + t - q.first;
+        if (on && t >= q.first && (uint32_t)t < q.count && at < kPlanTokens) s_src[at] = q.b * R + j;
+        before += (int)__builtin_popcountll(all);
+      }
+    }
+    __syncthreads();
+  }
+
+  constexpr int kEach = kPlanTokens / kPlanThreads;
+  int mine[kEach], run = 0;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int s = s_start[tid * kEach + e];
+    run = s > run ? s : run;
+    mine[e] = run;
+  }
+  const int before = fc::block_excl_max<int>(run, 0, s_scan_max);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int x = tid * kEach + e;
+    const int64_t at = w0 + x;
+    if (at >= n_slots) break;
+    const int start = mine[e] > before ? mine[e] : before;
+    int32_t sl = -1, po = -1, sr = -1;
+    if (start > 0 && (uint64_t)at < tokens) {
+      const Seq q = s_seq[start - 1];
+      if (q.ok) {
+        const int64_t p = q.pos0 + x;
+        const int idx = (int)(p / kPage);
+        int32_t page;
+        if (idx < q.held) {
+          page = table[(int64_t)q.b * max_pages + idx];
+        } else {
+          page = queue[(head_at + q.page0 + (uint32_t)(idx - q.held)) % (uint32_t)n_pages];
+          if (p % kPage == 0) table[(int64_t)q.b * max_pages + idx] = page;  // every new page starts with a token
+        }
+        sl = page >= 0 && page < n_pages ? page * kPage + (int32_t)(p % kPage) : -1;
+        po = (int32_t)p;
+        sr = mask ? s_src[x] : (int32_t)at;
+      }
+    }
+    slot[at] = sl;
+    pos[at] = po;
+    src[at] = sr;
+  }
+}
+
+// ------------------------------------------------------------------ write --
+
+constexpr int kWriteThreads = 256;
+constexpr int kUnitLanes = 8;                              // lanes of one token's key (or value) head
+constexpr int kUnits = kWriteThreads / kUnitLanes;         // units at work in a workgroup
+constexpr int kMaxTokens = 16;                             // tokens of a workgroup at most
+
+// A unit is one token's keys or values of one head.  Lane j of its eight holds
+// dims 8 j .. 8 j + 7 and the same 64 further on: the two halves of each
+// rotation, and quarters of two scale groups.
+__global__ void __launch_bounds__(kWriteThreads) k_paged_write(
+    uint8_t* __restrict__ pool, int n_pages, int Hkv, const uint16_t* __restrict__ k, int64_t k_stride,
+    const uint16_t* __restrict__ v, int64_t v_stride, int n_src, const int32_t* __restrict__ slot,
+    const int32_t* __restrict__ pos, const int32_t* __restrict__ src, int n, int tokens, double log2_base) {
+  __shared__ double2 s_turn[kMaxTokens * kHeadDim / 2];
+  const int tid = (int)threadIdx.x;
+  const int64_t i0 = (int64_t)blockIdx.x * tokens;
+  if (log2_base > 0.0) {
+    for (int x = tid; x < tokens * (kHeadDim / 2); x += kWriteThreads) {
+      const int64_t i = i0 + x / (kHeadDim / 2);
+      const int d = x % (kHeadDim / 2);
+      if (i < n) {
+        constexpr double kInvPi = 0.31830988618379067154;
+        const double half_turns = (double)pos[i] * exp2(-2.0 * d / (double)kHeadDim * log2_base) * kInvPi;
+        double s, c;
+        sincospi(half_turns - 2.0 * floor(half_turns * 0.5), &s, &c);
+        s_turn[x] = make_double2(s, c);
+      }
+    }
+    __syncthreads();
+  }
+  const int j = tid % kUnitLanes;
+  const int units = tokens * 2 * Hkv;
+  for (int u = tid / kUnitLanes; u < units; u += kUnits) {
+    const int tl = u / (2 * Hkv), h2 = u - tl * (2 * Hkv);
+    const bool is_v = h2 >= Hkv;
+    const int h = is_v ? h2 - Hkv : h2;
+    const int64_t i = i0 + tl;
+    if (i >= n) break;
+    const int sl = slot[i];
+    const int64_t row = src ? src[i] : i;
+    if (sl < 0 || sl >= n_pages * kPage || row < 0 || row >= n_src) continue;  // the unit's lanes go together
+    const uint16_t* p = (is_v ? v + row * v_stride : k + row * k_stride) + h * kHeadDim + 8 * j;
+    const uint4 lo = *(const uint4*)p, hi = *(const uint4*)(p + kHeadDim / 2);
+    float a[8], b[8];
+    fc::unpack8(lo, a);
+    fc::unpack8(hi, b);
+    if (!is_v && log2_base > 0.0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double2 t = s_turn[tl * (kHeadDim / 2) + 8 * j + e];
+        const double x0 = a[e], x1 = b[e];
+        a[e] = (float)(x0 * t.y - x1 * t.x);
+        b[e] = (float)(x1 * t.y + x0 * t.x);
+      }
+    }
+    uint32_t ma = 0, mb = 0;  // magnitudes compare as their bits, NaN above all
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t xa = __float_as_uint(a[e]) & 0x7FFFFFFFu, xb = __float_as_uint(b[e]) & 0x7FFFFFFFu;
+      ma = xa > ma ? xa : ma;
+      mb = xb > mb ? xb : mb;
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const uint32_t xa = __shfl_xor(ma, o), xb = __shfl_xor(mb, o);
+      ma = xa > ma ? xa : ma;
+      mb = xb > mb ? xb : mb;
+    }
+    const uint32_t sa = fc::scale_byte(ma), sb = fc::scale_byte(mb);
+    uint32_t ca = 0, cb = 0;
+#define FC_CODES(E)                                                                                            \
+  ca = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(ca, a[2 * E], a[2 * E + 1], fc::scale_of(sa), E);             \
+  cb = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(cb, b[2 * E], b[2 * E + 1], fc::scale_of(sb), E)
+    FC_CODES(0);
+    FC_CODES(1);
+    FC_CODES(2);
+    FC_CODES(3);
+#undef FC_CODES
+    if (sa == 255u) ca = 0;  // a NaN whatever the codes: always the same bytes
+    if (sb == 255u) cb = 0;
+    const int t = sl % kPage;
+    uint8_t* page = pool + ((int64_t)(sl / kPage) * Hkv + h) * kPageBytes;
+    uint8_t* codes = page + (is_v ? fc::kPageV : 0) + t * fc::kCodeRow + 4 * j;
+    *(uint32_t*)codes = ca;
+    *(uint32_t*)(codes + fc::kCodeRow / 2) = cb;
+    if (j % 4 == 0) {
+      const int g = j / 4;
+      page[is_v ? fc::v_scale_at(t, g) : fc::k_scale_at(t, g)] = (uint8_t)sa;
+      page[is_v ? fc::v_scale_at(t, g + 2) : fc::k_scale_at(t, g + 2)] = (uint8_t)sb;
+    }
+  }
+}
+
+// ------------------------------------------------------------------- read --
+
+constexpr int kReadThreads = 256;
+constexpr int kReadRows = 16;  // rows of a workgroup
+
+// Sixteen lanes per row and head, eight dims each; a workgroup takes 16 rows
+// (a quarter of a page where slots follow each other) through every head.
+__global__ void __launch_bounds__(kReadThreads) k_paged_read(const uint8_t* __restrict__ pool, int n_pages, int Hkv,
+                                                             const int32_t* __restrict__ slot, int n,
+                                                             uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
+  const int tid = (int)threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * kReadRows + tid / 16;
+  const int j = tid % 16;
+  if (i >= n) return;
+  const int sl = slot[i];
+  if (sl < 0 || sl >= n_pages * kPage) return;
+  const int t = sl % kPage;
+  for (int h = 0; h < Hkv; ++h) {
+    const uint8_t* page = pool + ((int64_t)(sl / kPage) * Hkv + h) * kPageBytes;
+    const int64_t to = (i * Hkv + h) * kHeadDim + 8 * j;
+#pragma unroll
+    for (int is_v = 0; is_v < 2; ++is_v) {
+      const uint32_t c = *(const uint32_t*)(page + (is_v ? fc::kPageV : 0) + t * fc::kCodeRow + 4 * j);
+      const float s = fc::scale_of(page[is_v ? fc::v_scale_at(t, j / 4) : fc::k_scale_at(t, j / 4)]);
+      uint4 w;
+      w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+      w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+      w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+      w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+      *(uint4*)((is_v ? v : k) + to) = w;
+    }
+  }
+}
+
+bool pool_ok(const void* pool, int32_t n_pages, int32_t Hkv) {
+  return pool && !((uintptr_t)pool & 15) && n_pages >= 1 && n_pages <= (1 << 25) - 1 && Hkv >= 1 && Hkv <= 1024;
+}
+
+}  // namespace
+
+extern "C" size_t fc_paged_pool_bytes(int32_t n_pages, int32_t Hkv) {
+  if (n_pages < 1 || n_pages > (1 << 25) - 1 || Hkv < 1 || Hkv > 1024) return 0;
+  return (size_t)n_pages * Hkv * FC_PAGE_HEAD_BYTES;
+}
+
+extern "C" fc_status fc_paged_plan(const int32_t* len, const int32_t* add, const int32_t* mask,
+                                   const int32_t* last_node, int32_t B, int32_t R, int32_t n_slots, int32_t* table,
+                                   int32_t max_pages, int32_t* queue, int32_t n_pages, const int64_t* ends,
+                                   int32_t* len_out, int32_t* cu, int32_t* slot, int32_t* pos, int32_t* src,
+                                   int64_t* ends_out, hipStream_t stream) {
+  if (B < 0 || B > 65536 || n_slots < 0 || n_slots >= (1 << 30) || max_pages < 1 || max_pages >= (1 << 25) ||
+      n_pages < 1 || n_pages > (1 << 25) - 1)
+    return FC_ERR_INVALID;
+  if (!mask != !last_node || (mask && (R < 1 || R > FC_MAX_TREE_ROWS))) return FC_ERR_INVALID;
+  if (B > 0 && (!len || !add || !table || !len_out)) return FC_ERR_INVALID;
+  if (!queue || !ends || !cu || !ends_out) return FC_ERR_INVALID;
+  if (n_slots > 0 && (!slot || !pos || !src)) return FC_ERR_INVALID;
+  if ((B > 0 && (len_out == len || len_out == add)) || ends_out == ends) return FC_ERR_INVALID;
+  (void)hipGetLastError();
+  const uint32_t windows = fc::div_up((uint64_t)n_slots, kPlanTokens);
+  hipLaunchKernelGGL(k_paged_plan, dim3(windows ? windows : 1), dim3(kPlanThreads), 0, stream, len, add, mask,
+                     last_node, B, R, n_slots, table, max_pages, queue, n_pages, ends, len_out, cu, slot, pos, src,
+                     ends_out);
+  FC_CHECK_LAUNCH();
+  return FC_OK;
+}
+
+extern "C" fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k,
+                                    int64_t k_stride, const uint16_t* v, int64_t v_stride, int32_t n_src,
+                                    const int32_t* slot, const int32_t* pos, const int32_t* src, int32_t n,
+                                    float rope_base, hipStream_t stream) {
+  if (!pool_ok(pool, n_pages, Hkv) || n < 0 || n_src < 0) return FC_ERR_INVALID;
+  if (!(rope_base == 0.0f || (rope_base > 1.0f && rope_base < __builtin_inff()))) return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || ((k_stride | v_stride) & 7)) return FC_ERR_INVALID;
+  if (n == 0 || n_src == 0) return FC_OK;
+  if (!k || !v || !slot || (rope_base != 0.0f && !pos)) return FC_ERR_INVALID;
+  if (((uintptr_t)k | (uintptr_t)v) & 15) return FC_ERR_INVALID;
+  const int fit = kUnits / (2 * Hkv);
+  const int tokens = fit < 1 ? 1 : fit > kMaxTokens ? kMaxTokens : fit;
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(k_paged_write, dim3(fc::div_up((uint64_t)n, (uint64_t)tokens)), dim3(kWriteThreads), 0, stream,
+                     pool, n_pages, Hkv, k, k_stride, v, v_stride, n_src, slot, pos, src, n, tokens,
+                     rope_base != 0.0f ? log2((double)rope_base) : 0.0);
+  FC_CHECK_LAUNCH();
+  return FC_OK;
+}
+
+extern "C" fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot,
+                                   int32_t n, uint16_t* k, uint16_t* v, hipStream_t stream) {
+  if (!pool_ok(pool, n_pages, Hkv) || n < 0) return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (n == 0) return FC_OK;
+  if (!slot || !k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return FC_ERR_INVALID;
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(k_paged_read, dim3(fc::div_up((uint64_t)n, kReadRows)), dim3(kReadThreads), 0, stream, pool,
+                     n_pages, Hkv, slot, n, k, v);
+  FC_CHECK_LAUNCH();
+  return FC_OK;
+}
