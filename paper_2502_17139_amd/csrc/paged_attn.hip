@@ -42,8 +42,8 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 constexpr int kTile = 16;                       // query rows of a tile
 constexpr int kParts = 3;                       // 6-bit parts of a query
 constexpr int kDTiles = kHeadDim / 16;          // output tiles of 16 dims
-constexpr int kRowBytes = kHeadDim * 2;         // a bf16 row in LDS
-constexpr int kValues = kPage * kRowBytes;      // a page's values in LDS: 16 KB
+constexpr int kRowBytes = kHeadDim * 2 + 32;    // a bf16 row in LDS
+constexpr int kValues = kPage * kRowBytes;      // a page's values in LDS: 18 KB
 constexpr int kTreeBlock = 32;                  // tree rows at a time: keys and values fill one such buffer
 constexpr int kXcds = 8;
 constexpr int kCus = 256;
@@ -75,9 +75,11 @@ __device__ __forceinline__ bool keep_finite(uint4& x) {
 
 __device__ __forceinline__ int clamp_len(int len, int most) { return len < 0 ? 0 : (len > most ? most : len); }
 
-// byte offset of 16-byte chunk c of row r of a bf16 tile in LDS: chunks are
-// swizzled by the row, so that neither whole rows nor columns collide in a bank
-__device__ __forceinline__ uint32_t chunk_at(int r, int c) { return (uint32_t)(r * kRowBytes + ((c ^ (r & 15)) << 4)); }
+// Byte offset of 16-byte chunk c of row r of a bf16 tile in LDS.  Rows are 32
+// bytes longer than their values: the transposing reads take 32 bytes of 16 rows
+// at a time, eight rows of which then fill the 64 banks once, and every read of
+// a page is one address and a constant.
+__device__ __forceinline__ constexpr uint32_t chunk_at(int r, int c) { return (uint32_t)(r * kRowBytes + c * 16); }
 
 // 32 floats, the even ones and the odd ones, as 6-bit values of scale f, and
 // back.  Both instructions take several passes over their registers, so the
@@ -221,56 +223,83 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
   }
 
   floatx4 o[NT][kDTiles];
-  float m_run[NT], l_run[NT];
+  // a row's running maximum m, 0 - m (0 while there is none) four times, and by
+  // how much a score may pass m before the row is scaled anew
+  float m_run[NT], l_run[NT], slack[NT];
+  floatx4 minus_m[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    m_run[i] = -INFINITY;
+    m_run[i] = slack[i] = -INFINITY;
     l_run[i] = 0.0f;
+    minus_m[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int t = 0; t < kDTiles; ++t) o[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // One step of the softmax: KT tiles of 16 scores (already -inf where a key is
-  // not allowed) become weights, and the row's sums and outputs take the new
-  // maximum.
-  const auto softmax = [&](auto& s, auto& pb, int i) {
-    constexpr int KT = sizeof(s) / sizeof(s[0]);
-    float mb = -INFINITY;
+  // One step of the softmax.  s holds scores less m (the products start from
+  // minus_m), -inf where a key is not allowed.  m is the maximum of what a row
+  // saw when it was last scaled: while no score passes it by more than 8, weights
+  // stay below 2^8 and neither sums nor outputs are touched (with bf16 weights a
+  // common factor costs no accuracy), so the usual step is a power of two, a sum
+  // and a rounding for each score.
+  const auto softmax = [&](auto& s, auto& pb) {
+    constexpr int KT = sizeof(s[0]) / sizeof(s[0][0]);
+    bool up = false;
+    float top[NT];
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+    for (int i = 0; i < NT; ++i) {
+      top[i] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mb = fmaxf(mb, s[t][e]);
-    mb = fmaxf(mb, __shfl_xor(mb, 16));
-    mb = fmaxf(mb, __shfl_xor(mb, 32));
-    const float m_new = fmaxf(m_run[i], mb);
-    const bool none = m_new == -INFINITY;  // no allowed key for this row yet
-    const float alpha = none ? 1.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
-    const float sub = none ? 0.0f : m_new;
-    float sum = 0.0f;
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(s[t][e] - sub);
-        sum += p;
-        pb[t / 2][4 * (t % 2) + e] = (__bf16)p;
+      for (int t = 0; t < KT; ++t) {
+        top[i] = fmaxf(fmaxf(top[i], s[i][t][0]), s[i][t][1]);
+        top[i] = fmaxf(fmaxf(top[i], s[i][t][2]), s[i][t][3]);
       }
-    m_run[i] = m_new;
-    l_run[i] = l_run[i] * alpha + sum;
+      up |= top[i] > slack[i];
+    }
+    if (__any(up)) {
 #pragma unroll
-    for (int t = 0; t < kDTiles; ++t) o[i][t] *= alpha;
+      for (int i = 0; i < NT; ++i) {
+        float mx = fmaxf(top[i], __shfl_xor(top[i], 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float was = 0.0f - minus_m[i][0];
+        const float m_new = fmaxf(m_run[i], was + mx);
+        const float by = m_new == -INFINITY ? 0.0f : m_new - was;
+        const float alpha = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) s[i][t] -= by;
+        l_run[i] *= alpha;
+#pragma unroll
+        for (int t = 0; t < kDTiles; ++t) o[i][t] *= alpha;
+        m_run[i] = m_new;
+        const float minus = m_new == -INFINITY ? 0.0f : -m_new;
+        minus_m[i] = floatx4{minus, minus, minus, minus};
+        slack[i] = m_new == -INFINITY ? -INFINITY : 8.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(s[i][t][e]);
+          l_run[i] += p;
+          pb[t / 2][i][4 * (t % 2) + e] = (__bf16)p;
+        }
+    }
   };
-  // O^T += V^T P^T over 32 keys at LDS byte address `base` (rows of 256 bytes):
-  // a transposing read gives lane (lg, lc) dims 16 t + lc of keys 4 lg + e, the
-  // second one keys 16 + 4 lg + e, as the weights lie
+  // O^T += V^T P^T over 32 keys at byte `base` of the buffers: a transposing read
+  // gives lane (lg, lc) dims 16 t + lc of keys 4 lg + e, the second one keys 16 +
+  // 4 lg + e, as the weights lie
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
+  const uint32_t v_lane = lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u;
   const auto values = [&](uint32_t base, const bf16x8 (&pb)[NT]) {
-    const int r0 = 4 * lg + (lc >> 2), r1 = r0 + 16, vq = lc & 3;
+    typedef __attribute__((address_space(3))) uint8_t lds_u8;
+    lds_u8* at = (lds_u8*)(uintptr_t)(v_lane + base);
 #pragma unroll
     for (int t = 0; t < kDTiles; ++t) {
-      const int cc = 2 * t + (vq >> 1);
-      const uint32_t half = (uint32_t)(vq & 1) * 8u;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(base + chunk_at(r0, cc) + half));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)(base + chunk_at(r1, cc) + half));
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(0, 2 * t)));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(16, 2 * t)));
       const bf16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
       for (int i = 0; i < NT; ++i) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[i], o[i][t], 0, 0, 0);
@@ -297,8 +326,6 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
       if (wr + WR * u < 4) vf[u] = *(const uint4*)(page + fc::kPageV + ((wr + WR * u) * 64 + lane) * 16);
     vs = *(const uint32_t*)(page + fc::kPageVScale + 4 * lane);
   };
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
-
   const int steps = (pg1 - pg0 + WK - 1) / WK;
   load(pg0 + grp);
   for (int it = 0; it < steps; ++it) {
@@ -314,9 +341,16 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
         const int i4 = wr + WR * u;
         if (i4 < 4) {
           const int key = i4 * 16 + (lane >> 2), g = lane & 3;
-          const float sc = fc::scale_of((vs >> (8 * i4)) & 255u);
-          const uint32_t c4[4] = {vf[u].x, vf[u].y, vf[u].z, vf[u].w};
-          const bool live = key < left;
+          uint32_t sb = (vs >> (8 * i4)) & 255u;
+          uint32_t c4[4] = {vf[u].x, vf[u].y, vf[u].z, vf[u].w};
+          if (left < kPage) {
+            const bool live = key < left;
+            sb = live ? sb : 127u;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) c4[c] = live ? c4[c] : 0u;
+          }
+          const float sc = fc::scale_of(sb);
+          uint8_t* dst = s_v + buf + chunk_at(key, 4 * g);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             uint4 d;
@@ -324,8 +358,7 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
             d.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 1));
             d.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 2));
             d.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 3));
-            if (!live) d = make_uint4(0u, 0u, 0u, 0u);
-            *(uint4*)(s_v + buf + chunk_at(key, 4 * g + c)) = d;
+            *(uint4*)(dst + 16 * c) = d;
           }
         }
       }
@@ -338,7 +371,7 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
         const int32x8 a = {(int)kf[t].x, (int)kf[t].y, (int)kf[t].z, (int)kf[t].w, 0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+          floatx4 acc = minus_m[i];
           // the scale operands' byte selectors are immediates
 #define FC_PART(S, T) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, qf[i][S], acc, 4, 2, T, (int)ks, S, qs[i])
           if (t == 0) { FC_PART(0, 0); FC_PART(1, 0); FC_PART(2, 0); }
@@ -353,21 +386,17 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
     load(pg + WK);
     if (use) {
       bf16x8 pb[2][NT];
+      if (left < kPage) {
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        if (left < kPage) {
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[i][t][e] = 16 * t + 4 * lg + e < left ? s[i][t][e] : -INFINITY;
-        }
-        bf16x8 p[2];
-        softmax(s[i], p, i);
-        pb[0][i] = p[0];
-        pb[1][i] = p[1];
       }
-      values(lds0 + buf, pb[0]);
-      values(lds0 + buf + 32 * kRowBytes, pb[1]);
+      softmax(s, pb);
+      values(buf, pb[0]);
+      values(buf + chunk_at(32, 0), pb[1]);
     }
   }
 
@@ -428,7 +457,8 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
           fc::unpack8(*(const uint4*)(kp + kHeadDim / 2), x1);
           v0 = *(const uint4*)vp;
           v1 = *(const uint4*)(vp + kHeadDim / 2);
-          if (keep_finite(v0) | keep_finite(v1)) atomicOr(&s_bad[it & 1][grp], 1u << r);
+          const bool bad0 = keep_finite(v0), bad1 = keep_finite(v1);
+          if (bad0 || bad1) atomicOr(&s_bad[it & 1][grp], 1u << r);
           if (A.log2_base > 0.0) {
             const int pos = position(j);
 #pragma unroll
@@ -454,7 +484,7 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
-          for (int i = 0; i < NT; ++i) s[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int i = 0; i < NT; ++i) s[i][t] = minus_m[i];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const bf16x8 a = *(const bf16x8*)(sk + chunk_at(16 * t + lc, 4 * c + lg));
@@ -465,7 +495,7 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
             }
           }
         }
-        bf16x8 pb[NT];
+        bf16x8 pb[1][NT];
         uint32_t allowed[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -482,11 +512,9 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
 #pragma unroll
           for (int u = 0; u < 8; ++u) s[i][u / 4][u % 4] = (allow >> u) & 1u ? s[i][u / 4][u % 4] : -INFINITY;
           allowed[i] = allow;
-          bf16x8 p[1];
-          softmax(s[i], p, i);
-          pb[i] = p[0];
         }
-        values(lds0 + (uint32_t)(grp * kBufs * kValues + kTreeBlock * kRowBytes), pb);
+        softmax(s, pb);
+        values((uint32_t)(grp * kBufs * kValues + kTreeBlock * kRowBytes), pb[0]);
         // A product with weight 0 is NaN where the value is not finite, so the
         // rows that do not see such a value must not meet it: it is 0 in LDS, and
         // the rows that do see it add it here.
@@ -499,7 +527,7 @@ __global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
             float weight = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (e == u) weight = (float)pb[i][e];
+              if (e == u) weight = (float)pb[0][i][e];
             weight = __shfl(weight, from);
             const bool sees = (__shfl(allowed[i], from) >> u) & 1u;
 #pragma unroll
