@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fastcoder.h"
 #include "fc_device.h"
 #include "fc_host.h"
@@ -35,18 +37,31 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx32 __attribute__((ext_vector_type(32)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef int int32x2 __attribute__((ext_vector_type(2)));
 typedef int int32x6 __attribute__((ext_vector_type(6)));
 typedef int int32x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int kTile = 16;                       // query rows of a tile
+constexpr int kWaves = 4;                       // of a workgroup: one for each SIMD
+constexpr int kThreads = kWaves * fc::kWave;
 constexpr int kParts = 3;                       // 6-bit parts of a query
 constexpr int kDTiles = kHeadDim / 16;          // output tiles of 16 dims
 constexpr int kRowBytes = kHeadDim * 2 + 32;    // a bf16 row in LDS
 constexpr int kValues = kPage * kRowBytes;      // a page's values in LDS: 18 KB
-constexpr int kTreeBlock = 32;                  // tree rows at a time: keys and values fill one such buffer
+constexpr int kSlot = 9 * 1024;                 // a page as it lies in memory, in LDS
+constexpr int kTreeTiles = 6;                   // tree rows of a workgroup: 96
+constexpr int kTreeRows = 16 * kTreeTiles;
+constexpr int kSixRow = 304;                    // a row of 6-bit parts in LDS: 4 groups x 3 parts x 24 bytes, 4 scale words
+constexpr int kSlot0 = kTreeRows * kSixRow + 512;  // free while the tree's rows are in use
+constexpr int kSlot1 = kValues;
+constexpr int kLds = kSlot0 + kSlot;            // 38 KB: four workgroups of a CU
+constexpr int kMostParts = 124;                 // of a prefix; with those of a tree's rows a merging wave takes 128
 constexpr int kXcds = 8;
 constexpr int kCus = 256;
+static_assert((kWaves + 1) * kTile * kSixRow <= kSlot0 && kSlot1 + kSlot <= kSlot0, "query rows, and both slots, apart");
+static_assert(kTreeRows * kRowBytes <= kSlot0, "the tree's values");
 
 struct Args {
   const uint16_t *q, *k_tree, *v_tree;
@@ -96,543 +111,904 @@ __device__ __forceinline__ floatx32 from_six(const int32x6& c, float f) {
   return r;
 }
 
-// parts that a prefix is cut into: each takes part_pages pages
+// 32 dims of a row as three 6-bit parts and their scale bytes.  The first
+// part's scale 2^e is the smallest with which the largest magnitude is at most
+// 7.5; it leaves at most 2^-2 * 2^e, the second (scale 2^(e - 4)) at most 2^-7,
+// the third (2^(e - 9)) at most 2^-12.  Scale byte 255: something is not finite.
+__device__ __forceinline__ void write_six(const float (&v)[32], uint8_t* row, int g) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int u = 0; u < 32; ++u) {
+    const uint32_t bits = __float_as_uint(v[u]) & 0x7FFFFFFFu;
+    top = bits > top ? bits : top;
+  }
+  int e = (int)((top + 0x0FFFFFu) >> 23) - 127 - 2;  // 7.5 = 1.875 * 2^2
+  e = e < -110 ? -110 : e;
+  floatx16 even, odd;
+#pragma unroll
+  for (int u = 0; u < 16; ++u) even[u] = v[2 * u], odd[u] = v[2 * u + 1];
+  uint32_t word = 0;
+#pragma unroll
+  for (int s = 0; s < kParts; ++s) {
+    const int es = e - (s == 0 ? 0 : s == 1 ? 4 : 9);
+    const float f = __uint_as_float((uint32_t)(es + 127) << 23);
+    const int32x6 c = to_six(even, odd, f);
+#pragma unroll
+    for (int u = 0; u < 3; ++u) *(int32x2*)(row + (g * kParts + s) * 24 + 8 * u) = int32x2{c[2 * u], c[2 * u + 1]};
+    if (s + 1 < kParts) {
+      const floatx32 r = from_six(c, f);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) even[u] -= r[2 * u], odd[u] -= r[2 * u + 1];
+    }
+    word |= (uint32_t)(top >= 0x7F800000u ? 255 : es + 127) << (8 * s);
+  }
+  *(uint32_t*)(row + 288 + 4 * g) = word;
+}
+
+// Group g (32 dims) of a row of 128 bf16 to LDS in 6-bit parts,
+// rotated and scaled.  The lane beside this one (lane ^ 1) has the group 64 dims
+// away, so the two share the angles: turn(e) gives the sine and cosine of the
+// pair's angle e, of which this lane asks for half.
+template <typename Turn>
+__device__ __forceinline__ void stage_six(const uint16_t* src, int g, float scale, bool rotate, Turn turn,
+                                          uint8_t* row) {
+  float v[32];
+  uint4 own[4], other[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    own[u] = *(const uint4*)(src + 32 * g + 8 * u);
+    other[u] = *(const uint4*)(src + 32 * (g ^ 2) + 8 * u);
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float x[8];
+    fc::unpack8(own[u], x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[8 * u + e] = x[e] * scale;
+  }
+  if (rotate) {
+    const bool upper = g >= 2;
+    const float sign = upper ? scale : -scale;
+    const uint32_t* y = (const uint32_t*)other;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      asm volatile("" ::: "memory");  // few of the angles in registers at a time
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        // angles d (the lower lane's) and d + 16 (the upper's)
+        const int d = 2 * u + e;
+        const float2 t = turn((upper ? 16 : 0) + d);
+        const float s = __uint_as_float(fc::dpp_mov<0xB1>(__float_as_uint(t.x)));
+        const float c = __uint_as_float(fc::dpp_mov<0xB1>(__float_as_uint(t.y)));
+        const float y0 = __uint_as_float(e ? y[u] & 0xFFFF0000u : y[u] << 16);
+        const float y1 = __uint_as_float(e ? y[8 + u] & 0xFFFF0000u : y[8 + u] << 16);
+        v[d] = v[d] * (upper ? c : t.y) + y0 * sign * (upper ? s : t.x);
+        v[16 + d] = v[16 + d] * (upper ? t.y : c) + y1 * sign * (upper ? t.x : s);
+      }
+    }
+  }
+  write_six(v, row, g);
+}
+// The group of the u-th of a row's four threads.
+__device__ __forceinline__ int group_of(int u) { return (u >> 1) | ((u & 1) << 1); }
+
+// A lane's operand of a row staged so: group lg of three parts, and their scales.
+struct Six {
+  int32x8 part[kParts];
+  int scales;
+};
+__device__ __forceinline__ Six read_six(const uint8_t* row, int lg) {
+  Six f;
+#pragma unroll
+  for (int s = 0; s < kParts; ++s) {
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      const int32x2 x = *(const int32x2*)(row + (lg * kParts + s) * 24 + 8 * u);
+      f.part[s][2 * u] = x[0], f.part[s][2 * u + 1] = x[1];
+    }
+    f.part[s][6] = f.part[s][7] = 0;
+  }
+  f.scales = *(const int*)(row + 288 + 4 * lg);
+  return f;
+}
+
+// Scores of 16 keys of a page (tile T) with 16 query rows, on top of `acc`.  The
+// scale operands' byte selectors are immediates.
+template <int T>
+__device__ __forceinline__ floatx4 score(const uint4& k, uint32_t ks, const Six& q, floatx4 acc) {
+  const int32x8 a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.part[0], acc, 4, 2, T, (int)ks, 0, q.scales);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.part[1], acc, 4, 2, T, (int)ks, 1, q.scales);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.part[2], acc, 4, 2, T, (int)ks, 2, q.scales);
+}
+
+// Scores are read by ordinary instructions some cycles after their product was
+// issued, and nothing but such a wait keeps those apart.  The compiler puts it in,
+// but counts it along one way only where a branch lies between (a page that needed
+// no cutting off was read too early, and rows came out as zeros).  So the wait
+// stands here, before any branch.
+__device__ __forceinline__ void settle(floatx4& a) { asm volatile("s_nop 7\n\ts_nop 3" : "+v"(a)); }
+__device__ __forceinline__ void settle(floatx4& a, floatx4& b) {
+  asm volatile("s_nop 7\n\ts_nop 3" : "+v"(a), "+v"(b));
+}
+__device__ __forceinline__ void settle(floatx4& a, floatx4& b, floatx4& c, floatx4& d) {
+  asm volatile("s_nop 7\n\ts_nop 3" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+}
+
+// Of 16 tree rows with 16 query rows, both in 6-bit parts: the products that
+// matter (a part is 2^-4 or less of the one before it).
+__device__ __forceinline__ floatx4 score_six(const Six& k, const Six& q, floatx4 acc) {
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[2], q.part[0], acc, 2, 2, 2, k.scales, 0, q.scales);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[1], q.part[1], acc, 2, 2, 1, k.scales, 1, q.scales);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[0], q.part[2], acc, 2, 2, 0, k.scales, 2, q.scales);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[1], q.part[0], acc, 2, 2, 1, k.scales, 0, q.scales);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[0], q.part[1], acc, 2, 2, 0, k.scales, 1, q.scales);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[0], q.part[0], acc, 2, 2, 0, k.scales, 0, q.scales);
+}
+
+// parts that a prefix is cut into, each of part_pages pages, and those that more
+// tree rows than one workgroup takes have to themselves
 __device__ __forceinline__ int parts_of(int pages, int part_pages) {
   return pages <= part_pages ? 1 : (pages + part_pages - 1) / part_pages;
 }
+__host__ __device__ __forceinline__ int more_parts(int n) { return n <= kTreeRows ? 0 : (n - 1) / kTreeRows; }
 
-// Rows of a (tree, key head): row r is tree row r / G, head r % G of the group.
-// A workgroup has WK groups of WR waves; a wave has NT tiles, wave w of a group
-// tiles w, w + WR.
-template <int NT, int WR, int WK>
-__global__ void __launch_bounds__(WR* WK* fc::kWave, 2) k_paged_attn(Args A) {
-  constexpr int kThreads = WR * WK * fc::kWave;
-  constexpr int kBufs = WR > 1 ? 2 : 1;  // waves that share values write one page's while they read another's
-  __shared__ __align__(16) uint8_t s_v[WK * kBufs * kValues];
-  __shared__ double s_freq[kHeadDim / 2];
-  __shared__ uint32_t s_bad[2][WK];  // tree rows of a block whose values are not all finite
-
-  const int tid = (int)threadIdx.x, lane = fc::lane_id();
-  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
-  const int grp = w / WR, wr = w - grp * WR;
-  const int lg = lane >> 4, lc = lane & 15;
-
-  // consecutive workgroups of one XCD share a key head's pages in its L2
-  const int total = (int)gridDim.x, x = (int)blockIdx.x;
-  const int lin = total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x;
-  const int chunk = lin % A.chunks, bk = lin / A.chunks;
-  const int b = bk / A.Hkv, kv = bk - b * A.Hkv;
-  const int G = A.H / A.Hkv, M = A.R * G;
-  const int tiles = (M + kTile - 1) / kTile;
-  const int tile0 = (int)((int64_t)tiles * chunk / A.chunks), tile1 = (int)((int64_t)tiles * (chunk + 1) / A.chunks);
-
-  const int P = clamp_len(A.prefix_len[b], A.max_len);
-  const int n = A.num_nodes ? clamp_len(A.num_nodes[b], A.R) : A.R;
-  const int pages = (P + kPage - 1) / kPage;
-  const int parts = parts_of(pages, A.part_pages), part = (int)blockIdx.y;
-  if (part >= parts) return;
-  const int pg0 = part * A.part_pages;
-  const int pg1 = parts == 1 ? pages : (pg0 + A.part_pages < pages ? pg0 + A.part_pages : pages);
-
-  if (tid < 2 * WK) s_bad[tid / WK][tid % WK] = 0;
-  if (A.log2_base > 0.0)
-    for (int d = tid; d < kHeadDim / 2; d += kThreads) s_freq[d] = exp2(-2.0 * d / (double)kHeadDim * A.log2_base);
-  __syncthreads();
-
-  // this wave's rows: tile, row of the matrix, tree row
-  int row[NT], tree_row[NT];
-  bool in[NT];
+// A query row's outputs (lane (lg, lc): dims 16 t + 4 lg + e of row lc), its
+// running maximum as 0 - m (0 while there is none), the sum of its weights, and by
+// how much a score may pass m before the row is scaled anew (-inf while there is
+// no m).
+struct Row {
+  floatx4 o[kDTiles];
+  floatx4 minus_m;
+  float l, slack;
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int t = tile0 + wr + WR * i;
-    row[i] = t * kTile + lc;
-    in[i] = t < tile1 && row[i] < M;
-    tree_row[i] = in[i] ? row[i] / G : 0;
+    for (int t = 0; t < kDTiles; ++t) o[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    minus_m = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    l = 0.0f;
+    slack = -INFINITY;
   }
-  const auto q_row = [&](int i) {
-    return A.q + ((int64_t)b * A.R + tree_row[i]) * A.q_stride + ((int64_t)kv * G + (row[i] - tree_row[i] * G)) * kHeadDim;
-  };
-  const auto position = [&](int r) { return P + (A.pos_ids ? A.pos_ids[(int64_t)b * A.R + r] : r); };
-  // scores are in units of log2: softmax weights are powers of two
-  const float scale = 1.44269504088896340736f / sqrtf((float)kHeadDim);
+  __device__ __forceinline__ float m() const { return slack == -INFINITY ? -INFINITY : 0.0f - minus_m[0]; }
+};
 
-  // Queries as three 6-bit parts: lane (lg, lc) holds dims 32 lg .. 32 lg + 31
-  // of row lc.  The first part's scale 2^e is the smallest with which the
-  // largest magnitude is at most 7.5; it leaves at most 2^-2 * 2^e, the second
-  // (scale 2^(e - 4)) at most 2^-7, the third (2^(e - 9)) at most 2^-12.
-  int32x8 qf[NT][kParts];
-  int qs[NT];
+// The softmax's usual step is a power of two, a sum and a rounding a score.  s
+// holds scores less m (the products start from minus_m), -inf where a key is not
+// allowed.  m is the maximum of what the row saw when it was last scaled: while no
+// score passes it by more than 8, weights stay below 2^8 and neither sums nor
+// outputs are touched (with bf16 weights a common factor costs no accuracy).
+template <int N>
+__device__ __forceinline__ float top_of(const floatx4 (&s)[N]) {
+  float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    float v[32];
-#pragma unroll
-    for (int u = 0; u < 32; ++u) v[u] = 0.0f;
-    if (in[i]) {
-      const uint16_t* p = q_row(i);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float own[8];
-        fc::unpack8(*(const uint4*)(p + 32 * lg + 8 * u), own);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * u + e] = own[e];
-      }
-      if (A.log2_base > 0.0) {
-        const int pos = position(tree_row[i]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          float other[8];
-          fc::unpack8(*(const uint4*)(p + ((32 * lg + 64) & 127) + 8 * u), other);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float s, c;
-            fc::rope_sincos(pos, s_freq[(32 * lg & 63) + 8 * u + e], s, c);
-            v[8 * u + e] = v[8 * u + e] * c + (lg < 2 ? -other[e] : other[e]) * s;
-          }
-        }
-      }
-    }
-    uint32_t top = 0;
-#pragma unroll
-    for (int u = 0; u < 32; ++u) {
-      v[u] *= scale;
-      const uint32_t bits = __float_as_uint(v[u]) & 0x7FFFFFFFu;
-      top = bits > top ? bits : top;
-    }
-    int e = (int)((top + 0x0FFFFFu) >> 23) - 127 - 2;  // 7.5 = 1.875 * 2^2
-    e = e < -110 ? -110 : e;
-    floatx16 even, odd;
-#pragma unroll
-    for (int u = 0; u < 16; ++u) even[u] = v[2 * u], odd[u] = v[2 * u + 1];
-    int word = 0;
-#pragma unroll
-    for (int s = 0; s < kParts; ++s) {
-      const int es = e - (s == 0 ? 0 : s == 1 ? 4 : 9);
-      const float f = __uint_as_float((uint32_t)(es + 127) << 23);
-      const int32x6 c = to_six(even, odd, f);
-#pragma unroll
-      for (int u = 0; u < 6; ++u) qf[i][s][u] = c[u];
-      qf[i][s][6] = qf[i][s][7] = 0;
-      if (s + 1 < kParts) {
-        const floatx32 r = from_six(c, f);
-#pragma unroll
-        for (int u = 0; u < 16; ++u) even[u] -= r[2 * u], odd[u] -= r[2 * u + 1];
-      }
-      word |= (top >= 0x7F800000u ? 255 : es + 127) << (8 * s);  // something not finite: NaN
-    }
-    qs[i] = word;
+  for (int t = 0; t < N; ++t) {
+    top = fmaxf(fmaxf(top, s[t][0]), s[t][1]);
+    top = fmaxf(fmaxf(top, s[t][2]), s[t][3]);
   }
-
-  floatx4 o[NT][kDTiles];
-  // a row's running maximum m, 0 - m (0 while there is none) four times, and by
-  // how much a score may pass m before the row is scaled anew
-  float m_run[NT], l_run[NT], slack[NT];
-  floatx4 minus_m[NT];
+  return top;
+}
+template <int N>
+__device__ __forceinline__ void raise(floatx4 (&s)[N], float top, Row& r) {
+  float mx = fmaxf(top, __shfl_xor(top, 16));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  // by how much m rises; a row that has no need keeps it, so that its result goes
+  // by its own scores alone
+  const float by = mx > r.slack ? mx : 0.0f;
+  const float alpha = r.slack == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-by);
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    m_run[i] = slack[i] = -INFINITY;
-    l_run[i] = 0.0f;
-    minus_m[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < N; ++t) s[t] -= by;
+  r.l *= alpha;
 #pragma unroll
-    for (int t = 0; t < kDTiles; ++t) o[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < kDTiles; ++t) r.o[t] *= alpha;
+  const float minus = r.minus_m[0] - by;
+  r.slack = mx > r.slack ? 8.0f : r.slack;
+  r.minus_m = floatx4{minus, minus, minus, minus};
+}
+template <int N>
+__device__ __forceinline__ void rescale(floatx4 (&s)[N], Row& r) {
+  const float top = top_of(s);
+  if (__any(top > r.slack)) raise(s, top, r);
+}
+// weights of 32 keys, in the lane layout of the value product's operand
+__device__ __forceinline__ bf16x8 weights(const floatx4& a, const floatx4& b, Row& r) {
+  bf16x8 pb;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float p = __builtin_amdgcn_exp2f(a[e]);
+    r.l += p;
+    pb[e] = (__bf16)p;
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float p = __builtin_amdgcn_exp2f(b[e]);
+    r.l += p;
+    pb[4 + e] = (__bf16)p;
+  }
+  return pb;
+}
 
-  // One step of the softmax.  s holds scores less m (the products start from
-  // minus_m), -inf where a key is not allowed.  m is the maximum of what a row
-  // saw when it was last scaled: while no score passes it by more than 8, weights
-  // stay below 2^8 and neither sums nor outputs are touched (with bf16 weights a
-  // common factor costs no accuracy), so the usual step is a power of two, a sum
-  // and a rounding for each score.
-  const auto softmax = [&](auto& s, auto& pb) {
-    constexpr int KT = sizeof(s[0]) / sizeof(s[0][0]);
-    bool up = false;
-    float top[NT];
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+// V^T of 32 keys, output tiles t0 and t0 + 1: a transposing read gives lane (lg,
+// lc) dims 16 t + lc of keys 4 lg + e, the second one of keys 16 + 4 lg + e, as the
+// weights lie.  `at` is this lane's place in the first of the 32 rows.  The fence
+// keeps reads ahead of what comes after them in the source.
+struct Frag {
+  bf16x4 lo[2], hi[2];
+};
+__device__ __forceinline__ void read_values(lds_u8* at, int t0, Frag& f) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      top[i] = -INFINITY;
+  for (int t = 0; t < 2; ++t) {
+    f.lo[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(0, 2 * (t0 + t))));
+    f.hi[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(16, 2 * (t0 + t))));
+  }
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void add_values(const Frag& f, int t0, const bf16x8& pb, Row& r) {
 #pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        top[i] = fmaxf(fmaxf(top[i], s[i][t][0]), s[i][t][1]);
-        top[i] = fmaxf(fmaxf(top[i], s[i][t][2]), s[i][t][3]);
+  for (int t = 0; t < 2; ++t) {
+    const bf16x8 a = {f.lo[t][0], f.lo[t][1], f.lo[t][2], f.lo[t][3], f.hi[t][0], f.hi[t][1], f.hi[t][2], f.hi[t][3]};
+    r.o[t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, r.o[t0 + t], 0, 0, 0);
+  }
+}
+__device__ __forceinline__ void all_values(lds_u8* at, const bf16x8& pb, Row& r) {
+  Frag f[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) read_values(at, 2 * u, f[u]);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) add_values(f[u], 2 * u, pb, r);
+}
+
+// 32 dims (16 bytes of codes, the scale in byte i4 of `scales`) of key i4 * 16 +
+// lane / 4 of a page's values, to bf16 in LDS.  A key past the prefix has weight 0,
+// and so that whatever its bytes hold does not matter its values are 0 too.
+__device__ __forceinline__ void unpack(const uint4& raw, uint32_t scales, int i4, int lane, int left, uint8_t* to) {
+  const int key = i4 * 16 + (lane >> 2), g = lane & 3;
+  uint32_t sb = (scales >> (8 * i4)) & 255u;
+  uint32_t c4[4] = {raw.x, raw.y, raw.z, raw.w};
+  if (left < kPage) {
+    const bool live = key < left;
+    sb = live ? sb : 127u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) c4[c] = live ? c4[c] : 0u;
+  }
+  const float sc = fc::scale_of(sb);
+  uint8_t* dst = to + chunk_at(key, 4 * g);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint4 d;
+    d.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 0));
+    d.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 1));
+    d.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 2));
+    d.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 3));
+    *(uint4*)(dst + 16 * c) = d;
+  }
+}
+
+// keys of a page's tile t that lie past the prefix do not count
+__device__ __forceinline__ void cut(floatx4& s, int t, int lg, int left) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = 16 * t + 4 * lg + e < left ? s[e] : -INFINITY;
+}
+
+// A pair's angle in revolutions a position, and its sine and cosine: reduced to
+// [0, 1) in double precision, so far positions keep full accuracy.
+__device__ __forceinline__ double angle_of(int d, double log2_base) {
+  return exp2(-2.0 * d / (double)kHeadDim * log2_base) * 0.15915494309189533577;
+}
+__device__ __forceinline__ float2 turn_of(double revolutions) {
+  const float f = (float)__builtin_amdgcn_fract(revolutions);
+  return make_float2(__builtin_amdgcn_sinf(f), __builtin_amdgcn_cosf(f));
+}
+__device__ __forceinline__ float score_scale() { return 1.44269504088896340736f / sqrtf((float)kHeadDim); }
+
+// What a workgroup works on.
+struct Work {
+  int bk, b, kv, G, M, P, n, part, parts, pg0, pg1, tree0;
+  bool tree;
+  __device__ __forceinline__ bool init(const Args& A, int bk_, int part_) {
+    bk = bk_, part = part_;
+    b = bk / A.Hkv, kv = bk - b * A.Hkv;
+    G = A.H / A.Hkv, M = A.R * G;
+    P = clamp_len(A.prefix_len[b], A.max_len);
+    n = A.num_nodes ? clamp_len(A.num_nodes[b], A.R) : A.R;
+    const int pages = (P + kPage - 1) / kPage, cached = parts_of(pages, A.part_pages);
+    parts = cached + more_parts(n);
+    if (part >= parts) return false;
+    // the last part of the prefix has the tree's first rows, the others their own parts
+    pg0 = part < cached ? part * A.part_pages : pages;
+    pg1 = part < cached - 1 ? pg0 + A.part_pages : pages;
+    tree0 = part < cached ? 0 : (part - cached + 1) * kTreeRows;
+    tree = part >= cached - 1 && n > 0;
+    return true;
+  }
+  __device__ __forceinline__ int position(const Args& A, int r) const {
+    return P + (A.pos_ids ? A.pos_ids[(int64_t)b * A.R + r] : r);
+  }
+  // rows past the last one: the last one, whose results nobody takes
+  __device__ __forceinline__ int row_at(int r) const { return r < M ? r : M - 1; }
+  __device__ __forceinline__ const uint16_t* q_row(const Args& A, int r) const {
+    const int tr = r / G;
+    return A.q + ((int64_t)b * A.R + tr) * A.q_stride + ((int64_t)kv * G + (r - tr * G)) * kHeadDim;
+  }
+  __device__ __forceinline__ const uint16_t* k_row(const Args& A, int j) const {
+    return A.k_tree + ((int64_t)b * A.R + j) * A.k_stride + (int64_t)kv * kHeadDim;
+  }
+  __device__ __forceinline__ const uint16_t* v_row(const Args& A, int j) const {
+    return A.v_tree + ((int64_t)b * A.R + j) * A.v_stride + (int64_t)kv * kHeadDim;
+  }
+  // bit 4 t + e, t < kt <= KT: query row tr may see tree row j0 + 16 t + 4 lg + e
+  template <int KT>
+  __device__ __forceinline__ uint32_t allowed(const Args& A, int tr, bool in, int j0, int lg) const {
+    uint32_t bits = 0;
+    const int32_t* mrow = A.mask ? A.mask + ((int64_t)b * A.R + tr) * A.R : nullptr;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const int j = j0 + 16 * t + 4 * lg;
+      if (j0 + 16 * t >= n) break;
+      int m[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = j + e <= tr;
+      if (mrow) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = mrow[j + e < n ? j + e : 0];
       }
-      up |= top[i] > slack[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bits |= (uint32_t)(in && j + e < n && m[e] == 1) << (4 * t + e);
     }
-    if (__any(up)) {
+    return bits;
+  }
+  // Values of 32 tree rows that are not finite are 0 in LDS: a product with weight
+  // 0 would be NaN, so the rows that do not see such a value must not meet it.  This
+  // adds them for the rows that do: bit j of `bad` marks row j0 + j, `see` holds
+  // the block's eight bits.
+  __device__ __forceinline__ void add_marked(const Args& A, uint32_t bad, int j0, const bf16x8& pb, uint32_t see,
+                                             int lg, int lc, Row& r) const {
+    for (; bad; bad &= bad - 1) {
+      const int j = __builtin_ctz(bad);
+      const int u = j / 16 * 4 + j % 4, from = j % 16 / 4 * 16 + lc;  // whose weights for row j these are
+      const uint16_t* vp = v_row(A, j0 + j) + 4 * lg;
+      float weight = 0.0f;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        float mx = fmaxf(top[i], __shfl_xor(top[i], 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float was = 0.0f - minus_m[i][0];
-        const float m_new = fmaxf(m_run[i], was + mx);
-        const float by = m_new == -INFINITY ? 0.0f : m_new - was;
-        const float alpha = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+      for (int e = 0; e < 8; ++e) weight = e == u ? (float)pb[e] : weight;
+      weight = __shfl(weight, from);
+      const bool sees = (__shfl(see, from) >> u) & 1u;
 #pragma unroll
-        for (int t = 0; t < KT; ++t) s[i][t] -= by;
-        l_run[i] *= alpha;
-#pragma unroll
-        for (int t = 0; t < kDTiles; ++t) o[i][t] *= alpha;
-        m_run[i] = m_new;
-        const float minus = m_new == -INFINITY ? 0.0f : -m_new;
-        minus_m[i] = floatx4{minus, minus, minus, minus};
-        slack[i] = m_new == -INFINITY ? -INFINITY : 8.0f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
+      for (int t = 0; t < kDTiles; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(s[i][t][e]);
-          l_run[i] += p;
-          pb[t / 2][i][4 * (t % 2) + e] = (__bf16)p;
+          const uint32_t x = (uint32_t)vp[16 * t + e] << 16;
+          r.o[t][e] += sees && (x & 0x7F800000u) == 0x7F800000u ? weight * __uint_as_float(x) : 0.0f;
         }
     }
-  };
-  // O^T += V^T P^T over 32 keys at byte `base` of the buffers: a transposing read
-  // gives lane (lg, lc) dims 16 t + lc of keys 4 lg + e, the second one keys 16 +
-  // 4 lg + e, as the weights lie
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
-  const uint32_t v_lane = lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u;
-  const auto values = [&](uint32_t base, const bf16x8 (&pb)[NT]) {
-    typedef __attribute__((address_space(3))) uint8_t lds_u8;
-    lds_u8* at = (lds_u8*)(uintptr_t)(v_lane + base);
+  }
+};
+
+// Rows of bf16 values to LDS, what is not finite marked in `bad` and 0; zeros from
+// row `left` on.
+template <typename Row16>
+__device__ __forceinline__ void stage_values(int first, int step, int rows, int left, Row16 row, uint8_t* to,
+                                             uint32_t* bad) {
+  for (int u = first; u < rows * 16; u += step) {
+    const int r = u / 16, c = u % 16;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (r < left) v = *(const uint4*)(row(r) + 8 * c);
+    if (keep_finite(v)) atomicOr(&bad[r / 32], 1u << (r % 32));
+    *(uint4*)(to + chunk_at(r, c)) = v;
+  }
+}
+
+// ---- waves that shared a tile's keys hand over to one of them, through LDS
+constexpr int kRec = kTile * kHeadDim + 2 * kTile;  // floats of a tile: outputs, maxima, weights
+__device__ __forceinline__ void whole(Row& r) {
+  r.l += __shfl_xor(r.l, 16);
+  r.l += __shfl_xor(r.l, 32);
+}
+__device__ __forceinline__ void give(const Row& r, float* rec) {
+  const int lane = fc::lane_id();
+#pragma unroll
+  for (int t = 0; t < kDTiles; ++t) *(floatx4*)(rec + (t * 64 + lane) * 4) = r.o[t];
+  if (lane < 16) rec[kTile * kHeadDim + lane] = r.m(), rec[kTile * kHeadDim + kTile + lane] = r.l;
+}
+__device__ __forceinline__ void take(Row& r, float& m, const float* rec) {
+  const int lane = fc::lane_id(), lc = lane & 15;
+  const float m2 = rec[kTile * kHeadDim + lc], l2 = rec[kTile * kHeadDim + kTile + lc];
+  const float both = fmaxf(m, m2);
+  const float a1 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - both);
+  const float a2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - both);
+  m = both;
+  r.l = r.l * a1 + l2 * a2;
+#pragma unroll
+  for (int t = 0; t < kDTiles; ++t) r.o[t] = r.o[t] * a1 + *(const floatx4*)(rec + (t * 64 + lane) * 4) * a2;
+}
+__device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& r, float m, int row) {
+  const int lg = fc::lane_id() >> 4;
+  if (W.parts > 1) {
+    const int64_t at = ((int64_t)W.bk * A.parts + W.part) * W.M + row;
+    if (lg == 0) A.part_ml[at] = make_float2(m, r.l);
+#pragma unroll
+    for (int t = 0; t < kDTiles; ++t) *(floatx4*)(A.part_o + at * kHeadDim + 16 * t + 4 * lg) = r.o[t];
+  } else {
+    // a row without a key has weight 0; a NaN stays one
+    const int tr = row / W.G;
+    const float inv = tr < W.n && r.l != 0.0f ? 1.0f / r.l : 0.0f;
+    uint16_t* dst = A.out + (((int64_t)W.b * A.R + tr) * A.H + W.kv * W.G + (row - tr * W.G)) * kHeadDim;
 #pragma unroll
     for (int t = 0; t < kDTiles; ++t) {
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(0, 2 * t)));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + chunk_at(16, 2 * t)));
-      const bf16x8 a = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      bf16x4 x;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) o[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[i], o[i][t], 0, 0, 0);
-    }
-  };
-
-  // a page on its way: every wave of a group loads the key codes it multiplies,
-  // and its share of the value codes (16 bytes a lane: 32 dims of a key)
-  constexpr int kVUnits = (4 + WR - 1) / WR;
-  uint4 kf[4], vf[kVUnits];
-  uint32_t ks, vs;
-  bool have;
-  const int32_t* table = A.table + (int64_t)b * A.max_pages;
-  const auto load = [&](int pg) {
-    const int id = pg < pg1 ? __builtin_amdgcn_readfirstlane(table[pg]) : -1;
-    have = id >= 0 && id < A.n_pages;
-    if (!have) return;
-    const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + kv) * kPageBytes;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) kf[t] = *(const uint4*)(page + (16 * t + lc) * fc::kCodeRow + 16 * lg);
-    ks = *(const uint32_t*)(page + fc::kPageKScale + 4 * lane);
-#pragma unroll
-    for (int u = 0; u < kVUnits; ++u)
-      if (wr + WR * u < 4) vf[u] = *(const uint4*)(page + fc::kPageV + ((wr + WR * u) * 64 + lane) * 16);
-    vs = *(const uint32_t*)(page + fc::kPageVScale + 4 * lane);
-  };
-  const int steps = (pg1 - pg0 + WK - 1) / WK;
-  load(pg0 + grp);
-  for (int it = 0; it < steps; ++it) {
-    const int pg = pg0 + it * WK + grp;
-    const int left = P - pg * kPage;  // keys of this page that exist, if below 64
-    const uint32_t buf = (uint32_t)(grp * kBufs + (kBufs > 1 ? it % kBufs : 0)) * kValues;
-    const bool use = have;
-    if (use) {
-      // values to bf16; a key past the prefix has weight 0, and so that
-      // whatever its bytes hold does not matter its values are 0 too
-#pragma unroll
-      for (int u = 0; u < kVUnits; ++u) {
-        const int i4 = wr + WR * u;
-        if (i4 < 4) {
-          const int key = i4 * 16 + (lane >> 2), g = lane & 3;
-          uint32_t sb = (vs >> (8 * i4)) & 255u;
-          uint32_t c4[4] = {vf[u].x, vf[u].y, vf[u].z, vf[u].w};
-          if (left < kPage) {
-            const bool live = key < left;
-            sb = live ? sb : 127u;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) c4[c] = live ? c4[c] : 0u;
-          }
-          const float sc = fc::scale_of(sb);
-          uint8_t* dst = s_v + buf + chunk_at(key, 4 * g);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint4 d;
-            d.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 0));
-            d.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 1));
-            d.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 2));
-            d.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c4[c], sc, 3));
-            *(uint4*)(dst + 16 * c) = d;
-          }
-        }
-      }
-    }
-    if (WR > 1) __syncthreads();
-    floatx4 s[NT][4];
-    if (use) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int32x8 a = {(int)kf[t].x, (int)kf[t].y, (int)kf[t].z, (int)kf[t].w, 0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          floatx4 acc = minus_m[i];
-          // the scale operands' byte selectors are immediates
-#define FC_PART(S, T) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, qf[i][S], acc, 4, 2, T, (int)ks, S, qs[i])
-          if (t == 0) { FC_PART(0, 0); FC_PART(1, 0); FC_PART(2, 0); }
-          if (t == 1) { FC_PART(0, 1); FC_PART(1, 1); FC_PART(2, 1); }
-          if (t == 2) { FC_PART(0, 2); FC_PART(1, 2); FC_PART(2, 2); }
-          if (t == 3) { FC_PART(0, 3); FC_PART(1, 3); FC_PART(2, 3); }
-#undef FC_PART
-          s[i][t] = acc;
-        }
-      }
-    }
-    load(pg + WK);
-    if (use) {
-      bf16x8 pb[2][NT];
-      if (left < kPage) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[i][t][e] = 16 * t + 4 * lg + e < left ? s[i][t][e] : -INFINITY;
-      }
-      softmax(s, pb);
-      values(buf, pb[0]);
-      values(buf + chunk_at(32, 0), pb[1]);
-    }
-  }
-
-  // the tree's own rows, in bf16, 32 at a time
-  if (part == parts - 1 && n > 0) {
-    bf16x8 qb[NT][4], ql[NT][4];  // rounded, and what that left over: only the key's rounding remains
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      float v[4][8];
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] = 0.0f;
-      if (in[i]) {
-        const uint16_t* p = q_row(i);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) fc::unpack8(*(const uint4*)(p + 32 * c + 8 * lg), v[c]);
-        if (A.log2_base > 0.0) {
-          const int pos = position(tree_row[i]);
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float sn, cs;
-              fc::rope_sincos(pos, s_freq[32 * c + 8 * lg + e], sn, cs);
-              const float x0 = v[c][e], x1 = v[c + 2][e];
-              v[c][e] = x0 * cs - x1 * sn;
-              v[c + 2][e] = x1 * cs + x0 * sn;
-            }
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = v[c][e] * scale;
-          qb[i][c][e] = (__bf16)x;
-          ql[i][c][e] = (__bf16)(x - (float)qb[i][c][e]);
-        }
-    }
-    const int blocks = (n + kTreeBlock - 1) / kTreeBlock;
-    uint8_t* sk = s_v + grp * kBufs * kValues;
-    uint8_t* sv = sk + kTreeBlock * kRowBytes;
-    for (int it = 0; it < (blocks + WK - 1) / WK; ++it) {
-      const int j0 = (it * WK + grp) * kTreeBlock;
-      __syncthreads();  // what was in the buffer has been read
-      for (int u = wr * fc::kWave + lane; u < kTreeBlock * 8; u += WR * fc::kWave) {
-        const int r = u / 8, c = u % 8, j = j0 + r;  // chunks c and c + 8 hold the pairs of a rotation
-        bf16x8 ka, kb;
-        uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
-        float x0[8], x1[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x0[e] = x1[e] = 0.0f;
-        if (j < n) {
-          const uint16_t* kp = A.k_tree + ((int64_t)b * A.R + j) * A.k_stride + (int64_t)kv * kHeadDim + 8 * c;
-          const uint16_t* vp = A.v_tree + ((int64_t)b * A.R + j) * A.v_stride + (int64_t)kv * kHeadDim + 8 * c;
-          fc::unpack8(*(const uint4*)kp, x0);
-          fc::unpack8(*(const uint4*)(kp + kHeadDim / 2), x1);
-          v0 = *(const uint4*)vp;
-          v1 = *(const uint4*)(vp + kHeadDim / 2);
-          const bool bad0 = keep_finite(v0), bad1 = keep_finite(v1);
-          if (bad0 || bad1) atomicOr(&s_bad[it & 1][grp], 1u << r);
-          if (A.log2_base > 0.0) {
-            const int pos = position(j);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float sn, cs;
-              fc::rope_sincos(pos, s_freq[8 * c + e], sn, cs);
-              const float a0 = x0[e], a1 = x1[e];
-              x0[e] = a0 * cs - a1 * sn;
-              x1[e] = a1 * cs + a0 * sn;
-            }
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ka[e] = (__bf16)x0[e], kb[e] = (__bf16)x1[e];
-        *(bf16x8*)(sk + chunk_at(r, c)) = ka;
-        *(bf16x8*)(sk + chunk_at(r, c + 8)) = kb;
-        *(uint4*)(sv + chunk_at(r, c)) = v0;
-        *(uint4*)(sv + chunk_at(r, c + 8)) = v1;
-      }
-      __syncthreads();
-      if (j0 < n) {
-        floatx4 s[NT][2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-          for (int i = 0; i < NT; ++i) s[i][t] = minus_m[i];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const bf16x8 a = *(const bf16x8*)(sk + chunk_at(16 * t + lc, 4 * c + lg));
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-              s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ql[i][c], s[i][t], 0, 0, 0);
-              s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qb[i][c], s[i][t], 0, 0, 0);
-            }
-          }
-        }
-        bf16x8 pb[1][NT];
-        uint32_t allowed[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          // bit 4 t + e: this lane's e-th key of tile t is allowed
-          uint32_t allow = 0;
-          if (in[i]) {
-            const int32_t* mrow = A.mask ? A.mask + ((int64_t)b * A.R + tree_row[i]) * A.R : nullptr;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const int j = j0 + 16 * (u / 4) + 4 * lg + u % 4;
-              if (j < n && (mrow ? mrow[j] == 1 : j <= tree_row[i])) allow |= 1u << u;
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < 8; ++u) s[i][u / 4][u % 4] = (allow >> u) & 1u ? s[i][u / 4][u % 4] : -INFINITY;
-          allowed[i] = allow;
-        }
-        softmax(s, pb);
-        values((uint32_t)(grp * kBufs * kValues + kTreeBlock * kRowBytes), pb[0]);
-        // A product with weight 0 is NaN where the value is not finite, so the
-        // rows that do not see such a value must not meet it: it is 0 in LDS, and
-        // the rows that do see it add it here.
-        for (uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[it & 1][grp]); bad; bad &= bad - 1) {
-          const int r = __builtin_ctz(bad);
-          const int u = r / 16 * 4 + r % 4, from = r % 16 / 4 * 16 + lc;  // whose weights for key r these are
-          const uint16_t* vp = A.v_tree + ((int64_t)b * A.R + j0 + r) * A.v_stride + (int64_t)kv * kHeadDim + 4 * lg;
-#pragma unroll
-          for (int i = 0; i < NT; ++i) {
-            float weight = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e == u) weight = (float)pb[0][i][e];
-            weight = __shfl(weight, from);
-            const bool sees = (__shfl(allowed[i], from) >> u) & 1u;
-#pragma unroll
-            for (int t = 0; t < kDTiles; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t bits = (uint32_t)vp[16 * t + e] << 16;
-                if (sees && (bits & 0x7F800000u) == 0x7F800000u) o[i][t][e] += weight * __uint_as_float(bits);
-              }
-          }
-        }
-      }
-      if (wr == 0 && lane == 0) s_bad[(it & 1) ^ 1][grp] = 0;  // of the block before, whose readers are past the barrier
-    }
-  }
-
-  // the row's whole weight
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    l_run[i] += __shfl_xor(l_run[i], 16);
-    l_run[i] += __shfl_xor(l_run[i], 32);
-  }
-
-  // groups that took other pages hand over to group 0, through LDS
-  if constexpr (WK > 1) {
-    constexpr int kRec = kTile * kHeadDim + 2 * kTile;  // floats of a tile: outputs, maxima, weights
-    static_assert((WK - 1) * WR * NT * kRec * 4 <= WK * kBufs * kValues, "hand-over fits the value buffers");
-    float* rec = (float*)s_v;
-    __syncthreads();
-    if (grp > 0) {
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        float* r = rec + (((grp - 1) * WR + wr) * NT + i) * kRec;
-#pragma unroll
-        for (int t = 0; t < kDTiles; ++t) *(floatx4*)(r + (t * 64 + lane) * 4) = o[i][t];
-        if (lg == 0) r[kTile * kHeadDim + lc] = m_run[i], r[kTile * kHeadDim + kTile + lc] = l_run[i];
-      }
-    }
-    __syncthreads();
-    if (grp > 0) return;
-#pragma unroll
-    for (int g = 1; g < WK; ++g)
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const float* r = rec + (((g - 1) * WR + wr) * NT + i) * kRec;
-        const float m2 = r[kTile * kHeadDim + lc], l2 = r[kTile * kHeadDim + kTile + lc];
-        const float m = fmaxf(m_run[i], m2);
-        const float a1 = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m);
-        const float a2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - m);
-        m_run[i] = m;
-        l_run[i] = l_run[i] * a1 + l2 * a2;
-#pragma unroll
-        for (int t = 0; t < kDTiles; ++t) o[i][t] = o[i][t] * a1 + *(const floatx4*)(r + (t * 64 + lane) * 4) * a2;
-      }
-  }
-
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    if (!in[i]) continue;
-    if (parts > 1) {
-      const int64_t at = ((int64_t)bk * A.parts + part) * M + row[i];
-      if (lg == 0) A.part_ml[at] = make_float2(m_run[i], l_run[i]);
-#pragma unroll
-      for (int t = 0; t < kDTiles; ++t) *(floatx4*)(A.part_o + at * kHeadDim + 16 * t + 4 * lg) = o[i][t];
-    } else {
-      // a row without a key has weight 0; a NaN stays one
-      const float inv = tree_row[i] < n && l_run[i] != 0.0f ? 1.0f / l_run[i] : 0.0f;
-      uint16_t* dst = A.out + (((int64_t)b * A.R + tree_row[i]) * A.H + kv * G + (row[i] - tree_row[i] * G)) * kHeadDim;
-#pragma unroll
-      for (int t = 0; t < kDTiles; ++t) {
-        bf16x4 r;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = inv == 0.0f ? (__bf16)0.0f : (__bf16)(o[i][t][e] * inv);
-        *(bf16x4*)(dst + 16 * t + 4 * lg) = r;
-      }
+      for (int e = 0; e < 4; ++e) x[e] = inv == 0.0f ? (__bf16)0.0f : (__bf16)(r.o[t][e] * inv);
+      *(bf16x4*)(dst + 16 * t + 4 * lg) = x;
     }
   }
 }
 
+// Up to five tiles of query rows.  A wave has two tiles and a part of each page's
+// keys: with KS 2 a pair of tiles for each two waves and 32 keys for each wave,
+// with KS 4 one pair of tiles and 16 keys.  (Two tiles share what they read of a
+// page's values, which is most of what goes through LDS.)  kFive: a fifth tile
+// besides, 16 keys for each wave.
+template <int KS, bool kFive>
+__device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_v, double* s_freq, uint32_t* s_bad,
+                                       int tile0, int tiles) {
+  static_assert(!kFive || KS == 2, "the fifth tile goes with two pairs");
+  constexpr int NB = KS == 2 ? 2 : 1;  // blocks of 32 tree rows of a wave, at most
+  const int tid = (int)threadIdx.x, lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
+  const int pair = KS == 2 ? w & 1 : 0, ks = KS == 2 ? w >> 1 : w;
+  const int lg = lane >> 4, lc = lane & 15;
+  const bool rotate = A.log2_base > 0.0;
+  int row[2];
+  bool in[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    row[i] = (tile0 + 2 * pair + i) * kTile + lc;
+    in[i] = 2 * pair + i < tiles && row[i] < W.M;
+  }
+  const bool five = kFive && tiles > kWaves;
+  const int row5 = (tile0 + kWaves) * kTile + lc;
+  const bool in5 = five && row5 < W.M;
+
+  // ---- queries, in 6-bit parts: a thread for each group of a row, through LDS
+  if (rotate && tid < kHeadDim / 2) s_freq[tid] = angle_of(tid, A.log2_base);
+  __syncthreads();
+  const auto stage_rows = [&](int rows, auto src, auto at, float by) {
+    for (int u = tid; u < 4 * rows; u += kThreads) {
+      const int r = u >> 2, g = group_of(u & 3);
+      const double pos = rotate ? (double)at(r) : 0.0;
+      stage_six(src(r), g, by, rotate, [&](int e) { return turn_of(pos * s_freq[32 * (g & 1) + e]); }, s_v + r * kSixRow);
+    }
+  };
+  stage_rows(
+      kTile * tiles, [&](int r) { return W.q_row(A, W.row_at(tile0 * kTile + r)); },
+      [&](int r) { return W.position(A, W.row_at(tile0 * kTile + r) / W.G); }, score_scale());
+  __syncthreads();
+  Six q[2], q5;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    q[i] = read_six(s_v + (kTile * (2 * pair + i < tiles ? 2 * pair + i : 0) + lc) * kSixRow, lg);
+  if (kFive) q5 = read_six(s_v + (kTile * (five ? kWaves : 0) + lc) * kSixRow, lg);
+  __syncthreads();  // the rows are read: their place is free
+
+  // ---- pages on their way: straight from memory into LDS as they lie (16 bytes
+  // a lane, no registers), one while another is used
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
+  const int32_t* table = A.table + (int64_t)W.b * A.max_pages;
+  // page numbers, 64 at a time in a register's lanes: read one by one they would
+  // be loads to wait for among the loads that are meant to stay in flight
+  int ids = 0;
+  bool coming = false;
+  const auto issue = [&](int pg) {
+    const int i = (pg - W.pg0) & 63;
+    if (i == 0) ids = pg + lane < W.pg1 ? table[pg + lane] : -1;
+    const int id = __builtin_amdgcn_readlane(ids, i);
+    coming = id >= 0 && id < A.n_pages;  // an absent page's loads give zeros, and none of its keys counts
+    const fc::int32x4 rsrc = fc::buffer_rsrc(A.pool + ((int64_t)(coming ? id : 0) * A.Hkv + W.kv) * kPageBytes,
+                                             coming ? (uint32_t)kPageBytes : 0u);
+    const uint32_t to = lds0 + (uint32_t)((pg - W.pg0) & 1 ? kSlot1 : kSlot0);
+    fc::lds_load16(to + (uint32_t)w * 1024u, (uint32_t)(w * 1024 + lane * 16), rsrc);
+    fc::lds_load16(to + (uint32_t)(w + 4) * 1024u, (uint32_t)((w + 4) * 1024 + lane * 16), rsrc);
+    if (w == 0) fc::lds_load16(to + 8u * 1024u, (uint32_t)(8 * 1024 + lane * 16), rsrc);
+  };
+  if (W.pg0 < W.pg1) issue(W.pg0);
+
+  lds_u8* const v_lane = (lds_u8*)(uintptr_t)(lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u);
+  Row me[2], extra;
+  me[0].clear();
+  me[1].clear();
+  if (kFive) extra.clear();
+
+  // ---- the tree's own rows: keys in 6-bit parts as the queries, values in bf16.
+  // Block k of 32 of them is for the waves with ks = k % KS; the second pair of
+  // waves has the fifth tile.
+  if (W.tree) {
+    const int left = W.n - W.tree0 < kTreeRows ? W.n - W.tree0 : kTreeRows;
+    if (tid < kTreeTiles / 2) s_bad[tid] = 0;
+    stage_rows(left, [&](int r) { return W.k_row(A, W.tree0 + r); }, [&](int r) { return W.position(A, W.tree0 + r); },
+               1.0f);
+    asm volatile("" ::: "memory");
+    const bool also = five && pair == 1;
+    uint32_t bits[3];  // eight for each block
+#pragma unroll
+    for (int i = 0; i < 3; ++i) bits[i] = 0;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int j0 = W.tree0 + 32 * (ks + KS * k);
+      if (32 * (ks + KS * k) >= left) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bits[i] |= W.template allowed<2>(A, in[i] ? row[i] / W.G : 0, in[i], j0, lg) << (8 * k);
+      if (also) bits[2] |= W.template allowed<2>(A, in5 ? row5 / W.G : 0, in5, j0, lg) << (8 * k);
+    }
+    __syncthreads();
+    bf16x8 pb[3][NB];
+    const auto tree_weights = [&](const Six& qq, uint32_t see, Row& r, bf16x8 (&p)[NB]) {
+      floatx4 s[2 * NB];
+#pragma unroll
+      for (int t = 0; t < 2 * NB; ++t) {
+        const int at = 32 * (ks + KS * (t / 2)) + 16 * (t % 2);
+        s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (at < left) s[t] = score_six(read_six(s_v + (at + lc) * kSixRow, lg), qq, r.minus_m);
+      }
+#pragma unroll
+      for (int k = 0; k < NB; ++k) settle(s[2 * k], s[2 * k + 1]);
+#pragma unroll
+      for (int u = 0; u < 8 * NB; ++u) s[u / 4][u % 4] = (see >> u) & 1u ? s[u / 4][u % 4] : -INFINITY;
+      rescale(s, r);
+#pragma unroll
+      for (int k = 0; k < NB; ++k) p[k] = weights(s[2 * k], s[2 * k + 1], r);
+    };
+    tree_weights(q[0], bits[0], me[0], pb[0]);
+    tree_weights(q[1], bits[1], me[1], pb[1]);
+    if (also) tree_weights(q5, bits[2], extra, pb[2]);
+    __syncthreads();  // the keys are read
+    stage_values(tid, kThreads, (left + 31) / 32 * 32, left, [&](int r) { return W.v_row(A, W.tree0 + r); }, s_v, s_bad);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int at = 32 * (ks + KS * k);
+      if (at >= left) break;
+      const uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[at / 32]);
+      Frag f[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) read_values(v_lane + chunk_at(1, 0) * at, 2 * u, f[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        add_values(f[u], 2 * u, pb[0][k], me[0]);
+        add_values(f[u], 2 * u, pb[1][k], me[1]);
+        if (also) add_values(f[u], 2 * u, pb[2][k], extra);
+      }
+      if (bad) {
+        W.add_marked(A, bad, W.tree0 + at, pb[0][k], bits[0] >> (8 * k), lg, lc, me[0]);
+        W.add_marked(A, bad, W.tree0 + at, pb[1][k], bits[1] >> (8 * k), lg, lc, me[1]);
+        if (also) W.add_marked(A, bad, W.tree0 + at, pb[2][k], bits[2] >> (8 * k), lg, lc, extra);
+      }
+    }
+  }
+
+  // ---- the prefix.  Between two barriers the waves unpack the page's values, a
+  // quarter each, and have their scores.
+  lds_u8* const v_mine = v_lane + chunk_at(KS == 2 ? 32 : 16, 0) * ks;
+  for (int pg = W.pg0; pg < W.pg1; ++pg) {
+    const int left = coming ? W.P - pg * kPage : 0;  // keys that exist, if below 64
+    const uint8_t* raw = s_v + ((pg - W.pg0) & 1 ? kSlot1 : kSlot0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the page is there; the values and the slot before it are free
+    if (pg + 1 < W.pg1) issue(pg + 1);
+    const uint32_t vs = *(const uint32_t*)(raw + fc::kPageVScale + 4 * lane);
+    const uint4 vraw = *(const uint4*)(raw + fc::kPageV + (w * 64 + lane) * 16);
+    const uint32_t kscales = *(const uint32_t*)(raw + fc::kPageKScale + 4 * lane);
+    const auto key = [&](int t) { return *(const uint4*)(raw + (16 * t + lc) * fc::kCodeRow + 16 * lg); };
+    if constexpr (KS == 2) {
+      const uint32_t mine = kscales >> (16 * ks);
+      const uint4 k0 = key(2 * ks), k1 = key(2 * ks + 1);
+      floatx4 s[2][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s[i][0] = score<0>(k0, mine, q[i], me[i].minus_m);
+        s[i][1] = score<1>(k1, mine, q[i], me[i].minus_m);
+      }
+      floatx4 s5[1] = {floatx4{0.0f, 0.0f, 0.0f, 0.0f}};
+      if (kFive && five) s5[0] = pair ? score<1>(k1, mine, q5, extra.minus_m) : score<0>(k0, mine, q5, extra.minus_m);
+      unpack(vraw, vs, w, lane, left, s_v);
+      settle(s[0][0], s[0][1], s[1][0], s[1][1]);
+      if (kFive) settle(s5[0]);
+      if (left < kPage) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) cut(s[i][0], 2 * ks, lg, left), cut(s[i][1], 2 * ks + 1, lg, left);
+        if (kFive && five) cut(s5[0], 2 * ks + pair, lg, left);
+      }
+      const float top0 = top_of(s[0]), top1 = top_of(s[1]);
+      if (__any(top0 > me[0].slack || top1 > me[1].slack)) {
+        raise(s[0], top0, me[0]);
+        raise(s[1], top1, me[1]);
+      }
+      bf16x8 pb5;
+      if (kFive && five) {
+        rescale(s5, extra);
+        __bf16 p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(s5[0][e]);
+          extra.l += x;
+          p[e] = (__bf16)x;
+        }
+        const __bf16 none = (__bf16)0.0f;
+        pb5 = pair ? bf16x8{none, none, none, none, p[0], p[1], p[2], p[3]}
+                   : bf16x8{p[0], p[1], p[2], p[3], none, none, none, none};
+      }
+      __syncthreads();  // the values are there
+      Frag f[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) read_values(v_mine, 2 * u, f[u]);
+      const bf16x8 p0 = weights(s[0][0], s[0][1], me[0]), p1 = weights(s[1][0], s[1][1], me[1]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        add_values(f[u], 2 * u, p0, me[0]);
+        add_values(f[u], 2 * u, p1, me[1]);
+        if (kFive && five) add_values(f[u], 2 * u, pb5, extra);
+      }
+    } else {
+      const uint4 k0 = key(ks);
+      floatx4 s[2][1];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s[i][0] = score<0>(k0, kscales >> (8 * ks), q[i], me[i].minus_m);
+      unpack(vraw, vs, w, lane, left, s_v);
+      settle(s[0][0], s[1][0]);
+      if (left < kPage) cut(s[0][0], ks, lg, left), cut(s[1][0], ks, lg, left);
+      rescale(s[0], me[0]);
+      rescale(s[1], me[1]);
+      __syncthreads();
+      bf16x4 lo[kDTiles], p[2];
+#pragma unroll
+      for (int t = 0; t < kDTiles; ++t)
+        lo[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(v_mine + chunk_at(0, 2 * t)));
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(s[i][0][e]);
+          me[i].l += x;
+          p[i][e] = (__bf16)x;
+        }
+#pragma unroll
+      for (int t = 0; t < kDTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          me[i].o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, lo[t]),
+                                                                 __builtin_bit_cast(shortx4, p[i]), me[i].o[t], 0, 0, 0);
+    }
+  }
+
+  // ---- the waves with the first keys take the others' rows, one tile after another
+  float* rec = (float*)s_v;
+  static_assert(((KS - 1) * (kWaves / KS) + 0) * kRec * 4 <= kLds && 3 * kRec * 4 <= kLds, "hand-over fits");
+  constexpr int kPairs = kWaves / KS;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    whole(me[i]);
+    float m = me[i].m();
+    __syncthreads();
+    if (ks > 0) give(me[i], rec + ((ks - 1) * kPairs + pair) * kRec);
+    __syncthreads();
+    if (ks == 0) {
+#pragma unroll
+      for (int g = 1; g < KS; ++g) take(me[i], m, rec + ((g - 1) * kPairs + pair) * kRec);
+      if (in[i]) finish(A, W, me[i], m, row[i]);
+    }
+  }
+  if (kFive && five) {
+    whole(extra);
+    float m = extra.m();
+    __syncthreads();
+    if (w > 0) give(extra, rec + (w - 1) * kRec);
+    __syncthreads();
+    if (w == 0) {
+#pragma unroll
+      for (int g = 0; g < kWaves - 1; ++g) take(extra, m, rec + g * kRec);
+      if (in5) finish(A, W, extra, m, row5);
+    }
+  }
+}
+
+template <bool kFive>
+__global__ void __launch_bounds__(kThreads, 2) k_paged_attn(Args A) {
+  __shared__ __align__(16) uint8_t s_v[kLds];
+  __shared__ double s_freq[kHeadDim / 2];
+  __shared__ uint32_t s_bad[kTreeTiles / 2];  // tree rows whose values are not all finite
+  // consecutive workgroups of one XCD share a key head's pages in its L2
+  const int total = (int)gridDim.x, x = (int)blockIdx.x;
+  const int lin = total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x;
+  const int chunk = lin % A.chunks;
+  Work W;
+  if (!W.init(A, lin / A.chunks, (int)blockIdx.y)) return;
+  const int tile0 = chunk * kWaves, all = (W.M + kTile - 1) / kTile;
+  const int tiles = chunk == A.chunks - 1 ? all - tile0 : kWaves;  // up to five with kFive
+  if (kFive || tiles > 2) attend<2, kFive>(A, W, s_v, s_freq, s_bad, tile0, tiles);
+  else attend<4, false>(A, W, s_v, s_freq, s_bad, tile0, tiles);
+}
+
+// One tile of query rows: the four waves go through every fourth page alone, two
+// pages on their way in a wave's registers, and wait for nobody until the end.
+__global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
+  __shared__ __align__(16) uint8_t s_v[kWaves * kValues];
+  __shared__ uint32_t s_bad[1];
+  const int tid = (int)threadIdx.x, lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
+  const int lg = lane >> 4, lc = lane & 15;
+  const int total = (int)gridDim.x, x = (int)blockIdx.x;
+  Work W;
+  if (!W.init(A, total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x, (int)blockIdx.y)) return;
+  const bool rotate = A.log2_base > 0.0, in = lc < W.M;
+
+  struct Page {
+    uint4 kf[4], vf[4];
+    uint32_t ks, vs;
+    bool have;
+  };
+  const int32_t* table = A.table + (int64_t)W.b * A.max_pages;
+  int pg_next = W.pg0 + w, ids = 0;
+  const auto load = [&](Page& p) {
+    // page numbers of 64 steps at a time, in a register's lanes
+    const int i = ((pg_next - W.pg0) / kWaves) & 63;
+    if (i == 0) ids = pg_next + kWaves * lane < W.pg1 ? table[pg_next + kWaves * lane] : -1;
+    const int id = __builtin_amdgcn_readlane(ids, i);
+    pg_next += kWaves;
+    p.have = id >= 0 && id < A.n_pages;
+    if (!p.have) return;
+    const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + W.kv) * kPageBytes;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) p.kf[t] = *(const uint4*)(page + (16 * t + lc) * fc::kCodeRow + 16 * lg);
+    p.ks = *(const uint32_t*)(page + fc::kPageKScale + 4 * lane);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) p.vf[t] = *(const uint4*)(page + fc::kPageV + (t * 64 + lane) * 16);
+    p.vs = *(const uint32_t*)(page + fc::kPageVScale + 4 * lane);
+  };
+  Page even, odd;
+  load(even);
+  load(odd);
+
+  // Meanwhile the few query and tree rows (16 at most): sines and cosines of every
+  // position once, then a lane for a quarter of each row.  Wave 0 has the tree's
+  // rows in its buffer, the others' hold the rest until their pages come.
+  uint8_t *six_k = s_v, *tree_v = s_v + kTile * kSixRow, *six_q = s_v + kValues;
+  float2* turns = (float2*)(s_v + 2 * kValues);
+  if (tid == 0) s_bad[0] = 0;
+  if (rotate) {
+    const double f = angle_of(lane, A.log2_base);
+    for (int r = w; r < A.R; r += kWaves) turns[r * 64 + lane] = turn_of((double)W.position(A, r) * f);
+  }
+  __syncthreads();
+  if (W.tree) stage_values(tid, kThreads, 32, W.n, [&](int r) { return W.v_row(A, r); }, tree_v, s_bad);
+  if (w == 0 || (w == 1 && W.tree && (lane >> 2) < W.n)) {
+    const int r = lane >> 2, g = group_of(lane & 3), qr = W.row_at(r), tr = w == 0 ? qr / W.G : r;
+    stage_six(w == 0 ? W.q_row(A, qr) : W.k_row(A, r), g, w == 0 ? score_scale() : 1.0f, rotate,
+              [&](int e) { return turns[tr * 64 + 32 * (g & 1) + e]; }, (w == 0 ? six_q : six_k) + r * kSixRow);
+  }
+  __syncthreads();
+  const Six q = read_six(six_q + lc * kSixRow, lg);
+  __syncthreads();
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
+  lds_u8* const v_lane = (lds_u8*)(uintptr_t)(lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u);
+  Row me;
+  me.clear();
+  if (W.tree && w == 0) {
+    const uint32_t see = W.allowed<1>(A, in ? lc / W.G : 0, in, 0, lg);
+    floatx4 s[2];
+    s[0] = score_six(read_six(six_k + lc * kSixRow, lg), q, me.minus_m);
+    settle(s[0]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[0][e] = (see >> e) & 1u ? s[0][e] : -INFINITY;
+      s[1][e] = -INFINITY;
+    }
+    rescale(s, me);
+    const bf16x8 pb = weights(s[0], s[1], me);
+    all_values(v_lane + kTile * kSixRow, pb, me);
+    const uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[0]);
+    if (bad) W.add_marked(A, bad, 0, pb, see, lg, lc, me);
+  }
+  uint8_t* mine = s_v + w * kValues;
+  lds_u8* const v_mine = v_lane + w * kValues;
+  const auto step = [&](Page& p, int pg) {
+    const int left = W.P - pg * kPage;
+    if (!p.have) {
+      load(p);
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) unpack(p.vf[t], p.vs, t, lane, left, mine);
+    floatx4 s[4];
+    s[0] = score<0>(p.kf[0], p.ks, q, me.minus_m);
+    s[1] = score<1>(p.kf[1], p.ks, q, me.minus_m);
+    s[2] = score<2>(p.kf[2], p.ks, q, me.minus_m);
+    s[3] = score<3>(p.kf[3], p.ks, q, me.minus_m);
+    load(p);
+    settle(s[0], s[1], s[2], s[3]);
+    if (left < kPage) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) cut(s[t], t, lg, left);
+    }
+    rescale(s, me);
+    all_values(v_mine, weights(s[0], s[1], me), me);
+    all_values(v_mine + chunk_at(32, 0), weights(s[2], s[3], me), me);
+  };
+  for (int pg = W.pg0 + w; pg < W.pg1; pg += 2 * kWaves) {
+    step(even, pg);
+    step(odd, pg + kWaves);
+  }
+
+  whole(me);
+  float m = me.m();
+  float* rec = (float*)s_v;
+  __syncthreads();
+  if (w > 0) give(me, rec + (w - 1) * kRec);
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int g = 0; g < kWaves - 1; ++g) take(me, m, rec + g * kRec);
+  if (in) finish(A, W, me, m, lc);
+}
+
 // The parts of a row put together: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m)
-// l_s with m the largest m_s.  16 lanes per row, eight dims each.  A prefix in
-// one part is in place already.
-__global__ void __launch_bounds__(256) k_paged_merge(Args A) {
+// l_s with m the largest m_s.  A wave per row: a lane has the weight of one or two
+// parts, then each 16 lanes add up every fourth part, eight dims a lane.  A prefix
+// in one part is in place already.
+constexpr int kMergeWaves = 4;
+__global__ void __launch_bounds__(kMergeWaves* fc::kWave) k_paged_merge(Args A) {
   const int G = A.H / A.Hkv, M = A.R * G;
-  const int blocks = (M + 15) / 16, bk = (int)blockIdx.x / blocks, b = bk / A.Hkv, kv = bk - b * A.Hkv;
-  const int r = ((int)blockIdx.x - bk * blocks) * 16 + (int)(threadIdx.x / 16), d = 8 * (int)(threadIdx.x % 16);
-  if (r >= M) return;
+  const int lane = fc::lane_id();
+  const int64_t at = (int64_t)blockIdx.x * kMergeWaves + (int)(threadIdx.x / fc::kWave);  // (tree, key head, row)
+  if (at >= (int64_t)A.B * A.Hkv * M) return;
+  const int64_t bk = at / M;
+  const int r = (int)(at - bk * M), b = (int)(bk / A.Hkv), kv = (int)(bk - (int64_t)b * A.Hkv);
   const int P = clamp_len(A.prefix_len[b], A.max_len);
-  const int parts = parts_of((P + kPage - 1) / kPage, A.part_pages);
-  if (parts == 1) return;
   const int n = A.num_nodes ? clamp_len(A.num_nodes[b], A.R) : A.R;
-  const int64_t at = (int64_t)bk * A.parts * M + r;
-  float m = -INFINITY, l = 0.0f;
-  for (int s = 0; s < parts; ++s) m = fmaxf(m, A.part_ml[at + (int64_t)s * M].x);
+  const int parts = parts_of((P + kPage - 1) / kPage, A.part_pages) + more_parts(n);
+  if (parts == 1) return;
+  const int64_t at0 = bk * A.parts * M + r;
+  const float2 none = make_float2(-INFINITY, 0.0f);
+  const float2 x = lane < parts ? A.part_ml[at0 + (int64_t)lane * M] : none;
+  const float2 y = lane + 64 < parts ? A.part_ml[at0 + (int64_t)(lane + 64) * M] : none;
+  float m = fmaxf(x.x, y.x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float wx = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);  // 0: a part without a key
+  const float wy = y.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y.x - m);
+  float l = wx * x.y + wy * y.y;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  const int d = 8 * (lane & 15);
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-  for (int s = 0; s < parts; ++s) {
-    const float2 ml = A.part_ml[at + (int64_t)s * M];
-    const float* po = A.part_o + (at + (int64_t)s * M) * kHeadDim + d;
-    const float w = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
-    l += w * ml.y;
+  for (int s0 = 0; s0 < parts; s0 += 16) {
+    floatx4 lo[4], hi[4];
+    float w[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += w * po[e];
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + 4 * u + (lane >> 4), i = s < parts ? s : parts - 1;
+      const float* po = A.part_o + (at0 + (int64_t)i * M) * kHeadDim + d;
+      lo[u] = *(const floatx4*)po;
+      hi[u] = *(const floatx4*)(po + 4);
+      const float ww = __shfl(wx, i & 63);
+      const float w2 = __shfl(wy, i & 63);
+      w[u] = s < parts ? (i < 64 ? ww : w2) : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[e] += w[u] * lo[u][e];
+        acc[4 + e] += w[u] * hi[u][e];
+      }
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    acc[e] += __shfl_xor(acc[e], 16);
+    acc[e] += __shfl_xor(acc[e], 32);
+  }
+  if (lane >= 16) return;
   const int i = r / G;
   const float inv = i < n && l != 0.0f ? 1.0f / l : 0.0f;
   bf16x8 res;
@@ -642,31 +1018,32 @@ __global__ void __launch_bounds__(256) k_paged_merge(Args A) {
 }
 
 struct Shape {
-  int nt, wr, wk, chunks, part_pages, parts;
+  int chunks, part_pages, parts;
+  bool alone, five;
 };
 
-// How a call is laid out.  Up to 128 query rows of a key head stay in one
-// workgroup, which then reads its pages once; waves that the rows do not need
-// are split over the pages.
+// How a call is laid out: a workgroup for every four tiles of query rows of a key
+// head (or five: 65 rows are four tiles and one row), parts of the pages where
+// that leaves the chip idle.
 Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   const int tiles = (R * (H / Hkv) + kTile - 1) / kTile;
-  const int chunks = (tiles + 7) / 8, most = (tiles + chunks - 1) / chunks;  // tiles of the largest chunk
   Shape s;
-  s.chunks = chunks;
-  s.nt = most > 1 ? 2 : 1;
-  s.wr = (most + 1) / 2;
-  s.wk = s.wr == 1 ? 4 : s.wr == 2 ? 2 : 1;
-  const int64_t wgs = (int64_t)B * Hkv * chunks;
+  s.alone = tiles == 1;
+  s.five = tiles % kWaves == 1 && tiles > 1;
+  s.chunks = s.five ? tiles / kWaves : (tiles + kWaves - 1) / kWaves;
+  const int64_t wgs = (int64_t)B * Hkv * s.chunks;
   const int64_t pages = ((int64_t)max_len + kPage - 1) / kPage;
-  int64_t parts = (2 * kCus + wgs - 1) / wgs;
-  const int64_t fit = (pages + 2 * s.wk - 1) / (2 * s.wk);  // two pages or more a wave
+  const int64_t slots = 2 * kCus;  // workgroups at once
+  int64_t each = s.alone ? 16 : 4;  // pages of a part, at least
+  int64_t parts = s.alone ? (2 * slots + wgs - 1) / wgs : wgs >= slots ? 1 : (slots + wgs - 1) / wgs;
+  if (parts > kMostParts) parts = kMostParts;
+  const int64_t fit = (pages + each - 1) / each;
   if (parts > fit) parts = fit;
-  if (parts > 64) parts = 64;
   if (parts < 1) parts = 1;
-  int64_t each = (pages + parts - 1) / parts;
-  each = (each + s.wk - 1) / s.wk * s.wk;
+  each = (pages + parts - 1) / parts;
+  if (s.alone) each = (each + kWaves - 1) / kWaves * kWaves;
   s.part_pages = each < 1 ? 1 : (int)each;
-  s.parts = pages <= s.part_pages ? 1 : (int)((pages + s.part_pages - 1) / s.part_pages);
+  s.parts = (pages <= s.part_pages ? 1 : (int)((pages + s.part_pages - 1) / s.part_pages)) + more_parts(R);
   return s;
 }
 
@@ -724,18 +1101,16 @@ extern "C" fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, con
   }
   const dim3 grid((uint32_t)B * (uint32_t)Hkv * (uint32_t)s.chunks, (uint32_t)s.parts);
   (void)hipGetLastError();
-#define FC_ATTN(NT, WR, WK) \
-  hipLaunchKernelGGL((k_paged_attn<NT, WR, WK>), grid, dim3(WR * WK * fc::kWave), 0, stream, a)
-  if (s.nt == 1) FC_ATTN(1, 1, 4);
-  else if (s.wr == 1) FC_ATTN(2, 1, 4);
-  else if (s.wr == 2) FC_ATTN(2, 2, 2);
-  else if (s.wr == 3) FC_ATTN(2, 3, 1);
-  else FC_ATTN(2, 4, 1);
-#undef FC_ATTN
+  if (s.alone)
+    hipLaunchKernelGGL(k_paged_attn_alone, grid, dim3(kThreads), 0, stream, a);
+  else if (s.five)
+    hipLaunchKernelGGL(k_paged_attn<true>, grid, dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(k_paged_attn<false>, grid, dim3(kThreads), 0, stream, a);
   FC_CHECK_LAUNCH();
   if (s.parts > 1) {
-    hipLaunchKernelGGL(k_paged_merge, dim3(fc::div_up((uint64_t)R * (H / Hkv), 16) * (uint32_t)B * (uint32_t)Hkv),
-                       dim3(256), 0, stream, a);
+    const uint64_t rows = (uint64_t)B * H * R;
+    hipLaunchKernelGGL(k_paged_merge, dim3(fc::div_up(rows, kMergeWaves)), dim3(kMergeWaves * fc::kWave), 0, stream, a);
     FC_CHECK_LAUNCH();
   }
   return FC_OK;
