@@ -54,14 +54,14 @@ constexpr int kSlot = 9 * 1024;                 // a page as it lies in memory, 
 constexpr int kTreeTiles = 6;                   // tree rows of a workgroup: 96
 constexpr int kTreeRows = 16 * kTreeTiles;
 constexpr int kSixRow = 304;                    // a row of 6-bit parts in LDS: 4 groups x 3 parts x 24 bytes, 4 scale words
-constexpr int kSlot0 = kTreeRows * kSixRow + 512;  // free while the tree's rows are in use
-constexpr int kSlot1 = kValues;
-constexpr int kLds = kSlot0 + kSlot;            // 38 KB: four workgroups of a CU
+constexpr int kSlots = 4;                       // pages on their way or in use
+constexpr int kSlot0 = 2 * kValues;             // behind two pages' values
+constexpr int kLds = kSlot0 + kSlots * kSlot;   // 72 KB: two workgroups of a CU
 constexpr int kMostParts = 124;                 // of a prefix; with those of a tree's rows a merging wave takes 128
 constexpr int kXcds = 8;
 constexpr int kCus = 256;
-static_assert((kWaves + 1) * kTile * kSixRow <= kSlot0 && kSlot1 + kSlot <= kSlot0, "query rows, and both slots, apart");
-static_assert(kTreeRows * kRowBytes <= kSlot0, "the tree's values");
+static_assert((kWaves + 1) * kTile * kSixRow <= kSlot0 && kTreeRows * kSixRow <= kSlot0 && kTreeRows * kRowBytes <= kSlot0,
+              "query and tree rows where the values go");
 
 struct Args {
   const uint16_t *q, *k_tree, *v_tree;
@@ -568,6 +568,34 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
   const int row5 = (tile0 + kWaves) * kTile + lc;
   const bool in5 = five && row5 < W.M;
 
+  // ---- pages on their way: straight from memory into LDS as they lie (16 bytes
+  // a lane, no registers), two while a third is used.  The keys' four chunks of 16
+  // bytes change places by the row, so that a wave reads 16 rows without two lanes
+  // in a bank.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
+  const int32_t* table = A.table + (int64_t)W.b * A.max_pages;
+  const auto slot_of = [&](int pg) { return kSlot0 + ((pg - W.pg0) & (kSlots - 1)) * kSlot; };
+  // page numbers, 64 at a time in a register's lanes: read one by one they would
+  // be loads to wait for among the loads that are meant to stay in flight
+  int ids = 0;
+  constexpr int kLoads = 3;  // of a wave and page
+  const auto issue = [&](int pg) {
+    const int i = (pg - W.pg0) & 63;
+    if (i == 0) ids = pg + lane < W.pg1 ? table[pg + lane] : -1;
+    const int id = __builtin_amdgcn_readlane(ids, i);
+    const bool there = id >= 0 && id < A.n_pages;  // an absent page's loads give zeros, and none of its keys counts
+    const fc::int32x4 rsrc = fc::buffer_rsrc(A.pool + ((int64_t)(there ? id : 0) * A.Hkv + W.kv) * kPageBytes,
+                                             there ? (uint32_t)kPageBytes : 0u);
+    const uint32_t to = lds0 + (uint32_t)slot_of(pg);
+    fc::lds_load16(to + (uint32_t)w * 1024u, (uint32_t)(w * 1024 + (lane ^ (lane >> 4)) * 16), rsrc);
+    fc::lds_load16(to + (uint32_t)(w + 4) * 1024u, (uint32_t)((w + 4) * 1024 + lane * 16), rsrc);
+    fc::lds_load16(to + 8u * 1024u, (uint32_t)(8 * 1024 + lane * 16), rsrc);  // the scales: every wave the same
+    return there;
+  };
+  bool here0 = false, here1 = false, here2 = false;  // whether page pg, pg + 1, pg + 2 is
+  if (W.pg0 < W.pg1) here0 = issue(W.pg0);
+  if (W.pg0 + 1 < W.pg1) here1 = issue(W.pg0 + 1);
+
   // ---- queries, in 6-bit parts: a thread for each group of a row, through LDS
   if (rotate && tid < kHeadDim / 2) s_freq[tid] = angle_of(tid, A.log2_base);
   __syncthreads();
@@ -588,28 +616,6 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
     q[i] = read_six(s_v + (kTile * (2 * pair + i < tiles ? 2 * pair + i : 0) + lc) * kSixRow, lg);
   if (kFive) q5 = read_six(s_v + (kTile * (five ? kWaves : 0) + lc) * kSixRow, lg);
   __syncthreads();  // the rows are read: their place is free
-
-  // ---- pages on their way: straight from memory into LDS as they lie (16 bytes
-  // a lane, no registers), one while another is used
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_v;
-  const int32_t* table = A.table + (int64_t)W.b * A.max_pages;
-  // page numbers, 64 at a time in a register's lanes: read one by one they would
-  // be loads to wait for among the loads that are meant to stay in flight
-  int ids = 0;
-  bool coming = false;
-  const auto issue = [&](int pg) {
-    const int i = (pg - W.pg0) & 63;
-    if (i == 0) ids = pg + lane < W.pg1 ? table[pg + lane] : -1;
-    const int id = __builtin_amdgcn_readlane(ids, i);
-    coming = id >= 0 && id < A.n_pages;  // an absent page's loads give zeros, and none of its keys counts
-    const fc::int32x4 rsrc = fc::buffer_rsrc(A.pool + ((int64_t)(coming ? id : 0) * A.Hkv + W.kv) * kPageBytes,
-                                             coming ? (uint32_t)kPageBytes : 0u);
-    const uint32_t to = lds0 + (uint32_t)((pg - W.pg0) & 1 ? kSlot1 : kSlot0);
-    fc::lds_load16(to + (uint32_t)w * 1024u, (uint32_t)(w * 1024 + lane * 16), rsrc);
-    fc::lds_load16(to + (uint32_t)(w + 4) * 1024u, (uint32_t)((w + 4) * 1024 + lane * 16), rsrc);
-    if (w == 0) fc::lds_load16(to + 8u * 1024u, (uint32_t)(8 * 1024 + lane * 16), rsrc);
-  };
-  if (W.pg0 < W.pg1) issue(W.pg0);
 
   lds_u8* const v_lane = (lds_u8*)(uintptr_t)(lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u);
   Row me[2], extra;
@@ -684,19 +690,31 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
     }
   }
 
-  // ---- the prefix.  Between two barriers the waves unpack the page's values, a
-  // quarter each, and have their scores.
+  // ---- the prefix.  Between two barriers the waves have a page's scores, add its
+  // values, and unpack the next one's, a quarter each.
+  const auto unpack_page = [&](int pg, bool here) {
+    const uint8_t* raw = s_v + slot_of(pg);
+    unpack(*(const uint4*)(raw + fc::kPageV + (w * 64 + lane) * 16), *(const uint32_t*)(raw + fc::kPageVScale + 4 * lane),
+           w, lane, here ? W.P - pg * kPage : 0, s_v + ((pg - W.pg0) & 1) * kValues);
+  };
   lds_u8* const v_mine = v_lane + chunk_at(KS == 2 ? 32 : 16, 0) * ks;
-  for (int pg = W.pg0; pg < W.pg1; ++pg) {
-    const int left = coming ? W.P - pg * kPage : 0;  // keys that exist, if below 64
-    const uint8_t* raw = s_v + ((pg - W.pg0) & 1 ? kSlot1 : kSlot0);
+  const uint32_t k_lane = (uint32_t)(lc * fc::kCodeRow + ((lg ^ (lc >> 2)) << 4));
+  if (W.pg0 < W.pg1) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // the page is there; the values and the slot before it are free
-    if (pg + 1 < W.pg1) issue(pg + 1);
-    const uint32_t vs = *(const uint32_t*)(raw + fc::kPageVScale + 4 * lane);
-    const uint4 vraw = *(const uint4*)(raw + fc::kPageV + (w * 64 + lane) * 16);
+    __syncthreads();  // the first pages are there, the place of their values is free
+    unpack_page(W.pg0, here0);
+  }
+  for (int pg = W.pg0; pg < W.pg1; ++pg) {
+    // the page after this one is there: only what was asked for last may be on its way
+    if (pg + 2 < W.pg1) here2 = issue(pg + 2);
+    if (pg + 2 < W.pg1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // and its values, for all; the values before them and their slot are free
+    const int left = here0 ? W.P - pg * kPage : 0;  // keys that exist, if below 64
+    const uint8_t* raw = s_v + slot_of(pg);
+    lds_u8* const values = v_mine + ((pg - W.pg0) & 1) * kValues;
     const uint32_t kscales = *(const uint32_t*)(raw + fc::kPageKScale + 4 * lane);
-    const auto key = [&](int t) { return *(const uint4*)(raw + (16 * t + lc) * fc::kCodeRow + 16 * lg); };
+    const auto key = [&](int t) { return *(const uint4*)(raw + t * 1024 + k_lane); };
     if constexpr (KS == 2) {
       const uint32_t mine = kscales >> (16 * ks);
       const uint4 k0 = key(2 * ks), k1 = key(2 * ks + 1);
@@ -708,7 +726,7 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       }
       floatx4 s5[1] = {floatx4{0.0f, 0.0f, 0.0f, 0.0f}};
       if (kFive && five) s5[0] = pair ? score<1>(k1, mine, q5, extra.minus_m) : score<0>(k0, mine, q5, extra.minus_m);
-      unpack(vraw, vs, w, lane, left, s_v);
+      if (pg + 1 < W.pg1) unpack_page(pg + 1, here1);
       settle(s[0][0], s[0][1], s[1][0], s[1][1]);
       if (kFive) settle(s5[0]);
       if (left < kPage) {
@@ -721,9 +739,12 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
         raise(s[0], top0, me[0]);
         raise(s[1], top1, me[1]);
       }
+      if (kFive && five) rescale(s5, extra);
+      Frag f0, f1, f2;
+      read_values(values, 0, f0);
+      read_values(values, 2, f1);
       bf16x8 pb5;
-      if (kFive && five) {
-        rescale(s5, extra);
+      if (kFive) {
         __bf16 p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -735,32 +756,32 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
         pb5 = pair ? bf16x8{none, none, none, none, p[0], p[1], p[2], p[3]}
                    : bf16x8{p[0], p[1], p[2], p[3], none, none, none, none};
       }
-      __syncthreads();  // the values are there
-      Frag f[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) read_values(v_mine, 2 * u, f[u]);
       const bf16x8 p0 = weights(s[0][0], s[0][1], me[0]), p1 = weights(s[1][0], s[1][1], me[1]);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        add_values(f[u], 2 * u, p0, me[0]);
-        add_values(f[u], 2 * u, p1, me[1]);
-        if (kFive && five) add_values(f[u], 2 * u, pb5, extra);
-      }
+      const auto add = [&](const Frag& f, int t0) {
+        add_values(f, t0, p0, me[0]);
+        add_values(f, t0, p1, me[1]);
+        if (kFive && five) add_values(f, t0, pb5, extra);
+      };
+      read_values(values, 4, f2);
+      add(f0, 0);
+      read_values(values, 6, f0);
+      add(f1, 2);
+      add(f2, 4);
+      add(f0, 6);
     } else {
       const uint4 k0 = key(ks);
       floatx4 s[2][1];
 #pragma unroll
       for (int i = 0; i < 2; ++i) s[i][0] = score<0>(k0, kscales >> (8 * ks), q[i], me[i].minus_m);
-      unpack(vraw, vs, w, lane, left, s_v);
+      if (pg + 1 < W.pg1) unpack_page(pg + 1, here1);
       settle(s[0][0], s[1][0]);
       if (left < kPage) cut(s[0][0], ks, lg, left), cut(s[1][0], ks, lg, left);
       rescale(s[0], me[0]);
       rescale(s[1], me[1]);
-      __syncthreads();
       bf16x4 lo[kDTiles], p[2];
 #pragma unroll
       for (int t = 0; t < kDTiles; ++t)
-        lo[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(v_mine + chunk_at(0, 2 * t)));
+        lo[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(values + chunk_at(0, 2 * t)));
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -777,6 +798,8 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
           me[i].o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(shortx4, lo[t]),
                                                                  __builtin_bit_cast(shortx4, p[i]), me[i].o[t], 0, 0, 0);
     }
+    here0 = here1;
+    here1 = here2;
   }
 
   // ---- the waves with the first keys take the others' rows, one tile after another
