@@ -254,76 +254,89 @@ __device__ __forceinline__ int parts_of(int pages, int part_pages) {
 __host__ __device__ __forceinline__ int more_parts(int n) { return n <= kTreeRows ? 0 : (n - 1) / kTreeRows; }
 
 // A query row's outputs (lane (lg, lc): dims 16 t + 4 lg + e of row lc), its
-// running maximum as 0 - m (0 while there is none), the sum of its weights, and by
-// how much a score may pass m before the row is scaled anew (-inf while there is
-// no m).
+// running maximum as 0 - m (0 while there is none), the sum of its weights, and
+// whether it is yet to see a key.
 struct Row {
   floatx4 o[kDTiles];
   floatx4 minus_m;
-  float l, slack;
+  float l;
+  bool first;
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int t = 0; t < kDTiles; ++t) o[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     minus_m = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     l = 0.0f;
-    slack = -INFINITY;
+    first = true;
   }
-  __device__ __forceinline__ float m() const { return slack == -INFINITY ? -INFINITY : 0.0f - minus_m[0]; }
+  __device__ __forceinline__ float m() const { return first ? -INFINITY : 0.0f - minus_m[0]; }
 };
 
-// The softmax's usual step is a power of two, a sum and a rounding a score.  s
-// holds scores less m (the products start from minus_m), -inf where a key is not
-// allowed.  m is the maximum of what the row saw when it was last scaled: while no
-// score passes it by more than 8, weights stay below 2^8 and neither sums nor
-// outputs are touched (with bf16 weights a common factor costs no accuracy).
+// The softmax's usual step is a power of two, a rounding and a share of a sum for
+// each score, and no maximum.  s holds scores less m (the products start from
+// minus_m), -inf where a key is not allowed.  m is the maximum of what the row saw
+// when it was last scaled; a factor common to a row's weights costs no accuracy,
+// bf16 and fp32 having the same exponents.  A step whose weights add up to 2^40 or
+// more (or to a NaN) is taken again with m raised to its maximum, and so is a
+// row's first.
+constexpr float kMostWeight = 1099511627776.0f;  // 2^40
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 template <int N>
-__device__ __forceinline__ float top_of(const floatx4 (&s)[N]) {
+__device__ __forceinline__ void raise(floatx4 (&s)[N], Row& r, bool need) {
   float top = -INFINITY;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     top = fmaxf(fmaxf(top, s[t][0]), s[t][1]);
     top = fmaxf(fmaxf(top, s[t][2]), s[t][3]);
   }
-  return top;
-}
-template <int N>
-__device__ __forceinline__ void raise(floatx4 (&s)[N], float top, Row& r) {
   float mx = fmaxf(top, __shfl_xor(top, 16));
   mx = fmaxf(mx, __shfl_xor(mx, 32));
+  int row_needs = need;
+  row_needs |= __shfl_xor(row_needs, 16);
+  row_needs |= __shfl_xor(row_needs, 32);
   // by how much m rises; a row that has no need keeps it, so that its result goes
   // by its own scores alone
-  const float by = mx > r.slack ? mx : 0.0f;
-  const float alpha = r.slack == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(-by);
+  const bool rise = row_needs != 0 && mx != -INFINITY;
+  const float by = rise ? mx : 0.0f;
+  const float alpha = r.first ? 0.0f : __builtin_amdgcn_exp2f(-by);
 #pragma unroll
   for (int t = 0; t < N; ++t) s[t] -= by;
   r.l *= alpha;
 #pragma unroll
   for (int t = 0; t < kDTiles; ++t) r.o[t] *= alpha;
   const float minus = r.minus_m[0] - by;
-  r.slack = mx > r.slack ? 8.0f : r.slack;
+  r.first = r.first && !rise;
   r.minus_m = floatx4{minus, minus, minus, minus};
 }
+// Rounded weights of N tiles of 16 keys, and their sum (of what the value product
+// sees).
 template <int N>
-__device__ __forceinline__ void rescale(floatx4 (&s)[N], Row& r) {
-  const float top = top_of(s);
-  if (__any(top > r.slack)) raise(s, top, r);
+__device__ __forceinline__ float weigh(const floatx4 (&s)[N], bf16x2 (&p)[2 * N]) {
+  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+  float sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      p[2 * t + e] = bf16x2{(__bf16)__builtin_amdgcn_exp2f(s[t][2 * e]), (__bf16)__builtin_amdgcn_exp2f(s[t][2 * e + 1])};
+      sum = __builtin_amdgcn_fdot2_f32_bf16(p[2 * t + e], one, sum, false);
+    }
+  return sum;
 }
-// weights of 32 keys, in the lane layout of the value product's operand
-__device__ __forceinline__ bf16x8 weights(const floatx4& a, const floatx4& b, Row& r) {
-  bf16x8 pb;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float p = __builtin_amdgcn_exp2f(a[e]);
-    r.l += p;
-    pb[e] = (__bf16)p;
+__device__ __forceinline__ bool too_much(float sum, const Row& r) {
+  return !(sum < (r.first ? -1.0f : kMostWeight));
+}
+template <int N>
+__device__ __forceinline__ void weights(floatx4 (&s)[N], Row& r, bf16x2 (&p)[2 * N]) {
+  float sum = weigh(s, p);
+  if (__any(too_much(sum, r))) {
+    raise(s, r, too_much(sum, r));
+    sum = weigh(s, p);
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float p = __builtin_amdgcn_exp2f(b[e]);
-    r.l += p;
-    pb[4 + e] = (__bf16)p;
-  }
-  return pb;
+  r.l += sum;
+}
+__device__ __forceinline__ bf16x8 join(const bf16x2& a, const bf16x2& b, const bf16x2& c, const bf16x2& d) {
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -366,6 +379,7 @@ __device__ __forceinline__ void unpack(const uint4& raw, uint32_t scales, int i4
   uint32_t sb = (scales >> (8 * i4)) & 255u;
   uint32_t c4[4] = {raw.x, raw.y, raw.z, raw.w};
   if (left < kPage) {
+    asm volatile("");  // a branch: few pages end early
     const bool live = key < left;
     sb = live ? sb : 127u;
 #pragma unroll
@@ -658,9 +672,10 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       for (int k = 0; k < NB; ++k) settle(s[2 * k], s[2 * k + 1]);
 #pragma unroll
       for (int u = 0; u < 8 * NB; ++u) s[u / 4][u % 4] = (see >> u) & 1u ? s[u / 4][u % 4] : -INFINITY;
-      rescale(s, r);
+      bf16x2 x[4 * NB];
+      weights(s, r, x);
 #pragma unroll
-      for (int k = 0; k < NB; ++k) p[k] = weights(s[2 * k], s[2 * k + 1], r);
+      for (int k = 0; k < NB; ++k) p[k] = join(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
     };
     tree_weights(q[0], bits[0], me[0], pb[0]);
     tree_weights(q[1], bits[1], me[1], pb[1]);
@@ -734,29 +749,26 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
         for (int i = 0; i < 2; ++i) cut(s[i][0], 2 * ks, lg, left), cut(s[i][1], 2 * ks + 1, lg, left);
         if (kFive && five) cut(s5[0], 2 * ks + pair, lg, left);
       }
-      const float top0 = top_of(s[0]), top1 = top_of(s[1]);
-      if (__any(top0 > me[0].slack || top1 > me[1].slack)) {
-        raise(s[0], top0, me[0]);
-        raise(s[1], top1, me[1]);
-      }
-      if (kFive && five) rescale(s5, extra);
       Frag f0, f1, f2;
       read_values(values, 0, f0);
       read_values(values, 2, f1);
+      bf16x2 x0[4], x1[4], x5[2];
+      float sum0 = weigh(s[0], x0), sum1 = weigh(s[1], x1);
+      if (__any(too_much(sum0, me[0]) || too_much(sum1, me[1]))) {
+        raise(s[0], me[0], too_much(sum0, me[0]));
+        raise(s[1], me[1], too_much(sum1, me[1]));
+        sum0 = weigh(s[0], x0), sum1 = weigh(s[1], x1);
+      }
+      me[0].l += sum0;
+      me[1].l += sum1;
+      const bf16x8 p0 = join(x0[0], x0[1], x0[2], x0[3]), p1 = join(x1[0], x1[1], x1[2], x1[3]);
       bf16x8 pb5;
       if (kFive) {
-        __bf16 p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s5[0][e]);
-          extra.l += x;
-          p[e] = (__bf16)x;
-        }
-        const __bf16 none = (__bf16)0.0f;
-        pb5 = pair ? bf16x8{none, none, none, none, p[0], p[1], p[2], p[3]}
-                   : bf16x8{p[0], p[1], p[2], p[3], none, none, none, none};
+        if (five) weights(s5, extra, x5);
+        else x5[0] = x5[1] = bf16x2{(__bf16)0.0f, (__bf16)0.0f};
+        const bf16x2 none = {(__bf16)0.0f, (__bf16)0.0f};
+        pb5 = pair ? join(none, none, x5[0], x5[1]) : join(x5[0], x5[1], none, none);
       }
-      const bf16x8 p0 = weights(s[0][0], s[0][1], me[0]), p1 = weights(s[1][0], s[1][1], me[1]);
       const auto add = [&](const Frag& f, int t0) {
         add_values(f, t0, p0, me[0]);
         add_values(f, t0, p1, me[1]);
@@ -776,21 +788,17 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       if (pg + 1 < W.pg1) unpack_page(pg + 1, here1);
       settle(s[0][0], s[1][0]);
       if (left < kPage) cut(s[0][0], ks, lg, left), cut(s[1][0], ks, lg, left);
-      rescale(s[0], me[0]);
-      rescale(s[1], me[1]);
       bf16x4 lo[kDTiles], p[2];
 #pragma unroll
       for (int t = 0; t < kDTiles; ++t)
         lo[t] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(values + chunk_at(0, 2 * t)));
       asm volatile("" ::: "memory");
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s[i][0][e]);
-          me[i].l += x;
-          p[i][e] = (__bf16)x;
-        }
+      for (int i = 0; i < 2; ++i) {
+        bf16x2 x[2];
+        weights(s[i], me[i], x);
+        p[i] = bf16x4{x[0][0], x[0][1], x[1][0], x[1][1]};
+      }
 #pragma unroll
       for (int t = 0; t < kDTiles; ++t)
 #pragma unroll
@@ -925,8 +933,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
       s[0][e] = (see >> e) & 1u ? s[0][e] : -INFINITY;
       s[1][e] = -INFINITY;
     }
-    rescale(s, me);
-    const bf16x8 pb = weights(s[0], s[1], me);
+    bf16x2 x[4];
+    weights(s, me, x);
+    const bf16x8 pb = join(x[0], x[1], x[2], x[3]);
     all_values(v_lane + kTile * kSixRow, pb, me);
     const uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[0]);
     if (bad) W.add_marked(A, bad, 0, pb, see, lg, lc, me);
@@ -952,9 +961,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) cut(s[t], t, lg, left);
     }
-    rescale(s, me);
-    all_values(v_mine, weights(s[0], s[1], me), me);
-    all_values(v_mine + chunk_at(32, 0), weights(s[2], s[3], me), me);
+    bf16x2 x[8];
+    weights(s, me, x);
+    all_values(v_mine, join(x[0], x[1], x[2], x[3]), me);
+    all_values(v_mine + chunk_at(32, 0), join(x[4], x[5], x[6], x[7]), me);
   };
   for (int pg = W.pg0 + w; pg < W.pg1; pg += 2 * kWaves) {
     step(even, pg);
