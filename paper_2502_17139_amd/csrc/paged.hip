@@ -19,16 +19,51 @@ using fc::kPageBytes;
 
 // ------------------------------------------------------------------- plan --
 
-constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 1024;  // tokens of the slot map that a workgroup writes
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / fc::kWave;
+constexpr int kPlanEach = 4;                           // tokens of a thread
+constexpr int kPlanTokens = kPlanThreads * kPlanEach;  // tokens of the slot map that a workgroup writes
+
+// Exclusive prefix sums of three values over the first `waves` waves of the
+// workgroup (no other holds one), and their totals, with one pass through LDS.
+struct Sums {
+  uint64_t x[3];
+};
+__device__ __forceinline__ Sums block_sums(const Sums& v, int waves, Sums* scratch, Sums& total) {
+  const int w = (int)threadIdx.x / fc::kWave;
+  Sums before = {{0, 0, 0}};
+  total = before;
+  if (w < waves) {
+    Sums inc;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) inc.x[i] = fc::wave_incl_sum_any(v.x[i]);
+    if (fc::lane_id() == fc::kWave - 1) scratch[w] = inc;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) before.x[i] = inc.x[i] - v.x[i];
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int k = 0; k < waves; ++k) {
+    const Sums s = scratch[k];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      before.x[i] += k < w ? s.x[i] : 0;
+      total.x[i] += s.x[i];
+    }
+  }
+  __syncthreads();
+  return before;
+}
 
 // Every workgroup scans all sequences (three prefix sums: tokens, new pages,
 // pages given back) and keeps, in LDS, those whose tokens fall into its own
 // window of the slot map; so no workgroup waits for another and one launch does
 // it all.  A window position that starts a sequence carries that sequence's
 // data; a running maximum over the positions takes each token to its start.
-// The scan is 8 bytes a sequence from L2: at the 65,536 sequences allowed it is
-// what costs, at the thousands of a serving batch it is not.
+// What it costs is latency: a load of the lengths, the sums, and for a tree's
+// step a load of each sequence's mask row; hence sixteen waves, one sequence's row
+// each.  The scan is 8 bytes a sequence from L2: at the 65,536 sequences allowed
+// it is what costs, at the thousands of a serving batch it is not.
 __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     const int32_t* __restrict__ len, const int32_t* __restrict__ add, const int32_t* __restrict__ mask,
     const int32_t* __restrict__ last_node, int B, int R, int n_slots, int32_t* table, int max_pages, int32_t* queue,
@@ -36,36 +71,35 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     int32_t* __restrict__ slot, int32_t* __restrict__ pos, int32_t* __restrict__ src,
     int64_t* __restrict__ ends_out) {
   struct Seq {  // of a window position that starts a sequence
-    int64_t pos0;       // position of the token at window position 0, were it this sequence's
+    int32_t pos0;    // position of the token at window position 0, were it this sequence's
     int32_t b;
-    int32_t held;       // pages it had
-    uint32_t page0;     // new pages taken before its own
-    uint32_t count;     // tokens
-    int32_t first;      // its token number at this window position
-    int32_t ok;
+    uint32_t page0;  // new pages taken before its own
+    uint32_t count;  // tokens
+    uint32_t first;  // its token number at this window position
+    int32_t last;    // its accepted row, -2 if the sequence does not fit
   };
   struct Back {  // pages that a sequence gives back
-    uint64_t to;
+    uint32_t to;
     int32_t b, from, count;
   };
-  __shared__ uint64_t s_scan[kPlanThreads / fc::kWave + 1];
-  __shared__ int s_scan_max[kPlanThreads / fc::kWave + 1];
+  __shared__ Sums s_scan[kPlanWaves];
+  __shared__ int s_scan_max[kPlanWaves + 1];
   __shared__ Seq s_seq[kPlanTokens];
-  __shared__ int s_start[kPlanTokens];  // window position + 1 where a sequence starts, else 0
+  __shared__ uint16_t s_start[kPlanTokens];  // window position + 1 where a sequence starts, else 0
+  __shared__ uint16_t s_list[kPlanTokens];   // those positions, in any order
   __shared__ int32_t s_src[kPlanTokens];
-  __shared__ int s_list[kPlanTokens];
   __shared__ Back s_back[kPlanThreads];
   __shared__ int s_listed, s_backs;
   __shared__ unsigned long long s_given;
 
-  const int tid = (int)threadIdx.x;
+  const int tid = (int)threadIdx.x, wave = tid / fc::kWave, lane = fc::lane_id();
   const int64_t w0 = (int64_t)blockIdx.x * kPlanTokens;
   const int64_t head = ends[0], tail = ends[1];
   const uint64_t held_free = tail > head ? (uint64_t)(tail - head) : 0;
   const uint64_t avail = held_free < (uint64_t)n_pages ? held_free : (uint64_t)n_pages;
   const uint64_t head_at = (uint64_t)head % (uint32_t)n_pages, tail_at = (uint64_t)tail % (uint32_t)n_pages;
   for (int x = tid; x < kPlanTokens; x += kPlanThreads) s_start[x] = 0, s_src[x] = -1;
-  if (tid == 0) s_listed = 0, s_given = 0;
+  if (tid == 0) s_listed = 0, s_given = 0, s_backs = 0;
   __syncthreads();
 
   uint64_t tokens = 0, taken = 0, given_back = 0;  // of the sequences before this chunk
@@ -79,41 +113,51 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     const uint64_t want = a > 0 ? (uint64_t)a : 0;
     int64_t now = n + a < 0 ? 0 : n + a;
     const int64_t held = (n + kPage - 1) / kPage, pages = (now + kPage - 1) / kPage;
-    uint64_t sum;
-    if (tid == 0) s_backs = 0;
-    const uint64_t first = tokens + fc::block_excl_sum<uint64_t>(want, s_scan, &sum);
-    tokens += sum;
-    const bool fits = a <= 0 || (pages <= max_pages && first + want <= (uint64_t)n_slots);
-    const uint64_t need = fits && a > 0 ? (uint64_t)(pages - held) : 0;
-    const uint64_t page0 = taken + fc::block_excl_sum<uint64_t>(need, s_scan, &sum);
-    taken += sum;
+    const uint64_t back = a < 0 ? (uint64_t)(held - pages) : 0;
+    const bool short_enough = a <= 0 || pages <= max_pages;
+    uint64_t need = short_enough && a > 0 ? (uint64_t)(pages - held) : 0;
+    int32_t last = in && mask ? last_node[b] : -1;
+    if (last >= R || last < 0) last = -1;
+    const int waves = B - b0 < kPlanThreads ? (int)fc::div_up((uint64_t)(B - b0), fc::kWave) : kPlanWaves;
+    Sums sum;
+    const Sums before = block_sums(Sums{{want, back, need}}, waves, s_scan, sum);
+    const uint64_t first = tokens + before.x[0], to = given_back + before.x[1];
+    uint64_t page0 = taken + before.x[2];
+    tokens += sum.x[0];
+    given_back += sum.x[1];
+    const bool fits = short_enough && (a <= 0 || first + want <= (uint64_t)n_slots);
+    if (tokens > (uint64_t)n_slots) {  // the same for all threads: some do not fit, and take no pages
+      need = fits ? need : 0;
+      page0 = taken + block_sums(Sums{{need, 0, 0}}, waves, s_scan, sum).x[0];
+      sum.x[2] = sum.x[0];
+    }
+    taken += sum.x[2];
     const bool ok = fits && (need == 0 || page0 + need <= avail);
     if (ok && need > 0) atomicMax(&s_given, (unsigned long long)(page0 + need));  // the sums only grow
     if (!ok) now = n;
-    const uint64_t back = a < 0 ? (uint64_t)(held - pages) : 0;
-    const uint64_t to = given_back + fc::block_excl_sum<uint64_t>(back, s_scan, &sum);
-    given_back += sum;
     if (in && blockIdx.x == 0) {
       len_out[b] = (int32_t)now;
       const uint64_t end = first + want;
       cu[b + 1] = (int32_t)(end < 0x7FFFFFFFu ? end : 0x7FFFFFFFu);
     }
     if (back > 0 && (uint32_t)b % gridDim.x == blockIdx.x)
-      s_back[atomicAdd(&s_backs, 1)] = Back{tail_at + to, b, (int32_t)pages, (int32_t)back};
+      s_back[atomicAdd(&s_backs, 1)] = Back{(uint32_t)((tail_at + to) % (uint32_t)n_pages), b, (int32_t)pages, (int32_t)back};
     if (want > 0 && (int64_t)first < w0 + kPlanTokens && (int64_t)(first + want) > w0) {
       const int x = (int64_t)first > w0 ? (int)((int64_t)first - w0) : 0;
-      s_seq[x] = Seq{n - ((int64_t)first - w0), b, (int32_t)held, (uint32_t)page0,
-                     (uint32_t)want, (int32_t)(w0 + x - (int64_t)first), ok ? 1 : 0};
-      s_start[x] = x + 1;
-      s_list[atomicAdd(&s_listed, 1)] = x;  // any order: each writes its own places
+      s_seq[x] = Seq{(int32_t)(n - ((int64_t)first - w0)), b, (uint32_t)page0, (uint32_t)want,
+                     (uint32_t)(w0 + x - (int64_t)first), ok ? last : -2};
+      s_start[x] = (uint16_t)(x + 1);
+      s_list[atomicAdd(&s_listed, 1)] = (uint16_t)x;
     }
     __syncthreads();
-    for (int i = 0; i < s_backs; ++i) {
+    const int backs = s_backs;
+    for (int i = wave; i < backs; i += kPlanWaves) {
       const Back r = s_back[i];
-      for (int j = tid; j < r.count; j += kPlanThreads)
+      for (int j = lane; j < r.count; j += fc::kWave)
         queue[(r.to + (uint32_t)j) % (uint32_t)n_pages] = table[(int64_t)r.b * max_pages + r.from + j];
     }
     __syncthreads();
+    if (tid == 0) s_backs = 0;
   }
   if (tid == 0 && blockIdx.x == 0) {
     cu[0] = 0;
@@ -124,63 +168,67 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
   // a tree step's source rows: a wave per sequence takes the rows that the
   // accepted row may see, in order
   if (mask) {
-    const int lane = fc::lane_id();
-    for (int i = tid / fc::kWave; i < s_listed; i += kPlanThreads / fc::kWave) {
+    const int listed = s_listed;
+    for (int i = wave; i < listed; i += kPlanWaves) {
       const int x = s_list[i];
       const Seq q = s_seq[x];
-      const int last = last_node[q.b];
-      if (last < 0 || last >= R) continue;
-      const int32_t* row = mask + ((int64_t)q.b * R + last) * R;
+      if (q.last < 0) continue;
+      const int32_t* row = mask + ((int64_t)q.b * R + q.last) * R;
       int before = 0;
+#pragma unroll 2
       for (int j0 = 0; j0 < R; j0 += fc::kWave) {
         const int j = j0 + lane;
         const bool on = j < R && row[j] == 1;
         const uint64_t all = fc::ballot(on);
-        const int t = before + (int)__builtin_popcountll(all & fc::lanemask_lt());
-        const int at = x + t - q.first;
-        if (on && t >= q.first && (uint32_t)t < q.count && at < kPlanTokens) s_src[at] = q.b * R + j;
+        const uint32_t t = (uint32_t)(before + (int)__builtin_popcountll(all & fc::lanemask_lt()));
+        const uint32_t at = x + t - q.first;
+        if (on && t >= q.first && t < q.count && at < kPlanTokens) s_src[at] = q.b * R + j;
         before += (int)__builtin_popcountll(all);
       }
     }
     __syncthreads();
   }
 
-  constexpr int kEach = kPlanTokens / kPlanThreads;
-  int mine[kEach], run = 0;
+  int start[kPlanEach], run = 0;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int s = s_start[tid * kEach + e];
-    run = s > run ? s : run;
-    mine[e] = run;
+  for (int e = 0; e < kPlanEach; ++e) {
+    const int x = s_start[tid * kPlanEach + e];
+    run = x > run ? x : run;
+    start[e] = run;
   }
   const int before = fc::block_excl_max<int>(run, 0, s_scan_max);
+  int32_t sl[kPlanEach], po[kPlanEach], sr[kPlanEach];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int x = tid * kEach + e;
+  for (int e = 0; e < kPlanEach; ++e) {
+    const int x = tid * kPlanEach + e;
     const int64_t at = w0 + x;
-    if (at >= n_slots) break;
-    const int start = mine[e] > before ? mine[e] : before;
-    int32_t sl = -1, po = -1, sr = -1;
-    if (start > 0 && (uint64_t)at < tokens) {
-      const Seq q = s_seq[start - 1];
-      if (q.ok) {
-        const int64_t p = q.pos0 + x;
-        const int idx = (int)(p / kPage);
-        int32_t page;
-        if (idx < q.held) {
-          page = table[(int64_t)q.b * max_pages + idx];
-        } else {
-          page = queue[(head_at + q.page0 + (uint32_t)(idx - q.held)) % (uint32_t)n_pages];
-          if (p % kPage == 0) table[(int64_t)q.b * max_pages + idx] = page;  // every new page starts with a token
-        }
-        sl = page >= 0 && page < n_pages ? page * kPage + (int32_t)(p % kPage) : -1;
-        po = (int32_t)p;
-        sr = mask ? s_src[x] : (int32_t)at;
-      }
+    const int from = start[e] > before ? start[e] : before;
+    sl[e] = po[e] = sr[e] = -1;
+    if (from == 0 || (uint64_t)at >= tokens || at >= n_slots) continue;
+    const Seq q = s_seq[from - 1];
+    if (q.last == -2) continue;
+    const int32_t p = q.pos0 + x;
+    const int32_t n = q.pos0 + (from - 1) - (int32_t)q.first;  // tokens it had
+    const int idx = p / kPage, held = (n + kPage - 1) / kPage;
+    int32_t page;
+    if (idx < held) {
+      page = table[(int64_t)q.b * max_pages + idx];
+    } else {
+      const uint32_t i = (uint32_t)head_at + q.page0 + (uint32_t)(idx - held);  // less than 2 n_pages
+      page = queue[i < (uint32_t)n_pages ? i : i - (uint32_t)n_pages];
+      if (p % kPage == 0) table[(int64_t)q.b * max_pages + idx] = page;  // every new page starts with a token
     }
-    slot[at] = sl;
-    pos[at] = po;
-    src[at] = sr;
+    sl[e] = page >= 0 && page < n_pages ? page * kPage + p % kPage : -1;
+    po[e] = p;
+    sr[e] = mask ? s_src[x] : (int32_t)at;
+  }
+#pragma unroll
+  for (int e = 0; e < kPlanEach; ++e) {
+    const int64_t at = w0 + tid * kPlanEach + e;
+    if (at >= n_slots) return;
+    slot[at] = sl[e];
+    pos[at] = po[e];
+    src[at] = sr[e];
   }
 }
 
