@@ -149,20 +149,24 @@ __device__ __forceinline__ void write_six(const float (&v)[32], uint8_t* row, in
 // rotated and scaled.  The lane beside this one (lane ^ 1) has the group 64 dims
 // away, so the two share the angles: turn(e) gives the sine and cosine of the
 // pair's angle e, of which this lane asks for half.
-template <typename Turn>
-__device__ __forceinline__ void stage_six(const uint16_t* src, int g, float scale, bool rotate, Turn turn,
-                                          uint8_t* row) {
-  float v[32];
+struct Group {
   uint4 own[4], other[4];
+};
+__device__ __forceinline__ void load_group(const uint16_t* src, int g, Group& x) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    own[u] = *(const uint4*)(src + 32 * g + 8 * u);
-    other[u] = *(const uint4*)(src + 32 * (g ^ 2) + 8 * u);
+    x.own[u] = *(const uint4*)(src + 32 * g + 8 * u);
+    x.other[u] = *(const uint4*)(src + 32 * (g ^ 2) + 8 * u);
   }
+}
+template <typename Turn>
+__device__ __forceinline__ void stage_six(const Group& in, int g, float scale, bool rotate, Turn turn, uint8_t* row) {
+  float v[32];
+  const uint4(&other)[4] = in.other;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     float x[8];
-    fc::unpack8(own[u], x);
+    fc::unpack8(in.own[u], x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[8 * u + e] = x[e] * scale;
   }
@@ -450,25 +454,20 @@ struct Work {
   __device__ __forceinline__ const uint16_t* v_row(const Args& A, int j) const {
     return A.v_tree + ((int64_t)b * A.R + j) * A.v_stride + (int64_t)kv * kHeadDim;
   }
-  // bit 4 t + e, t < kt <= KT: query row tr may see tree row j0 + 16 t + 4 lg + e
-  template <int KT>
-  __device__ __forceinline__ uint32_t allowed(const Args& A, int tr, bool in, int j0, int lg) const {
+  // bit e: query row tr may see tree row 4 lg + e, of at most 16
+  __device__ __forceinline__ uint32_t allowed(const Args& A, int tr, bool in, int lg) const {
     uint32_t bits = 0;
-    const int32_t* mrow = A.mask ? A.mask + ((int64_t)b * A.R + tr) * A.R : nullptr;
+    const int j = 4 * lg;
+    int m[4];
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const int j = j0 + 16 * t + 4 * lg;
-      if (j0 + 16 * t >= n) break;
-      int m[4];
+    for (int e = 0; e < 4; ++e) m[e] = j + e <= tr;
+    if (A.mask) {
+      const int32_t* mrow = A.mask + ((int64_t)b * A.R + tr) * A.R;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = j + e <= tr;
-      if (mrow) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m[e] = mrow[j + e < n ? j + e : 0];
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) bits |= (uint32_t)(in && j + e < n && m[e] == 1) << (4 * t + e);
+      for (int e = 0; e < 4; ++e) m[e] = mrow[j + e < n ? j + e : 0];
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bits |= (uint32_t)(in && j + e < n && m[e] == 1) << e;
     return bits;
   }
   // Values of 32 tree rows that are not finite are 0 in LDS: a product with weight
@@ -494,6 +493,47 @@ struct Work {
           r.o[t][e] += sees && (x & 0x7F800000u) == 0x7F800000u ? weight * __uint_as_float(x) : 0.0f;
         }
     }
+  }
+};
+
+// Which of `left` (at most 96) tree rows, from tree0 on, the query rows tr0 .. tr1
+// may see.  load() asks for the mask's rows, four of a wave at a time, all on their
+// way together; store() leaves them as bits: to[3 i + k], bit j: row tr0 + i may
+// see tree row tree0 + 32 k + j.
+struct See {
+  static constexpr int kTimes = (kWaves + 1) * kTile / (4 * kWaves);
+  int m[kTimes][4][2];
+  template <typename F>
+  __device__ __forceinline__ static void each(int tr0, int tr1, int w, F f) {
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k)
+      if (4 * (kWaves * k + w) <= tr1 - tr0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(k, i, 4 * (kWaves * k + w) + i);
+      }
+  }
+  __device__ __forceinline__ void load(const Args& A, const Work& W, int tr0, int tr1, int left, int w) {
+    const int lane = fc::lane_id();
+    if (!A.mask) return;
+    each(tr0, tr1, w, [&](int k, int i, int at) {
+      const int32_t* row = A.mask + ((int64_t)W.b * A.R + (tr0 + at < tr1 ? tr0 + at : tr1)) * A.R + W.tree0;
+      m[k][i][0] = row[lane < left ? lane : 0];
+      m[k][i][1] = row[lane + 64 < left ? lane + 64 : 0];
+    });
+  }
+  __device__ __forceinline__ void store(const Args& A, const Work& W, int tr0, int tr1, int left, int w,
+                                        uint32_t* to) const {
+    const int lane = fc::lane_id();
+    each(tr0, tr1, w, [&](int k, int i, int at) {
+      const bool a = A.mask ? m[k][i][0] == 1 : W.tree0 + lane <= tr0 + at;
+      const bool b = A.mask ? m[k][i][1] == 1 : W.tree0 + lane + 64 <= tr0 + at;
+      const uint64_t lo = fc::ballot(lane < left && a), hi = fc::ballot(lane + 64 < left && b);
+      if (lane == 0 && tr0 + at <= tr1) {
+        to[3 * at] = (uint32_t)lo;
+        to[3 * at + 1] = (uint32_t)(lo >> 32);
+        to[3 * at + 2] = (uint32_t)hi;
+      }
+    });
   }
 };
 
@@ -563,7 +603,7 @@ __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& 
 // besides, 16 keys for each wave.
 template <int KS, bool kFive>
 __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_v, double* s_freq, uint32_t* s_bad,
-                                       int tile0, int tiles) {
+                                       uint32_t* s_see, int tile0, int tiles) {
   static_assert(!kFive || KS == 2, "the fifth tile goes with two pairs");
   constexpr int NB = KS == 2 ? 2 : 1;  // blocks of 32 tree rows of a wave, at most
   const int tid = (int)threadIdx.x, lane = fc::lane_id();
@@ -608,28 +648,57 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
   };
   bool here0 = false, here1 = false, here2 = false;  // whether page pg, pg + 1, pg + 2 is
   if (W.pg0 < W.pg1) here0 = issue(W.pg0);
-  if (W.pg0 + 1 < W.pg1) here1 = issue(W.pg0 + 1);
+  if (!W.tree && W.pg0 + 1 < W.pg1) here1 = issue(W.pg0 + 1);
 
-  // ---- queries, in 6-bit parts: a thread for each group of a row, through LDS
+  // ---- queries and the tree's keys, in 6-bit parts through LDS: a thread for each
+  // group of a row, the next one's loads on their way; queries where the second
+  // page will lie, or where values will if there is no tree
+  static_assert(kTreeRows * kSixRow <= kSlot0 && (kWaves + 1) * kTile * kSixRow <= (kSlots - 1) * kSlot, "rows fit");
+  uint8_t* const six_q = s_v + (W.tree ? kSlot0 + kSlot : 0);
+  const int row0 = tile0 * kTile, rows = W.M - row0 < kTile * tiles ? W.M - row0 : kTile * tiles;
+  const int left = !W.tree ? 0 : W.n - W.tree0 < kTreeRows ? W.n - W.tree0 : kTreeRows;  // tree rows
+  const int tr0 = row0 / W.G, tr1 = (row0 + rows - 1) / W.G;
+  See mask;
   if (rotate && tid < kHeadDim / 2) s_freq[tid] = angle_of(tid, A.log2_base);
+  if (W.tree) {
+    if (tid < kTreeTiles / 2) s_bad[tid] = 0;
+    mask.load(A, W, tr0, tr1, left, w);
+  }
   __syncthreads();
-  const auto stage_rows = [&](int rows, auto src, auto at, float by) {
-    for (int u = tid; u < 4 * rows; u += kThreads) {
+  {
+    const int units = 4 * (rows + left);
+    const auto load = [&](int u, Group& x, int& at) {
+      const int r = (u < units ? u : units - 1) >> 2, qr = row0 + r, kr = W.tree0 + r - rows;
+      load_group(r < rows ? W.q_row(A, qr) : W.k_row(A, kr), group_of(u & 3), x);
+      if (rotate) at = W.position(A, r < rows ? qr / W.G : kr);
+    };
+    Group x;
+    int at = 0;
+    load(tid, x, at);
+    for (int u = tid; u < units; u += kThreads) {
+      Group next;
+      int next_at = 0;
+      load(u + kThreads, next, next_at);
       const int r = u >> 2, g = group_of(u & 3);
-      const double pos = rotate ? (double)at(r) : 0.0;
-      stage_six(src(r), g, by, rotate, [&](int e) { return turn_of(pos * s_freq[32 * (g & 1) + e]); }, s_v + r * kSixRow);
+      const double pos = (double)at;
+      stage_six(x, g, r < rows ? score_scale() : 1.0f, rotate,
+                [&](int e) { return turn_of(pos * s_freq[32 * (g & 1) + e]); },
+                r < rows ? six_q + r * kSixRow : s_v + (r - rows) * kSixRow);
+      x = next;
+      at = next_at;
     }
-  };
-  stage_rows(
-      kTile * tiles, [&](int r) { return W.q_row(A, W.row_at(tile0 * kTile + r)); },
-      [&](int r) { return W.position(A, W.row_at(tile0 * kTile + r) / W.G); }, score_scale());
+  }
+  if (W.tree) mask.store(A, W, tr0, tr1, left, w, s_see);
   __syncthreads();
+  // rows past the last one: the last one, whose results nobody takes
+  const auto query = [&](int tile) {
+    const int r = kTile * tile + lc;
+    return read_six(six_q + (r < rows ? r : rows - 1) * kSixRow, lg);
+  };
   Six q[2], q5;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    q[i] = read_six(s_v + (kTile * (2 * pair + i < tiles ? 2 * pair + i : 0) + lc) * kSixRow, lg);
-  if (kFive) q5 = read_six(s_v + (kTile * (five ? kWaves : 0) + lc) * kSixRow, lg);
-  __syncthreads();  // the rows are read: their place is free
+  for (int i = 0; i < 2; ++i) q[i] = query(2 * pair + i);
+  if (kFive) q5 = query(kWaves);
 
   lds_u8* const v_lane = (lds_u8*)(uintptr_t)(lds0 + chunk_at(4 * lg + (lc >> 2), 0) + (uint32_t)(lc & 3) * 8u);
   Row me[2], extra;
@@ -641,33 +710,53 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
   // Block k of 32 of them is for the waves with ks = k % KS; the second pair of
   // waves has the fifth tile.
   if (W.tree) {
-    const int left = W.n - W.tree0 < kTreeRows ? W.n - W.tree0 : kTreeRows;
-    if (tid < kTreeTiles / 2) s_bad[tid] = 0;
-    stage_rows(left, [&](int r) { return W.k_row(A, W.tree0 + r); }, [&](int r) { return W.position(A, W.tree0 + r); },
-               1.0f);
-    asm volatile("" ::: "memory");
-    const bool also = five && pair == 1;
-    uint32_t bits[3];  // eight for each block
+    constexpr int kLoaded = kTreeRows * kHeadDim * 2 / 16 / kThreads;
+    uint4 v[kLoaded];  // a thread's values: row tid / 16 of each 16
 #pragma unroll
-    for (int i = 0; i < 3; ++i) bits[i] = 0;
+    for (int i = 0; i < kLoaded; ++i) {
+      const int r = 16 * i + tid / 16;
+      v[i] = *(const uint4*)(W.v_row(A, W.tree0 + (r < left ? r : left - 1)) + 8 * (tid % 16));
+    }
+    const bool also = five && pair == 1;
+    uint32_t bits[3] = {0, 0, 0};  // eight for each block
+    floatx4 s[3][2 * NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      const int j0 = W.tree0 + 32 * (ks + KS * k);
-      if (32 * (ks + KS * k) >= left) break;
+      const int block = ks + KS * k;
+      const auto see = [&](int r) {  // bit 4 t + e: the block's row 16 t + 4 lg + e
+        const uint32_t word = s_see[(r / W.G - tr0) * (kTreeTiles / 2) + block];
+        return (((word >> (4 * lg)) & 0xFu) | ((word >> (12 + 4 * lg)) & 0xF0u)) << (8 * k);
+      };
+      if (32 * block < left) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) bits[i] |= W.template allowed<2>(A, in[i] ? row[i] / W.G : 0, in[i], j0, lg) << (8 * k);
-      if (also) bits[2] |= W.template allowed<2>(A, in5 ? row5 / W.G : 0, in5, j0, lg) << (8 * k);
-    }
-    __syncthreads();
-    bf16x8 pb[3][NB];
-    const auto tree_weights = [&](const Six& qq, uint32_t see, Row& r, bf16x8 (&p)[NB]) {
-      floatx4 s[2 * NB];
-#pragma unroll
-      for (int t = 0; t < 2 * NB; ++t) {
-        const int at = 32 * (ks + KS * (t / 2)) + 16 * (t % 2);
-        s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (at < left) s[t] = score_six(read_six(s_v + (at + lc) * kSixRow, lg), qq, r.minus_m);
+        for (int i = 0; i < 2; ++i)
+          if (in[i]) bits[i] |= see(row[i]);
+        if (also && in5) bits[2] |= see(row5);
       }
+#pragma unroll
+      for (int t = 2 * k; t < 2 * k + 2; ++t) {
+        const int j = 32 * block + 16 * (t % 2);
+        s[0][t] = s[1][t] = s[2][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (j < left) {
+          const Six key = read_six(s_v + (j + lc < left ? j + lc : left - 1) * kSixRow, lg);
+          s[0][t] = score_six(key, q[0], s[0][t]);
+          s[1][t] = score_six(key, q[1], s[1][t]);
+          if (also) s[2][t] = score_six(key, q5, s[2][t]);
+        }
+      }
+    }
+    __syncthreads();  // queries and keys are read
+#pragma unroll
+    for (int i = 0; i < kLoaded; ++i) {
+      const int r = 16 * i + tid / 16;
+      if (16 * i >= (left + 31) / 32 * 32) break;
+      if (r >= left) v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (keep_finite(v[i])) atomicOr(&s_bad[r / 32], 1u << (r % 32));
+      *(uint4*)(s_v + chunk_at(r, tid % 16)) = v[i];
+    }
+    if (W.pg0 + 1 < W.pg1) here1 = issue(W.pg0 + 1);
+    bf16x8 pb[3][NB];
+    const auto tree_weights = [&](floatx4 (&s)[2 * NB], uint32_t see, Row& r, bf16x8 (&p)[NB]) {
 #pragma unroll
       for (int k = 0; k < NB; ++k) settle(s[2 * k], s[2 * k + 1]);
 #pragma unroll
@@ -677,11 +766,9 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
 #pragma unroll
       for (int k = 0; k < NB; ++k) p[k] = join(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
     };
-    tree_weights(q[0], bits[0], me[0], pb[0]);
-    tree_weights(q[1], bits[1], me[1], pb[1]);
-    if (also) tree_weights(q5, bits[2], extra, pb[2]);
-    __syncthreads();  // the keys are read
-    stage_values(tid, kThreads, (left + 31) / 32 * 32, left, [&](int r) { return W.v_row(A, W.tree0 + r); }, s_v, s_bad);
+    tree_weights(s[0], bits[0], me[0], pb[0]);
+    tree_weights(s[1], bits[1], me[1], pb[1]);
+    if (also) tree_weights(s[2], bits[2], extra, pb[2]);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
@@ -810,34 +897,37 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
     here1 = here2;
   }
 
-  // ---- the waves with the first keys take the others' rows, one tile after another
+  // ---- waves that share a tile: the one with ks = i takes tile i from the others,
+  // the last wave the fifth tile
   float* rec = (float*)s_v;
-  static_assert(((KS - 1) * (kWaves / KS) + 0) * kRec * 4 <= kLds && 3 * kRec * 4 <= kLds, "hand-over fits");
-  constexpr int kPairs = kWaves / KS;
+  constexpr int kOthers = (kWaves / KS) * 2 * (KS - 1);
+  static_assert((kOthers + (kFive ? kWaves - 1 : 0)) * kRec * 4 <= kLds, "hand-over fits");
+  const auto rec_of = [&](int i, int from) {
+    return rec + ((pair * 2 + i) * (KS - 1) + (from < i ? from : from - 1)) * kRec;
+  };
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    whole(me[i]);
-    float m = me[i].m();
-    __syncthreads();
-    if (ks > 0) give(me[i], rec + ((ks - 1) * kPairs + pair) * kRec);
-    __syncthreads();
-    if (ks == 0) {
+  for (int i = 0; i < 2; ++i) whole(me[i]);
+  if (kFive) whole(extra);
+  __syncthreads();
 #pragma unroll
-      for (int g = 1; g < KS; ++g) take(me[i], m, rec + ((g - 1) * kPairs + pair) * kRec);
+  for (int i = 0; i < 2; ++i)
+    if (ks != i) give(me[i], rec_of(i, ks));
+  if (kFive && five && w < kWaves - 1) give(extra, rec + (kOthers + w) * kRec);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (ks == i) {
+      float m = me[i].m();
+#pragma unroll
+      for (int g = 0; g < KS; ++g)
+        if (g != i) take(me[i], m, rec_of(i, g));
       if (in[i]) finish(A, W, me[i], m, row[i]);
     }
-  }
-  if (kFive && five) {
-    whole(extra);
+  if (kFive && five && w == kWaves - 1) {
     float m = extra.m();
-    __syncthreads();
-    if (w > 0) give(extra, rec + (w - 1) * kRec);
-    __syncthreads();
-    if (w == 0) {
 #pragma unroll
-      for (int g = 0; g < kWaves - 1; ++g) take(extra, m, rec + g * kRec);
-      if (in5) finish(A, W, extra, m, row5);
-    }
+    for (int g = 0; g < kWaves - 1; ++g) take(extra, m, rec + (kOthers + g) * kRec);
+    if (in5) finish(A, W, extra, m, row5);
   }
 }
 
@@ -846,6 +936,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn(Args A) {
   __shared__ __align__(16) uint8_t s_v[kLds];
   __shared__ double s_freq[kHeadDim / 2];
   __shared__ uint32_t s_bad[kTreeTiles / 2];  // tree rows whose values are not all finite
+  __shared__ uint32_t s_see[(kWaves + 1) * kTile * (kTreeTiles / 2)];  // and those that each row may see
   // consecutive workgroups of one XCD share a key head's pages in its L2
   const int total = (int)gridDim.x, x = (int)blockIdx.x;
   const int lin = total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x;
@@ -854,8 +945,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn(Args A) {
   if (!W.init(A, lin / A.chunks, (int)blockIdx.y)) return;
   const int tile0 = chunk * kWaves, all = (W.M + kTile - 1) / kTile;
   const int tiles = chunk == A.chunks - 1 ? all - tile0 : kWaves;  // up to five with kFive
-  if (kFive || tiles > 2) attend<2, kFive>(A, W, s_v, s_freq, s_bad, tile0, tiles);
-  else attend<4, false>(A, W, s_v, s_freq, s_bad, tile0, tiles);
+  if (kFive || tiles > 2) attend<2, kFive>(A, W, s_v, s_freq, s_bad, s_see, tile0, tiles);
+  else attend<4, false>(A, W, s_v, s_freq, s_bad, s_see, tile0, tiles);
 }
 
 // One tile of query rows: the four waves go through every fourth page alone, two
@@ -912,7 +1003,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   if (W.tree) stage_values(tid, kThreads, 32, W.n, [&](int r) { return W.v_row(A, r); }, tree_v, s_bad);
   if (w == 0 || (w == 1 && W.tree && (lane >> 2) < W.n)) {
     const int r = lane >> 2, g = group_of(lane & 3), qr = W.row_at(r), tr = w == 0 ? qr / W.G : r;
-    stage_six(w == 0 ? W.q_row(A, qr) : W.k_row(A, r), g, w == 0 ? score_scale() : 1.0f, rotate,
+    Group x;
+    load_group(w == 0 ? W.q_row(A, qr) : W.k_row(A, r), g, x);
+    stage_six(x, g, w == 0 ? score_scale() : 1.0f, rotate,
               [&](int e) { return turns[tr * 64 + 32 * (g & 1) + e]; }, (w == 0 ? six_q : six_k) + r * kSixRow);
   }
   __syncthreads();
@@ -924,7 +1017,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   Row me;
   me.clear();
   if (W.tree && w == 0) {
-    const uint32_t see = W.allowed<1>(A, in ? lc / W.G : 0, in, 0, lg);
+    const uint32_t see = W.allowed(A, in ? lc / W.G : 0, in, lg);
     floatx4 s[2];
     s[0] = score_six(read_six(six_k + lc * kSixRow, lg), q, me.minus_m);
     settle(s[0]);
