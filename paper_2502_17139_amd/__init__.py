@@ -654,11 +654,12 @@ class _Launch:
     tensors come from the pool of the stream that it runs on."""
 
     def __init__(self, stream, tensors):
-        self.device = next(t for t in tensors if t is not None).device
+        self.device = tensors[0].device
+        self.index = tensors[0].get_device()  # -1: the CPU
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != self.index:
                 raise ValueError(f"tensors on {self.device} and {t.device}: one device expected")
-        if self.device.type != "cuda":
+        if self.index < 0:
             raise ValueError("device tensor expected")
         if isinstance(stream, torch.cuda.Stream) and stream.device != self.device:
             raise ValueError(f"a stream of {self.device} expected, not of {stream.device}")
@@ -666,16 +667,18 @@ class _Launch:
 
     def __enter__(self):
         self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
+        if self.before != self.index:
             torch.cuda.set_device(self.device)
         return self
 
     def __exit__(self, *_):
-        if self.before != self.device.index:
+        if self.before != self.index:
             torch.cuda.set_device(self.before)
 
     def raw(self) -> int:
-        return _stream(self.stream)
+        if self.stream is not None:
+            return self.stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(self.index)
 
     def empty(self, shape, dtype) -> torch.Tensor:
         if self.stream is None:
@@ -693,6 +696,8 @@ def _rows(name: str, t: torch.Tensor, heads: int | None = None) -> int:
     D = FC_TREE_ATTN_HEAD_DIM
     if t.shape[-1] != D or (heads is not None and t.shape[-2] != heads):
         raise ValueError(f"{name} must have rows of [{'heads' if heads is None else heads}][{D}]")
+    if t.is_contiguous():
+        return t.shape[-2] * D
     row = t.stride(-3) if t.shape[-3] > 1 else (t.stride(0) if t.dim() == 4 and t.shape[0] > 1 else t.shape[-2] * D)
     if t.numel() and (t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != D) or
                       (t.dim() == 4 and t.shape[0] > 1 and t.stride(0) != t.shape[1] * row)):
@@ -754,11 +759,13 @@ def fc_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
     ins = (length, add, mask, last_node, table, queue, ends)
     with _Launch(stream, (*ins, *given)) as on:
         if out is None:
-            out = {f: on.empty(shape, dt) for f, shape, dt in zip(PLAN_FIELDS, shapes, _PLAN_DTYPES)}
-        o = [_ptr(out[f]) for f in PLAN_FIELDS]
+            sizes = (B, B + 1, n_slots, n_slots, n_slots)
+            out = dict(zip(PLAN_FIELDS, on.empty((sum(sizes),), i32).split(sizes)))  # one block, a call's own
+            out["ends"] = on.empty((2,), torch.int64)
+        p = _ptrs((length, add, table, queue, ends, *[out[f] for f in PLAN_FIELDS]))
         _check("fc_paged_plan", lib().fc_paged_plan(
-            _ptr(length), _ptr(add), _ptr(mask), _ptr(last_node), B, R, n_slots, _ptr(table), max_pages, _ptr(queue),
-            queue.numel(), _ptr(ends), *o, on.raw()))
+            p[0], p[1], _ptr(mask), _ptr(last_node), B, R, n_slots, p[2], max_pages, p[3], queue.numel(), *p[4:],
+            on.raw()))
     return out
 
 
@@ -802,6 +809,7 @@ def fc_paged_read(pool: torch.Tensor, slot: torch.Tensor, out=None, stream=None)
     return k, v
 
 
+@functools.lru_cache(maxsize=1024)  # it goes by the sizes alone
 def fc_paged_attention_workspace_bytes(B: int, R: int, H: int, Hkv: int, max_len: int) -> int:
     return int(lib().fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len))
 
@@ -843,10 +851,12 @@ def fc_paged_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tens
             out = on.empty((B, R, H, D), torch.bfloat16)
         if workspace is None and need > 0:
             workspace = on.empty((need,), torch.uint8)
+        p = _ptrs((pool, table, prefix_len, out) if tree is None else
+                  (pool, table, prefix_len, out, nodes, mask, pos_ids))
         _check("fc_paged_attention", lib().fc_paged_attention(
-            q.data_ptr(), qs, k_tree.data_ptr(), ks, v_tree.data_ptr(), vs, _ptr(pool), n_pages, _ptr(table),
-            max_pages, _ptr(prefix_len), _ptr(nodes), _ptr(mask), _ptr(pos_ids), B, R, H, Hkv, D, max_len, rope_base,
-            _ptr(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), on.raw()))
+            q.data_ptr(), qs, k_tree.data_ptr(), ks, v_tree.data_ptr(), vs, p[0], n_pages, p[1], max_pages, p[2],
+            *(p[4:] or (None, None, None)), B, R, H, Hkv, D, max_len, rope_base, p[3], _ptr(workspace),
+            0 if workspace is None else workspace.numel(), on.raw()))
     return out
 
 

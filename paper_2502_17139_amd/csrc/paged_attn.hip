@@ -1093,9 +1093,10 @@ __global__ void __launch_bounds__(kMergeWaves* fc::kWave) k_paged_merge(Args A) 
   const int parts = parts_of((P + kPage - 1) / kPage, A.part_pages) + more_parts(n);
   if (parts == 1) return;
   const int64_t at0 = bk * A.parts * M + r;
-  const float2 none = make_float2(-INFINITY, 0.0f);
-  const float2 x = lane < parts ? A.part_ml[at0 + (int64_t)lane * M] : none;
-  const float2 y = lane + 64 < parts ? A.part_ml[at0 + (int64_t)(lane + 64) * M] : none;
+  const bool has_x = lane < parts, has_y = lane + 64 < parts;
+  float2 x = A.part_ml[at0 + (int64_t)(has_x ? lane : 0) * M], y = A.part_ml[at0 + (int64_t)(has_y ? lane + 64 : 0) * M];
+  if (!has_x) x = make_float2(-INFINITY, 0.0f);
+  if (!has_y) y = make_float2(-INFINITY, 0.0f);
   float m = fmaxf(x.x, y.x);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
@@ -1159,9 +1160,13 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   s.chunks = s.five ? tiles / kWaves : (tiles + kWaves - 1) / kWaves;
   const int64_t wgs = (int64_t)B * Hkv * s.chunks;
   const int64_t pages = ((int64_t)max_len + kPage - 1) / kPage;
+  // As many parts as fill the card once (a sequence of 131,000 tokens, 8 key heads:
+  // 34.8 us, twice as many 42.5; 64 sequences of up to 8,192: 58.7 in one part, 61.5
+  // in two), of 4 pages at least, or 16 where each wave takes every fourth (16
+  // sequences of 2,048: 20.4 us, of 4 pages 20.7).
   const int64_t slots = 2 * kCus;  // workgroups at once
-  int64_t each = s.alone ? 16 : 4;  // pages of a part, at least
-  int64_t parts = s.alone ? (2 * slots + wgs - 1) / wgs : wgs >= slots ? 1 : (slots + wgs - 1) / wgs;
+  int64_t each = s.alone ? 16 : 4;
+  int64_t parts = (slots + wgs - 1) / wgs;
   if (parts > kMostParts) parts = kMostParts;
   const int64_t fit = (pages + each - 1) / each;
   if (parts > fit) parts = fit;
