@@ -620,18 +620,19 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * aligned; rows at or past num_nodes[b], and rows that may attend to nothing,
  * are 0.
  *
- * Rotated and scaled queries meet the cached keys as the sum of three 6-bit
- * parts (together within 2^-13 of the largest of each 32 dims), and the tree's
- * rotated keys, rounded to bf16, as the sum of two bf16 ones; softmax weights
- * are rounded to bf16, sums are fp32.  What is not finite among the keys and
- * values that a row attends to, or in its query, shows in its result (a NaN, an
- * infinity among values too); absent, masked and later tokens do not count,
- * whatever they hold.
+ * Rotated and scaled queries are the sum of three 6-bit parts (together within
+ * 2^-13 of the largest of each 32 dims), and so are the tree's rotated keys;
+ * softmax weights are rounded to bf16, sums are fp32.  What is not finite among
+ * the keys and values that a row attends to, or in its query, shows in its result
+ * (a NaN, an infinity among values too); absent, masked and later tokens do not
+ * count, whatever they hold.  Values of a magnitude of 2^96 or more may overflow
+ * the sums.
  *
  * ws holds fc_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (may
  * be NULL where that is 0); its contents on entry do not matter.  How a prefix
  * is cut into parts depends on the sizes and its own length; the same call gives
- * the same bits every time.  1 <= R <= FC_MAX_TREE_ROWS, H % Hkv == 0, D =
+ * the same bits every time, and a row's do not depend on the other rows.  B <=
+ * 65536, 1 <= R <= FC_MAX_TREE_ROWS, Hkv <= 1024, H <= 8192, H % Hkv == 0, D =
  * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
  */
 size_t fc_paged_attention_workspace_bytes(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len);

@@ -118,6 +118,32 @@ def test_plan_of_accepted_rows_matches_oracle(B, R):
     _plan(length, add, table, queue, [0, B], int(add.sum()) + 3, t["mask"], last)
 
 
+def test_plan_of_many_sequences():
+    """More sequences than a workgroup has threads, most of them short, and more
+    accepted paths than one: chunks whose sums go on, and slots that run out."""
+    rng = np.random.default_rng(3)
+    B = 2600
+    length = rng.integers(0, 150, B).astype(np.int32)
+    held = -(-length // 64)
+    perm = rng.permutation(int(held.sum()) + 900).astype(np.int32)
+    table, at = np.full((B, 4), -1, np.int32), 0
+    for b in range(B):
+        table[b, :held[b]] = perm[at:at + held[b]]
+        at += held[b]
+    queue = np.concatenate([perm[at:], np.full(at, -1, np.int32)])
+    add = rng.integers(-70, 40, B).astype(np.int32)
+    add[rng.random(B) < 0.02] = 200         # more than a table holds, at times
+    total = int(np.maximum(add, 0).sum())
+    for n_slots in (total, total // 3, 1, total + 5000):
+        say(f"plan of {B} sequences, {n_slots} of {total} slots")
+        _plan(length, add, table, queue, [0, 900], n_slots)
+    t = trees(rng, 1100, 9)
+    last = rng.integers(-2, 10, 1100).astype(np.int32)
+    add = np.array([t["pos_ids"][b, min(max(last[b], 0), 8)] + 1 for b in range(1100)], np.int32)
+    say("plan of 1100 accepted paths, some of no row")
+    _plan(length[:1100], add, table[:1100], queue, [0, 900], int(add.sum()), t["mask"], last)
+
+
 def test_plan_of_bad_tables_and_lengths():
     """Lengths past the table, table entries outside the pool, a ring whose
     ends say more than it can hold: nothing outside the buffers is touched and
@@ -254,7 +280,7 @@ def bound(o, mean, far, keys):
 
 
 def attend(rng, B, R, H, Hkv, lens, tree=None, rope_base=10000.0, pool=None, table=None, max_len=None, qscale=1.0,
-           n_pages=None, kw=None, width=None):
+           n_pages=None, kw=None, width=None, q=None):
     """One call against the oracle, within the bound; returns the result."""
     if pool is None:
         n_pages = n_pages or max(1, sum(-(-max(n, 0) // 64) for n in lens))
@@ -262,7 +288,8 @@ def attend(rng, B, R, H, Hkv, lens, tree=None, rope_base=10000.0, pool=None, tab
     if table is None:
         width = width or max(1, max(-(-max(n, 0) // 64) for n in lens))
         table = rng.integers(0, pool.shape[0], (B, width)).astype(np.int32)
-    q, kt, vt = bf16(rng, B, R, H, D, scale=qscale), bf16(rng, B, R, Hkv, D), bf16(rng, B, R, Hkv, D)
+    q = bf16(rng, B, R, H, D, scale=qscale) if q is None else q
+    kt, vt = bf16(rng, B, R, Hkv, D), bf16(rng, B, R, Hkv, D)
     plen = np.asarray(lens, np.int32)
     got = fc.fc_paged_attention(q.cuda(), kt.cuda(), vt.cuda(), pool, dev(table), dev(plen), tree=on_gpu(tree),
                                 max_len=max_len, rope_base=rope_base, **(kw or {}))
@@ -328,6 +355,55 @@ def test_attention_bounds_and_far_positions():
     table[0, [0, 700, 2046]] = [3, 4, 5]
     attend(rng, 1, 5, 4, 2, [131_000], pool=pool, table=table)
     attend(rng, 1, 5, 4, 2, [131_000], trees(rng, 1, 5), pool=pool, table=table, rope_base=1e6)
+
+
+def _along(rng, u, sizes, Hkv):
+    """A pool of one page per size: keys of that size along u (a row of signs)
+    or, every third, against it, and a little noise."""
+    n = len(sizes)
+    way = np.where(np.arange(64 * n) % 3 == 2, -1.0, 1.0) * np.repeat(sizes, 64)
+    k = way[:, None, None] * u + rng.standard_normal((64 * n, Hkv, D)) * 0.02
+    pool = torch.zeros((n, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_write(pool, torch.from_numpy(k).to(BF).cuda(), bf16(rng, 64 * n, Hkv, D).cuda(),
+                      dev(np.arange(64 * n, dtype=np.int32)), rope_base=0.0)
+    return pool
+
+
+@pytest.mark.parametrize("R,G", [(1, 1), (5, 2), (30, 1), (64, 1), (65, 1), (70, 4)])
+def test_attention_of_scores_far_apart(R, G):
+    """Scores that grow by far more than a weight's range from page to page, fall
+    so, or do both: between nothing and e^90 apart, each row its own way."""
+    rng = np.random.default_rng(R)
+    u = rng.choice([-1.0, 1.0], D)
+    for sizes in (np.linspace(0, 8, 12), np.linspace(8, 0, 12), np.abs(np.linspace(-8, 8, 12)),
+                  8 * (np.arange(12) % 5 == 3)):
+        pool = _along(rng, u, sizes, 1)
+        c = np.where(np.arange(R * G) % 4 == 3, -1.0, 1.0) * rng.uniform(0, 1, R * G)  # score: c * size * 128 / sqrt(128)
+        q = torch.from_numpy(c.reshape(1, R, G, 1) * u).to(BF)
+        say(f"scores far apart R={R} G={G} sizes {sizes[0]:.0f} to {sizes[-1]:.0f}")
+        for lens in ([768], [747]):
+            attend(rng, 1, R, G, 1, lens, pool=pool, table=np.arange(12, dtype=np.int32)[None], rope_base=0.0, q=q)
+
+
+def test_attention_rows_do_not_move_each_other():
+    """A row's bits are its own: other rows of its wave whose scores lie far
+    apart, or are not finite, change nothing."""
+    rng = np.random.default_rng(21)
+    u = rng.choice([-1.0, 1.0], D)
+    pool = _along(rng, u, np.linspace(0, 8, 12), 1)
+    table, plen = dev(np.arange(12, dtype=np.int32)[None]), dev(np.array([760], np.int32))
+    for R in (1, 9, 33, 65):
+        G = 3 if R == 1 else 1
+        q = bf16(rng, 1, R, G, D, scale=0.3)
+        kt, vt = bf16(rng, 1, R, 1, D), bf16(rng, 1, R, 1, D)
+        other = q.clone()
+        change = np.arange(R * G) % 3 != 0
+        other.view(R * G, D)[torch.from_numpy(change)] = torch.from_numpy(u).to(BF)
+        other.view(R * G, D)[1] = float("nan")
+        say(f"rows do not move each other R={R}")
+        a, b = (fc.fc_paged_attention(x.cuda(), kt.cuda(), vt.cuda(), pool, table, plen, rope_base=0.0) for x in (q, other))
+        a, b = (x.view(R * G, D).view(torch.int16).cpu().numpy() for x in (a, b))
+        assert np.array_equal(a[~change], b[~change]) and not np.array_equal(a[change], b[change])
 
 
 def test_attention_of_masks_that_leave_nothing():
