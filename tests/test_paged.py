@@ -205,6 +205,27 @@ def test_writes_match_oracle(Hkv, n_pages, n_src, n, rope_base):
     _write_case(rng, n_pages, Hkv, max(n, n_src), n, rope_base, scale=1e-3, use_src=False)
 
 
+def test_writes_of_long_runs():
+    """Enough tokens for several a workgroup: runs of positions, broken ones, far
+    ones, and the same bytes as in writes of a few tokens each."""
+    rng = np.random.default_rng(4)
+    for Hkv, n in ((1, 33_000), (8, 9_001), (48, 1_300)):
+        pages = -(-n // 64)
+        pos = np.arange(n) % 700 + np.repeat(rng.integers(0, 2 ** 30, -(-n // 700)), 700)[:n]
+        pos[rng.random(n) < 0.01] = 5
+        k, v = bf16(rng, n, Hkv, D).cuda(), bf16(rng, n, Hkv, D).cuda()
+        slot, pos = dev(rng.permutation(64 * pages)[:n].astype(np.int32)), dev(pos.astype(np.int32))
+        pools = [torch.zeros((pages, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        say(f"writes of long runs, {n} tokens of {Hkv} heads")
+        fc.fc_paged_write(pools[0], k, v, slot, pos)
+        for i in range(0, n, 1000):
+            fc.fc_paged_write(pools[1], k[i:i + 1000], v[i:i + 1000], slot[i:i + 1000], pos[i:i + 1000])
+        assert torch.equal(pools[0], pools[1])
+        at, x = rng.integers(0, n, 40), host(pools[0])  # the same rows again by the oracle: nothing changes
+        again = oracle.paged_write(x, f64(k[at]), f64(v[at]), host(slot)[at], host(pos)[at])
+        assert np.array_equal(again, x)
+
+
 def test_writes_of_every_kind_of_value():
     """Ties, the edges of the scales, zeros of both signs, the smallest and
     largest numbers, infinities and NaN: not rotated, and turned by nothing at
