@@ -3,8 +3,8 @@
 //
 // The rows of a tree that share a key head - its R rows times the H / Hkv query
 // heads of the group - are one matrix of queries, cut into tiles of 16 rows.  A
-// workgroup takes some of a (tree, key head)'s tiles and some of its pages; its
-// waves are split over the tiles first and over the pages with what is left.
+// workgroup of four waves takes up to five of a (tree, key head)'s tiles and a
+// part of its pages.
 //
 // Per page of 64 keys a wave computes the transposed scores S^T = K Q^T and
 // O^T += V^T P^T, which keeps a lane's scores where the second product wants
@@ -13,9 +13,35 @@
 // the cache's own format, so no key is ever unpacked.  Its other operand has at
 // most 6 bits at the full rate, so a query is the sum of three 6-bit parts, each
 // with the scale of what the last one left over: three products of 16 cycles
-// where bf16 would take four and the unpacking.  The value codes are unpacked to
-// bf16 in LDS (their scales vary along the sum, which the matrix cores do not
-// take) by the waves that share them, and read back transposed.
+// where bf16 would take four and the unpacking.  The tree's own keys, which are
+// not cached yet, are three such parts too.  The value codes are unpacked to bf16
+// in LDS (their scales vary along the sum, which the matrix cores do not take),
+// a quarter of a page by each wave, and read back transposed.
+//
+// How the work is split:
+// - one tile (a decoded token, a short chain): the waves go through every fourth
+//   page alone, out of registers, without a barrier until the end.  One row over
+//   131,000 tokens, 8 key heads: 30 us and 5 for the join, where a copy of its bytes
+//   takes 29; bound by memory.  64 rows over up to 8,192: 61 us in place of 41, as
+//   long as the longest take.
+// - more: two pairs of waves, each wave with two tiles and half of a page's keys,
+//   and a fifth tile (a tree's 65th row) split over all four waves.  One tile a wave
+//   and twice the waves a SIMD would be faster where there is no fifth tile (64
+//   trees of 64 rows over 2,048 tokens: 225 us against 254), but reads every page
+//   again for it (65 rows: 406 against 330); a tree's root and its 64 drafted rows
+//   make the fifth tile the usual case.  A workgroup of five waves leaves one SIMD
+//   with two of them (458).
+// - up to two tiles: the four waves take 16 keys each.
+// Prefixes are cut into parts where there are too few workgroups to fill the card,
+// and joined by k_paged_merge.
+//
+// What bounds the second form, at 64 trees of 65 rows, 32 heads, 2,048 tokens (281
+// us; a copy of its bytes takes 143, its products 128): a page takes a pair of
+// workgroups about 2,900 cycles, of which a SIMD's vector unit is at work for 46 %
+// and its matrix unit for 26 %.  The two do not overlap within a wave - scores,
+// weights, values follow one another - and 254 registers leave two waves a SIMD to
+// fill the gaps.  A third of the time is what comes before and after the pages:
+// queries and tree rows to 6-bit parts, and the hand-over.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -145,10 +171,11 @@ __device__ __forceinline__ void write_six(const float (&v)[32], uint8_t* row, in
   *(uint32_t*)(row + 288 + 4 * g) = word;
 }
 
-// Group g (32 dims) of a row of 128 bf16 to LDS in 6-bit parts,
-// rotated and scaled.  The lane beside this one (lane ^ 1) has the group 64 dims
-// away, so the two share the angles: turn(e) gives the sine and cosine of the
-// pair's angle e, of which this lane asks for half.
+// Groups of 32 dims of rows of 128 bf16 on their way to LDS in 6-bit parts, rotated
+// and scaled.  The lane beside this one (lane ^ 1) has the group 64 dims away, so
+// the two share the angles, in double precision: turn(d) gives the sine and cosine
+// of this lane's d-th angle, of the 16 from first_angle on.
+__device__ __forceinline__ int first_angle(int g) { return 32 * (g & 1) + (g >= 2 ? 16 : 0); }
 struct Group {
   uint4 own[4], other[4];
 };
@@ -176,12 +203,11 @@ __device__ __forceinline__ void stage_six(const Group& in, int g, float scale, b
     const uint32_t* y = (const uint32_t*)other;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      asm volatile("" ::: "memory");  // few of the angles in registers at a time
+      if (u % 4 == 0) asm volatile("" ::: "memory");  // eight of the angles in registers at a time
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        // angles d (the lower lane's) and d + 16 (the upper's)
         const int d = 2 * u + e;
-        const float2 t = turn((upper ? 16 : 0) + d);
+        const float2 t = turn(d);
         const float s = __uint_as_float(fc::dpp_mov<0xB1>(__float_as_uint(t.x)));
         const float c = __uint_as_float(fc::dpp_mov<0xB1>(__float_as_uint(t.y)));
         const float y0 = __uint_as_float(e ? y[u] & 0xFFFF0000u : y[u] << 16);
@@ -675,6 +701,11 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       load_group(r < rows ? W.q_row(A, qr) : W.k_row(A, kr), group_of(u & 3), x);
       if (rotate) at = W.position(A, r < rows ? qr / W.G : kr);
     };
+    double freq[16];  // of the lane's angles, in every row the same ones
+    if (rotate) {
+#pragma unroll
+      for (int d = 0; d < 16; ++d) freq[d] = s_freq[first_angle(group_of(tid & 3)) + d];
+    }
     Group x;
     int at = 0;
     load(tid, x, at);
@@ -685,7 +716,7 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       const int r = u >> 2, g = group_of(u & 3);
       const double pos = (double)at;
       stage_six(x, g, r < rows ? score_scale() : 1.0f, rotate,
-                [&](int e) { return turn_of(pos * s_freq[32 * (g & 1) + e]); },
+                [&](int d) { return turn_of(pos * freq[d]); },
                 r < rows ? six_q + r * kSixRow : s_v + (r - rows) * kSixRow);
       x = next;
       at = next_at;
@@ -953,7 +984,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn(Args A) {
 }
 
 // One tile of query rows: the four waves go through every fourth page alone, two
-// pages on their way in a wave's registers, and wait for nobody until the end.
+// pages on their way in a wave's registers, and wait for nobody until the end.  One
+// row over 3,000 tokens, 8 key heads: 13 us, of which the start - queries, tree rows,
+// the first pages' latency - is 9; one over 131,000: 30 us (4.8 TB/s).
 __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   __shared__ __align__(16) uint8_t s_v[kWaves * kValues];
   __shared__ uint32_t s_bad[1];
@@ -1009,7 +1042,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
     Group x;
     load_group(w == 0 ? W.q_row(A, qr) : W.k_row(A, r), g, x);
     stage_six(x, g, w == 0 ? score_scale() : 1.0f, rotate,
-              [&](int e) { return turns[tr * 64 + 32 * (g & 1) + e]; }, (w == 0 ? six_q : six_k) + r * kSixRow);
+              [&](int d) { return turns[tr * 64 + first_angle(g) + d]; }, (w == 0 ? six_q : six_k) + r * kSixRow);
   }
   __syncthreads();
   const Six q = read_six(six_q + lc * kSixRow, lg);
@@ -1082,7 +1115,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
 // The parts of a row put together: sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m)
 // l_s with m the largest m_s.  A wave per row: a lane has the weight of one or two
 // parts, then each 16 lanes add up every fourth part, eight dims a lane.  A prefix
-// in one part is in place already.
+// in one part is in place already.  4 us for 32 rows of 3 parts, 5 for 2,080 of 12 or
+// 32 of 64: a launch and three round trips to memory.
 constexpr int kMergeWaves = 4;
 __global__ void __launch_bounds__(kMergeWaves* fc::kWave) k_paged_merge(Args A) {
   const int G = A.H / A.Hkv, M = A.R * G;
