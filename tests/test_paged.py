@@ -290,7 +290,8 @@ def make_pool(rng, n_pages, Hkv):
 def bound(o, mean, far, keys):
     """What roundings may move a result by.  A score of a cached key: the three
     parts of a query leave 2^-13 of the largest of its 32 dims; of a tree's key:
-    query and key are bf16 (2^-8 each, so 2^-7 + 2^-16 together); both: the
+    no more than query and key in bf16 would (2^-8 each, so 2^-7 + 2^-16
+    together); both: the
     hardware's sine and cosine (2^-18 each of a pair's two products) and fp32.
     Scores that move by delta at most move each weight by e^(2 delta) - 1 of
     itself; weights are rounded to bf16 (2^-8), sums are fp32, and so is the
