@@ -752,6 +752,8 @@ def fc_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
         R = mask.shape[-1]
         _expect("mask", mask, i32, (B, R, R))
         _expect("last_node", last_node, i32, (B,))
+    if not 0 <= n_slots < 2 ** 30:
+        raise ValueError(f"n_slots must be in [0, 2^30), not {n_slots}")
     shapes = ((B,), (B + 1,), (n_slots,), (n_slots,), (n_slots,), (2,))
     if out is not None:
         _expect_all(PLAN_FIELDS, [out.get(f) for f in PLAN_FIELDS], _PLAN_DTYPES, shapes)
@@ -845,6 +847,8 @@ def fc_paged_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tens
     _expect("workspace", workspace, torch.uint8, optional=True)
     if max_len is None:
         max_len = max_pages * FC_PAGE_TOKENS
+    if abs(max_len) >= 2 ** 31:  # the library takes 32 bits of it, and refuses those out of range
+        raise ValueError(f"max_len must be a 32-bit number, not {max_len}")
     need = fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len)
     with _Launch(stream, (q, k_tree, v_tree, pool, table, prefix_len, nodes, mask, pos_ids, out, workspace)) as on:
         if out is None:

@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kWriteThreads) k_paged_write(
       const int x = tid / fc::kWave * each + e;
       if (x >= tokens || i0 + x >= n) break;
       const int p = pos[i0 + x];
-      if (e > 0 && p - 1 == at) t = make_double2(t.x * one.y + t.y * one.x, t.y * one.y - t.x * one.x);
+      if (e > 0 && (int64_t)p == (int64_t)at + 1) t = make_double2(t.x * one.y + t.y * one.x, t.y * one.y - t.x * one.x);
       else t = turn((double)p * freq);
       at = p;
       s_turn[x * fc::kWave + d] = t;

@@ -213,6 +213,7 @@ def test_writes_of_long_runs():
         pages = -(-n // 64)
         pos = np.arange(n) % 700 + np.repeat(rng.integers(0, 2 ** 30, -(-n // 700)), 700)[:n]
         pos[rng.random(n) < 0.01] = 5
+        pos[100:103] = 2 ** 31 - 1, -2 ** 31, 1 - 2 ** 31  # no run, and one of far positions before 0
         k, v = bf16(rng, n, Hkv, D).cuda(), bf16(rng, n, Hkv, D).cuda()
         slot, pos = dev(rng.permutation(64 * pages)[:n].astype(np.int32)), dev(pos.astype(np.int32))
         pools = [torch.zeros((pages, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda") for _ in range(2)]
@@ -221,7 +222,7 @@ def test_writes_of_long_runs():
         for i in range(0, n, 1000):
             fc.fc_paged_write(pools[1], k[i:i + 1000], v[i:i + 1000], slot[i:i + 1000], pos[i:i + 1000])
         assert torch.equal(pools[0], pools[1])
-        at, x = rng.integers(0, n, 40), host(pools[0])  # the same rows again by the oracle: nothing changes
+        at, x = np.r_[100:103, rng.integers(0, n, 40)], host(pools[0])  # the same rows again by the oracle: nothing changes
         again = oracle.paged_write(x, f64(k[at]), f64(v[at]), host(slot)[at], host(pos)[at])
         assert np.array_equal(again, x)
 

@@ -168,3 +168,15 @@ def test_plan_and_write_bindings_refuse():
         fc.fc_paged_write(s["pool"], torch.zeros((6, 3, 128), dtype=BF), k, slot, slot)
     with pytest.raises(ValueError, match="v must"):
         fc.fc_paged_read(s["pool"], slot, out=(torch.zeros((4, 2, 128), dtype=BF), torch.zeros((3, 2, 128), dtype=BF)))
+
+
+def test_bindings_refuse_numbers_out_of_range():
+    """Numbers that the C call would take 32 bits of."""
+    s = _inputs()
+    for max_len in (2 ** 31, 2 ** 32 + 64, -2 ** 31):
+        with pytest.raises(ValueError, match="max_len"):
+            fc.fc_paged_attention(**s, max_len=max_len)
+    st = fc.paged_state(2, 3, 9, "cpu")
+    for n_slots in (-1, 2 ** 30, 2 ** 32):
+        with pytest.raises(ValueError, match="n_slots"):
+            fc.fc_paged_plan(st["len"], st["len"], st["table"], st["queue"], st["ends"], n_slots)
