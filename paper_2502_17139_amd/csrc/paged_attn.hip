@@ -566,20 +566,6 @@ struct See {
   }
 };
 
-// Rows of bf16 values to LDS, what is not finite marked in `bad` and 0; zeros from
-// row `left` on.
-template <typename Row16>
-__device__ __forceinline__ void stage_values(int first, int step, int rows, int left, Row16 row, uint8_t* to,
-                                             uint32_t* bad) {
-  for (int u = first; u < rows * 16; u += step) {
-    const int r = u / 16, c = u % 16;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r < left) v = *(const uint4*)(row(r) + 8 * c);
-    if (keep_finite(v)) atomicOr(&bad[r / 32], 1u << (r % 32));
-    *(uint4*)(to + chunk_at(r, c)) = v;
-  }
-}
-
 // ---- waves that shared a tile's keys hand over to one of them, through LDS
 constexpr int kRec = kTile * kHeadDim + 2 * kTile;  // floats of a tile: outputs, maxima, weights
 __device__ __forceinline__ void whole(Row& r) {
@@ -998,6 +984,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   if (!W.init(A, total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x, (int)blockIdx.y)) return;
   const bool rotate = A.log2_base > 0.0, in = lc < W.M;
 
+  // The few query and tree rows (16 at most) are asked for ahead of the pages, which
+  // would be waited for with them otherwise: a lane for a quarter of each row in
+  // waves 0 (queries) and 1 (tree keys), one chunk of values a thread.
+  const int six_r = lane >> 2, six_g = group_of(lane & 3), tree_r = six_r < W.n ? six_r : W.n - 1;
+  const bool has_six = w == 0 || (w == 1 && W.tree && six_r < W.n);
+  Group six;
+  if (w == 0) load_group(W.q_row(A, W.row_at(six_r)), six_g, six);
+  if (w == 1 && W.tree) load_group(W.k_row(A, tree_r), six_g, six);
+  uint4 tree_values = make_uint4(0u, 0u, 0u, 0u);  // of row tid / 16; the rows from 16 on are zeros
+  if (W.tree) tree_values = *(const uint4*)(W.v_row(A, tid / 16 < W.n ? tid / 16 : W.n - 1) + 8 * (tid % 16));
+
   struct Page {
     uint4 kf[4], vf[4];
     uint32_t ks, vs;
@@ -1025,9 +1022,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   load(even);
   load(odd);
 
-  // Meanwhile the few query and tree rows (16 at most): sines and cosines of every
-  // position once, then a lane for a quarter of each row.  Wave 0 has the tree's
-  // rows in its buffer, the others' hold the rest until their pages come.
+  // Meanwhile those rows go to LDS: sines and cosines of every position once, then
+  // 6-bit parts.  Wave 0 has the tree's rows in its buffer, the others' hold the
+  // rest until their pages come.
   uint8_t *six_k = s_v, *tree_v = s_v + kTile * kSixRow, *six_q = s_v + kValues;
   float2* turns = (float2*)(s_v + 2 * kValues);
   if (tid == 0) s_bad[0] = 0;
@@ -1036,13 +1033,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
     for (int r = w; r < A.R; r += kWaves) turns[r * 64 + lane] = turn_of((double)W.position(A, r) * f);
   }
   __syncthreads();
-  if (W.tree) stage_values(tid, kThreads, 32, W.n, [&](int r) { return W.v_row(A, r); }, tree_v, s_bad);
-  if (w == 0 || (w == 1 && W.tree && (lane >> 2) < W.n)) {
-    const int r = lane >> 2, g = group_of(lane & 3), qr = W.row_at(r), tr = w == 0 ? qr / W.G : r;
-    Group x;
-    load_group(w == 0 ? W.q_row(A, qr) : W.k_row(A, r), g, x);
-    stage_six(x, g, w == 0 ? score_scale() : 1.0f, rotate,
-              [&](int d) { return turns[tr * 64 + first_angle(g) + d]; }, (w == 0 ? six_q : six_k) + r * kSixRow);
+  if (W.tree) {
+    const int r = tid / 16, c = tid % 16;
+    if (r >= W.n) tree_values = make_uint4(0u, 0u, 0u, 0u);
+    if (keep_finite(tree_values)) atomicOr(&s_bad[0], 1u << r);
+    *(uint4*)(tree_v + chunk_at(r, c)) = tree_values;
+    *(uint4*)(tree_v + chunk_at(kTile + r, c)) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (has_six) {
+    const int tr = w == 0 ? W.row_at(six_r) / W.G : six_r;
+    stage_six(six, six_g, w == 0 ? score_scale() : 1.0f, rotate,
+              [&](int d) { return turns[tr * 64 + first_angle(six_g) + d]; }, (w == 0 ? six_q : six_k) + six_r * kSixRow);
   }
   __syncthreads();
   const Six q = read_six(six_q + lc * kSixRow, lg);
