@@ -61,10 +61,11 @@ __device__ __forceinline__ Sums block_sums(const Sums& v, int waves, Sums* scrat
 // it all.  A window position that starts a sequence carries that sequence's
 // data; a running maximum over the positions takes each token to its start.
 // What it costs is latency: a load of the lengths, the sums, and for a tree's
-// step a load of each sequence's mask row; hence sixteen waves, one sequence's row
-// each, and 4,096 tokens a workgroup, so that few workgroups scan.  64 accepted
-// paths 10.6 us (18 with four waves), 512 prompts of a million slots 25.4 (39; 64
-// with 1,024 tokens a workgroup; a copy of its bytes takes 2.4).  The scan is 8 bytes
+// step a load of each sequence's mask row; hence sixteen waves, four sequences' rows
+// at a time each, and 4,096 tokens a workgroup, so that few workgroups scan.  64
+// accepted paths 8.7 us (18 with four waves and a row at a time), 512 prompts of a
+// million slots 20.8 (39; 64 with 1,024 tokens a workgroup; a copy of its bytes
+// takes 2.4).  The scan is 8 bytes
 // a sequence from L2: at the 65,536 sequences allowed it is what costs, at the
 // thousands of a serving batch it is not.
 __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
@@ -100,7 +101,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
   const int64_t head = ends[0], tail = ends[1];
   const uint64_t held_free = tail > head ? (uint64_t)(tail - head) : 0;
   const uint64_t avail = held_free < (uint64_t)n_pages ? held_free : (uint64_t)n_pages;
-  const uint64_t head_at = (uint64_t)head % (uint32_t)n_pages, tail_at = (uint64_t)tail % (uint32_t)n_pages;
+  // the first chunk's inputs, on their way while LDS is cleared
+  const int32_t len0 = tid < B ? len[tid] : 0, add0 = tid < B ? add[tid] : 0;
+  const int32_t last0 = tid < B && mask ? last_node[tid] : -1;
   for (int x = tid; x < kPlanTokens; x += kPlanThreads) s_start[x] = 0, s_src[x] = -1;
   if (tid == 0) s_listed = 0, s_given = 0, s_backs = 0;
   __syncthreads();
@@ -110,16 +113,16 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     const int b = b0 + tid;
     const bool in = b < B;
     const int64_t cap = (int64_t)max_pages * kPage;
-    int64_t n = in ? len[b] : 0;
+    int64_t n = b0 == 0 ? len0 : in ? len[b] : 0;
     n = n < 0 ? 0 : n > cap ? cap : n;
-    const int64_t a = in ? add[b] : 0;
+    const int64_t a = b0 == 0 ? add0 : in ? add[b] : 0;
     const uint64_t want = a > 0 ? (uint64_t)a : 0;
     int64_t now = n + a < 0 ? 0 : n + a;
     const int64_t held = (n + kPage - 1) / kPage, pages = (now + kPage - 1) / kPage;
     const uint64_t back = a < 0 ? (uint64_t)(held - pages) : 0;
     const bool short_enough = a <= 0 || pages <= max_pages;
     uint64_t need = short_enough && a > 0 ? (uint64_t)(pages - held) : 0;
-    int32_t last = in && mask ? last_node[b] : -1;
+    int32_t last = b0 == 0 ? last0 : in && mask ? last_node[b] : -1;
     if (last >= R || last < 0) last = -1;
     const int waves = B - b0 < kPlanThreads ? (int)fc::div_up((uint64_t)(B - b0), fc::kWave) : kPlanWaves;
     Sums sum;
@@ -136,7 +139,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     }
     taken += sum.x[2];
     const bool ok = fits && (need == 0 || page0 + need <= avail);
-    if (ok && need > 0) atomicMax(&s_given, (unsigned long long)(page0 + need));  // the sums only grow
+    // the sums only grow: of a wave's sequences that take pages the last one has the most
+    const uint64_t takes = fc::ballot(ok && need > 0);
+    if (takes && lane == 63 - __builtin_clzll(takes)) atomicMax(&s_given, (unsigned long long)(page0 + need));
     if (!ok) now = n;
     if (in && blockIdx.x == 0) {
       len_out[b] = (int32_t)now;
@@ -144,13 +149,18 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
       cu[b + 1] = (int32_t)(end < 0x7FFFFFFFu ? end : 0x7FFFFFFFu);
     }
     if (back > 0 && (uint32_t)b % gridDim.x == blockIdx.x)
-      s_back[atomicAdd(&s_backs, 1)] = Back{(uint32_t)((tail_at + to) % (uint32_t)n_pages), b, (int32_t)pages, (int32_t)back};
-    if (want > 0 && (int64_t)first < w0 + kPlanTokens && (int64_t)(first + want) > w0) {
+      s_back[atomicAdd(&s_backs, 1)] = Back{(uint32_t)(((uint64_t)tail + to) % (uint32_t)n_pages), b, (int32_t)pages, (int32_t)back};
+    const bool here = want > 0 && (int64_t)first < w0 + kPlanTokens && (int64_t)(first + want) > w0;
+    const uint64_t in_wave = fc::ballot(here);
+    int at = 0;
+    if (in_wave && lane == 0) at = atomicAdd(&s_listed, (int)__builtin_popcountll(in_wave));
+    at = __shfl(at, 0) + (int)__builtin_popcountll(in_wave & fc::lanemask_lt());
+    if (here) {
       const int x = (int64_t)first > w0 ? (int)((int64_t)first - w0) : 0;
       s_seq[x] = Seq{(int32_t)(n - ((int64_t)first - w0)), b, (uint32_t)page0, (uint32_t)want,
                      (uint32_t)(w0 + x - (int64_t)first), ok ? last : -2};
       s_start[x] = (uint16_t)(x + 1);
-      s_list[atomicAdd(&s_listed, 1)] = (uint16_t)x;
+      s_list[at] = (uint16_t)x;
     }
     __syncthreads();
     const int backs = s_backs;
@@ -171,27 +181,41 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
   // a tree step's source rows: a wave per sequence takes the rows that the
   // accepted row may see, in order
   if (mask) {
+    constexpr int kAtOnce = 4;  // sequences of a wave whose rows are on their way together
     const int listed = s_listed;
-    for (int i = wave; i < listed; i += kPlanWaves) {
-      const int x = s_list[i];
-      const Seq q = s_seq[x];
-      if (q.last < 0) continue;
-      const int32_t* row = mask + ((int64_t)q.b * R + q.last) * R;
-      int before = 0;
-#pragma unroll 2
+    for (int i0 = wave; i0 < listed; i0 += kAtOnce * kPlanWaves) {
+      int x[kAtOnce], before[kAtOnce];
+      Seq q[kAtOnce];
+      const int32_t* row[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + u * kPlanWaves;
+        x[u] = s_list[i < listed ? i : i0];
+        q[u] = s_seq[x[u]];
+        if (i >= listed) q[u].last = -1;
+        row[u] = mask + ((int64_t)q[u].b * R + (q[u].last < 0 ? 0 : q[u].last)) * R;
+        before[u] = 0;
+      }
       for (int j0 = 0; j0 < R; j0 += fc::kWave) {
         const int j = j0 + lane;
-        const bool on = j < R && row[j] == 1;
-        const uint64_t all = fc::ballot(on);
-        const uint32_t t = (uint32_t)(before + (int)__builtin_popcountll(all & fc::lanemask_lt()));
-        const uint32_t at = x + t - q.first;
-        if (on && t >= q.first && t < q.count && at < kPlanTokens) s_src[at] = q.b * R + j;
-        before += (int)__builtin_popcountll(all);
+        int32_t m[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) m[u] = row[u][j < R ? j : 0];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const bool on = j < R && m[u] == 1 && q[u].last >= 0;
+          const uint64_t all = fc::ballot(on);
+          const uint32_t t = (uint32_t)(before[u] + (int)__builtin_popcountll(all & fc::lanemask_lt()));
+          const uint32_t to = x[u] + t - q[u].first;
+          if (on && t >= q[u].first && t < q[u].count && to < kPlanTokens) s_src[to] = q[u].b * R + j;
+          before[u] += (int)__builtin_popcountll(all);
+        }
       }
     }
     __syncthreads();
   }
 
+  const uint32_t head_at = (uint32_t)((uint64_t)head % (uint32_t)n_pages);
   int start[kPlanEach], run = 0;
 #pragma unroll
   for (int e = 0; e < kPlanEach; ++e) {
@@ -217,7 +241,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     if (idx < held) {
       page = table[(int64_t)q.b * max_pages + idx];
     } else {
-      const uint32_t i = (uint32_t)head_at + q.page0 + (uint32_t)(idx - held);  // less than 2 n_pages
+      const uint32_t i = head_at + q.page0 + (uint32_t)(idx - held);  // less than 2 n_pages
       page = queue[i < (uint32_t)n_pages ? i : i - (uint32_t)n_pages];
       if (p % kPage == 0) table[(int64_t)q.b * max_pages + idx] = page;  // every new page starts with a token
     }

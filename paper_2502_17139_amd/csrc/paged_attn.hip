@@ -21,8 +21,8 @@
 // How the work is split:
 // - one tile (a decoded token, a short chain): the waves go through every fourth
 //   page alone, out of registers, without a barrier until the end.  One row over
-//   131,000 tokens, 8 key heads: 30 us and 5 for the join, where a copy of its bytes
-//   takes 29; bound by memory.  64 rows over up to 8,192: 61 us in place of 41, as
+//   131,000 tokens, 8 key heads: 29 us and 5 for the join, where a copy of its bytes
+//   takes 29; bound by memory.  64 rows over up to 8,192: 60 us in place of 41, as
 //   long as the longest take.
 // - more: two pairs of waves, each wave with two tiles and half of a page's keys,
 //   and a fifth tile (a tree's 65th row) split over all four waves.  One tile a wave
@@ -972,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn(Args A) {
 // One tile of query rows: the four waves go through every fourth page alone, two
 // pages on their way in a wave's registers, and wait for nobody until the end.  One
 // row over 3,000 tokens, 8 key heads: 13 us, of which the start - queries, tree rows,
-// the first pages' latency - is 9; one over 131,000: 30 us (4.8 TB/s).
+// the first pages' latency - is 9; one over 131,000: 29 us (4.9 TB/s).
 __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   __shared__ __align__(16) uint8_t s_v[kWaves * kValues];
   __shared__ uint32_t s_bad[1];
