@@ -621,8 +621,10 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * are 0.
  *
  * Rotated and scaled queries are the sum of three 6-bit parts (together within
- * 2^-13 of the largest of each 32 dims), and so are the tree's rotated keys;
- * softmax weights are rounded to bf16, sums are fp32.  What is not finite among
+ * 2^-13 of the largest of each 32 dims), and so are the tree's rotated keys; of the
+ * nine products of a tree key's parts and a query's the three smallest are left out
+ * (in each dim together at most 2^-11 of the product of the two groups' largest).
+ * Softmax weights are rounded to bf16, sums are fp32.  What is not finite among
  * the keys and values that a row attends to, or in its query, shows in its result
  * (a NaN, an infinity among values too); absent, masked and later tokens do not
  * count, whatever they hold.  Values of a magnitude of 2^96 or more may overflow

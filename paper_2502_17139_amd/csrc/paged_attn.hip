@@ -265,8 +265,11 @@ __device__ __forceinline__ void settle(floatx4& a, floatx4& b, floatx4& c, float
   asm volatile("s_nop 7\n\ts_nop 3" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
 }
 
-// Of 16 tree rows with 16 query rows, both in 6-bit parts: the products that
-// matter (a part is 2^-4 or less of the one before it).
+// Of 16 tree rows with 16 query rows, both in 6-bit parts, six of the nine products.
+// With the first parts' scales 2^e and 2^f, second parts are at most 2^-2 and third
+// ones 2^-7 of theirs, so the three left out (second with third, third with both)
+// add up to 2 * 2^-9 + 2^-14 of 2^(e + f) a dim, where the groups' largest are above
+// 3.75 of theirs: 2^-11 of the product of those.
 __device__ __forceinline__ floatx4 score_six(const Six& k, const Six& q, floatx4 acc) {
   acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[2], q.part[0], acc, 2, 2, 2, k.scales, 0, q.scales);
   acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k.part[1], q.part[1], acc, 2, 2, 1, k.scales, 1, q.scales);
