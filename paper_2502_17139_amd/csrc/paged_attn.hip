@@ -471,9 +471,11 @@ struct Work {
     tree = part >= cached - 1 && n > 0;
     return true;
   }
-  __device__ __forceinline__ int position(const Args& A, int r) const {
-    return P + (A.pos_ids ? A.pos_ids[(int64_t)b * A.R + r] : r);
+  // a tree row's position behind the prefix; their sum may pass 32 bits
+  __device__ __forceinline__ int behind(const Args& A, int r) const {
+    return A.pos_ids ? A.pos_ids[(int64_t)b * A.R + r] : r;
   }
+  __device__ __forceinline__ double position(int behind) const { return (double)P + (double)behind; }
   // rows past the last one: the last one, whose results nobody takes
   __device__ __forceinline__ int row_at(int r) const { return r < M ? r : M - 1; }
   __device__ __forceinline__ const uint16_t* q_row(const Args& A, int r) const {
@@ -688,7 +690,7 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
     const auto load = [&](int u, Group& x, int& at) {
       const int r = (u < units ? u : units - 1) >> 2, qr = row0 + r, kr = W.tree0 + r - rows;
       load_group(r < rows ? W.q_row(A, qr) : W.k_row(A, kr), group_of(u & 3), x);
-      if (rotate) at = W.position(A, r < rows ? qr / W.G : kr);
+      if (rotate) at = W.behind(A, r < rows ? qr / W.G : kr);
     };
     double freq[16];  // of the lane's angles, in every row the same ones
     if (rotate) {
@@ -703,7 +705,7 @@ __device__ __forceinline__ void attend(const Args& A, const Work& W, uint8_t* s_
       int next_at = 0;
       load(u + kThreads, next, next_at);
       const int r = u >> 2, g = group_of(u & 3);
-      const double pos = (double)at;
+      const double pos = W.position(at);
       stage_six(x, g, r < rows ? score_scale() : 1.0f, rotate,
                 [&](int d) { return turn_of(pos * freq[d]); },
                 r < rows ? six_q + r * kSixRow : s_v + (r - rows) * kSixRow);
@@ -1033,7 +1035,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_attn_alone(Args A) {
   if (tid == 0) s_bad[0] = 0;
   if (rotate) {
     const double f = angle_of(lane, A.log2_base);
-    for (int r = w; r < A.R; r += kWaves) turns[r * 64 + lane] = turn_of((double)W.position(A, r) * f);
+    for (int r = w; r < A.R; r += kWaves) turns[r * 64 + lane] = turn_of(W.position(W.behind(A, r)) * f);
   }
   __syncthreads();
   if (W.tree) {
