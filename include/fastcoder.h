@@ -635,7 +635,8 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * is cut into parts depends on the sizes and its own length; the same call gives
  * the same bits every time, and a row's do not depend on the other rows.  B <=
  * 65536, 1 <= R <= FC_MAX_TREE_ROWS, Hkv <= 1024, H <= 8192, H % Hkv == 0, D =
- * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
+ * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise, and where B * Hkv times the
+ * tiles of 16 rows that R * H / Hkv make passes 2^31 - 1).
  */
 size_t fc_paged_attention_workspace_bytes(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len);
 fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,

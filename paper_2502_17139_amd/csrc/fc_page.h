@@ -21,6 +21,11 @@ constexpr int kPageBytes = kPageVScale + kPageScales;
 static_assert(kPageBytes == FC_PAGE_HEAD_BYTES, "page layout");
 static_assert(kPage == 64 && kHeadDim == 128, "lane layouts");
 
+// Workgroups of a launch.  It takes fewer than 2^32 threads in a dimension, so a
+// longer call is several launches; this many keep the card busy for so long that
+// one launch more does not show.
+constexpr int64_t kMostGroups = 1 << 20;
+
 // Byte of a page that holds the scale of group g of token t.  Keys: lane 16 g +
 // t % 16 of a wave finds its four 16-token tiles' scales in one word, which is
 // how the score product's lanes hold them.  Values: lane 4 (t % 16) + g does,

@@ -463,10 +463,17 @@ extern "C" fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv,
   if (((uintptr_t)k | (uintptr_t)v) & 15) return FC_ERR_INVALID;
   const int tokens = tokens_of(n, Hkv);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(k_paged_write, dim3(fc::div_up((uint64_t)n, (uint64_t)tokens)), dim3(kWriteThreads), 0, stream,
-                     pool, n_pages, Hkv, k, k_stride, v, v_stride, n_src, slot, pos, src, n, tokens,
-                     rope_base != 0.0f ? log2((double)rope_base) : 0.0);
-  FC_CHECK_LAUNCH();
+  const int64_t most = fc::kMostGroups * tokens;
+  for (int64_t i = 0; i < n; i += most) {
+    const int32_t now = (int32_t)(n - i < most ? n - i : most);
+    const int64_t row0 = src ? 0 : i;  // without src the rows go along with the slots
+    if (row0 >= n_src) break;
+    hipLaunchKernelGGL(k_paged_write, dim3(fc::div_up((uint64_t)now, (uint64_t)tokens)), dim3(kWriteThreads), 0, stream,
+                       pool, n_pages, Hkv, k + row0 * k_stride, k_stride, v + row0 * v_stride, v_stride,
+                       (int)(n_src - row0), slot + i, pos ? pos + i : nullptr, src ? src + i : nullptr, now, tokens,
+                       rope_base != 0.0f ? log2((double)rope_base) : 0.0);
+    FC_CHECK_LAUNCH();
+  }
   return FC_OK;
 }
 
@@ -477,8 +484,13 @@ extern "C" fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t
   if (n == 0) return FC_OK;
   if (!slot || !k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return FC_ERR_INVALID;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(k_paged_read, dim3(fc::div_up((uint64_t)n, kReadRows)), dim3(kReadThreads), 0, stream, pool,
-                     n_pages, Hkv, slot, n, k, v);
-  FC_CHECK_LAUNCH();
+  constexpr int64_t kMost = fc::kMostGroups * kReadRows;
+  for (int64_t i = 0; i < n; i += kMost) {
+    const int32_t now = (int32_t)(n - i < kMost ? n - i : kMost);
+    const int64_t to = i * Hkv * kHeadDim;
+    hipLaunchKernelGGL(k_paged_read, dim3(fc::div_up((uint64_t)now, kReadRows)), dim3(kReadThreads), 0, stream, pool,
+                       n_pages, Hkv, slot + i, now, k + to, v + to);
+    FC_CHECK_LAUNCH();
+  }
   return FC_OK;
 }

@@ -1221,6 +1221,14 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   return s;
 }
 
+// Trees of a launch (and of the join after it): at least two at the largest sizes.
+// Those behind them are a launch of their own, which uses the workspace again.
+int32_t trees_at_once(int32_t B, int32_t R, int32_t H, int32_t Hkv, const Shape& s) {
+  const int64_t wgs = (int64_t)Hkv * s.chunks, joins = ((int64_t)H * R + kMergeWaves - 1) / kMergeWaves;
+  const int64_t most = fc::kMostGroups / (wgs > joins ? wgs : joins);
+  return B < most ? B : (int32_t)most;
+}
+
 size_t carve(void* p, int64_t rows, float2** ml, float** o) {
   fc::Carver c(p);
   *ml = c.take<float2>((size_t)rows);
@@ -1240,7 +1248,7 @@ extern "C" size_t fc_paged_attention_workspace_bytes(int32_t B, int32_t R, int32
   const Shape s = shape_of(B, R, H, Hkv, max_len);
   float2* ml;
   float* o;
-  return s.parts > 1 ? carve(nullptr, (int64_t)B * Hkv * s.parts * R * (H / Hkv), &ml, &o) : 0;
+  return s.parts > 1 ? carve(nullptr, (int64_t)trees_at_once(B, R, H, Hkv, s) * H * R * s.parts, &ml, &o) : 0;
 }
 
 extern "C" fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,
@@ -1262,30 +1270,39 @@ extern "C" fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, con
   if (!q || !k_tree || !v_tree || !pool || !table || !prefix_len || !out) return FC_ERR_INVALID;
   if (((uintptr_t)q | (uintptr_t)k_tree | (uintptr_t)v_tree | (uintptr_t)pool | (uintptr_t)out) & 15)
     return FC_ERR_INVALID;
-  // workgroups are numbered with 31 bits
+  // sizes whose queries alone would pass 2^39 bytes
   if ((int64_t)B * Hkv * (((int64_t)R * (H / Hkv) + kTile - 1) / kTile) > 0x7FFFFFFF) return FC_ERR_UNSUPPORTED;
   const Shape s = shape_of(B, R, H, Hkv, max_len);
-  Args a = {q, k_tree, v_tree, q_stride, k_stride, v_stride, pool, table, prefix_len, num_nodes, mask, pos_ids,
-            n_pages, max_pages, B, R, H, Hkv, max_len, s.chunks, s.part_pages, s.parts,
-            rope_base != 0.0f ? log2((double)rope_base) : 0.0, out, nullptr, nullptr};
+  const int32_t at_once = trees_at_once(B, R, H, Hkv, s);
+  float2* part_ml = nullptr;
+  float* part_o = nullptr;
   if (s.parts > 1) {
     if (!ws || ws_bytes < fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len)) return FC_ERR_WORKSPACE;
     if ((uintptr_t)ws & 15) return FC_ERR_INVALID;
-    carve(ws, (int64_t)B * Hkv * s.parts * R * (H / Hkv), &a.part_ml, &a.part_o);
+    carve(ws, (int64_t)at_once * H * R * s.parts, &part_ml, &part_o);
   }
-  const dim3 grid((uint32_t)B * (uint32_t)Hkv * (uint32_t)s.chunks, (uint32_t)s.parts);
   (void)hipGetLastError();
-  if (s.alone)
-    hipLaunchKernelGGL(k_paged_attn_alone, grid, dim3(kThreads), 0, stream, a);
-  else if (s.five)
-    hipLaunchKernelGGL(k_paged_attn<true>, grid, dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(k_paged_attn<false>, grid, dim3(kThreads), 0, stream, a);
-  FC_CHECK_LAUNCH();
-  if (s.parts > 1) {
-    const uint64_t rows = (uint64_t)B * H * R;
-    hipLaunchKernelGGL(k_paged_merge, dim3(fc::div_up(rows, kMergeWaves)), dim3(kMergeWaves * fc::kWave), 0, stream, a);
+  for (int32_t b = 0; b < B; b += at_once) {
+    const int32_t now = B - b < at_once ? B - b : at_once;
+    const int64_t row = (int64_t)b * R;
+    const Args a = {q + row * q_stride, k_tree + row * k_stride, v_tree + row * v_stride, q_stride, k_stride, v_stride,
+                    pool, table + (int64_t)b * max_pages, prefix_len + b, num_nodes ? num_nodes + b : nullptr,
+                    mask ? mask + row * R : nullptr, pos_ids ? pos_ids + row : nullptr, n_pages, max_pages, now, R, H,
+                    Hkv, max_len, s.chunks, s.part_pages, s.parts, rope_base != 0.0f ? log2((double)rope_base) : 0.0,
+                    out + row * H * kHeadDim, part_ml, part_o};
+    const dim3 grid((uint32_t)now * (uint32_t)Hkv * (uint32_t)s.chunks, (uint32_t)s.parts);
+    if (s.alone)
+      hipLaunchKernelGGL(k_paged_attn_alone, grid, dim3(kThreads), 0, stream, a);
+    else if (s.five)
+      hipLaunchKernelGGL(k_paged_attn<true>, grid, dim3(kThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL(k_paged_attn<false>, grid, dim3(kThreads), 0, stream, a);
     FC_CHECK_LAUNCH();
+    if (s.parts > 1) {
+      const uint64_t rows = (uint64_t)now * H * R;
+      hipLaunchKernelGGL(k_paged_merge, dim3(fc::div_up(rows, kMergeWaves)), dim3(kMergeWaves * fc::kWave), 0, stream, a);
+      FC_CHECK_LAUNCH();
+    }
   }
   return FC_OK;
 }

@@ -27,3 +27,74 @@ def test_positions_past_32_bits(R, H):
     row = lambda h, s=1.0: bf16(rng, 2, R, h, 128, scale=s)  # noqa: E731
     say(f"positions past 32 bits R={R}")
     check(row(H, 3.0), row(1), row(1), pool, table, [150, 60], t)
+
+
+def test_more_rows_than_one_launch_takes():
+    """Writes and reads of more tokens than a launch's workgroups hold, rows given
+    in order and by number, are what shorter calls make of them."""
+    n, piece = 2 ** 24 + 70, 2 ** 20 + 33
+    pages = -(-n // 64)
+    torch.manual_seed(1)
+    x = torch.randn((n, 1, 128), dtype=torch.bfloat16, device="cuda")
+    slot = torch.arange(n, dtype=torch.int32, device="cuda")
+    pos = slot.flip(0).contiguous()
+    pools = [torch.zeros((pages, 1, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda") for _ in "ab"]
+    say("writes and reads of more than a launch")
+    fc.fc_paged_write(pools[0], x, x, slot, pos)
+    for i in range(0, n, piece):
+        fc.fc_paged_write(pools[1], x[i:i + piece], x[i:i + piece], slot[i:i + piece], pos[i:i + piece])
+    assert torch.equal(pools[0], pools[1]) and pools[0][-1].any()
+    few = 1000                                    # rows that exist: the others are skipped
+    pools[1][few // 64:].fill_(0)
+    fc.fc_paged_write(pools[1], x[:few], x[:few], slot, pos)
+    assert torch.equal(pools[1][:few // 64], pools[0][:few // 64]) and not pools[1][few // 64 + 1:].any()
+    del pools[1], x
+    got = fc.fc_paged_read(pools[0], slot)
+    for i in range(0, n, piece):
+        want = fc.fc_paged_read(pools[0], slot[i:i + piece])
+        assert torch.equal(got[0][i:i + piece], want[0]) and torch.equal(got[1][i:i + piece], want[1])
+
+
+def test_more_workgroups_than_a_dimension_takes():
+    """Slot maps of 2^24 workgroups and more, all but a few entries empty."""
+    rng = np.random.default_rng(1)
+    n, Hkv = 2 ** 25 + 70, 32                     # one or two tokens of a workgroup
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    src, pos = torch.full_like(slot, -1), torch.zeros_like(slot)
+    at = torch.tensor([0, 5, 2 ** 20, 2 ** 21 - 1, 2 ** 21, 2 ** 24 + 1, n - 1], device="cuda")
+    few = torch.arange(len(at), dtype=torch.int32, device="cuda")
+    slot[at], src[at], pos[at] = few * 9, few.flip(0), few * 1000
+    k, v = bf16(rng, len(at), Hkv, 128).cuda(), bf16(rng, len(at), Hkv, 128).cuda()
+    pools = [torch.zeros((1, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda") for _ in "ab"]
+    say("more workgroups than a dimension takes: write")
+    fc.fc_paged_write(pools[0], k, v, slot, pos, src=src)
+    fc.fc_paged_write(pools[1], k, v, slot[at], pos[at], src=src[at])
+    assert torch.equal(pools[0], pools[1]) and pools[0].any()
+    del slot, src, pos
+    say("more workgroups than a dimension takes: read")
+    n, want = 2 ** 28 + 70, fc.fc_paged_read(pools[0], few * 9)
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")   # rows without a slot are not touched,
+    slot[:len(at)] = few * 9                                        # so only the first ones are allocated
+    got = [torch.zeros_like(x) for x in want]
+    code = fc.lib().fc_paged_read(pools[0].data_ptr(), 1, Hkv, 128, slot.data_ptr(), n, got[0].data_ptr(),
+                                  got[1].data_ptr(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert code == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("B,R,Hkv,piece", [(65536, 1, 256, 30000), (6000, 97, 8, 2500)])
+def test_more_trees_than_one_launch_takes(B, R, Hkv, piece):
+    """2^24 workgroups of single tokens, and joins of more rows than a launch
+    takes: the bits of calls with fewer trees."""
+    rng = np.random.default_rng(2)
+    pool = make_pool(rng, 40, Hkv)
+    torch.manual_seed(2)
+    x = torch.randn((B, R, Hkv, 128), dtype=torch.bfloat16, device="cuda")
+    table = torch.randint(0, 40, (B, 2), dtype=torch.int32, device="cuda")
+    plen = torch.randint(0, 129, (B,), dtype=torch.int32, device="cuda")
+    say(f"attention of {B} trees of {R} rows")
+    got = fc.fc_paged_attention(x, x, x, pool, table, plen)
+    for i in range(0, B, piece):
+        want = fc.fc_paged_attention(*[x[i:i + piece]] * 3, pool, table[i:i + piece], plen[i:i + piece])
+        assert torch.equal(got[i:i + piece], want), i
+    assert (fc.fc_paged_attention_workspace_bytes(B, R, Hkv, Hkv, 128) > 0) == (R > 96)
