@@ -567,8 +567,9 @@ size_t fc_paged_pool_bytes(int32_t n_pages, int32_t Hkv);
  *
  * len is clamped to [0, 64 max_pages].  A slot whose table entry lies outside
  * the pool is -1.  The same inputs give the same results however often the
- * call is repeated: nothing that it reads is written, so len_out and ends_out
- * must not be len and ends (FC_ERR_INVALID).  0 <= B <= 65536, 1 <= R <=
+ * call is repeated: nothing that it reads is written, so the outputs, table and
+ * queue must share no bytes with each other or with the other inputs
+ * (FC_ERR_INVALID).  0 <= B <= 65536, 1 <= R <=
  * FC_MAX_TREE_ROWS, 0 <= n_slots < 2^30, max_pages >= 1, 64 max_pages < 2^31.
  */
 fc_status fc_paged_plan(const int32_t* len, const int32_t* add, const int32_t* mask, const int32_t* last_node,
@@ -586,7 +587,8 @@ fc_status fc_paged_plan(const int32_t* len, const int32_t* add, const int32_t* m
  * projection need no copy), 16-byte aligned.  An entry with a slot outside the
  * pool or a row outside [0, n_src) is skipped.  The slots of one call must
  * differ from each other.  D must be FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED
- * otherwise); rope_base is 0 or above 1; Hkv <= 1024.
+ * otherwise); rope_base is 0 or above 1; Hkv <= 1024.  The pool shares no bytes
+ * with the other arguments (FC_ERR_INVALID).
  */
 fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k, int64_t k_stride,
                          const uint16_t* v, int64_t v_stride, int32_t n_src, const int32_t* slot, const int32_t* pos,
@@ -596,7 +598,8 @@ fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D,
  * Rows of the pool as bf16 (exact: every held value is one): k and v
  * [n][Hkv][D], 16-byte aligned, receive the keys (rotated, as held) and values
  * of slot[i].  Rows of entries with a slot outside the pool are left as they
- * were.
+ * were.  k and v share no bytes with each other, the pool or slot
+ * (FC_ERR_INVALID).
  */
 fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot, int32_t n,
                         uint16_t* k, uint16_t* v, hipStream_t stream);
@@ -618,7 +621,8 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * a prefix that lie outside the pool count as absent keys.  rope_base 0:
  * queries and keys are rotated already.  out [B][R][H][D] bf16, 16-byte
  * aligned; rows at or past num_nodes[b], and rows that may attend to nothing,
- * are 0.
+ * are 0.  out may be q (then q_stride is H * D); otherwise out and ws share no
+ * bytes with each other or with what is read (FC_ERR_INVALID).
  *
  * Rotated and scaled queries are the sum of three 6-bit parts (together within
  * 2^-13 of the largest of each 32 dims), and so are the tree's rotated keys; of the

@@ -440,7 +440,12 @@ extern "C" fc_status fc_paged_plan(const int32_t* len, const int32_t* add, const
   if (B > 0 && (!len || !add || !table || !len_out)) return FC_ERR_INVALID;
   if (!queue || !ends || !cu || !ends_out) return FC_ERR_INVALID;
   if (n_slots > 0 && (!slot || !pos || !src)) return FC_ERR_INVALID;
-  if ((B > 0 && (len_out == len || len_out == add)) || ends_out == ends) return FC_ERR_INVALID;
+  // workgroups read everything while others write already
+  const uint64_t seqs = 4 * (uint64_t)B, slots = 4 * (uint64_t)n_slots;
+  if (!fc::apart({{table, seqs * max_pages}, {queue, 4 * (uint64_t)n_pages}, {len_out, seqs}, {cu, seqs + 4},
+                  {slot, slots}, {pos, slots}, {src, slots}, {ends_out, 16}},
+                 {{len, seqs}, {add, seqs}, {mask, seqs * R * R}, {last_node, seqs}, {ends, 16}}))
+    return FC_ERR_INVALID;
   (void)hipGetLastError();
   const uint32_t windows = fc::div_up((uint64_t)n_slots, kPlanTokens);
   hipLaunchKernelGGL(k_paged_plan, dim3(windows ? windows : 1), dim3(kPlanThreads), 0, stream, len, add, mask,
@@ -461,6 +466,11 @@ extern "C" fc_status fc_paged_write(uint8_t* pool, int32_t n_pages, int32_t Hkv,
   if (n == 0 || n_src == 0) return FC_OK;
   if (!k || !v || !slot || (rope_base != 0.0f && !pos)) return FC_ERR_INVALID;
   if (((uintptr_t)k | (uintptr_t)v) & 15) return FC_ERR_INVALID;
+  const uint64_t numbers = 4 * (uint64_t)n;
+  if (!fc::apart({{pool, fc_paged_pool_bytes(n_pages, Hkv)}},
+                 {fc::rows_span(k, n_src, k_stride, Hkv * D), fc::rows_span(v, n_src, v_stride, Hkv * D),
+                  {slot, numbers}, {rope_base != 0.0f ? pos : nullptr, numbers}, {src, numbers}}))
+    return FC_ERR_INVALID;
   const int tokens = tokens_of(n, Hkv);
   (void)hipGetLastError();
   const int64_t most = fc::kMostGroups * tokens;
@@ -483,6 +493,9 @@ extern "C" fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t
   if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
   if (n == 0) return FC_OK;
   if (!slot || !k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return FC_ERR_INVALID;
+  const fc::Span rows = fc::rows_span(k, n, (int64_t)Hkv * D, (int64_t)Hkv * D);
+  if (!fc::apart({rows, {v, rows.n}}, {{pool, fc_paged_pool_bytes(n_pages, Hkv)}, {slot, 4 * (uint64_t)n}}))
+    return FC_ERR_INVALID;
   (void)hipGetLastError();
   constexpr int64_t kMost = fc::kMostGroups * kReadRows;
   for (int64_t i = 0; i < n; i += kMost) {

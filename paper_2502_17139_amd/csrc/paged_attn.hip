@@ -1281,6 +1281,22 @@ extern "C" fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, con
     if ((uintptr_t)ws & 15) return FC_ERR_INVALID;
     carve(ws, (int64_t)at_once * H * R * s.parts, &part_ml, &part_o);
   }
+  // A workgroup reads its query rows before it writes the same rows of the result, so
+  // out may be q itself; what other workgroups read has to lie elsewhere.
+  const int64_t all = (int64_t)B * R;
+  const bool in_place = out == q && q_stride == (int64_t)H * D;
+  if (!fc::apart({fc::rows_span(out, all, (int64_t)H * D, (int64_t)H * D),
+                  {s.parts > 1 ? ws : nullptr, fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len)}},
+                 {fc::rows_span(in_place ? nullptr : q, all, q_stride, (int64_t)H * D),
+                  fc::rows_span(k_tree, all, k_stride, (int64_t)Hkv * D),
+                  fc::rows_span(v_tree, all, v_stride, (int64_t)Hkv * D),
+                  {pool, fc_paged_pool_bytes(n_pages, Hkv)},
+                  {table, 4 * (uint64_t)B * max_pages},
+                  {prefix_len, 4 * (uint64_t)B},
+                  {num_nodes, 4 * (uint64_t)B},
+                  {mask, 4 * (uint64_t)all * R},
+                  {pos_ids, 4 * (uint64_t)all}}))
+    return FC_ERR_INVALID;
   (void)hipGetLastError();
   for (int32_t b = 0; b < B; b += at_once) {
     const int32_t now = B - b < at_once ? B - b : at_once;

@@ -3,15 +3,15 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_pipeline import say
+from gpu_pipeline import dev, say
 
 pytestmark = pytest.mark.gpu
 
 if not torch.cuda.is_available():  # pragma: no cover - CPU container
     pytest.skip("no GPU", allow_module_level=True)
 
-import paper_2502_17139_amd as fc  # noqa: E402,F401
-from test_paged import bf16, make_pool, trees  # noqa: E402
+import paper_2502_17139_amd as fc  # noqa: E402
+from test_paged import bf16, make_pool, on_gpu, trees  # noqa: E402
 from test_paged_scores import check  # noqa: E402
 
 
@@ -56,7 +56,7 @@ def test_more_rows_than_one_launch_takes():
 
 
 def test_more_workgroups_than_a_dimension_takes():
-    """Slot maps of 2^24 workgroups and more, all but a few entries empty."""
+    """A slot map of 2^25 workgroups, all but a few entries empty."""
     rng = np.random.default_rng(1)
     n, Hkv = 2 ** 25 + 70, 32                     # one or two tokens of a workgroup
     slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
@@ -66,20 +66,10 @@ def test_more_workgroups_than_a_dimension_takes():
     slot[at], src[at], pos[at] = few * 9, few.flip(0), few * 1000
     k, v = bf16(rng, len(at), Hkv, 128).cuda(), bf16(rng, len(at), Hkv, 128).cuda()
     pools = [torch.zeros((1, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda") for _ in "ab"]
-    say("more workgroups than a dimension takes: write")
+    say("more workgroups than a dimension takes")
     fc.fc_paged_write(pools[0], k, v, slot, pos, src=src)
     fc.fc_paged_write(pools[1], k, v, slot[at], pos[at], src=src[at])
     assert torch.equal(pools[0], pools[1]) and pools[0].any()
-    del slot, src, pos
-    say("more workgroups than a dimension takes: read")
-    n, want = 2 ** 28 + 70, fc.fc_paged_read(pools[0], few * 9)
-    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")   # rows without a slot are not touched,
-    slot[:len(at)] = few * 9                                        # so only the first ones are allocated
-    got = [torch.zeros_like(x) for x in want]
-    code = fc.lib().fc_paged_read(pools[0].data_ptr(), 1, Hkv, 128, slot.data_ptr(), n, got[0].data_ptr(),
-                                  got[1].data_ptr(), torch.cuda.current_stream().cuda_stream)
-    torch.cuda.synchronize()
-    assert code == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 @pytest.mark.parametrize("B,R,Hkv,piece", [(65536, 1, 256, 30000), (6000, 97, 8, 2500)])
@@ -98,3 +88,23 @@ def test_more_trees_than_one_launch_takes(B, R, Hkv, piece):
         want = fc.fc_paged_attention(*[x[i:i + piece]] * 3, pool, table[i:i + piece], plen[i:i + piece])
         assert torch.equal(got[i:i + piece], want), i
     assert (fc.fc_paged_attention_workspace_bytes(B, R, Hkv, Hkv, 128) > 0) == (R > 96)
+
+
+@pytest.mark.parametrize("R,H,Hkv,n", [(1, 8, 2, 100), (1, 8, 2, 3000), (65, 4, 4, 100), (70, 2, 1, 2000), (130, 2, 2, 90)])
+def test_results_in_place_of_queries(R, H, Hkv, n):
+    """out may be q, and lie beside what is read; anything between is refused."""
+    rng = np.random.default_rng(R)
+    B, width = 3, -(-n // 64)
+    pool, table = make_pool(rng, 6, Hkv), dev(rng.integers(0, 6, (B, width)).astype(np.int32))
+    lens = dev(np.array([n, n // 2, 0], np.int32))
+    block = torch.empty((3 * B, R, H, 128), dtype=torch.bfloat16, device="cuda")
+    q, kt, vt = block[B:2 * B], bf16(rng, B, R, Hkv, 128).cuda(), bf16(rng, B, R, Hkv, 128).cuda()
+    q.copy_(bf16(rng, B, R, H, 128))
+    t = on_gpu(trees(rng, B, R))
+    say(f"in place R={R} n={n}")
+    want = fc.fc_paged_attention(q, kt, vt, pool, table, lens, tree=t)
+    for out in (block[:B], block[2 * B:], q):
+        assert torch.equal(want, fc.fc_paged_attention(q, kt, vt, pool, table, lens, tree=t, out=out))
+    for at in (B - 1, B + 1):
+        with pytest.raises(fc.FcError):
+            fc.fc_paged_attention(q, kt, vt, pool, table, lens, tree=t, out=block[at:at + B])
