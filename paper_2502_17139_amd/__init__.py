@@ -705,9 +705,17 @@ def _rows(name: str, t: torch.Tensor, heads: int | None = None) -> int:
     return row
 
 
+def _in_32_bits(**sizes) -> None:
+    """Sizes that the library takes 32 bits of; it refuses those out of range."""
+    for name, n in sizes.items():
+        if abs(n) >= 2 ** 31:
+            raise ValueError(f"{name} must be a 32-bit number, not {n}")
+
+
 def _pool(pool: torch.Tensor) -> tuple:
     if pool.dtype != torch.uint8 or pool.dim() != 3 or pool.shape[2] != FC_PAGE_HEAD_BYTES:
         raise ValueError(f"pool must be uint8 [n_pages][Hkv][{FC_PAGE_HEAD_BYTES}]")
+    _in_32_bits(n_pages=pool.shape[0], Hkv=pool.shape[1])
     return int(pool.shape[0]), int(pool.shape[1])
 
 
@@ -740,6 +748,7 @@ def fc_paged_plan(length: torch.Tensor, add: torch.Tensor, table: torch.Tensor, 
     if table.dim() != 2 or queue.dim() != 1:
         raise ValueError("table [B][max_pages] and queue [n_pages] expected")
     B, max_pages = table.shape
+    _in_32_bits(B=B, max_pages=max_pages, n_pages=queue.numel())
     i32 = torch.int32
     for name, t, dt, shape in (("length", length, i32, (B,)), ("add", add, i32, (B,)), ("table", table, i32, None),
                                ("queue", queue, i32, None), ("ends", ends, torch.int64, (2,))):
@@ -781,8 +790,8 @@ def fc_paged_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot: t
     ks, vs = _rows("k", k, Hkv), _rows("v", v, Hkv)
     if k.shape != v.shape:
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
-    n_src = k.numel() // (Hkv * FC_TREE_ATTN_HEAD_DIM)
-    n = slot.numel()
+    n_src, n = k.shape[:-2].numel(), slot.numel()
+    _in_32_bits(rows=n_src, slots=n)
     _expect("slot", slot, torch.int32, (n,))
     _expect("pos", pos, torch.int32, (n,), optional=rope_base == 0)
     _expect("src", src, torch.int32, (n,), optional=True)
@@ -797,6 +806,7 @@ def fc_paged_read(pool: torch.Tensor, slot: torch.Tensor, out=None, stream=None)
     of slots outside the pool are left as they were."""
     n_pages, Hkv = _pool(pool)
     n = slot.numel()
+    _in_32_bits(slots=n)
     _expect("slot", slot, torch.int32, (n,))
     shape = (n, Hkv, FC_TREE_ATTN_HEAD_DIM)
     if out is not None:
@@ -847,8 +857,7 @@ def fc_paged_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tens
     _expect("workspace", workspace, torch.uint8, optional=True)
     if max_len is None:
         max_len = max_pages * FC_PAGE_TOKENS
-    if abs(max_len) >= 2 ** 31:  # the library takes 32 bits of it, and refuses those out of range
-        raise ValueError(f"max_len must be a 32-bit number, not {max_len}")
+    _in_32_bits(max_len=max_len, B=B, max_pages=max_pages)
     need = fc_paged_attention_workspace_bytes(B, R, H, Hkv, max_len)
     with _Launch(stream, (q, k_tree, v_tree, pool, table, prefix_len, nodes, mask, pos_ids, out, workspace)) as on:
         if out is None:

@@ -180,3 +180,25 @@ def test_bindings_refuse_numbers_out_of_range():
     for n_slots in (-1, 2 ** 30, 2 ** 32):
         with pytest.raises(ValueError, match="n_slots"):
             fc.fc_paged_plan(st["len"], st["len"], st["table"], st["queue"], st["ends"], n_slots)
+
+
+def test_bindings_refuse_sizes_out_of_range():
+    """Tensors of more entries than 32 bits number (2^32 + 5 would pass as 5), and
+    pools without a key head."""
+    s, st, one = _inputs(), fc.paged_state(2, 3, 9, "cpu"), torch.zeros(1, dtype=I32)
+    long = one.expand(2 ** 32 + 5)
+    k = torch.zeros((6, 2, 128), dtype=BF)
+    wide, many = one.expand(2, 2 ** 32 + 5), k[:1].expand(2 ** 32 + 6, 2, 128)
+    plan = (st["len"], st["len"], st["table"], st["queue"], st["ends"])
+    for call in (lambda: fc.fc_paged_write(s["pool"], k, k, long, long),
+                 lambda: fc.fc_paged_write(s["pool"], many, many, one, one),
+                 lambda: fc.fc_paged_read(s["pool"], long),
+                 lambda: fc.fc_paged_read(s["pool"][:1].expand(2 ** 32 + 1, 2, 8704), one),
+                 lambda: fc.fc_paged_attention(**{**s, "table": wide}, max_len=64),
+                 lambda: fc.fc_paged_plan(*plan[:2], wide, *plan[3:], 3),
+                 lambda: fc.fc_paged_plan(*plan[:3], long, plan[4], 3)):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
+    none = torch.zeros((5, 0, 8704), dtype=torch.uint8)
+    with pytest.raises((ValueError, fc.FcError)):
+        fc.fc_paged_write(none, k[:, :0], k[:, :0], one, one)
