@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_pipeline import dev, say
+import oracle
+from gpu_pipeline import dev, host, say
 
 pytestmark = pytest.mark.gpu
 
@@ -11,7 +12,7 @@ if not torch.cuda.is_available():  # pragma: no cover - CPU container
     pytest.skip("no GPU", allow_module_level=True)
 
 import paper_2502_17139_amd as fc  # noqa: E402
-from test_paged import bf16, make_pool, on_gpu, trees  # noqa: E402
+from test_paged import bf16, f64, make_pool, on_gpu, trees  # noqa: E402
 from test_paged_scores import check  # noqa: E402
 
 
@@ -108,3 +109,23 @@ def test_results_in_place_of_queries(R, H, Hkv, n):
     for at in (B - 1, B + 1):
         with pytest.raises(fc.FcError):
             fc.fc_paged_attention(q, kt, vt, pool, table, lens, tree=t, out=block[at:at + B])
+
+
+@pytest.mark.parametrize("Hkv,n_pages", [(1, 1), (2, 3), (8, 2), (33, 1)])
+def test_writes_at_the_ends_of_the_pool(Hkv, n_pages):
+    """Each slot once: the pool's first and last, and those just outside of it,
+    whose rows go nowhere."""
+    rng = np.random.default_rng(Hkv)
+    last = 64 * n_pages - 1
+    slot = np.concatenate([[0, last, last + 1, -1, 2 ** 31 - 1, -2 ** 31], 1 + rng.permutation(last - 1)[:40]])
+    slot = rng.permutation(slot).astype(np.int32)
+    n = len(slot)
+    assert len(set(slot.tolist())) == n
+    k, v = bf16(rng, n, Hkv, 128), bf16(rng, n, Hkv, 128)
+    pos = rng.integers(0, 5000, n).astype(np.int32)
+    before = rng.integers(0, 256, (n_pages, Hkv, fc.FC_PAGE_HEAD_BYTES)).astype(np.uint8)
+    guarded = dev(np.concatenate([before, before]))      # what lies behind the pool stays as it is
+    say(f"writes at the ends of {n_pages} pages of {Hkv} heads")
+    fc.fc_paged_write(guarded[:n_pages], k.cuda(), v.cuda(), dev(slot), dev(pos))
+    assert np.array_equal(host(guarded[:n_pages]), oracle.paged_write(before, f64(k), f64(v), slot, pos))
+    assert np.array_equal(host(guarded[n_pages:]), before)
