@@ -12,7 +12,7 @@ if not torch.cuda.is_available():  # pragma: no cover - CPU container
     pytest.skip("no GPU", allow_module_level=True)
 
 import paper_2502_17139_amd as fc  # noqa: E402
-from test_paged import bf16, f64, make_pool, on_gpu, trees  # noqa: E402
+from test_paged import _plan, bf16, f64, make_pool, on_gpu, trees  # noqa: E402
 from test_paged_scores import check  # noqa: E402
 
 
@@ -129,3 +129,34 @@ def test_writes_at_the_ends_of_the_pool(Hkv, n_pages):
     fc.fc_paged_write(guarded[:n_pages], k.cuda(), v.cuda(), dev(slot), dev(pos))
     assert np.array_equal(host(guarded[:n_pages]), oracle.paged_write(before, f64(k), f64(v), slot, pos))
     assert np.array_equal(host(guarded[n_pages:]), before)
+
+
+@pytest.mark.parametrize("B,R", [(300, 65), (1500, 33), (250, 256)])
+def test_accepted_paths_across_workgroups_of_the_plan(B, R):
+    """A workgroup plans 4,096 slots: paths that begin before one and end in it."""
+    rng = np.random.default_rng(B)
+    mask, depth = np.zeros((B, R, R), np.int32), np.zeros((B, R), np.int64)
+    for b in range(B):
+        for i in range(R):
+            if i:
+                p = i - 1 if rng.random() < 0.9 else int(rng.integers(0, i))
+                mask[b, i], depth[b, i] = mask[b, p], depth[b, p] + 1
+            mask[b, i, i] = 1
+    last = rng.integers(R // 2, R, B).astype(np.int32)
+    add = (depth[np.arange(B), last] + 1).astype(np.int32)
+    add[::7] += 2                                        # more tokens than rows
+    start = np.cumsum(add) - add
+    crossing = start // 4096 != (start + add - 1) // 4096
+    assert crossing.any()
+    length = rng.integers(0, 100, B).astype(np.int32)
+    held = -(-length // 64)
+    perm = rng.permutation(int(held.sum()) + 4 * B).astype(np.int32)
+    table, at = np.full((B, 6), -1, np.int32), 0
+    for b in range(B):
+        table[b, :held[b]] = perm[at:at + held[b]]
+        at += held[b]
+    queue = np.concatenate([perm[at:], np.full(at, -1, np.int32)])
+    say(f"accepted paths across workgroups B={B} R={R} tokens={add.sum()}")
+    r = _plan(length, add, table, queue, [0, 4 * B], int(add.sum()) + 9, mask, last)
+    for b in np.flatnonzero(crossing):
+        assert (r["slot"][start[b]:start[b] + add[b]] >= 0).all()
