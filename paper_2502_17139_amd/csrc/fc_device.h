@@ -284,18 +284,6 @@ __device__ __forceinline__ void lds_load16(uint32_t lds, uint32_t voff, int32x4 
 }
 
 
-// sin and cos of the rotary angle position * freq, freq = base^(-2d/D) of
-// the pair (d, d + D/2).  The angle is taken in revolutions and reduced to
-// [0, 1) in double precision, so large positions keep full accuracy; the
-// hardware sine and cosine then take revolutions directly.
-__device__ __forceinline__ void rope_sincos(int pos, double freq, float& s, float& c) {
-  constexpr double kInv2Pi = 0.15915494309189533577;
-  const double rev = (double)pos * freq * kInv2Pi;
-  const float f = (float)(rev - floor(rev));
-  s = __builtin_amdgcn_sinf(f);
-  c = __builtin_amdgcn_cosf(f);
-}
-
 // 8 bf16 as floats.
 __device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};

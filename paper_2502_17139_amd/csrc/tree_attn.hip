@@ -69,7 +69,18 @@ __device__ __forceinline__ __bf16 f2bf(float x) { return (__bf16)x; }
 // byte offset inside a block part of 16-byte chunk c of row r (swizzled)
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) { return (uint32_t)(r * kRowBytes + ((c ^ (r & 15)) << 4)); }
 
-using fc::rope_sincos;
+// sin and cos of the rotary angle position * freq, freq = base^(-2d/D) of
+// the pair (d, d + D/2).  The angle is taken in revolutions and reduced to
+// [0, 1) in double precision, so large positions keep full accuracy; the
+// hardware sine and cosine then take revolutions directly.
+__device__ __forceinline__ void rope_sincos(int pos, double freq, float& s, float& c) {
+  constexpr double kInv2Pi = 0.15915494309189533577;
+  const double rev = (double)pos * freq * kInv2Pi;
+  const float f = (float)(rev - floor(rev));
+  s = __builtin_amdgcn_sinf(f);
+  c = __builtin_amdgcn_cosf(f);
+}
+
 using fc::unpack8;
 
 __device__ __forceinline__ int clamp_len(int len, int most) { return len < 0 ? 0 : (len > most ? most : len); }
