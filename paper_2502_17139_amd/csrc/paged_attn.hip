@@ -1203,13 +1203,19 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   s.chunks = s.five ? tiles / kWaves : (tiles + kWaves - 1) / kWaves;
   const int64_t wgs = (int64_t)B * Hkv * s.chunks;
   const int64_t pages = ((int64_t)max_len + kPage - 1) / kPage;
-  // As many parts as fill the card once (a sequence of 131,000 tokens, 8 key heads:
-  // 34.8 us, twice as many 42.5; 64 sequences of up to 8,192: 58.7 in one part, 61.5
-  // in two), of 4 pages at least, or 16 where each wave takes every fourth (16
-  // sequences of 2,048: 20.4 us, of 4 pages 20.7).
+  // As many parts as the card takes at once.  From 64 pages on, one more where they
+  // do not come out even, so that up to twice as many workgroups start: sequences
+  // that are shorter than the longest then leave room that these take (40 trees of
+  // 65 rows, 8 key heads, up to 8,192 tokens: 125 us, 174 without; 33 single tokens
+  // 40 and 50; but equal lengths lose a little, 63 single tokens 110 and 102).
+  // Shorter prefixes only pay the second round and the join for it (63 single tokens
+  // over 2,048: 37 us, 29 without; 15 trees, 32 key heads: 106 and 76).  Parts have 4
+  // pages at least, or 16 where each wave takes every fourth: 16 single tokens over
+  // 2,048 17.9 us, with 4 19.0; a single one over 1,000 12.3 and 16.8, and from 3,000
+  // on no difference.
   const int64_t slots = 2 * kCus;  // workgroups at once
   int64_t each = s.alone ? 16 : 4;
-  int64_t parts = (slots + wgs - 1) / wgs;
+  int64_t parts = (slots + (pages < 64 ? 0 : wgs - 1)) / wgs;
   if (parts > kMostParts) parts = kMostParts;
   const int64_t fit = (pages + each - 1) / each;
   if (parts > fit) parts = fit;

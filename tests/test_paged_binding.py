@@ -202,3 +202,18 @@ def test_bindings_refuse_sizes_out_of_range():
     none = torch.zeros((5, 0, 8704), dtype=torch.uint8)
     with pytest.raises((ValueError, fc.FcError)):
         fc.fc_paged_write(none, k[:, :0], k[:, :0], one, one)
+
+
+def test_short_prefixes_are_cut_for_one_round_of_workgroups(L):
+    """512 workgroups run at once.  Prefixes of fewer than 64 pages are cut into no
+    more parts than that leaves room for, so a nearly full card pays for no join:
+    63 sequences of 8 key heads are as whole as 64."""
+    size = fc.fc_paged_attention_workspace_bytes
+    parts = lambda B, R, H, Hkv, n: size(B, R, H, Hkv, n) // (520 * B * R * H) or 1  # noqa: E731
+    for n in (700, 2048, 4032):
+        for B in range(1, 70):
+            assert parts(B, 1, 32, 8, n) == 1 or B * 8 * parts(B, 1, 32, 8, n) <= 512, (B, n)
+            assert parts(B, 65, 32, 32, n) == 1 or B * 32 * parts(B, 65, 32, 32, n) <= 512, (B, n)
+    assert size(63, 1, 32, 8, 2048) == size(64, 1, 32, 8, 2048) == size(15, 65, 32, 32, 2048) == 0
+    assert parts(1, 1, 32, 8, 3000) == 3 and parts(16, 1, 32, 8, 4032) == 4
+    assert parts(63, 1, 32, 8, 8192) == 2 and parts(64, 1, 32, 8, 8192) == 1
