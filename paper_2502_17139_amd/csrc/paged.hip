@@ -64,10 +64,11 @@ __device__ __forceinline__ Sums block_sums(const Sums& v, int waves, Sums* scrat
 // step a load of each sequence's mask row; hence sixteen waves, four sequences' rows
 // at a time each, and 4,096 tokens a workgroup, so that few workgroups scan.  64
 // accepted paths 8.7 us (18 with four waves and a row at a time), 512 prompts of a
-// million slots 20.8 (39; 64 with 1,024 tokens a workgroup; a copy of its bytes
-// takes 2.4).  The scan is 8 bytes
-// a sequence from L2: at the 65,536 sequences allowed it is what costs, at the
-// thousands of a serving batch it is not.
+// million slots 21 (39; 64 with 1,024 tokens a workgroup; a copy of its bytes
+// takes 2.4): a window's 24 bytes a position make 148 KB of LDS, so a CU has one
+// workgroup, and 385 of them are two rounds.  The scan is 8 bytes a sequence from L2:
+// at the 65,536 sequences allowed it is what costs, at the thousands of a serving
+// batch it is not.
 __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(
     const int32_t* __restrict__ len, const int32_t* __restrict__ add, const int32_t* __restrict__ mask,
     const int32_t* __restrict__ last_node, int B, int R, int n_slots, int32_t* table, int max_pages, int32_t* queue,
@@ -279,9 +280,10 @@ __device__ __forceinline__ double2 turn(double half_turns) {
 // A unit is one token's keys or values of one head.  Lane j of its eight holds
 // dims 8 j .. 8 j + 7 and the same 64 further on: the two halves of each
 // rotation, and quarters of two scale groups.  12 prompts of up to 4,096 tokens, 32
-// key heads: 131 us, 70 % of the rate of a large copy; what it waits for is the
-// pages' short rows, 64 bytes of codes and four of scales a unit.  One accepted path
-// of each of 64 sequences: 4.2 us, a launch and the latency of a load.
+// key heads: 132 us, 70 % of the rate of a large copy.  113 MiB reach memory for the
+// 91 written (rows of 64 bytes, scales byte by byte), 5 us of the 40 that are missing;
+// the others may be the angles, which a workgroup of one token waits for.  One
+// accepted path of each of 64 sequences: 4.4 us, a launch and the latency of a load.
 __global__ void __launch_bounds__(kWriteThreads) k_paged_write(
     uint8_t* __restrict__ pool, int n_pages, int Hkv, const uint16_t* __restrict__ k, int64_t k_stride,
     const uint16_t* __restrict__ v, int64_t v_stride, int n_src, const int32_t* __restrict__ slot,

@@ -25,23 +25,27 @@
 //   takes 29; bound by memory.  64 rows over up to 8,192: 60 us in place of 41, as
 //   long as the longest take.
 // - more: two pairs of waves, each wave with two tiles and half of a page's keys,
-//   and a fifth tile (a tree's 65th row) split over all four waves.  One tile a wave
-//   and twice the waves a SIMD would be faster where there is no fifth tile (64
-//   trees of 64 rows over 2,048 tokens: 225 us against 254), but reads every page
-//   again for it (65 rows: 406 against 330); a tree's root and its 64 drafted rows
-//   make the fifth tile the usual case.  A workgroup of five waves leaves one SIMD
-//   with two of them (458).
+//   and a fifth tile (a tree's 65th row) split over all four waves.  64 trees over
+//   2,048 tokens, 32 key heads: 271 us of 65 rows, 224 of 64.  Tried when these took
+//   330 and 254 (every step of the softmax had its maximum then): one tile a wave
+//   and twice the waves a SIMD 225 for 64 rows, but 406 for 65, as it reads every
+//   page again for the fifth tile, and a tree's root and its 64 drafted rows make
+//   that the usual case; a workgroup of five waves 458, as one SIMD has two of them.
 // - up to two tiles: the four waves take 16 keys each.
 // Prefixes are cut into parts where there are too few workgroups to fill the card,
-// and joined by k_paged_merge.
+// and joined by k_paged_merge.  So are trees of more than 96 rows, whose further rows
+// are parts of their own: 96 rows 426 us, 97 486, 101 602, 128 701, 256 1,699 (the same
+// 64 trees); the fp32 results of all rows that they leave are 215 MB at 101 rows,
+// written and read again.
 //
-// What bounds the second form, at 64 trees of 65 rows, 32 heads, 2,048 tokens (281
+// What bounds the second form, at 64 trees of 65 rows, 32 heads, 2,048 tokens (271
 // us; a copy of its bytes takes 143, its products 128): a page takes a pair of
 // workgroups about 2,900 cycles, of which a SIMD's vector unit is at work for 46 %
 // and its matrix unit for 26 %.  The two do not overlap within a wave - scores,
 // weights, values follow one another - and 254 registers leave two waves a SIMD to
-// fill the gaps.  A third of the time is what comes before and after the pages:
-// queries and tree rows to 6-bit parts, and the hand-over.
+// fill the gaps.  A third of the time is what comes before and after the pages
+// (without any, the call takes 89 us): queries and tree rows to 6-bit parts, the
+// tree's own scores, and the hand-over.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
