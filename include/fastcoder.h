@@ -631,8 +631,8 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * Softmax weights are rounded to bf16, sums are fp32.  What is not finite among
  * the keys and values that a row attends to, or in its query, shows in its result
  * (a NaN, an infinity among values too); absent, masked and later tokens do not
- * count, whatever they hold.  Values of a magnitude of 2^96 or more may overflow
- * the sums.
+ * count, whatever they hold.  Values of a magnitude of 2^76 or more may overflow
+ * the sums: at 2^95 they do over half a million tokens.
  *
  * ws holds fc_paged_attention_workspace_bytes(...) bytes, 16-byte aligned (may
  * be NULL where that is 0); its contents on entry do not matter.  How a prefix

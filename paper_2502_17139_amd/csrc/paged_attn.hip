@@ -312,8 +312,9 @@ struct Row {
 // each score, and no maximum.  s holds scores less m (the products start from
 // minus_m), -inf where a key is not allowed.  m is the maximum of what the row saw
 // when it was last scaled; a factor common to a row's weights costs no accuracy,
-// bf16 and fp32 having the same exponents, as long as values of 2^96 and more stay
-// out.  A step whose weights add up to 2^24 or more (or to a NaN) is taken again
+// bf16 and fp32 having the same exponents, as long as the sums do not overflow: each
+// step adds less than 2^24 times the largest value, and the 2^31 tokens that a table
+// may hold are 2^27 steps at most, so values below 2^76 stay in.  A step whose weights add up to 2^24 or more (or to a NaN) is taken again
 // with m raised to its maximum, and so is a row's first: rare enough (scores of 24
 // bits above what came before) to cost nothing.  Against a maximum in every step,
 // with rows scaled anew from 2^8 on: 64 trees of 65 rows over 2,048 tokens 300 ->

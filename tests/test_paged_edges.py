@@ -160,3 +160,25 @@ def test_accepted_paths_across_workgroups_of_the_plan(B, R):
     r = _plan(length, add, table, queue, [0, 4 * B], int(add.sum()) + 9, mask, last)
     for b in np.flatnonzero(crossing):
         assert (r["slot"][start[b]:start[b] + add[b]] >= 0).all()
+
+
+@pytest.mark.parametrize("R", [1, 20, 65])
+def test_large_values_behind_low_first_scores(R):
+    """Weights go by what a row saw first: here all but the first pages have scores
+    17.5 bits above those, so that half a million weights of 2^17.5 meet values just
+    below the largest that the sums are good for."""
+    B, Hkv, width = 64, 8, 8192
+    k, v = torch.zeros((128, Hkv, 128)), torch.zeros((128, Hkv, 128))
+    k[64:], v[64:] = 1.0, 1.5 * 2.0 ** 75
+    pool = torch.zeros((2, Hkv, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_write(pool, k.bfloat16().cuda(), v.bfloat16().cuda(), dev(np.arange(128, dtype=np.int32)), rope_base=0.0)
+    table = np.ones((B, width), np.int32)
+    table[:, :4] = 0
+    q = torch.full((B, R, Hkv, 128), 1.0703125, dtype=torch.bfloat16, device="cuda")    # 17.47 / (128 log2(e) / sqrt(128))
+    none = torch.zeros_like(q)
+    t = dict(num_nodes=np.full(B, R, np.int32), mask=np.zeros((B, R, R), np.int32), pos_ids=np.zeros((B, R), np.int32))
+    say(f"large values R={R}")
+    got = f64(fc.fc_paged_attention(q, none, none, pool, dev(table), dev(np.full(B, 64 * width, np.int32)),
+                                    tree=on_gpu(t), rope_base=0.0))
+    # the first pages weigh 2^-28; equal weights cancel but for their sums' rounding, and 1.5 is a bf16
+    assert np.abs(got / (1.5 * 2.0 ** 75) - 1).max() <= 2.0 ** -8
