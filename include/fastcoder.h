@@ -625,7 +625,7 @@ fc_status fc_paged_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32
  * bytes with each other or with what is read (FC_ERR_INVALID).
  *
  * Rotated and scaled queries are the sum of three 6-bit parts (together within
- * 2^-13 of the largest of each 32 dims), and so are the tree's rotated keys; of the
+ * 2^-13 of the largest of each 32 dims, or 2^-122 if that is more), and so are the tree's rotated keys; of the
  * nine products of a tree key's parts and a query's the three smallest are left out
  * (in each dim together at most 2^-11 of the product of the two groups' largest).
  * Softmax weights are rounded to bf16, sums are fp32.  What is not finite among

@@ -144,7 +144,8 @@ __device__ __forceinline__ floatx32 from_six(const int32x6& c, float f) {
 // 32 dims of a row as three 6-bit parts and their scale bytes.  The first
 // part's scale 2^e is the smallest with which the largest magnitude is at most
 // 7.5; it leaves at most 2^-2 * 2^e, the second (scale 2^(e - 4)) at most 2^-7,
-// the third (2^(e - 9)) at most 2^-12.  Scale byte 255: something is not finite.
+// the third (2^(e - 9)) at most 2^-12.  e is -110 at least, which keeps the scales of
+// the products above the least that a byte holds.  Scale byte 255: something is not finite.
 __device__ __forceinline__ void write_six(const float (&v)[32], uint8_t* row, int g) {
   uint32_t top = 0;
 #pragma unroll

@@ -182,3 +182,17 @@ def test_large_values_behind_low_first_scores(R):
                                     tree=on_gpu(t), rope_base=0.0))
     # the first pages weigh 2^-28; equal weights cancel but for their sums' rounding, and 1.5 is a bf16
     assert np.abs(got / (1.5 * 2.0 ** 75) - 1).max() <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("R", [1, 9, 40])
+@pytest.mark.parametrize("small,large", [(-105, 100), (-116, 110), (100, -110)])
+def test_sizes_far_apart(R, small, large):
+    """Queries below the least scale of their parts against keys near the largest,
+    and the other way round: scores of the usual size."""
+    rng = np.random.default_rng(R)
+    k, v = bf16(rng, 128, 2, 128, scale=2.0 ** large), bf16(rng, 128, 2, 128)
+    pool = torch.zeros((2, 2, fc.FC_PAGE_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_write(pool, k.cuda(), v.cuda(), dev(np.arange(128, dtype=np.int32)), rope_base=0.0)
+    say(f"sizes far apart R={R} {small} {large}")
+    check(bf16(rng, 1, R, 4, 128, scale=2.0 ** (small + 3)), bf16(rng, 1, R, 2, 128, scale=2.0 ** large),
+          bf16(rng, 1, R, 2, 128), pool, np.array([[1, 0]], np.int32), [100], norm=False)
