@@ -196,3 +196,53 @@ def test_sizes_far_apart(R, small, large):
     say(f"sizes far apart R={R} {small} {large}")
     check(bf16(rng, 1, R, 4, 128, scale=2.0 ** (small + 3)), bf16(rng, 1, R, 2, 128, scale=2.0 ** large),
           bf16(rng, 1, R, 2, 128), pool, np.array([[1, 0]], np.int32), [100], norm=False)
+
+
+def _some_calls(rng, n):
+    """Attention inputs of n calls with prefixes in parts, and what each gives alone."""
+    pool = make_pool(rng, 12, 2)
+    calls = []
+    for i in range(n):
+        R = (1, 9, 65)[i % 3]
+        row = lambda h: bf16(rng, 2, R, h, 128).cuda()  # noqa: E731
+        calls.append(dict(q=row(8), k_tree=row(2), v_tree=row(2), pool=pool,
+                          table=dev(rng.integers(0, 12, (2, 30)).astype(np.int32)),
+                          prefix_len=dev(np.array([1900 - i, 700], np.int32)), tree=on_gpu(trees(rng, 2, R))))
+    want = [fc.fc_paged_attention(**c) for c in calls]
+    torch.cuda.synchronize()
+    return calls, want
+
+
+def test_calls_at_once_on_several_streams():
+    """Calls side by side on their own streams, each with its own scratch memory."""
+    calls, want = _some_calls(np.random.default_rng(30), 6)
+    streams = [torch.cuda.Stream() for _ in calls]
+    say("calls on several streams")
+    for _ in range(3):
+        got = [[fc.fc_paged_attention(**c, stream=s) for _ in range(4)] for c, s in zip(calls, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(w, x) for w, g in zip(want, got) for x in g)
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured graphs with one workspace, replayed in turn with eager work and
+    other bytes in the workspace between."""
+    calls, want = _some_calls(np.random.default_rng(31), 3)
+    need = max(fc.fc_paged_attention_workspace_bytes(2, c["q"].shape[1], 8, 2, 30 * 64) for c in calls)
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    say("graphs that share a workspace")
+    graphs, outs = [], []
+    for c in calls:
+        out = torch.empty_like(c["q"])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            fc.fc_paged_attention(**c, out=out, workspace=ws)
+        graphs.append(g)
+        outs.append(out)
+    for turn in range(4):
+        for i in ((0, 1, 2), (2, 0, 1), (1, 1, 0), (0, 2, 2))[turn]:
+            outs[i].fill_(7.0)
+            graphs[i].replay()
+            assert torch.equal(outs[i], want[i]), (turn, i)
+            ws.fill_(255)
+            assert torch.equal(fc.fc_paged_attention(**calls[i]), want[i])
