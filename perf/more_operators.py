@@ -1,0 +1,723 @@
+"""An 8-bit paged cache that forgets, as measured cases.
+
+A serving program whose sequences outgrow their share of the cache holds keys and
+values in 8 bits, counts what attention each cached token gets, and drops the
+least attended ones.  What is left no longer lies at its position, so positions
+go into queries and keys before the cache sees them:
+
+- norm: queries and keys of a step, normed for each head and rotated by their
+  positions in one pass;
+- write: the step's key and value rows, rounded to 8 bits with a scale for each
+  block of 32 tokens and head, into their pages, and read back from them;
+- attention: a tree's rows (or one token's) over the cached prefix and their own
+  ancestors, and the logarithm of each row's sum;
+- weights: the attention that the step's rows pay to every cached token, added to
+  what it got before;
+- evict: the tokens of each head that got least leave the cache, the others move
+  together, and are read back.
+
+A page holds 64 tokens of one key head in 16,512 bytes: 64 x 128 bytes of key
+codes, token by token; four times 128 x 16 bytes of value codes, for each 16
+tokens dim by dim; then the scale bytes of the keys' two blocks of 32 tokens, of
+the values' two, and 124 bytes that are not used.  A code is a sign, four bits
+of exponent and three of mantissa (largest value 448, 127 is a NaN); a block's
+scale is 2^(byte - 127).
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+PAGE = 64            # tokens of a page
+BLOCK = 32           # tokens that share a scale
+DIM = 128            # dims of a head
+CODES = PAGE * DIM
+PAGE_BYTES = 2 * CODES + 128
+EPS = 1e-6
+ROPE_BASE = 10000.0
+MAX_DEPTH = 10       # of a draft tree
+
+
+# ------------------------------------------------------------------ cases --
+
+def listed() -> list:
+    return [
+        # one token of one sequence: the smallest call, where latency counts
+        dict(name="norm_1", kind="norm", tokens=1, heads=32, kv_heads=8, longest=3000, weights=True),
+        # the queries and keys of long prompts, a layer at a time
+        dict(name="norm_prompts", kind="norm", tokens=24571, heads=32, kv_heads=8, longest=131072, weights=True),
+        # the accepted rows' keys and values go into their pages: every step and layer
+        dict(name="write_64_accepted", kind="write", batch=64, rows=65, kv_heads=8, heads=32, add=11, longest=4096),
+        # the keys and values of long prompts
+        dict(name="write_prompts", kind="write", batch=12, rows=0, kv_heads=32, heads=32, add=4096, longest=1000),
+        # one token of one sequence
+        dict(name="decode_1", kind="attention", batch=1, rows=1, heads=32, kv_heads=8, prefix=3000, ragged=False),
+        # one token of one sequence with a long cache
+        dict(name="decode_1_long", kind="attention", batch=1, rows=1, heads=32, kv_heads=8, prefix=131000,
+             ragged=False),
+        # one token each of a batch of sequences of every length
+        dict(name="decode_64", kind="attention", batch=64, rows=1, heads=32, kv_heads=8, prefix=8192, ragged=True),
+        # a batch of trees, grouped key heads, prefixes of every length
+        dict(name="tree_48_grouped", kind="attention", batch=48, rows=65, heads=32, kv_heads=8, prefix=4096,
+             ragged=True),
+        # what the accepted rows of a batch of trees attended to
+        dict(name="weights_48_accepted", kind="weights", batch=48, rows=65, heads=32, kv_heads=8, add=11,
+             longest=4096),
+        # what the rows of a prompt attended to, its own earlier ones
+        dict(name="weights_prompt", kind="weights", batch=1, rows=0, heads=32, kv_heads=8, add=2011, longest=0),
+        # a batch of sequences is cut to a quarter of the longest
+        dict(name="evict_48", kind="evict", batch=48, kv_heads=8, longest=4096, budget=1000, ragged=True),
+        # one long sequence is cut to less than half
+        dict(name="evict_1_long", kind="evict", batch=1, kv_heads=8, longest=131000, budget=60001, ragged=False),
+    ]
+
+
+def _log_int(rng, lo: int, hi: int) -> int:
+    """An integer spread evenly over the logarithm of [lo, hi]."""
+    return min(hi, max(lo, int(round(lo * (hi / lo) ** rng.random()))))
+
+
+def draw(rng) -> dict:
+    kind = rng.choice(["norm", "write", "attention", "attention", "attention", "weights", "evict"])
+    heads, kv_heads = rng.choice([(32, 32), (32, 8), (40, 8), (16, 16), (12, 4), (8, 1), (5, 5)])
+    if kind == "norm":
+        return dict(kind=kind, tokens=_log_int(rng, 1, 24571 * 40 // (heads + kv_heads)), heads=heads,
+                    kv_heads=kv_heads, longest=_log_int(rng, 64, 131072), weights=rng.random() < 0.8)
+    if kind == "write":
+        trees = rng.random() < 0.5
+        batch = _log_int(rng, 1, 128 if trees else 12)
+        return dict(kind=kind, batch=batch, rows=rng.choice([65, 33, 101]) if trees else 0, kv_heads=kv_heads,
+                    heads=heads, add=11 if trees else _log_int(rng, 1, 4096), longest=_log_int(rng, 1, 4096))
+    if kind == "weights":
+        trees = rng.random() < 0.6
+        if trees:
+            longest = _log_int(rng, 1, 8192)
+            most = min(48 * 4096 * 8 / (longest * kv_heads), 48 * 4096 * 32 / (longest * heads), 64)
+            return dict(kind=kind, batch=_log_int(rng, 1, max(1, int(most))), rows=rng.choice([1, 65, 33]), heads=heads,
+                        kv_heads=kv_heads, add=11, longest=longest)
+        add = _log_int(rng, 1, 1000)
+        return dict(kind=kind, batch=rng.choice([1, 2, 3]), rows=0, heads=heads, kv_heads=kv_heads, add=add,
+                    longest=rng.choice([0, 0, _log_int(rng, 1, 300)]))
+    if kind == "evict":
+        longest = _log_int(rng, 2, 131000)
+        batch = _log_int(rng, 1, max(1, min(64, 131000 // (longest * max(kv_heads, 8) // 8))))
+        return dict(kind=kind, batch=batch, kv_heads=kv_heads, longest=longest,
+                    budget=_log_int(rng, 1, longest), ragged=rng.random() < 0.6)
+    rows = rng.choice([1, 1, 1, 2, 7, 17, 33, 65, 65, 101, 256])
+    prefix = _log_int(rng, 1, 131072 if rows < 3 else 16384)
+    # no more keys and no more products than the largest listed case
+    most = min(48 * 4096 * 16 / (prefix * kv_heads), 48 * 4096 * 65 * 32 / (prefix * max(rows, 8) * heads), 64)
+    return dict(kind=kind, batch=_log_int(rng, 1, max(1, int(most))), rows=rows, heads=heads, kv_heads=kv_heads,
+                prefix=prefix, ragged=rng.random() < 0.6)
+
+
+# ----------------------------------------------------------------- inputs --
+
+def _gen(seed: int, role: int) -> torch.Generator:
+    g = torch.Generator(device="cuda")
+    g.manual_seed((seed * 1_000_003 + role) & 0x7FFFFFFFFFFF)
+    return g
+
+
+def _int32(values) -> torch.Tensor:
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _lengths(case) -> list:
+    """The sequences' cached tokens: the same for every seed, so that work() knows them."""
+    n, most = case["batch"], case.get("prefix", case.get("longest"))
+    if not case.get("ragged", True):
+        return [most] * n
+    rng = random.Random(most * 1013 + n)
+    lens = [rng.choice([0, 1, rng.randint(0, most), rng.randint(0, most), rng.randint(most // 2, most)])
+            for _ in range(n)]
+    lens[0] = most
+    return lens
+
+
+def _adds(case, lens) -> list:
+    """Tokens that each sequence gains: accepted rows, or a prompt's."""
+    rng = random.Random(case["add"] * 37 + case["batch"])
+    if case["rows"] == 1:
+        return [1] * len(lens)
+    adds = [rng.randint(1, case["add"]) if case["rows"] else rng.choice([0, case["add"], rng.randint(0, case["add"])])
+            for _ in lens]
+    adds[0] = case["add"]
+    return adds
+
+
+def _budgets(case, lens) -> list:
+    """Tokens that each sequence may keep, some more than it has."""
+    rng = random.Random(case["budget"] * 41 + case["batch"])
+    if not case["ragged"]:
+        return [case["budget"]] * len(lens)
+    return [case["budget"]] + [rng.choice([case["budget"], case["budget"], rng.randint(0, case["budget"])])
+                               for _ in lens[1:]]
+
+
+def _protected(case) -> tuple:
+    """First and last tokens that stay whatever they got."""
+    return (4, min(128, case["budget"] // 4 + 1))
+
+
+def _trees(g: torch.Generator, B: int, R: int) -> dict:
+    """Draft trees: every row's parent is an earlier row, rows at most MAX_DEPTH below the root."""
+    u = torch.rand((B, R), generator=g, device="cuda")
+    pos = torch.zeros((B, R), dtype=torch.int64, device="cuda")
+    mask = torch.zeros((B, R, R), dtype=torch.int32, device="cuda")
+    mask[:, 0, 0] = 1
+    at = torch.arange(B, device="cuda")
+    for i in range(1, R):
+        p = (i - 1 - (u[:, i] * u[:, i] * i).long()).clamp(min=0)
+        p = torch.where(pos[at, p] < MAX_DEPTH, p, torch.zeros_like(p))
+        pos[:, i] = pos[at, p] + 1
+        mask[:, i] = mask[at, p]
+        mask[:, i, i] = 1
+    lost = (torch.rand(B, generator=g, device="cuda") * min(R, 8)).long()
+    nodes = R - lost if R > 1 else torch.ones(B, dtype=torch.int64, device="cuda")
+    return dict(num_nodes=nodes.int(), pos_ids=pos.int(), mask=mask)
+
+
+def _tables(g: torch.Generator, lens, spare: int):
+    """Block tables of the sequences, every page somewhere in a pool."""
+    held = [-(-n // PAGE) for n in lens]
+    n_pages = sum(held) + spare
+    perm = torch.randperm(n_pages, generator=g, device="cuda").int()
+    at = torch.arange(max(max(held), 1), device="cuda")[None]
+    count = torch.tensor(held, device="cuda")[:, None]
+    first = torch.cumsum(count, 0) - count
+    table = torch.where(at < count, perm[(first + at).clamp(max=n_pages - 1)], torch.full_like(perm[:1], -1))
+    return table.contiguous(), n_pages
+
+
+def _heads(g: torch.Generator, n: int, heads: int) -> torch.Tensor:
+    """Keys or values as a model has them: some channels much larger than the others."""
+    x = torch.randn((n, heads, DIM), generator=g, device="cuda")
+    x[..., 5::37] *= 4
+    return x
+
+
+def _pool(g: torch.Generator, n_pages: int, hkv: int) -> torch.Tensor:
+    """Pages of rounded keys and values, a thousand or two at a time."""
+    pool = torch.zeros((n_pages, hkv, PAGE_BYTES), dtype=torch.uint8, device="cuda")
+    flat = pool.view(-1, PAGE_BYTES)
+    for a in range(0, flat.shape[0], 2048):
+        part = flat[a:a + 2048]
+        x = _heads(g, 2 * part.shape[0] * PAGE, 1).view(2, -1, PAGE, DIM)
+        for i in (0, 1):
+            codes, scales = _round(x[i].unflatten(1, (2, BLOCK)))
+            _codes(part)[i].copy_(_laid(codes.flatten(1, 2), i))
+            part[:, 2 * CODES + 2 * i:2 * CODES + 2 * i + 2] = scales
+    return pool
+
+
+def _slots(table: torch.Tensor, lens, adds):
+    """Where the tokens after each sequence's cached ones go, in pages that its table already names."""
+    start, count = torch.tensor(lens, device="cuda"), torch.tensor(adds, device="cuda").clamp(min=0)
+    seq = torch.repeat_interleave(torch.arange(len(lens), device="cuda"), count)
+    t = torch.arange(seq.numel(), device="cuda") - (torch.cumsum(count, 0) - count)[seq]
+    pos = start[seq] + t
+    return (table[seq, pos // PAGE] * PAGE + pos % PAGE).int(), seq, t
+
+
+def prepare(case, seed):
+    g = _gen(seed, 1)
+    hkv = case["kv_heads"]
+    if case["kind"] == "norm":
+        n, H = case["tokens"], case["heads"]
+        # the rows lie in the output of a fused projection: query heads, then keys, then values
+        qkv = torch.cat([_heads(g, n, H + hkv) * 3, _heads(g, n, hkv)], 1).bfloat16()
+        w = [(1 + 0.2 * torch.randn(DIM, generator=g, device="cuda")).bfloat16() if case["weights"] else None for _ in "qk"]
+        return dict(kind="norm", q=qkv[:, :H], k=qkv[:, H:H + hkv], weights=w,
+                    pos=torch.randint(0, case["longest"], (n,), generator=g, device="cuda").int(),
+                    out=[torch.zeros((n, h, DIM), dtype=torch.bfloat16, device="cuda") for h in (H, hkv)])
+    lens = _lengths(case)
+    if case["kind"] == "write":
+        adds = _adds(case, lens)
+        table, n_pages = _tables(g, [n + a for n, a in zip(lens, adds)], 3)
+        slot, seq, t = _slots(table, lens, adds)
+        n, R, H = slot.numel(), case["rows"], case["heads"]
+        rows = case["batch"] * R if R else n
+        qkv = torch.cat([_heads(g, rows, H), _heads(g, rows, 2 * hkv)], 1).bfloat16()
+        src = torch.arange(n, device="cuda") if not R else seq * R + (t * 6).clamp(max=R - 1)
+        return dict(kind="write", pool=_pool(g, n_pages, hkv), k=qkv[:, H:H + hkv], v=qkv[:, H + hkv:], slot=slot,
+                    src=src.int(), out=[torch.zeros((n, hkv, DIM), dtype=torch.bfloat16, device="cuda") for _ in "kv"])
+    if case["kind"] == "weights":
+        adds, R, H = _adds(case, lens), case["rows"], case["heads"]
+        new = [n + a for n, a in zip(lens, adds)]
+        table, n_pages = _tables(g, new, 1)
+        _, seq, t = _slots(table, lens, adds)
+        n = seq.numel()
+        src = (torch.arange(n, device="cuda") if not R else seq * R + (t * 6).clamp(max=R - 1)).int()
+        s = dict(kind="weights", pool=_pool(g, n_pages, hkv), table=table, length=_int32(lens), new_length=_int32(new),
+                 cu=_int32([sum(adds[:b]) for b in range(len(adds) + 1)]), src=src, max_len=max(new),
+                 q=(torch.randn((case["batch"] * R if R else n, H, DIM), generator=g, device="cuda") * 1.2).bfloat16(),
+                 weights=torch.rand((n_pages, hkv, PAGE), generator=g, device="cuda") ** 4 * 3,
+                 lens=lens, adds=adds)
+        score, seen = _row_scores(s)
+        lse = torch.logsumexp(score.masked_fill_(~seen, -math.inf), -1)  # [B][rows][H]
+        s["lse"] = torch.zeros((s["q"].shape[0], H), device="cuda")
+        s["lse"][src.long()] = lse[seq, t]
+        return s
+    if case["kind"] == "evict":
+        budgets = _budgets(case, lens)
+        table, n_pages = _tables(g, lens, 1)
+        slot = _slots(table, [0] * len(lens), [min(n, k) for n, k in zip(lens, budgets)])[0]
+        first, recent = _protected(case)
+        return dict(kind="evict", pool=_pool(g, n_pages, hkv), table=table, length=_int32(lens), budget=_int32(budgets),
+                    weights=torch.rand((n_pages, hkv, PAGE), generator=g, device="cuda") ** 6 * 40, first=first,
+                    recent=recent, max_len=max(lens), slot=slot,
+                    out=[torch.zeros((slot.numel(), hkv, DIM), dtype=torch.bfloat16, device="cuda") for _ in "kv"])
+    table, n_pages = _tables(g, lens, 1)
+    B, R, H = case["batch"], case["rows"], case["heads"]
+    # scores of a standard deviation of about two: some keys matter, none alone
+    return dict(kind="attention", pool=_pool(g, n_pages, hkv), table=table, prefix_len=_int32(lens), max_len=max(lens),
+                q=(torch.randn((B, R, H, DIM), generator=g, device="cuda") * 1.2).bfloat16(),
+                k=_heads(g, B * R, hkv).bfloat16().view(B, R, hkv, DIM),
+                v=_heads(g, B * R, hkv).bfloat16().view(B, R, hkv, DIM),
+                tree=_trees(g, B, R) if R > 1 else None,
+                out=torch.zeros((B, R, H, DIM), dtype=torch.bfloat16, device="cuda"),
+                lse=torch.zeros((B, R, H), device="cuda"))
+
+
+# ------------------------------------------------------------ plain forms --
+
+_tables_of = {}
+
+
+def _power(e: torch.Tensor) -> torch.Tensor:
+    """float32 2^e for integers in [-126, 127], exactly."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _values() -> torch.Tensor:
+    """The value of each code: [256]."""
+    if "values" not in _tables_of:
+        _tables_of["values"] = torch.arange(256, device="cuda").byte().view(torch.float8_e4m3fn).float()
+    return _tables_of["values"]
+
+
+def _codes(pages: torch.Tensor) -> list:
+    """The key codes [..][64][128] and value codes [..][4][128][16] of pages [..][16,512], in place."""
+    return [pages[..., :CODES].unflatten(-1, (PAGE, DIM)),
+            pages[..., CODES:2 * CODES].unflatten(-1, (PAGE // 16, DIM, 16))]
+
+
+def _laid(codes: torch.Tensor, i: int) -> torch.Tensor:
+    """Codes [..][64][128] as a page holds them: keys (0) as they are, values (1) dim by dim for each 16 tokens."""
+    return codes if i == 0 else codes.unflatten(-2, (PAGE // 16, 16)).transpose(-1, -2)
+
+
+def _unlaid(codes: torch.Tensor, i: int) -> torch.Tensor:
+    return codes if i == 0 else codes.transpose(-1, -2).flatten(-3, -2)
+
+
+def _exponent(top: torch.Tensor) -> torch.Tensor:
+    """The least e in [-117, 119] with top <= 448 * 2^e, or the largest."""
+    frac, exp = torch.frexp(top)
+    e = torch.where(frac <= 0.875, exp - 9, exp - 8)  # 448 = 0.875 * 2^9
+    return torch.where(top == 0, torch.full_like(e, -117), e).clamp(-117, 119)
+
+
+def _largest(x: torch.Tensor) -> torch.Tensor:
+    """The magnitudes that a scale has to reach: those of what is finite."""
+    return torch.where(torch.isfinite(x), x.abs(), torch.zeros_like(x))
+
+
+def _encode(x: torch.Tensor, e: torch.Tensor) -> torch.Tensor:
+    """Codes of float32 x at the scale 2^e: the nearest, ties to the even one; what is not finite is a NaN."""
+    y = (x * _power(-e)).clamp(-448, 448)
+    return torch.where(torch.isfinite(x), y, torch.nan).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _round(x: torch.Tensor):
+    """Codes [..][32][128] and scale bytes [..] of blocks of float32 rows."""
+    e = _exponent(_largest(x).amax((-1, -2)))
+    return _encode(x, e[..., None, None]), (e + 127).byte()
+
+
+def _scale(byte: torch.Tensor) -> torch.Tensor:
+    return _power(byte.int() - 127)
+
+
+def _held(pages: torch.Tensor, i: int) -> torch.Tensor:
+    """float32 [..][64][128] that pages' keys (0) or values (1) stand for."""
+    codes = _unlaid(_codes(pages)[i], i)
+    x = torch.index_select(_values(), 0, codes.reshape(-1).int()).view(codes.shape)
+    s = _scale(pages[..., 2 * CODES + 2 * i:2 * CODES + 2 * i + 2])
+    return x * torch.repeat_interleave(s, BLOCK, -1)[..., None]
+
+
+def _norm(s):
+    c = s["pos"].double()[:, None] * ROPE_BASE ** (-2 * torch.arange(DIM // 2, device="cuda", dtype=torch.float64) / DIM)
+    c, sn = torch.cos(c).float()[:, None], torch.sin(c).float()[:, None]
+    out = []
+    for x, w in zip((s["q"], s["k"]), s["weights"]):
+        x = x.float()
+        if w is not None:
+            x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * w.float()
+        a, b = x[..., :DIM // 2], x[..., DIM // 2:]
+        out.append(torch.cat([a * c - b * sn, b * c + a * sn], -1).bfloat16())
+    return out
+
+
+def _write(s):
+    rows, slot = s["src"].long(), s["slot"].long()
+    block, of = torch.unique_consecutive(slot // BLOCK, return_inverse=True)
+    page, half, hkv = block // 2, block % 2, s["pool"].shape[1]
+    heads = torch.arange(hkv, device="cuda")[None]
+    fresh = torch.zeros(block.numel(), dtype=torch.bool, device="cuda").index_fill_(0, of[slot % BLOCK == 0], True)[:, None]
+    for i, x in enumerate((s["k"], s["v"])):
+        x = x[rows].float()
+        top = torch.zeros((block.numel(), hkv), device="cuda")
+        top = top.scatter_reduce(0, of[:, None].expand(-1, hkv), _largest(x).amax(-1), "amax")
+        e = _exponent(top)
+        byte = s["pool"][page[:, None], heads, (2 * CODES + 2 * i + half)[:, None]]
+        was = byte.int() - 127
+        e = torch.where(fresh, e, torch.maximum(e, was.clamp(-117, 119)))
+        # the block's other rows: none in a new block, else at the new scale
+        t = (half[:, None] * BLOCK + torch.arange(BLOCK, device="cuda"))[:, None, :, None]
+        d = torch.arange(DIM, device="cuda")
+        at = t * DIM + d if i == 0 else CODES + t // 16 * (16 * DIM) + d * 16 + t % 16
+        at_page, at_head = page[:, None, None, None], heads[:, :, None, None]
+        old = s["pool"][at_page, at_head, at]
+        again = _encode(torch.index_select(_values(), 0, old.reshape(-1).int()).view(old.shape), (e - was)[..., None, None])
+        codes = torch.where((e == was)[..., None, None], old, again)
+        codes = torch.where(fresh[..., None, None], torch.zeros_like(codes), codes)
+        codes[of, :, slot % BLOCK] = _encode(x, e[of][..., None])
+        s["pool"][at_page, at_head, at] = codes
+        s["pool"][page[:, None], heads, (2 * CODES + 2 * i + half)[:, None]] = (e + 127).byte()
+    return _read(s)
+
+
+def _read(s):
+    page, t = (s["slot"] // PAGE).long(), (s["slot"] % PAGE).long()
+    heads, d = torch.arange(s["pool"].shape[1], device="cuda")[None, :, None], torch.arange(DIM, device="cuda")
+    out = []
+    for i in (0, 1):
+        at = t[:, None] * DIM + d if i == 0 else CODES + t[:, None] // 16 * (16 * DIM) + d * 16 + t[:, None] % 16
+        x = torch.index_select(_values(), 0, s["pool"][page[:, None, None], heads, at[:, None]].reshape(-1).int())
+        sc = _scale(s["pool"][page[:, None, None], heads, (2 * CODES + 2 * i + t // BLOCK)[:, None, None]])
+        out.append((x.view(t.numel(), -1, DIM) * sc).bfloat16())
+    return out
+
+
+def _cached(s, i: int) -> torch.Tensor:
+    """float32 [B][hkv][tokens][128] of the sequences' pages."""
+    n_pages = -(-s["max_len"] // PAGE)
+    x = _held(s["pool"][s["table"][:, :n_pages].clamp(min=0).long()], i)  # [B][pages][hkv][64][128]
+    return x.transpose(1, 2).flatten(2, 3)
+
+
+def _attention(s):
+    B, R, H, _ = s["q"].shape
+    hkv, tree = s["k"].shape[2], s["tree"]
+    nodes = tree["num_nodes"] if tree else torch.ones(B, dtype=torch.int32, device="cuda")
+    k, v = (torch.cat([_cached(s, i), x.float().transpose(1, 2)], 2) for i, x in enumerate((s["k"], s["v"])))
+    rows = s["q"].float().view(B, R, hkv, H // hkv, DIM).transpose(1, 2).reshape(B, hkv, R * (H // hkv), DIM)
+    score = (torch.matmul(rows, k.transpose(2, 3)) * DIM ** -0.5).view(B, hkv, R, H // hkv, -1)
+    cached = torch.arange(k.shape[2] - R, device="cuda")[None] < s["prefix_len"][:, None]
+    at = torch.arange(R, device="cuda")
+    seen = tree["mask"] == 1 if tree else torch.ones((B, 1, 1), dtype=torch.bool, device="cuda")
+    seen = seen & (at[None, None] < nodes[:, None, None])
+    allowed = torch.cat([cached[:, None].expand(B, R, -1), seen], 2)[:, None, :, None]
+    score = score.masked_fill_(~allowed, -math.inf)
+    lse = torch.logsumexp(score, -1)
+    score = score.sub_(lse[..., None]).exp_()
+    out = torch.matmul(score.view(B, hkv, R * (H // hkv), -1), v).view(B, hkv, R, H // hkv, DIM)
+    out = out.transpose(1, 2).reshape(B, R, H, DIM)
+    off = (at[None] >= nodes[:, None])[:, :, None]
+    return dict(out=out.masked_fill(off[..., None], 0).bfloat16(),
+                lse=lse.transpose(1, 2).reshape(B, R, H).masked_fill(off, -math.inf))
+
+
+def _row_scores(s):
+    """Scores [B][rows][H][tokens] of each sequence's new rows with its cached tokens, and which they see."""
+    most, H = max(s["adds"]), s["q"].shape[1]
+    hkv, B = s["pool"].shape[1], s["table"].shape[0]
+    t = torch.arange(most, device="cuda")
+    there = t[None] < (s["new_length"] - s["length"])[:, None]
+    at = (s["cu"][:-1, None] + t).clamp(max=max(s["src"].numel() - 1, 0)).long()
+    q = s["q"][s["src"].long()[at]].float().view(B, most, hkv, H // hkv, DIM).transpose(1, 2)
+    k = _cached(s, 0)
+    score = torch.matmul(q.reshape(B, hkv, -1, DIM), k.transpose(2, 3)) * DIM ** -0.5
+    score = score.view(B, hkv, most, H // hkv, -1).transpose(1, 2).flatten(2, 3)
+    seen = torch.arange(k.shape[2], device="cuda") <= s["length"][:, None, None] + t[:, None]
+    return score, (seen & there[..., None])[:, :, None]
+
+
+def _weights(s):
+    score, seen = _row_scores(s)
+    B, most, H, L = score.shape
+    hkv = s["pool"].shape[1]
+    t = torch.arange(most, device="cuda")
+    at = (s["cu"][:-1, None] + t).clamp(max=max(s["src"].numel() - 1, 0)).long()
+    lse = s["lse"][s["src"].long()[at]]  # [B][rows][H]
+    w = score.sub_(lse[..., None]).exp_().masked_fill_(~seen, 0)
+    got = w.view(B, most, hkv, H // hkv, L).sum((1, 3))  # [B][hkv][tokens]
+    tok = torch.arange(L, device="cuda")
+    was = s["weights"][s["table"][:, :L // PAGE].clamp(min=0).long()].transpose(1, 2).flatten(2, 3)
+    new = torch.where(tok < s["length"][:, None, None], was + got, got)
+    live = (tok < s["new_length"][:, None]) & (s["new_length"] > s["length"])[:, None]
+    page = torch.where(live, s["table"][:, tok // PAGE].long(), s["weights"].shape[0])
+    flat = torch.cat([s["weights"], s["weights"].new_zeros(1, *s["weights"].shape[1:])])
+    flat[page[:, None], torch.arange(hkv, device="cuda")[None, :, None], (tok % PAGE)[None, None]] = new
+    s["weights"].copy_(flat[:-1])
+    return s["weights"]
+
+
+def _evict(s):
+    B, hkv, L = s["table"].shape[0], s["pool"].shape[1], -(-s["max_len"] // PAGE) * PAGE
+    length, keep = s["length"].long(), torch.minimum(s["length"], s["budget"].clamp(min=0)).long()
+    tok = torch.arange(L, device="cuda")
+    pages = s["table"][:, :L // PAGE].clamp(min=0).long()
+    w = s["weights"][pages].transpose(1, 2).flatten(2, 3)  # [B][hkv][tokens]
+    rank = torch.where(w > 0, w, torch.zeros_like(w)).view(torch.int32).long()
+    ends = length[:, None, None]
+    late = tok >= ends - keep[:, None, None].clamp(max=s["recent"])
+    rank = rank + late.long() * 2 ** 34 + (tok < s["first"]).long() * 2 ** 33
+    rank = torch.where(tok < ends, rank, torch.full_like(rank, -1))
+    order = torch.sort(rank, dim=-1, descending=True, stable=True).indices
+    kept = torch.zeros((B, hkv, L), dtype=torch.bool, device="cuda")
+    kept = kept.scatter(-1, order, (tok < keep[:, None, None]).expand(B, hkv, L))
+    # kept tokens in their order, then the others
+    to = torch.sort((~kept).byte(), dim=-1, stable=True).indices
+    live = (tok < keep[:, None]) & (keep < length)[:, None]
+    blocks = torch.where(live[:, ::BLOCK], pages[:, tok[::BLOCK] // PAGE] * 2 + tok[::BLOCK] // BLOCK % 2,
+                         2 * s["pool"].shape[0])
+    cut = s["pool"].new_zeros((s["pool"].shape[0] + 1, *s["pool"].shape[1:]))
+    heads = torch.arange(hkv, device="cuda")[None, :, None]
+    for i in (0, 1):
+        x = _held(s["pool"][pages], i).transpose(1, 2).flatten(2, 3)
+        x = torch.gather(x, 2, to[..., None].expand(-1, -1, -1, DIM)) if L else x
+        x = torch.where(live[:, None, :, None], x, torch.zeros_like(x)).unflatten(2, (-1, BLOCK))
+        codes, scales = _round(x)
+        cut[:-1] = s["pool"]
+        view = _unlaid(_codes(cut)[i], i).unflatten(-2, (2, BLOCK)).clone()  # [pages][hkv][2][32][128]
+        at = (blocks // 2)[:, None], heads, (blocks % 2)[:, None]
+        view[at] = codes
+        _codes(cut)[i].copy_(_laid(view.flatten(-3, -2), i))
+        cut[at[0], heads, 2 * CODES + 2 * i + at[2]] = scales
+        s["pool"].copy_(cut[:-1])
+    flat = torch.cat([s["weights"], s["weights"].new_zeros(1, hkv, PAGE)])
+    page = torch.where(live, pages[:, tok // PAGE], s["pool"].shape[0])
+    flat[page[:, None], heads, (tok % PAGE)[None, None]] = torch.gather(w, 2, to)
+    s["weights"].copy_(flat[:-1])
+    k, v = _read(s)
+    return dict(add=(keep - length).int(), weights=s["weights"], k=k, v=v)
+
+
+def run(s):
+    if own:
+        import paper_2502_17139_amd as fc
+
+        if s["kind"] == "norm":
+            return list(fc.fc_norm_rotate(s["q"], s["k"], *s["weights"], pos=s["pos"], eps=EPS, rope_base=ROPE_BASE,
+                                          out=s["out"]))
+        if s["kind"] == "write":
+            fc.fc_paged8_write(s["pool"], s["k"], s["v"], s["slot"], src=s["src"])
+            return list(fc.fc_paged8_read(s["pool"], s["slot"], out=s["out"]))
+        if s["kind"] == "weights":
+            fc.fc_paged8_weights(s["weights"], s["q"], s["lse"], s["pool"], s["table"], s["length"], s["new_length"],
+                                 s["cu"], src=s["src"], max_len=s["max_len"])
+            return s["weights"]
+        if s["kind"] == "evict":
+            add = fc.fc_paged8_evict(s["pool"], s["weights"], s["table"], s["length"], s["budget"], first=s["first"],
+                                     recent=s["recent"], max_len=s["max_len"])
+            k, v = fc.fc_paged8_read(s["pool"], s["slot"], out=s["out"])
+            return dict(add=add, weights=s["weights"], k=k, v=v)
+        fc.fc_paged8_attention(s["q"], s["k"], s["v"], s["pool"], s["table"], s["prefix_len"], tree=s["tree"],
+                               max_len=s["max_len"], out=s["out"], lse=s["lse"])
+        return dict(out=s["out"], lse=s["lse"])
+    return dict(norm=_norm, write=_write, weights=_weights, evict=_evict, attention=_attention)[s["kind"]](s)
+
+
+# ------------------------------------------------------------------- work --
+
+def work(case) -> dict:
+    hkv = case["kv_heads"]
+    row = 2 * DIM  # bytes of a bfloat16 row, and of a cached token's keys and values
+    scales = 4 / PAGE
+    if case["kind"] == "norm":
+        n, h = case["tokens"], case["heads"] + hkv
+        return dict(bytes=n * (h * 2 * row + 4) + 2 * row, flops=n * h * DIM * 10)
+    lens = _lengths(case)
+    if case["kind"] == "write":
+        n = sum(_adds(case, lens))
+        # two rows in, their codes out and in again, two rows out
+        return dict(bytes=n * (hkv * (2 * row + 2 * (row + scales) + 2 * row) + 8), flops=n * hkv * 8 * DIM)
+    if case["kind"] == "weights":
+        adds, H = _adds(case, lens), case["heads"]
+        tokens, rows = sum(n + a for n, a in zip(lens, adds)), sum(adds)
+        pairs = sum(a * n + a * (a + 1) // 2 for n, a in zip(lens, adds))
+        return dict(bytes=tokens * hkv * (DIM + scales / 2 + 4) + sum(lens) * hkv * 4 + rows * (H * (row + 4) + 4),
+                    flops=2 * DIM * H * pairs)
+    if case["kind"] == "evict":
+        keep = [min(n, k) for n, k in zip(lens, _budgets(case, lens))]
+        cut = [(n, k) for n, k in zip(lens, keep) if k < n]
+        held, gone_in = sum(k for _, k in cut), sum(n for n, _ in cut)
+        # weights in, kept rows in and out again, the rows read back
+        return dict(bytes=hkv * (gone_in * 4 + held * (2 * (row + scales) + 4) + sum(keep) * (row + 2 * row)), flops=0)
+    B, R, H = case["batch"], case["rows"], case["heads"]
+    keys, rows = sum(lens), B * R
+    return dict(bytes=keys * hkv * (row + scales) + rows * (H * (2 * row + 4) + hkv * 2 * row) + (4 * rows * R if R > 1 else 0),
+                flops=4 * DIM * H * (R * keys + B * R * R))
+
+
+# ------------------------------------------------------------------ exact --
+
+def _two(e: torch.Tensor) -> torch.Tensor:
+    """float64 2^e for integers e, exactly."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _exact_page(pages: torch.Tensor, part: int) -> torch.Tensor:
+    """float64 [..][64][128] of the keys (0) or values (1) of pages' bytes: sign, four exponent bits, three of mantissa."""
+    b = pages[..., part * 8192:part * 8192 + 8192].long()
+    b = b.unflatten(-1, (64, 128)) if part == 0 else b.unflatten(-1, (4, 128, 16)).movedim(-1, -2).flatten(-3, -2)
+    ex, man = (b >> 3) & 15, (b & 7).double()
+    mag = torch.where(ex == 0, man * 2.0 ** -9, (1 + man / 8) * _two(ex - 7))
+    mag = torch.where((b & 127) == 127, torch.nan, mag)
+    sc = _two(pages[..., 16384 + 2 * part:16386 + 2 * part].long() - 127)
+    return torch.where(b >= 128, -mag, mag) * sc.repeat_interleave(32, -1)[..., None]
+
+
+def _exact_round(x: torch.Tensor, e: torch.Tensor) -> torch.Tensor:
+    """The value that each element of float64 x is held as at the scale 2^e."""
+    a = x.abs() * _two(-e)
+    step = _two(torch.floor(torch.log2(a.clamp(min=2.0 ** -6))) - 3)
+    step = torch.where(a >= 16 * step, step * 2, torch.where((a < 8 * step) & (step > 2.0 ** -9), step / 2, step))
+    return torch.copysign((torch.round(a / step) * step).clamp(max=448.0) * _two(e), x)  # torch.round: ties to even
+
+
+def _exact_exponent(top: torch.Tensor) -> torch.Tensor:
+    e = torch.ceil(torch.log2((top / 448).clamp(min=2.0 ** -200)))
+    e = torch.where(top > 448 * _two(e), e + 1, torch.where(top <= 448 * _two(e - 1), e - 1, e))
+    return e.clamp(-117, 119)
+
+
+def _exact_write(s) -> list:
+    slot = s["slot"].tolist()
+    runs = [i for i in range(len(slot)) if i == 0 or slot[i] // 32 != slot[i - 1] // 32] + [len(slot)]
+    out = []
+    for part, x in enumerate((s["k"], s["v"])):
+        x = x[s["src"].long()].double()
+        tops = [x[a:b].abs().amax((0, 2)) for a, b in zip(runs, runs[1:])]
+        need = _exact_exponent(torch.stack(tops))
+        first = torch.tensor(runs[:-1], device="cuda")
+        block = s["slot"][first].long() // 32
+        was = s["pool"][block // 2, :, 16384 + 2 * part + block % 2].double() - 127
+        new = torch.tensor([any(t % 32 == 0 for t in slot[a:b]) for a, b in zip(runs, runs[1:])], device="cuda")
+        e = torch.where(new[:, None], need, torch.maximum(need, was.clamp(-117, 119)))
+        each = torch.repeat_interleave(e, torch.diff(torch.tensor(runs, device="cuda")), 0)
+        out.append(_exact_round(x, each[..., None]))
+    return out
+
+
+def _exact_norm(s) -> list:
+    th = s["pos"].double()[:, None] * torch.exp(-torch.arange(64, device="cuda").double() / 64 * math.log(ROPE_BASE))
+    turn, out = torch.polar(torch.ones_like(th), th)[:, None], []
+    for x, w in zip((s["q"], s["k"]), s["weights"]):
+        x = x.double()
+        if w is not None:
+            x = x / torch.sqrt((x * x).sum(-1, keepdim=True) / 128 + EPS) * w.double()
+        z = torch.complex(x[..., :64], x[..., 64:]) * turn
+        out.append(torch.cat([z.real, z.imag], -1))
+    return out
+
+
+def _exact_attention(s, lens) -> dict:
+    B, R, H, _ = s["q"].shape
+    hkv = s["k"].shape[2]
+    out = torch.zeros((B, R, H, 128), dtype=torch.float64, device="cuda")
+    lse = torch.full((B, R, H), -math.inf, dtype=torch.float64, device="cuda")
+    for b, p in enumerate(lens):
+        n = int(s["tree"]["num_nodes"][b]) if s["tree"] else R
+        pages = s["pool"][s["table"][b, :(p + 63) // 64].long()]
+        seen = s["tree"]["mask"][b, :n, :n] == 1 if s["tree"] else torch.ones((1, 1), dtype=torch.bool, device="cuda")
+        hidden = torch.cat([torch.zeros((n, p), dtype=torch.bool, device="cuda"), ~seen], 1)
+        for h in range(hkv):
+            k = torch.cat([_exact_page(pages[:, h], 0).reshape(-1, 128)[:p], s["k"][b, :n, h].double()])
+            v = torch.cat([_exact_page(pages[:, h], 1).reshape(-1, 128)[:p], s["v"][b, :n, h].double()])
+            hs = slice(h * (H // hkv), (h + 1) * (H // hkv))
+            a = torch.einsum("nhd,kd->hnk", s["q"][b, :n, hs].double(), k) / math.sqrt(128)
+            a = a.masked_fill(hidden, -math.inf)
+            top = a.amax(-1, keepdim=True)
+            a = torch.exp(a - top)
+            total = a.sum(-1, keepdim=True)
+            out[b, :n, hs] = torch.einsum("hnk,kd->nhd", a / total, v)
+            lse[b, :n, hs] = (top + torch.log(total))[..., 0].T
+    return dict(out=out, lse=lse)
+
+
+def _exact_weights(s, lens, adds) -> torch.Tensor:
+    got = s["weights"].double()
+    H, hkv = s["q"].shape[1], s["pool"].shape[1]
+    for b, (p, a) in enumerate(zip(lens, adds)):
+        if a < 1:
+            continue
+        at = s["table"][b, :(p + a + 63) // 64].long()
+        rows = s["src"][int(s["cu"][b]):int(s["cu"][b]) + a].long()
+        late = torch.arange(p + a, device="cuda")[None] > p + torch.arange(a, device="cuda")[:, None]
+        for h in range(hkv):
+            k = _exact_page(s["pool"][at, h], 0).reshape(-1, 128)[:p + a]
+            hs = slice(h * (H // hkv), (h + 1) * (H // hkv))
+            x = torch.einsum("nhd,kd->hnk", s["q"][rows, hs].double(), k) / math.sqrt(128)
+            w = torch.exp(x - s["lse"][rows, hs].double().T[..., None]).masked_fill(late, 0).sum((0, 1))
+            mine = got[at, h].reshape(-1)
+            mine[:p] += w[:p]
+            mine[p:p + a] = w[p:]
+            got[at, h] = mine.view(-1, 64)
+    return got
+
+
+def _exact_evict(s, lens, budgets) -> dict:
+    ws, ks, vs = s["weights"].double(), [], []
+    hkv = s["pool"].shape[1]
+    for b, (n, budget) in enumerate(zip(lens, budgets)):
+        keep = min(n, budget)
+        if keep == 0:
+            continue
+        at = s["table"][b, :(n + 63) // 64].long()
+        k, v = ([_exact_page(s["pool"][at, h], part).reshape(-1, 128) for h in range(hkv)] for part in (0, 1))
+        if keep < n:
+            recent = min(s["recent"], keep)
+            first = min(s["first"], keep - recent, n - recent)
+            heavy = keep - recent - first
+            for h in range(hkv):
+                w = ws[at, h].reshape(-1)
+                middle = w[first:n - recent].clamp(min=0)
+                best = torch.sort(middle, descending=True, stable=True).indices[:heavy] + first
+                stay = torch.cat([torch.arange(first, device="cuda"), best.sort().values,
+                                  torch.arange(n - recent, n, device="cuda")])
+                moved = w.clone()
+                moved[:keep] = w[stay]
+                ws[at, h] = moved.view(-1, 64)
+                for x in (k, v):
+                    rows = torch.zeros(((keep + 31) // 32 * 32, 128), dtype=torch.float64, device="cuda")
+                    rows[:keep] = x[h][stay]
+                    rows = rows.view(-1, 32, 128)
+                    x[h] = _exact_round(rows, _exact_exponent(rows.abs().amax((1, 2), keepdim=True))).view(-1, 128)
+        ks.append(torch.stack([x[:keep] for x in k], 1))
+        vs.append(torch.stack([x[:keep] for x in v], 1))
+    none = torch.zeros((0, hkv, 128), dtype=torch.float64, device="cuda")
+    add = torch.tensor([min(k - n, 0) for n, k in zip(lens, budgets)], dtype=torch.int32, device="cuda")
+    return dict(add=add, weights=ws, k=torch.cat([none, *ks]), v=torch.cat([none, *vs]))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "norm":
+        return _exact_norm(s)
+    if case["kind"] == "write":
+        return _exact_write(s)
+    lens = _lengths(case)
+    if case["kind"] == "weights":
+        return _exact_weights(s, lens, _adds(case, lens))
+    if case["kind"] == "evict":
+        return _exact_evict(s, lens, _budgets(case, lens))
+    return _exact_attention(s, lens)
