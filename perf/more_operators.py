@@ -519,18 +519,18 @@ def run(s):
             return list(fc.fc_norm_rotate(s["q"], s["k"], *s["weights"], pos=s["pos"], eps=EPS, rope_base=ROPE_BASE,
                                           out=s["out"]))
         if s["kind"] == "write":
-            fc.fc_paged8_write(s["pool"], s["k"], s["v"], s["slot"], src=s["src"])
-            return list(fc.fc_paged8_read(s["pool"], s["slot"], out=s["out"]))
+            fc.fc_paged_byte_write(s["pool"], s["k"], s["v"], s["slot"], src=s["src"])
+            return list(fc.fc_paged_byte_read(s["pool"], s["slot"], out=s["out"]))
         if s["kind"] == "weights":
-            fc.fc_paged8_weights(s["weights"], s["q"], s["lse"], s["pool"], s["table"], s["length"], s["new_length"],
+            fc.fc_paged_byte_weights(s["weights"], s["q"], s["lse"], s["pool"], s["table"], s["length"], s["new_length"],
                                  s["cu"], src=s["src"], max_len=s["max_len"])
             return s["weights"]
         if s["kind"] == "evict":
-            add = fc.fc_paged8_evict(s["pool"], s["weights"], s["table"], s["length"], s["budget"], first=s["first"],
+            add = fc.fc_paged_byte_evict(s["pool"], s["weights"], s["table"], s["length"], s["budget"], first=s["first"],
                                      recent=s["recent"], max_len=s["max_len"])
-            k, v = fc.fc_paged8_read(s["pool"], s["slot"], out=s["out"])
+            k, v = fc.fc_paged_byte_read(s["pool"], s["slot"], out=s["out"])
             return dict(add=add, weights=s["weights"], k=k, v=v)
-        fc.fc_paged8_attention(s["q"], s["k"], s["v"], s["pool"], s["table"], s["prefix_len"], tree=s["tree"],
+        fc.fc_paged_byte_attention(s["q"], s["k"], s["v"], s["pool"], s["table"], s["prefix_len"], tree=s["tree"],
                                max_len=s["max_len"], out=s["out"], lse=s["lse"])
         return dict(out=s["out"], lse=s["lse"])
     return dict(norm=_norm, write=_write, weights=_weights, evict=_evict, attention=_attention)[s["kind"]](s)
