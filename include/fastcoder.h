@@ -651,6 +651,161 @@ fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, const uint16_t
                              uint16_t* out, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* 8-bit paged cache                                                         */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Queries and keys normed for each head and rotated by their positions in one
+ * pass: what a cache is written from and attended with where a token's place in
+ * it is not its position (fc_paged_byte_evict), and with rope_base 0 for the 4-bit
+ * cache too.  Per head of D values y = x / sqrt(mean(x^2) + eps) * w, then the
+ * pair (d, d + D/2) turns by pos[i] * rope_base^(-2d/D).  fp32 throughout, angles
+ * reduced in double precision, one rounding to bf16.
+ *
+ * q [n][H][D], k [n][Hkv][D] bf16, rows q_stride and k_stride elements apart
+ * (multiples of 8, at least the row's length; slices of a fused projection need
+ * no copy), 16-byte aligned; H or Hkv may be 0 (that tensor and its result are not
+ * read).  q_weight, k_weight [D] bf16, 16-byte aligned, or NULL: that tensor is not
+ * normed.  rope_base 0: not rotated, pos is not read.  q_out and k_out, at their
+ * own strides, may be q and k themselves (same strides); otherwise a result shares
+ * no bytes with anything that is read (FC_ERR_INVALID).  0 <= H, Hkv <= 8192; eps
+ * is not negative; D must be FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
+ */
+fc_status fc_norm_rotate(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                         const uint16_t* q_weight, const uint16_t* k_weight, const int32_t* pos, int32_t n, int32_t H,
+                         int32_t Hkv, int32_t D, float eps, float rope_base, uint16_t* q_out, int64_t q_out_stride,
+                         uint16_t* k_out, int64_t k_out_stride, hipStream_t stream);
+
+/*
+ * The paged cache in 8 bits, for the same tables, slots and plans (fc_paged_plan):
+ * pool [n_pages][Hkv][FC_PAGE8_HEAD_BYTES] bytes (one per layer), 16-byte aligned.
+ * The bytes of a (page, key head) are 64 x 128 key codes, token by token; four times
+ * 128 x 16 value codes, for each 16 tokens dim by dim; the scale bytes of the keys'
+ * two blocks of FC_PAGE8_BLOCK tokens, then of the values' two; 124 bytes that are
+ * not used.  A code is a sign, four bits of exponent (bias 7) and three of mantissa,
+ * 127 and 255 being NaN: magnitudes up to 448, 2^-9 the least.  A block's scale is
+ * 2^(byte - 127), the smallest power of two in [2^-117, 2^119] of which no finite
+ * magnitude exceeds 448.  Codes are the nearest ones, ties to the even code; larger
+ * magnitudes saturate; what is not finite is held as a NaN, which concerns no other
+ * value.  Keys are held as given: rotated, if the model rotates them.
+ *
+ * A block lives from the call that writes its first row: such a call gives it the
+ * scale of the rows that it writes there, and the others read as zeros.  A call that
+ * writes other rows raises the scale where they need it, and then rounds the codes
+ * that were there to the new one (exactly, unless they become less than 2^-6 of it).
+ */
+#define FC_PAGE8_BLOCK 32
+#define FC_PAGE8_HEAD_BYTES 16512
+
+/* Bytes of one layer's pool (0 for sizes out of range). */
+size_t fc_paged_byte_pool_bytes(int32_t n_pages, int32_t Hkv);
+
+/*
+ * Rounds rows of keys and values to 8 bits and places them: row src[i] of k and v
+ * (row i without src) goes to slot[i].  k, v: as for fc_paged_write.  Entries whose
+ * slots lie in one block have to follow one another (as fc_paged_plan gives them),
+ * and slots have to differ: what the blocks hold is left open otherwise.  An entry
+ * with a slot outside the pool or a row outside [0, n_src) is skipped.  D must be
+ * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise); Hkv <= 1024.  The pool
+ * shares no bytes with the other arguments (FC_ERR_INVALID).
+ */
+fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k, int64_t k_stride,
+                          const uint16_t* v, int64_t v_stride, int32_t n_src, const int32_t* slot, const int32_t* src,
+                          int32_t n, hipStream_t stream);
+
+/*
+ * Rows of the pool as bf16 (exact: every held value is one): as fc_paged_read.
+ */
+fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot, int32_t n,
+                         uint16_t* k, uint16_t* v, hipStream_t stream);
+
+/*
+ * fc_paged_attention over the 8-bit cache, with queries and keys that are rotated
+ * already (so without positions): row i of tree b attends to the prefix_len[b] cached
+ * tokens of its table row and to the tree rows j < num_nodes[b] with mask[b][i][j] =
+ * 1.  Arguments, limits, clamping and the handling of absent pages, empty rows and
+ * shared bytes (out may be q) are those of fc_paged_attention.  lse [B][R][H] fp32, if
+ * not NULL, receives the natural logarithm of each row's sum of exp(score), -infinity
+ * for a row that attends to nothing or lies at or past num_nodes[b].
+ *
+ * Queries, keys and values enter their products exactly; softmax weights are rounded
+ * to bf16, sums are fp32.  What is not finite among the keys and values that a row
+ * attends to, or in its query, shows in its result; absent, masked and later tokens do
+ * not count, whatever they hold.  Values of a magnitude of 2^78 or more may overflow
+ * the sums.
+ *
+ * ws holds fc_paged_byte_attention_workspace_bytes(...) bytes, 16-byte aligned (may be NULL
+ * where that is 0); its contents on entry do not matter.  How a prefix is cut into
+ * parts depends on the sizes and its own length; the same call gives the same bits
+ * every time, and a row's do not depend on the other rows.
+ */
+size_t fc_paged_byte_attention_workspace_bytes(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len);
+fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,
+                              const uint16_t* v_tree, int64_t v_stride, const uint8_t* pool, int32_t n_pages,
+                              const int32_t* table, int32_t max_pages, const int32_t* prefix_len,
+                              const int32_t* num_nodes, const int32_t* mask, int32_t B, int32_t R, int32_t H,
+                              int32_t Hkv, int32_t D, int32_t max_len, uint16_t* out, float* lse, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The attention that a step's rows pay to the cached tokens, counted for each key
+ * head: weights [n_pages][Hkv][FC_PAGE_TOKENS] fp32 lie as the pool's tokens do.  To
+ * be called once the step's accepted rows are in the cache (after fc_paged_byte_write).
+ *
+ * Sequence b had len[b] cached tokens and has new_len[b]; the new ones are its rows
+ * t = 0 .. new_len[b] - len[b] - 1: row number src[cu[b] + t] of q (cu[b] + t without
+ * src) - len, new_len, cu and src as fc_paged_plan takes and gives them, src with n
+ * entries.  Row t sees the tokens up to len[b] + t and pays token j the weight
+ * exp(q . key_j / sqrt(D) - lse), for each of its heads; lse [n_rows][H] fp32 as
+ * fc_paged_byte_attention gives it for the row (-infinity: the row pays nothing).  A token
+ * below len[b] gets what the rows pay added to its weight; a new one's weight becomes
+ * what they pay.  Weights of other tokens, and of sequences without new ones, are
+ * left as they were.
+ *
+ * q [n_rows][H][D] bf16, rows q_stride elements apart (a multiple of 8), 16-byte
+ * aligned.  len and new_len are clamped to [0, max_len]; rows whose number lies
+ * outside [0, n_rows), or whose place outside [0, n), pay nothing.  Table entries
+ * outside the pool count as absent keys.  The pages of a call's sequences have to
+ * differ.  Sums are fp32, in an order that depends on the sizes alone.  weights shares
+ * no bytes with the other arguments (FC_ERR_INVALID).  B <= 65536, Hkv <= 1024, H <=
+ * 8192, H % Hkv == 0, D = FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
+ */
+fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, int64_t q_stride, const float* lse, int32_t n_rows,
+                            const uint8_t* pool, int32_t n_pages, const int32_t* table, int32_t max_pages,
+                            const int32_t* len, const int32_t* new_len, const int32_t* cu, const int32_t* src, int32_t n,
+                            int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_len, hipStream_t stream);
+
+/*
+ * Cuts sequences to budget[b] tokens: those that got least attention leave the cache,
+ * each key head its own ones.  Of a sequence with more tokens than its budget (at
+ * least 0) a head keeps the last `recent` tokens as far as the budget goes, then the
+ * first `first` ones, then the others; of those that the budget takes in part (the
+ * first ones or the others) the heaviest, and of equal ones the earlier.  A weight
+ * that is not above 0 (a NaN, too) counts as 0.  The tokens that
+ * stay keep their order and move to places 0 .. budget[b] - 1 of the sequence's
+ * table row, with their weights.  Their blocks are rounded anew, each as rows written
+ * to a new block are: its scale may fall, and values that were held stay exact unless
+ * they become less than 2^-6 of it.  The rest of the last block reads as zeros.
+ *
+ * add [B] receives min(budget[b] - len[b], 0): as fc_paged_plan's add, with the same
+ * len, it gives the pages back that are no longer needed.  Every layer's pool is cut
+ * by a call with its own weights.  len is clamped to [0, max_len].  Weights and pages
+ * past the budget are left as they were.  Tokens of table entries outside the pool
+ * have weight 0 and read as zeros, and nothing is written there.  The pages of a
+ * call's sequences have to differ.
+ *
+ * ws holds fc_paged_byte_evict_workspace_bytes(...) bytes, 16-byte aligned; its contents
+ * on entry do not matter.  pool, weights, add and ws share no bytes with each other
+ * or with the other arguments (FC_ERR_INVALID).  B <= 65536, Hkv <= 1024, first and
+ * recent are not negative, max_len <= 64 max_pages, D = FC_TREE_ATTN_HEAD_DIM
+ * (FC_ERR_UNSUPPORTED otherwise).
+ */
+size_t fc_paged_byte_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len);
+fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* table,
+                          int32_t max_pages, const int32_t* len, const int32_t* budget, int32_t B, int32_t max_len,
+                          int32_t first, int32_t recent, int32_t* add, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Decode-trace replay                                                       */
 /* ------------------------------------------------------------------------ */
 

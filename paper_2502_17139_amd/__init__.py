@@ -29,6 +29,8 @@ FC_MAX_CACHE_TOKENS = 16384
 FC_TREE_ATTN_HEAD_DIM = 128
 FC_PAGE_TOKENS = 64
 FC_PAGE_HEAD_BYTES = 8704
+FC_PAGE8_BLOCK = 32
+FC_PAGE8_HEAD_BYTES = 16512
 
 FC_ERR_WORKSPACE = 2
 STATUS = {0: "FC_OK", 1: "FC_ERR_INVALID", 2: "FC_ERR_WORKSPACE", 3: "FC_ERR_DEVICE", 4: "FC_ERR_UNSUPPORTED"}
@@ -45,7 +47,9 @@ EXPORTS = (
     "fc_tree_attention", "fc_tree_attention_workspace_bytes", "fc_tree_attention_ws", "fc_replay_init",
     "fc_replay_run", "fc_retrieve_noalloc_max_bytes", "fc_retrieve_noalloc", "fc_datastore_build_stats",
     "fc_paged_pool_bytes", "fc_paged_plan", "fc_paged_write", "fc_paged_read", "fc_paged_attention_workspace_bytes",
-    "fc_paged_attention",
+    "fc_paged_attention", "fc_norm_rotate", "fc_paged_byte_pool_bytes", "fc_paged_byte_write", "fc_paged_byte_read",
+    "fc_paged_byte_attention_workspace_bytes", "fc_paged_byte_attention", "fc_paged_byte_weights",
+    "fc_paged_byte_evict_workspace_bytes", "fc_paged_byte_evict",
 )
 
 
@@ -192,6 +196,24 @@ def lib() -> ctypes.CDLL:
     L.fc_verify_accept.restype = ctypes.c_int
     L.fc_verify_accept.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     L.fc_replay_init.restype = ctypes.c_int
+    L.fc_norm_rotate.restype = ctypes.c_int
+    L.fc_norm_rotate.argtypes = [vp, i64] * 2 + [vp] * 3 + [i32] * 4 + [f32] * 2 + [vp, i64] * 2 + [vp]
+    L.fc_paged_byte_pool_bytes.restype = sz
+    L.fc_paged_byte_pool_bytes.argtypes = [i32] * 2
+    L.fc_paged_byte_write.restype = ctypes.c_int
+    L.fc_paged_byte_write.argtypes = [vp, i32, i32, i32, vp, i64, vp, i64, i32, vp, vp, i32, vp]
+    L.fc_paged_byte_read.restype = ctypes.c_int
+    L.fc_paged_byte_read.argtypes = [vp, i32, i32, i32, vp, i32, vp, vp, vp]
+    L.fc_paged_byte_attention_workspace_bytes.restype = sz
+    L.fc_paged_byte_attention_workspace_bytes.argtypes = [i32] * 5
+    L.fc_paged_byte_attention.restype = ctypes.c_int
+    L.fc_paged_byte_attention.argtypes = [vp, i64] * 3 + [vp, i32, vp, i32] + [vp] * 3 + [i32] * 6 + [vp] * 3 + [sz, vp]
+    L.fc_paged_byte_weights.restype = ctypes.c_int
+    L.fc_paged_byte_weights.argtypes = [vp, vp, i64, vp, i32, vp, i32, vp, i32] + [vp] * 4 + [i32] * 6 + [vp]
+    L.fc_paged_byte_evict_workspace_bytes.restype = sz
+    L.fc_paged_byte_evict_workspace_bytes.argtypes = [i32] * 3
+    L.fc_paged_byte_evict.restype = ctypes.c_int
+    L.fc_paged_byte_evict.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, vp] + [i32] * 4 + [vp, vp, sz, vp]
     L.fc_replay_init.argtypes = [ctypes.POINTER(FcReplay), vp]
     L.fc_replay_run.restype = ctypes.c_int
     L.fc_replay_run.argtypes = [ctypes.POINTER(FcStore), i32, ctypes.POINTER(FcReplay), i32, i32, vp]
@@ -871,6 +893,236 @@ def fc_paged_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tens
             *(p[4:] or (None, None, None)), B, R, H, Hkv, D, max_len, rope_base, p[3], _ptr(workspace),
             0 if workspace is None else workspace.numel(), on.raw()))
     return out
+
+
+# ----------------------------------------------------- 8-bit paged cache ----
+
+def fc_norm_rotate(q: torch.Tensor | None, k: torch.Tensor | None, q_weight: torch.Tensor | None = None,
+                   k_weight: torch.Tensor | None = None, pos: torch.Tensor | None = None, eps: float = 1e-6,
+                   rope_base: float = 10000.0, out=None, stream=None) -> tuple:
+    """Queries and keys (bf16 [rows][heads][D] or [B][R][heads][D], rows at any
+    even distance) normed for each head with their weights (bf16 [D]; None: not
+    normed) and rotated by their rows' positions (int32; rope_base 0: not
+    rotated) in one pass.  Either may be None.  Returns both, bf16, in out, whose
+    tensors may be q and k themselves."""
+    given = [t for t in (q, k) if t is not None]
+    if not given:
+        raise ValueError("q or k is required")
+    lead = given[0].shape[:-2]
+    n, D = lead.numel(), FC_TREE_ATTN_HEAD_DIM
+    _in_32_bits(rows=n)
+    _expect("pos", pos, torch.int32, optional=rope_base == 0)
+    if pos is not None and pos.numel() != n:
+        raise ValueError(f"pos must hold {n} numbers, not {pos.numel()}")
+    outs = (None, None) if out is None else tuple(out)
+    if len(outs) != 2:
+        raise ValueError("out is a pair: queries and keys")
+    for name, t, o, w in zip("qk", (q, k), outs, (q_weight, k_weight)):
+        if t is None:
+            if o is not None or w is not None:
+                raise ValueError(f"{name} is required with its weight or result")
+            continue
+        if t.shape[:-2] != lead:
+            raise ValueError(f"q and k differ in rows: {tuple(q.shape)} and {tuple(k.shape)}")
+        if o is None and out is not None:
+            raise ValueError(f"out has to hold {name}'s result")
+        _expect(f"{name}'s result", o, torch.bfloat16, t.shape, optional=True)
+        _expect(f"{name}_weight", w, torch.bfloat16, (D,), optional=True)
+    with _Launch(stream, (*given, q_weight, k_weight, pos, *outs)) as on:
+        if out is None:
+            outs = tuple(None if t is None else on.empty(tuple(t.shape), torch.bfloat16) for t in (q, k))
+        at = []
+        for name, t in (("q", q), ("k", k), ("q's result", outs[0]), ("k's result", outs[1])):
+            at += [None, 0] if t is None else [t.data_ptr(), _rows(name, t)]
+        heads = [0 if t is None else t.shape[-2] for t in (q, k)]
+        _check("fc_norm_rotate", lib().fc_norm_rotate(
+            *at[:4], _ptr(q_weight), _ptr(k_weight), _ptr(pos), n, *heads, D, eps, rope_base, *at[4:], on.raw()))
+    return outs
+
+
+def _pool8(pool: torch.Tensor) -> tuple:
+    if pool.dtype != torch.uint8 or pool.dim() != 3 or pool.shape[2] != FC_PAGE8_HEAD_BYTES:
+        raise ValueError(f"pool must be uint8 [n_pages][Hkv][{FC_PAGE8_HEAD_BYTES}]")
+    _in_32_bits(n_pages=pool.shape[0], Hkv=pool.shape[1])
+    return int(pool.shape[0]), int(pool.shape[1])
+
+
+def paged_byte_pool(n_pages: int, Hkv: int, device) -> torch.Tensor:
+    """One layer's pool of 8-bit pages (paged_state keeps its books, too)."""
+    return _empty((n_pages, Hkv, FC_PAGE8_HEAD_BYTES), torch.uint8, device)
+
+
+def paged_token_weights(n_pages: int, Hkv: int, device) -> torch.Tensor:
+    """One layer's weights of cached tokens, as fc_paged_byte_weights counts them."""
+    return torch.zeros((n_pages, Hkv, FC_PAGE_TOKENS), dtype=torch.float32, device=device)
+
+
+def fc_paged_byte_pool_bytes(n_pages: int, Hkv: int) -> int:
+    return int(lib().fc_paged_byte_pool_bytes(n_pages, Hkv))
+
+
+def fc_paged_byte_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor,
+                    src: torch.Tensor | None = None, stream=None) -> None:
+    """Rounds rows of k (rotated already) and v (bf16 [rows][Hkv][D] or
+    [B][R][Hkv][D], rows at any even distance) to 8 bits into the pool: row src[i]
+    (or i) to slot[i].  Slots in one block of 32 tokens follow one another, as
+    fc_paged_plan gives them."""
+    n_pages, Hkv = _pool8(pool)
+    ks, vs = _rows("k", k, Hkv), _rows("v", v, Hkv)
+    if k.shape != v.shape:
+        raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
+    n_src, n = k.shape[:-2].numel(), slot.numel()
+    _in_32_bits(rows=n_src, slots=n)
+    _expect("slot", slot, torch.int32, (n,))
+    _expect("src", src, torch.int32, (n,), optional=True)
+    with _Launch(stream, (pool, k, v, slot, src)) as on:
+        _check("fc_paged_byte_write", lib().fc_paged_byte_write(
+            _ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, k.data_ptr(), ks, v.data_ptr(), vs, n_src, _ptr(slot),
+            _ptr(src), n, on.raw()))
+
+
+def fc_paged_byte_read(pool: torch.Tensor, slot: torch.Tensor, out=None, stream=None) -> tuple:
+    """Keys and values of slots, bf16 [n][Hkv][D] each; rows of slots outside the
+    pool are left as they were."""
+    n_pages, Hkv = _pool8(pool)
+    n = slot.numel()
+    _in_32_bits(slots=n)
+    _expect("slot", slot, torch.int32, (n,))
+    shape = (n, Hkv, FC_TREE_ATTN_HEAD_DIM)
+    if out is not None:
+        for name, t in zip(("k", "v"), out):
+            _expect(name, t, torch.bfloat16, shape)
+    with _Launch(stream, (pool, slot, *(out or ()))) as on:
+        if out is None:
+            out = on.empty(shape, torch.bfloat16), on.empty(shape, torch.bfloat16)
+        k, v = out
+        _check("fc_paged_byte_read", lib().fc_paged_byte_read(_ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, _ptr(slot), n,
+                                                      _ptr(k), _ptr(v), on.raw()))
+    return k, v
+
+
+@functools.lru_cache(maxsize=1024)  # it goes by the sizes alone
+def fc_paged_byte_attention_workspace_bytes(B: int, R: int, H: int, Hkv: int, max_len: int) -> int:
+    return int(lib().fc_paged_byte_attention_workspace_bytes(B, R, H, Hkv, max_len))
+
+
+def fc_paged_byte_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pool: torch.Tensor,
+                        table: torch.Tensor, prefix_len: torch.Tensor, tree: dict | None = None,
+                        max_len: int | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                        stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """fc_paged_attention over the 8-bit cache, with queries and keys that are
+    rotated already (fc_norm_rotate): bf16 q [B][R][H][D], k/v_tree [B][R][Hkv][D]
+    (rows at any even distance); of a tree num_nodes and mask are read.  Returns
+    bf16 [B][R][H][D]; lse, fp32 [B][R][H], receives each row's logarithm of the
+    sum of exp(score) if it is given."""
+    if q.dim() != 4 or table.dim() != 2:
+        raise ValueError("q [B][R][H][D] and table [B][max_pages] expected")
+    n_pages, Hkv = _pool8(pool)
+    B, R, H, D = q.shape
+    qs, ks, vs = _rows("q", q), _rows("k_tree", k_tree, Hkv), _rows("v_tree", v_tree, Hkv)
+    for name, t in (("k_tree", k_tree), ("v_tree", v_tree)):
+        _expect(name, t, torch.bfloat16, (B, R, Hkv, D))
+    max_pages = table.shape[1]
+    _expect("table", table, torch.int32, (B, max_pages))
+    _expect("prefix_len", prefix_len, torch.int32, (B,))
+    nodes = mask = None
+    if tree is not None:
+        nodes, mask = tree["num_nodes"], tree["mask"]
+        _expect("num_nodes", nodes, torch.int32, (B,))
+        _expect("mask", mask, torch.int32, (B, R, R))
+    _expect("out", out, torch.bfloat16, (B, R, H, D), optional=True)
+    _expect("lse", lse, torch.float32, (B, R, H), optional=True)
+    _expect("workspace", workspace, torch.uint8, optional=True)
+    if max_len is None:
+        max_len = max_pages * FC_PAGE_TOKENS
+    _in_32_bits(max_len=max_len, B=B, max_pages=max_pages)
+    need = fc_paged_byte_attention_workspace_bytes(B, R, H, Hkv, max_len)
+    with _Launch(stream, (q, k_tree, v_tree, pool, table, prefix_len, nodes, mask, out, lse, workspace)) as on:
+        if out is None:
+            out = on.empty((B, R, H, D), torch.bfloat16)
+        if workspace is None and need > 0:
+            workspace = on.empty((need,), torch.uint8)
+        p = _ptrs((pool, table, prefix_len, out) if tree is None else (pool, table, prefix_len, out, nodes, mask))
+        _check("fc_paged_byte_attention", lib().fc_paged_byte_attention(
+            q.data_ptr(), qs, k_tree.data_ptr(), ks, v_tree.data_ptr(), vs, p[0], n_pages, p[1], max_pages, p[2],
+            *(p[4:] or (None, None)), B, R, H, Hkv, D, max_len, p[3], _ptr(lse), _ptr(workspace),
+            0 if workspace is None else workspace.numel(), on.raw()))
+    return out
+
+
+def _token_weights(weights: torch.Tensor, n_pages: int, Hkv: int) -> None:
+    _expect("weights", weights, torch.float32, (n_pages, Hkv, FC_PAGE_TOKENS))
+
+
+def fc_paged_byte_weights(weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, pool: torch.Tensor,
+                      table: torch.Tensor, length: torch.Tensor, new_length: torch.Tensor, cu: torch.Tensor,
+                      src: torch.Tensor | None = None, max_len: int | None = None, stream=None) -> None:
+    """The attention that the rows of a step's new tokens pay to every cached
+    token, added to weights (fp32 [n_pages][Hkv][64]; new tokens': set): q (bf16
+    [rows][H][D] or [B][R][H][D]) and lse (fp32, the same but for D) as
+    fc_paged_byte_attention took and gave them, length before the step, new_length, cu
+    and src from its plan (src None: rows follow one another).  After
+    fc_paged_byte_write."""
+    if table.dim() != 2:
+        raise ValueError("table [B][max_pages] expected")
+    n_pages, Hkv = _pool8(pool)
+    _token_weights(weights, n_pages, Hkv)
+    qs = _rows("q", q)
+    H, n_rows = q.shape[-2], q.shape[:-2].numel()
+    _expect("lse", lse, torch.float32, q.shape[:-1])
+    B, max_pages = table.shape
+    i32 = torch.int32
+    for name, t, shape in (("table", table, None), ("length", length, (B,)), ("new_length", new_length, (B,)),
+                           ("cu", cu, (B + 1,))):
+        _expect(name, t, i32, shape)
+    _expect("src", src, i32, optional=True)
+    n = n_rows if src is None else src.numel()
+    if max_len is None:
+        max_len = max_pages * FC_PAGE_TOKENS
+    _in_32_bits(max_len=max_len, B=B, max_pages=max_pages, rows=n_rows, src=n)
+    with _Launch(stream, (weights, q, lse, pool, table, length, new_length, cu, src)) as on:
+        w, lse_at, pool_at, table_at, len_at, new_at, cu_at = _ptrs((weights, lse, pool, table, length, new_length, cu))
+        _check("fc_paged_byte_weights", lib().fc_paged_byte_weights(
+            w, q.data_ptr(), qs, lse_at, n_rows, pool_at, n_pages, table_at, max_pages, len_at, new_at, cu_at, _ptr(src),
+            n, B, H, Hkv, FC_TREE_ATTN_HEAD_DIM, max_len, on.raw()))
+
+
+@functools.lru_cache(maxsize=1024)  # it goes by the sizes alone
+def fc_paged_byte_evict_workspace_bytes(B: int, Hkv: int, max_len: int) -> int:
+    return int(lib().fc_paged_byte_evict_workspace_bytes(B, Hkv, max_len))
+
+
+def fc_paged_byte_evict(pool: torch.Tensor, weights: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                    budget: torch.Tensor, first: int = 0, recent: int = 0, max_len: int | None = None,
+                    add: torch.Tensor | None = None, stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Cuts sequences to budget[b] tokens: each key head keeps the last `recent`,
+    the first `first`, and of the others those of most weight, in their order.
+    Returns add [B], what each sequence loses: with the same length fc_paged_plan
+    gives the pages back.  Scratch memory as in fc_tree_attention."""
+    if table.dim() != 2:
+        raise ValueError("table [B][max_pages] expected")
+    n_pages, Hkv = _pool8(pool)
+    _token_weights(weights, n_pages, Hkv)
+    B, max_pages = table.shape
+    i32 = torch.int32
+    for name, t, shape in (("table", table, None), ("length", length, (B,)), ("budget", budget, (B,))):
+        _expect(name, t, i32, shape)
+    _expect("add", add, i32, (B,), optional=True)
+    _expect("workspace", workspace, torch.uint8, optional=True)
+    if max_len is None:
+        max_len = max_pages * FC_PAGE_TOKENS
+    _in_32_bits(max_len=max_len, B=B, max_pages=max_pages, first=first, recent=recent)
+    need = fc_paged_byte_evict_workspace_bytes(B, Hkv, max_len)
+    with _Launch(stream, (pool, weights, table, length, budget, add, workspace)) as on:
+        if add is None:
+            add = on.empty((B,), i32)
+        if workspace is None and need > 0:
+            workspace = on.empty((need,), torch.uint8)
+        p = _ptrs((pool, weights, table, length, budget, add))
+        _check("fc_paged_byte_evict", lib().fc_paged_byte_evict(
+            p[0], p[1], n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, p[2], max_pages, p[3], p[4], B, max_len, first, recent, p[5],
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), on.raw()))
+    return add
 
 
 # ----------------------------------------------------------------- tree ----

@@ -1,0 +1,178 @@
+// Queries and keys normed for each head and rotated by their positions in one pass
+// (fc_norm_rotate).
+//
+// y = x / sqrt(mean(x^2) + eps) * w over a head's 128 dims, then the pair (d, d + 64)
+// turns by position * base^(-2d/128).  All of it in fp32 (angles reduced in double
+// precision), one rounding to bf16 at the end.  Bound by memory: 512 bytes a head.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fastcoder.h"
+#include "fc_device.h"
+#include "fc_host.h"
+
+namespace {
+
+constexpr int kDim = FC_TREE_ATTN_HEAD_DIM;
+constexpr int kThreads = 256;
+constexpr int kUnitLanes = 8;                     // lanes of one head: dims 8 j .. 8 j + 7 and the same 64 further on
+constexpr int kUnits = kThreads / kUnitLanes;     // heads at work in a workgroup
+constexpr int kMostTokens = 4;                    // of a workgroup: a wave of angles each
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+struct Args {
+  const uint16_t* x[2];     // queries, keys
+  const uint16_t* w[2];     // their weights, or none
+  uint16_t* y[2];
+  int64_t x_stride[2], y_stride[2];
+  const int32_t* pos;
+  int64_t n;
+  int H, Hkv, tokens;
+  float eps;
+  double log2_base;  // 0: no rotation
+};
+
+// A workgroup takes `tokens` tokens, and blockIdx.y's share of their heads.
+__global__ void __launch_bounds__(kThreads) k_norm_rotate(Args A) {
+  __shared__ float2 s_turn[kMostTokens * kDim / 2];
+  const int tid = (int)threadIdx.x, j = tid % kUnitLanes;
+  const int64_t i0 = (int64_t)blockIdx.x * A.tokens;
+  const int heads = A.H + A.Hkv;
+  const int here = A.n - i0 < A.tokens ? (int)(A.n - i0) : A.tokens;
+  if (A.log2_base > 0.0) {
+    // a wave's lanes are a token's angles: sine and cosine of a fraction of a turn
+    const int d = tid % fc::kWave;
+    for (int t = tid / fc::kWave; t < here; t += kThreads / fc::kWave) {
+      const double f = exp2(-2.0 * d / (double)kDim * A.log2_base) * 0.15915494309189533577;
+      const float part = (float)__builtin_amdgcn_fract((double)A.pos[i0 + t] * f);
+      s_turn[t * (kDim / 2) + d] = make_float2(__builtin_amdgcn_sinf(part), __builtin_amdgcn_cosf(part));
+    }
+    __syncthreads();
+  }
+  const int units = here * heads;
+  for (int u = (int)blockIdx.y * kUnits + tid / kUnitLanes; u < units; u += (int)gridDim.y * kUnits) {
+    const int t = u / heads, h2 = u - t * heads;
+    const int is_k = h2 >= A.H;
+    const int h = is_k ? h2 - A.H : h2;
+    const uint16_t* p = A.x[is_k] + (i0 + t) * A.x_stride[is_k] + h * kDim + 8 * j;
+    const uint4 lo = *(const uint4*)p, hi = *(const uint4*)(p + kDim / 2);
+    float a[8], b[8];
+    fc::unpack8(lo, a);
+    fc::unpack8(hi, b);
+    const uint16_t* wp = A.w[is_k];
+    if (wp) {
+      const uint4 w_lo = *(const uint4*)(wp + 8 * j), w_hi = *(const uint4*)(wp + kDim / 2 + 8 * j);
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += a[e] * a[e] + b[e] * b[e];
+      sum += __shfl_xor(sum, 1);
+      sum += __shfl_xor(sum, 2);
+      sum += __shfl_xor(sum, 4);
+      const float r = 1.0f / sqrtf(sum * (1.0f / kDim) + A.eps);
+      float wa[8], wb[8];
+      fc::unpack8(w_lo, wa);
+      fc::unpack8(w_hi, wb);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[e] = a[e] * r * wa[e], b[e] = b[e] * r * wb[e];
+    }
+    if (A.log2_base > 0.0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 s = s_turn[t * (kDim / 2) + 8 * j + e];
+        const float x0 = a[e], x1 = b[e];
+        a[e] = x0 * s.y - x1 * s.x;
+        b[e] = x1 * s.y + x0 * s.x;
+      }
+    }
+    bf16x8 ya, yb;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ya[e] = (__bf16)a[e], yb[e] = (__bf16)b[e];
+    uint16_t* to = A.y[is_k] + (i0 + t) * A.y_stride[is_k] + h * kDim + 8 * j;
+    *(bf16x8*)to = ya;
+    *(bf16x8*)(to + kDim / 2) = yb;
+  }
+}
+
+// Rows of two tensors: n of len elements each, at their strides.
+struct Rows {
+  const uint16_t* p;
+  int64_t stride, len;
+};
+// Whether rows share no bytes: their spans are apart, or they lie beside each other
+// at the same distance, as slices of one projection do.
+bool rows_apart(const Rows& a, const Rows& b, int64_t n) {
+  if (!a.p || !b.p || n <= 0) return true;
+  if (fc::apart({fc::rows_span(a.p, n, a.stride, a.len)}, {fc::rows_span(b.p, n, b.stride, b.len)})) return true;
+  if (a.stride != b.stride) return false;
+  const int64_t bytes = 2 * a.stride, off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+  const int64_t m = ((off % bytes) + bytes) % bytes;
+  return m >= 2 * a.len && m + 2 * b.len <= bytes;
+}
+
+}  // namespace
+
+extern "C" fc_status fc_norm_rotate(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                                    const uint16_t* q_weight, const uint16_t* k_weight, const int32_t* pos, int32_t n,
+                                    int32_t H, int32_t Hkv, int32_t D, float eps, float rope_base, uint16_t* q_out,
+                                    int64_t q_out_stride, uint16_t* k_out, int64_t k_out_stride, hipStream_t stream) {
+  if (n < 0 || H < 0 || H > 8192 || Hkv < 0 || Hkv > 8192) return FC_ERR_INVALID;
+  if (!(rope_base == 0.0f || (rope_base > 1.0f && rope_base < __builtin_inff()))) return FC_ERR_INVALID;
+  if (!(eps >= 0.0f && eps < __builtin_inff())) return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  const Rows in[2] = {{q, q_stride, (int64_t)H * D}, {k, k_stride, (int64_t)Hkv * D}};
+  const Rows out[2] = {{q_out, q_out_stride, in[0].len}, {k_out, k_out_stride, in[1].len}};
+  const uint16_t* w[2] = {q_weight, k_weight};
+  for (int i = 0; i < 2; ++i) {
+    if (in[i].len == 0) continue;
+    if (in[i].stride < in[i].len || out[i].stride < in[i].len || ((in[i].stride | out[i].stride) & 7))
+      return FC_ERR_INVALID;
+  }
+  if (n == 0 || H + Hkv == 0) return FC_OK;
+  if (rope_base != 0.0f && !pos) return FC_ERR_INVALID;
+  for (int i = 0; i < 2; ++i) {
+    if (in[i].len == 0) continue;
+    if (!in[i].p || !out[i].p) return FC_ERR_INVALID;
+    if (((uintptr_t)in[i].p | (uintptr_t)out[i].p | (uintptr_t)w[i]) & 15) return FC_ERR_INVALID;
+  }
+  // A head is read before it is written, by the same lanes, so a result may take the
+  // place of its own rows; of nothing else.
+  for (int i = 0; i < 2; ++i) {
+    if (out[i].len == 0) continue;
+    for (int o = 0; o < 2; ++o) {
+      if (in[o].len == 0) continue;
+      const bool in_place = o == i && out[i].p == in[i].p && out[i].stride == in[i].stride;
+      if (!in_place && !rows_apart(out[i], in[o], n)) return FC_ERR_INVALID;
+    }
+    if (i == 1 && out[0].len && !rows_apart(out[0], out[1], n)) return FC_ERR_INVALID;
+    const fc::Span rows = fc::rows_span(out[i].p, n, out[i].stride, out[i].len);
+    if (!fc::apart({rows}, {{H ? q_weight : nullptr, 2 * (uint64_t)D},
+                            {Hkv ? k_weight : nullptr, 2 * (uint64_t)D},
+                            {rope_base != 0.0f ? pos : nullptr, 4 * (uint64_t)n}}))
+      return FC_ERR_INVALID;
+  }
+  // Long calls take four tokens a workgroup, which share their start; short ones a
+  // token, its heads spread over workgroups.
+  Args a = {{q, k}, {q_weight, k_weight}, {q_out, k_out}, {q_stride, k_stride}, {q_out_stride, k_out_stride}, pos, n, H,
+            Hkv, 1, eps, rope_base != 0.0f ? log2((double)rope_base) : 0.0};
+  a.tokens = n >= 4096 ? kMostTokens : 1;
+  const uint32_t y = n >= 1024 ? 1u : fc::div_up((uint64_t)(H + Hkv), kUnits);
+  (void)hipGetLastError();
+  // a launch takes fewer than 2^32 threads in a dimension
+  constexpr int64_t kMost = (int64_t)1 << 22;
+  for (int64_t i = 0; i < n; i += kMost) {
+    Args now = a;
+    now.n = n - i < kMost ? n - i : kMost;
+    now.pos = pos ? pos + i : nullptr;
+    for (int s = 0; s < 2; ++s) {
+      if (in[s].len == 0) continue;
+      now.x[s] = in[s].p + i * in[s].stride;
+      now.y[s] = a.y[s] + i * out[s].stride;
+    }
+    hipLaunchKernelGGL(k_norm_rotate, dim3(fc::div_up((uint64_t)now.n, (uint64_t)a.tokens), y), dim3(kThreads), 0, stream,
+                       now);
+    FC_CHECK_LAUNCH();
+  }
+  return FC_OK;
+}

@@ -1,0 +1,361 @@
+// The 8-bit paged cache on gfx950: rows into pages (fc_paged_byte_write) and out of
+// them (fc_paged_byte_read).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fastcoder.h"
+#include "fc_device.h"
+#include "fc_host.h"
+#include "fc_page8.h"
+
+namespace {
+
+using fc::kBlock8;
+using fc::kDim8;
+using fc::kPage8;
+using fc::kPage8Bytes;
+using fc::kQuarter8;
+
+// ------------------------------------------------------------------ write --
+
+constexpr int kWriteThreads = 256;
+constexpr int kWriteWaves = kWriteThreads / fc::kWave;
+constexpr int kMostWindow = 32;  // entries whose runs a workgroup looks after
+
+struct Write {
+  uint8_t* pool;
+  const uint16_t* x[2];  // keys, values
+  int64_t stride[2];
+  const int32_t *slot, *src;
+  int64_t first, n;      // entries [0, n) exist; this launch's begin at `first`
+  int64_t n_src;
+  int n_pages, Hkv, window;
+};
+
+// Magnitudes of a wave's rows, joined: all lanes get the largest.
+__device__ __forceinline__ uint32_t wave_top(uint32_t m) {
+#pragma unroll
+  for (int o = 1; o < fc::kWave; o <<= 1) {
+    const uint32_t x = (uint32_t)__shfl_xor((int)m, o);
+    m = x > m ? x : m;
+  }
+  return m;
+}
+
+// What a block's scale becomes, and what its other rows' codes are multiplied by.
+struct Scaled {
+  int e;
+  float inv;      // 2^-e
+  float again;    // 2^(e_old - e)
+  bool recode;    // the scale rose: codes that were there are rounded anew
+};
+__device__ __forceinline__ Scaled rescale(uint32_t top, uint32_t byte, bool fresh) {
+  Scaled s;
+  s.e = fc::exponent8(top);
+  const int was = fc::clamp_exp8((int)byte - 127);
+  if (!fresh && was > s.e) s.e = was;
+  s.recode = !fresh && s.e > was;
+  s.inv = fc::power8(-s.e);
+  s.again = was - s.e < -126 ? 0.0f : fc::power8(was - s.e);
+  return s;
+}
+
+// The entries of one block, which follow one another, are a run; a wave takes a run's
+// keys or values of one head, so that a block has one writer.  It reads the rows, has
+// their largest magnitude by exchange within the wave, and writes codes: key rows as
+// they are, values dim by dim.  A block that the run begins (its first row is among
+// the run's) is written whole, with zeros in the rows that are not there yet; in
+// others the key rows alone and all of the values, whose 16-byte pieces hold other
+// tokens too, unless the scale rises and all codes are rounded anew.
+__global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
+  const int lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
+  const int64_t i0 = A.first + (int64_t)blockIdx.x * A.window;
+  const int blocks = A.n_pages * (kPage8 / kBlock8);
+  const auto block_at = [&](int64_t i) {  // of entry i; -1: none
+    const int b = A.slot[i] >> 5;
+    return b >= 0 && b < blocks ? b : -1;
+  };
+  const int64_t mine = i0 + lane;
+  const bool in = lane < A.window && mine < A.n;
+  const int b_mine = in ? block_at(mine) : -1;
+  const int b_before = in && mine > 0 ? block_at(mine - 1) : -1;
+  const uint64_t leads = fc::ballot(b_mine >= 0 && b_mine != b_before);
+  const int each = 2 * A.Hkv, tasks = (int)__popcll(leads) * each;
+  for (int task = (int)blockIdx.y * kWriteWaves + w; task < tasks; task += (int)gridDim.y * kWriteWaves) {
+    uint64_t left = leads;
+    for (int skip = task / each; skip > 0; --skip) left &= left - 1;
+    const int64_t i = i0 + __builtin_ctzll(left);
+    const int part = task % each, is_v = part >= A.Hkv, h = is_v ? part - A.Hkv : part;
+    // the run: up to 32 entries, a lane each
+    const bool could = lane < kBlock8 && i + lane < A.n;
+    const int slot = could ? A.slot[i + lane] : -1;
+    const int64_t row = could ? (A.src ? (int64_t)A.src[i + lane] : i + lane) : -1;
+    const int block = __builtin_amdgcn_readfirstlane(slot) >> 5;
+    const uint64_t others = fc::ballot(lane >= kBlock8 || !could || (slot >> 5) != block);
+    const int run = others ? (int)__builtin_ctzll(others) : kBlock8;
+    const bool there = lane < run && row >= 0 && row < A.n_src;
+    const int t = slot & (kBlock8 - 1);
+    uint32_t have = 0;  // rows of the block that are written
+    {
+      uint32_t bit = there ? 1u << t : 0u;
+#pragma unroll
+      for (int o = 1; o < kBlock8; o <<= 1) bit |= (uint32_t)__shfl_xor((int)bit, o);
+      have = (uint32_t)__builtin_amdgcn_readfirstlane((int)bit);
+    }
+    if (!have) continue;
+    const bool fresh = have & 1u;
+    // where each row of the block comes from: lane t has row t's
+    int from = -1;
+    for (int e = 0; e < run; ++e) {
+      const int te = __builtin_amdgcn_readlane(t, e), re = __builtin_amdgcn_readlane(there ? (int)row : -1, e);
+      if (lane == te && re >= 0) from = re;
+    }
+    uint8_t* page = A.pool + ((int64_t)(block >> 1) * A.Hkv + h) * kPage8Bytes;
+    const int half = block & 1;
+    uint8_t* scale = page + fc::kPage8Scales + 2 * is_v + half;
+    const uint32_t byte = *scale;
+    const uint16_t* x = A.x[is_v] + h * kDim8;
+    const int64_t stride = A.stride[is_v];
+    if (!is_v) {
+      // eight lanes a row, 16 dims each; eight rows at a time
+      const int c = lane & 7;
+      uint4 raw[4][2];
+      bool live[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int r = __shfl(from, 8 * p + (lane >> 3));
+        live[p] = r >= 0;
+        raw[p][0] = raw[p][1] = make_uint4(0u, 0u, 0u, 0u);
+        if (live[p]) {
+          const uint4* at = (const uint4*)(x + (int64_t)r * stride + 16 * c);
+          raw[p][0] = at[0];
+          raw[p][1] = at[1];
+        }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float v[8];
+          fc::unpack8(raw[p][u], v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t m = fc::reach8(v[e]);
+            top = m > top ? m : top;
+          }
+        }
+      const Scaled s = rescale(wave_top(top), byte, fresh);
+      uint8_t* to = page + half * (kBlock8 * kDim8) + (lane >> 3) * kDim8 + 16 * c;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        uint4* at = (uint4*)(to + p * 8 * kDim8);
+        if (live[p]) {
+          uint32_t o[4];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            float v[8];
+            fc::unpack8(raw[p][u], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fc::to_code8(v[e], s.inv);
+            o[2 * u] = fc::codes8(v[0], v[1], v[2], v[3]);
+            o[2 * u + 1] = fc::codes8(v[4], v[5], v[6], v[7]);
+          }
+          *at = make_uint4(o[0], o[1], o[2], o[3]);
+        } else if (fresh) {
+          *at = make_uint4(0u, 0u, 0u, 0u);
+        } else if (s.recode) {
+          const uint4 old = *at;
+          *at = make_uint4(fc::recode8(old.x, s.again), fc::recode8(old.y, s.again), fc::recode8(old.z, s.again),
+                           fc::recode8(old.w, s.again));
+        }
+      }
+      if (lane == 0) *scale = (uint8_t)(s.e + 127);
+    } else {
+      // two dims a lane, every row of the block; rows that the run does not have read
+      // one that it has, for nothing
+      const int any = __builtin_amdgcn_readlane(from, __builtin_ctz(have));
+      const uint32_t* at = (const uint32_t*)x + lane;
+      uint32_t raw[kBlock8];
+#pragma unroll
+      for (int r = 0; r < kBlock8; ++r) {
+        const int f = __builtin_amdgcn_readlane(from, r);
+        raw[r] = *(const uint32_t*)((const uint16_t*)at + (int64_t)(f >= 0 ? f : any) * stride);
+      }
+      uint8_t* to = page + fc::kPage8V + half * (kBlock8 * kDim8) + lane * 2 * kQuarter8;
+      uint4 old[2][2];
+      const bool merge = !fresh && have != 0xFFFFFFFFu;
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          old[q][d] = make_uint4(0u, 0u, 0u, 0u);
+          if (merge) old[q][d] = *(const uint4*)(to + q * (kQuarter8 * kDim8) + d * kQuarter8);
+        }
+      uint32_t top = 0;
+#pragma unroll
+      for (int r = 0; r < kBlock8; ++r) {
+        const uint32_t a = fc::reach8(__uint_as_float(raw[r] << 16)), b = fc::reach8(__uint_as_float(raw[r] & 0xFFFF0000u));
+        top = a > top ? a : top;
+        top = b > top ? b : top;
+      }
+      const Scaled s = rescale(wave_top(top), byte, fresh);
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          uint32_t o[4];
+          const uint32_t was[4] = {old[q][d].x, old[q][d].y, old[q][d].z, old[q][d].w};
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t bits = raw[16 * q + 4 * i4 + e];
+              v[e] = fc::to_code8(__uint_as_float(d ? bits & 0xFFFF0000u : bits << 16), s.inv);
+            }
+            const uint32_t nibble = (have >> (16 * q + 4 * i4)) & 15u;
+            const uint32_t keep = ((nibble & 1u) | (nibble & 2u) << 7 | (nibble & 4u) << 14 | (nibble & 8u) << 21) * 255u;
+            uint32_t rest = was[i4];
+            if (s.recode) rest = fc::recode8(rest, s.again);
+            o[i4] = (fc::codes8(v[0], v[1], v[2], v[3]) & keep) | (rest & ~keep);
+          }
+          *(uint4*)(to + q * (kQuarter8 * kDim8) + d * kQuarter8) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+      if (lane == 0) *scale = (uint8_t)(s.e + 127);
+    }
+  }
+}
+
+// ------------------------------------------------------------------- read --
+
+constexpr int kReadThreads = 256;
+constexpr int kReadWaves = kReadThreads / fc::kWave;
+constexpr int kReadRows = 16;  // entries of a workgroup
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pair8(uint32_t w, float s, bool high) {
+  const bf16x2 r = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// A wave takes 16 entries through every fourth head.  Keys: 16 lanes a row, eight dims
+// each.  Values: two dims a lane, 16 tokens of them in two loads; entries of one such
+// quarter that follow one another, as the tokens of a sequence do, share the loads.
+__global__ void __launch_bounds__(kReadThreads) k_paged8_read(const uint8_t* __restrict__ pool, int n_pages, int Hkv,
+                                                              const int32_t* __restrict__ slot, int64_t first, int64_t n,
+                                                              uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
+  const int lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
+  const int64_t i0 = first + (int64_t)blockIdx.x * kReadRows;
+  int sl = lane < kReadRows && i0 + lane < n ? slot[i0 + lane] : -1;
+  if (sl >= n_pages * kPage8) sl = -1;
+  for (int h = (int)blockIdx.y * kReadWaves + w; h < Hkv; h += (int)gridDim.y * kReadWaves) {
+    const int c = lane & 15;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int e = 4 * p + (lane >> 4), s = __shfl(sl, e);
+      if (s < 0) continue;
+      const int t = s % kPage8;
+      const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
+      const uint2 x = *(const uint2*)(page + fc::k8_at(t, 8 * c));
+      const float f = fc::scale8(page[fc::kPage8Scales + t / kBlock8]);
+      *(uint4*)(k + ((i0 + e) * Hkv + h) * kDim8 + 8 * c) =
+          make_uint4(pair8(x.x, f, false), pair8(x.x, f, true), pair8(x.y, f, false), pair8(x.y, f, true));
+    }
+    int at = -1;  // the quarter in registers
+    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+    float f = 0.0f;
+    for (int e = 0; e < kReadRows; ++e) {
+      const int s = __builtin_amdgcn_readlane(sl, e);
+      if (s < 0) continue;
+      const int t = s % kPage8;
+      if (s / kQuarter8 != at) {
+        at = s / kQuarter8;
+        const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
+        const uint4* from = (const uint4*)(page + fc::v8_at(t & ~(kQuarter8 - 1), 2 * lane));
+        a = from[0];
+        b = from[1];
+        f = fc::scale8(page[fc::kPage8Scales + 2 + t / kBlock8]);
+      }
+      const int u = t % kQuarter8;
+      const uint32_t wa = u < 8 ? (u < 4 ? a.x : a.y) : (u < 12 ? a.z : a.w);
+      const uint32_t wb = u < 8 ? (u < 4 ? b.x : b.y) : (u < 12 ? b.z : b.w);
+      const uint32_t both = ((wa >> (8 * (u & 3))) & 255u) | (((wb >> (8 * (u & 3))) & 255u) << 8);
+      *(uint32_t*)(v + ((i0 + e) * Hkv + h) * kDim8 + 2 * lane) = pair8(both, f, false);
+    }
+  }
+}
+
+bool pool_ok(const void* pool, int32_t n_pages, int32_t Hkv) {
+  return pool && !((uintptr_t)pool & 15) && fc_paged_byte_pool_bytes(n_pages, Hkv) > 0;
+}
+
+// Workgroups over a call's heads: enough that a short call fills the card.
+uint32_t over_heads(int64_t groups, int64_t tasks) {
+  const int64_t want = (4 * 256 + groups - 1) / groups;
+  return (uint32_t)(want < 1 ? 1 : want > tasks ? tasks : want);
+}
+
+// A launch takes fewer than 2^32 threads in a dimension, so a longer call is several.
+constexpr int64_t kMostGroups = 1 << 20;
+
+}  // namespace
+
+extern "C" size_t fc_paged_byte_pool_bytes(int32_t n_pages, int32_t Hkv) {
+  if (n_pages < 1 || n_pages > (1 << 25) - 1 || Hkv < 1 || Hkv > 1024) return 0;
+  return (size_t)n_pages * Hkv * FC_PAGE8_HEAD_BYTES;
+}
+
+extern "C" fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k,
+                                     int64_t k_stride, const uint16_t* v, int64_t v_stride, int32_t n_src,
+                                     const int32_t* slot, const int32_t* src, int32_t n, hipStream_t stream) {
+  if (!pool_ok(pool, n_pages, Hkv) || n < 0 || n_src < 0) return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || ((k_stride | v_stride) & 7)) return FC_ERR_INVALID;
+  if (n == 0 || n_src == 0) return FC_OK;
+  if (!k || !v || !slot) return FC_ERR_INVALID;
+  if (((uintptr_t)k | (uintptr_t)v) & 15) return FC_ERR_INVALID;
+  const uint64_t numbers = 4 * (uint64_t)n;
+  if (!fc::apart({{pool, fc_paged_byte_pool_bytes(n_pages, Hkv)}},
+                 {fc::rows_span(k, n_src, k_stride, Hkv * D), fc::rows_span(v, n_src, v_stride, Hkv * D),
+                  {slot, numbers}, {src, numbers}}))
+    return FC_ERR_INVALID;
+  // A window of 32 entries begins one run or two of a prompt's; single tokens, each a
+  // run of its own, are spread further.
+  const int window = n >= 8192 ? kMostWindow : n >= 1024 ? 8 : 1;
+  Write a = {pool, {k, v}, {k_stride, v_stride}, slot, src, 0, n, n_src, n_pages, Hkv, window};
+  const int64_t groups = fc::div_up((uint64_t)n, (uint64_t)window);
+  const uint32_t y = over_heads(groups, (2 * (int64_t)Hkv + kWriteWaves - 1) / kWriteWaves);
+  (void)hipGetLastError();
+  for (int64_t g = 0; g < groups; g += kMostGroups) {
+    a.first = g * window;
+    const uint32_t now = (uint32_t)(groups - g < kMostGroups ? groups - g : kMostGroups);
+    hipLaunchKernelGGL(k_paged8_write, dim3(now, y), dim3(kWriteThreads), 0, stream, a);
+    FC_CHECK_LAUNCH();
+  }
+  return FC_OK;
+}
+
+extern "C" fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot,
+                                    int32_t n, uint16_t* k, uint16_t* v, hipStream_t stream) {
+  if (!pool_ok(pool, n_pages, Hkv) || n < 0) return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (n == 0) return FC_OK;
+  if (!slot || !k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return FC_ERR_INVALID;
+  const fc::Span rows = fc::rows_span(k, n, (int64_t)Hkv * D, (int64_t)Hkv * D);
+  if (!fc::apart({rows, {v, rows.n}}, {{pool, fc_paged_byte_pool_bytes(n_pages, Hkv)}, {slot, 4 * (uint64_t)n}}))
+    return FC_ERR_INVALID;
+  const int64_t groups = fc::div_up((uint64_t)n, kReadRows);
+  const uint32_t y = over_heads(groups, (Hkv + kReadWaves - 1) / kReadWaves);
+  (void)hipGetLastError();
+  for (int64_t g = 0; g < groups; g += kMostGroups) {
+    const uint32_t now = (uint32_t)(groups - g < kMostGroups ? groups - g : kMostGroups);
+    hipLaunchKernelGGL(k_paged8_read, dim3(now, y), dim3(kReadThreads), 0, stream, pool, n_pages, Hkv, slot,
+                       g * kReadRows, (int64_t)n, k, v);
+    FC_CHECK_LAUNCH();
+  }
+  return FC_OK;
+}

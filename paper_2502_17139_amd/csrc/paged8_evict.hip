@@ -1,0 +1,525 @@
+// What cached tokens are worth on gfx950: the attention that they get
+// (fc_paged_byte_weights), and the eviction of those that got least (fc_paged_byte_evict).
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fastcoder.h"
+#include "fc_device.h"
+#include "fc_host.h"
+#include "fc_page8.h"
+
+namespace {
+
+using fc::kBlock8;
+using fc::kDim8;
+using fc::kPage8;
+using fc::kPage8Bytes;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ int clamp_len(int len, int most) { return len < 0 ? 0 : (len > most ? most : len); }
+
+// ---------------------------------------------------------------- weights --
+
+constexpr int kTile = 16;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * fc::kWave;
+constexpr int kKTiles = kPage8 / 16;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Weights {
+  float* weights;
+  const uint16_t* q;
+  int64_t q_stride;
+  const float* lse;
+  const uint8_t* pool;
+  const int32_t *table, *len, *new_len, *cu, *src;
+  int n_rows, n_pages, max_pages, n, H, Hkv, max_len;
+};
+
+__device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
+  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+  const bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+  return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+// Sixteen values a lane to their sums over the 16 lanes of a row: lane lc gets the sum
+// of value lc.
+__device__ __forceinline__ float sum_of_own(float (&v)[16], int lc) {
+#pragma unroll
+  for (int half = 8; half >= 1; half >>= 1) {
+    const bool up = lc & half;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const float keep = up ? v[half + i] : v[i], send = up ? v[i] : v[half + i];
+      v[i] = keep + __shfl_xor(send, half);
+    }
+  }
+  return v[0];
+}
+
+// A wave holds a page's keys as bf16 and goes through the sequence's rows, 16 at a
+// time, next ones on their way: S^T = K Q^T as in attention, so that lane (lg, lc) has
+// row lc's scores with keys 16 lg + 4 t + e, whose weights it adds up over the rows;
+// at the end the 16 lanes' sums are joined.  kShared: the waves of a workgroup take one
+// page, every fourth 16 rows each (prompts: many rows, few pages); otherwise a page
+// each.  Nothing is added by two workgroups, so sums have one order.
+template <bool kShared>
+__global__ void __launch_bounds__(kThreads, 2) k_paged8_weights(Weights A) {
+  __shared__ float s_sum[kWaves - 1][kPage8];
+  const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
+  const int b = (int)blockIdx.y, kv = (int)blockIdx.z;
+  const int pg = kShared ? (int)blockIdx.x : (int)blockIdx.x * kWaves + w;
+  const int len = clamp_len(A.len[b], A.max_len), end = clamp_len(A.new_len[b], A.max_len);
+  const int G = A.H / A.Hkv;
+  const int64_t M = (int64_t)(end - len) * G;
+  if (M <= 0 || pg * kPage8 >= end) return;  // with kShared: all waves of the workgroup
+  const int id = A.table[(int64_t)b * A.max_pages + pg];
+  if (id < 0 || id >= A.n_pages) return;
+  const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + kv) * kPage8Bytes;
+  const int key_row = 16 * (lc >> 2) + (lc & 3);
+  bf16x8 key[kKTiles][4];
+#pragma unroll
+  for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint4 c = *(const uint4*)(page + (key_row + 4 * t) * kDim8 + 64 * u + 16 * lg);
+      key[t][2 * u] = widen(c.x, c.y);
+      key[t][2 * u + 1] = widen(c.z, c.w);
+    }
+  const float scale = fc::scale8(page[fc::kPage8Scales + (lg >> 1)]) * (kLog2e / sqrtf((float)kDim8));
+  const int key0 = pg * kPage8 + 16 * lg;  // the lane's first key
+  float got[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) got[i] = 0.0f;
+
+  const int cu = A.cu[b];
+  struct Rows {
+    bf16x8 q[4];
+    float minus;  // 0 - lse, base 2
+    int last;     // the last key that the row sees; -1: it pays nothing
+  };
+  const auto load = [&](int64_t r, Rows& x) {
+    // a row past the last one: the last one, for nothing
+    const bool in = r < M;
+    const int64_t rr = in ? r : M - 1;
+    const int t = (int)(rr / G), h = kv * G + (int)(rr - (int64_t)t * G);
+    const int64_t at = (int64_t)cu + t;
+    bool ok = in && at >= 0 && at < A.n;
+    int64_t row = ok ? (A.src ? (int64_t)A.src[at] : at) : 0;
+    ok = ok && row >= 0 && row < A.n_rows;
+    if (!ok) row = 0;
+    const uint16_t* p = A.q + row * A.q_stride + (int64_t)h * kDim8 + 16 * lg;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x.q[u] = *(const bf16x8*)(p + 64 * (u / 2) + 8 * (u % 2));
+    const float lse = A.lse[row * A.H + h];
+    x.minus = 0.0f - lse * kLog2e;
+    x.last = ok && lse != -INFINITY ? len + t : -1;
+  };
+  // rows that come before the page's first key see nothing of it
+  const int64_t skip = (int64_t)pg * kPage8 - len;
+  int64_t tile = skip > 0 ? skip * G / kTile : 0;
+  const int64_t step = kShared ? kWaves : 1;
+  if (kShared) tile += w;
+  Rows x;
+  if (tile * kTile < M) load(tile * kTile + lc, x);
+  for (; tile * kTile < M; tile += step) {
+    Rows next = x;
+    if ((tile + step) * kTile < M) load((tile + step) * kTile + lc, next);
+    floatx4 s[kKTiles];
+#pragma unroll
+    for (int t = 0; t < kKTiles; ++t) {
+      s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[t][u], x.q[u], s[t], 0, 0, 0);
+    }
+    // a product's result is read only some cycles after it was issued
+    asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
+#pragma unroll
+    for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, x.minus));
+        got[4 * t + e] += key0 + 4 * t + e <= x.last ? p : 0.0f;
+      }
+    x = next;
+  }
+  float sum = sum_of_own(got, lc);  // of key 16 lg + lc
+  if (kShared) {
+    if (w > 0) s_sum[w - 1][lane] = sum;
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int g = 0; g < kWaves - 1; ++g) sum += s_sum[g][lane];
+  }
+  const int j = key0 + lc;
+  float* to = A.weights + ((int64_t)id * A.Hkv + kv) * kPage8 + lane;
+  if (j < end) *to = j < len ? *to + sum : sum;
+}
+
+// ------------------------------------------------------------------ evict --
+
+constexpr int kSelThreads = 1024;
+constexpr int kSelWaves = kSelThreads / fc::kWave;
+constexpr int kBins = 2048;
+
+struct Evict {
+  uint8_t* pool;
+  float* weights;
+  const int32_t *table, *len, *budget;
+  int32_t* add;
+  int32_t* from;    // [B][Hkv][max_len] token that moves to each place
+  int32_t* before;  // [B][Hkv][pages + 1] tokens that stay, ahead of each page
+  int32_t* flags;   // [B][Hkv][pages + 1] pages whose tokens are read; the last: pages begun
+  int n_pages, Hkv, max_pages, max_len, pages, first, recent;
+};
+
+// How a sequence is cut: its length, how many stay, the tokens that do by their place
+// (before lo, from late on), and those of which the `heavy` heaviest do (lo .. hi - 1):
+// what lies between, or the first ones where the budget does not take all of them.
+struct Cut {
+  int n, keep, lo, hi, late, heavy;
+  __device__ __forceinline__ Cut(const Evict& A, int b) {
+    n = clamp_len(A.len[b], A.max_len);
+    keep = clamp_len(A.budget[b], n);
+    const int recent = A.recent < keep ? A.recent : keep, rest = keep - recent;
+    late = n - recent;
+    const bool all = A.first <= rest;
+    lo = all ? A.first : 0;
+    hi = all || A.first > late ? late : A.first;
+    heavy = rest - lo;
+  }
+};
+
+// A weight as a number that sorts as it does: 0 for what is not above 0.
+__device__ __forceinline__ uint32_t rank_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
+
+// A workgroup finds what one head of one sequence keeps: the weight of the last one to
+// stay, 11 bits at a time from the top, by counting; then, in order, which tokens are
+// above it, and of those that equal it the first ones.  A wave's lanes are a page's
+// tokens.
+__global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
+  __shared__ uint32_t s_bins[kBins];
+  __shared__ uint32_t s_sum[kSelWaves + 1];
+  __shared__ uint32_t s_bin, s_left;
+  __shared__ uint32_t s_wave[2][kSelWaves];
+  const int tid = (int)threadIdx.x, lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
+  const int kv = (int)blockIdx.x, b = (int)blockIdx.y;
+  const Cut c(A, b);
+  if (kv == 0 && tid == 0) A.add[b] = c.keep - c.n;
+  if (c.keep >= c.n || c.keep == 0) return;
+  const int64_t bk = (int64_t)b * A.Hkv + kv;
+  const int32_t* table = A.table + (int64_t)b * A.max_pages;
+  int32_t* flags = A.flags + bk * (A.pages + 1);
+  const int pages = (c.n + kPage8 - 1) / kPage8;
+  for (int p = tid; p <= A.pages; p += kSelThreads) flags[p] = 0;
+  const auto weight = [&](int p) {
+    const int id = table[p];
+    const bool there = id >= 0 && id < A.n_pages;
+    return there ? rank_of(A.weights[((int64_t)id * A.Hkv + kv) * kPage8 + lane]) : 0u;
+  };
+  const int lo = c.lo, hi = c.hi;
+  const uint32_t heavy = (uint32_t)c.heavy;
+  uint32_t found = 0, left = heavy;  // the bits of the last one to stay, and how many of those that share them do
+  if (heavy > 0) {
+    for (int level = 0; level < 3; ++level) {
+      const int shift = level == 0 ? 20 : level == 1 ? 9 : 0, bits = level == 2 ? 9 : 11;
+      for (int i = tid; i < kBins; i += kSelThreads) s_bins[i] = 0;
+      __syncthreads();
+      for (int p = w; p < pages; p += kSelWaves) {
+        const int t = p * kPage8 + lane;
+        const uint32_t r = weight(p);
+        if (t >= lo && t < hi && (level == 0 || (r >> (shift + bits)) == found))
+          atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1u)], 1u);
+      }
+      __syncthreads();
+      // two bins a thread, from the largest down
+      const int top = kBins - 1 - 2 * tid;
+      const uint32_t x = s_bins[top], y = s_bins[top - 1];
+      const uint32_t ahead = fc::block_excl_sum<uint32_t>(x + y, s_sum, nullptr);
+      if (ahead < left && left <= ahead + x) s_bin = (uint32_t)top, s_left = left - ahead;
+      else if (ahead + x < left && left <= ahead + x + y) s_bin = (uint32_t)top - 1, s_left = left - ahead - x;
+      __syncthreads();
+      found = found << bits | s_bin;
+      left = s_left;
+      __syncthreads();
+    }
+  }
+  // each wave's pages follow one another; first how many it has of either kind
+  const int p0 = (int)((int64_t)pages * w / kSelWaves), p1 = (int)((int64_t)pages * (w + 1) / kSelWaves);
+  const auto kinds = [&](int p, uint64_t& stays, uint64_t& equal) {
+    const int t = p * kPage8 + lane;
+    const uint32_t r = weight(p);
+    const bool by_weight = heavy > 0 && t >= lo && t < hi;
+    stays = fc::ballot(t < lo || (t >= c.late && t < c.n) || (by_weight && r > found));
+    equal = fc::ballot(by_weight && r == found);
+  };
+  uint32_t sure = 0, maybe = 0;
+  for (int p = p0; p < p1; ++p) {
+    uint64_t stays, equal;
+    kinds(p, stays, equal);
+    sure += (uint32_t)__popcll(stays);
+    maybe += (uint32_t)__popcll(equal);
+  }
+  if (lane == 0) s_wave[0][w] = sure, s_wave[1][w] = maybe;
+  __syncthreads();
+  sure = maybe = 0;
+  for (int i = 0; i < w; ++i) sure += s_wave[0][i], maybe += s_wave[1][i];
+  int32_t* before = A.before + bk * (A.pages + 1);
+  int32_t* from = A.from + bk * A.max_len;
+  for (int p = p0; p < p1; ++p) {
+    uint64_t stays, equal;
+    kinds(p, stays, equal);
+    const uint32_t at = sure + (maybe < left ? maybe : left);
+    const uint64_t below = fc::lanemask_lt();
+    const bool taken = ((equal >> lane) & 1u) && maybe + (uint32_t)__popcll(equal & below) < left;
+    const uint64_t all = stays | fc::ballot(taken);
+    if (lane == 0) before[p] = (int32_t)at;
+    if ((all >> lane) & 1u) from[at + (uint32_t)__popcll(all & below)] = p * kPage8 + lane;
+    sure += (uint32_t)__popcll(stays);
+    maybe += (uint32_t)__popcll(equal);
+  }
+  if (tid == 0) before[pages] = c.keep;
+}
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveWaves = kMoveThreads / fc::kWave;
+
+// A workgroup brings 64 tokens to one page of their new places.  They come from this
+// page and later ones; it reads them into registers, says so, waits until the pages
+// ahead of it that read from this one have said so too (two at most), and writes.
+// Pages are begun in the order of a counter, so that whoever is waited for has begun,
+// and nobody waits before it has read: the wait ends.  Two waves a block of 32: keys 16
+// bytes a lane, values a dim a lane, whose bytes lie 16 apart.
+__global__ void __launch_bounds__(kMoveThreads) k_evict_move(Evict A) {
+  __shared__ int s_page;
+  __shared__ uint32_t s_top[2][kMoveWaves];
+  __shared__ int s_from[kPage8];
+  __shared__ int64_t s_base[kPage8];   // of the page that a token comes from; -1: none
+  __shared__ int s_exp[2][kPage8];     // of its keys' and values' scale
+  const int tid = (int)threadIdx.x, lane = fc::lane_id();
+  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
+  const int kv = (int)blockIdx.y, b = (int)blockIdx.z;
+  const Cut c(A, b);
+  if (c.keep >= c.n || (int)blockIdx.x * kPage8 >= c.keep) return;
+  const int64_t bk = (int64_t)b * A.Hkv + kv;
+  const int32_t* table = A.table + (int64_t)b * A.max_pages;
+  int32_t* flags = A.flags + bk * (A.pages + 1);
+  if (tid == 0) s_page = __hip_atomic_fetch_add(&flags[A.pages], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const int pg = __builtin_amdgcn_readfirstlane(s_page);
+  const int here = c.keep - pg * kPage8 < kPage8 ? c.keep - pg * kPage8 : kPage8;  // tokens of the page
+  const int32_t* from = A.from + bk * A.max_len + (int64_t)pg * kPage8;
+  float weight = 0.0f;
+  if (tid < kPage8) {
+    const int t = tid < here ? from[tid] : -1;
+    const int id = t >= 0 ? table[t / kPage8] : -1;
+    const bool there = id >= 0 && id < A.n_pages;
+    const int64_t base = there ? ((int64_t)id * A.Hkv + kv) : -1;
+    s_from[tid] = t % kPage8;
+    s_base[tid] = base;
+    const uint8_t* scales = A.pool + (there ? base : 0) * kPage8Bytes + fc::kPage8Scales + (there ? t % kPage8 / kBlock8 : 0);
+    s_exp[0][tid] = there ? fc::clamp_exp8((int)scales[0] - 127) : fc::kLeastExp8;
+    s_exp[1][tid] = there ? fc::clamp_exp8((int)scales[2] - 127) : fc::kLeastExp8;
+    if (there) weight = A.weights[base * kPage8 + t % kPage8];
+  }
+  __syncthreads();
+  const int half = w >> 1, t0 = half * kBlock8;  // the wave's block
+  // keys: 16 rows a wave, eight lanes each
+  uint4 k[2];
+  int k_exp[2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int t = t0 + 16 * (w & 1) + 8 * p + (lane >> 3);
+    const int64_t base = s_base[t];
+    k[p] = make_uint4(0u, 0u, 0u, 0u);
+    k_exp[p] = s_exp[0][t];
+    if (base >= 0) k[p] = *(const uint4*)(A.pool + base * kPage8Bytes + s_from[t] * kDim8 + 16 * (lane & 7));
+  }
+  // values: every token of the block, one dim a lane
+  const int d = 64 * (w & 1) + lane;
+  uint32_t v[kBlock8];
+#pragma unroll
+  for (int i = 0; i < kBlock8; ++i) {
+    const int64_t base = s_base[t0 + i];
+    v[i] = 0;
+    if (base >= 0) v[i] = A.pool[base * kPage8Bytes + fc::v8_at(s_from[t0 + i], d)];
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all of it is here
+  __syncthreads();
+  if (tid == 0) __hip_atomic_store(&flags[pg], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+  // the largest magnitudes of the block, then its codes
+  const auto magnitude = [&](float x, int e) { return fc::reach8(x * fc::power8(e)); };
+  uint32_t top[2] = {0, 0};
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const uint32_t words[4] = {k[p].x, k[p].y, k[p].z, k[p].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi) {
+        const fc::floatx2_8 x = hi ? __builtin_amdgcn_cvt_pk_f32_fp8((int)words[i], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)words[i], false);
+        const uint32_t a = magnitude(x[0], k_exp[p]), m = magnitude(x[1], k_exp[p]);
+        top[0] = a > top[0] ? a : top[0];
+        top[0] = m > top[0] ? m : top[0];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < kBlock8; ++i) {
+    const uint32_t a = magnitude(__builtin_amdgcn_cvt_f32_fp8((int)v[i], 0), s_exp[1][t0 + i]);
+    top[1] = a > top[1] ? a : top[1];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int o = 1; o < fc::kWave; o <<= 1) {
+      const uint32_t x = (uint32_t)__shfl_xor((int)top[i], o);
+      top[i] = x > top[i] ? x : top[i];
+    }
+    if (lane == 0) s_top[i][w] = top[i];
+  }
+  __syncthreads();
+  int e[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t x = s_top[i][w & ~1], y = s_top[i][w | 1];
+    e[i] = fc::exponent8(x > y ? x : y);
+  }
+  const auto ratio = [&](int was, int now) { return was - now < -126 ? 0.0f : fc::power8(was - now); };
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const float f = ratio(k_exp[p], e[0]);
+    k[p] = make_uint4(fc::recode8(k[p].x, f), fc::recode8(k[p].y, f), fc::recode8(k[p].z, f), fc::recode8(k[p].w, f));
+  }
+  uint32_t codes[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      x[u] = __builtin_amdgcn_cvt_f32_fp8((int)v[4 * i + u], 0) * ratio(s_exp[1][t0 + 4 * i + u], e[1]);
+    codes[i] = fc::codes8(x[0], x[1], x[2], x[3]);
+  }
+
+  // tokens of this page stay for pages ahead: those have to be read
+  const int32_t* before = A.before + bk * (A.pages + 1);
+  const int q0 = before[pg] / kPage8, q1 = (before[pg + 1] - 1) / kPage8;
+  if (tid == 0 && before[pg] < before[pg + 1]) {
+    for (int q = q0; q <= q1 && q < pg; ++q)
+      while (__hip_atomic_load(&flags[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0) __builtin_amdgcn_s_sleep(1);
+  }
+  __syncthreads();
+  const int to = table[pg];
+  if (to < 0 || to >= A.n_pages) return;
+  const int64_t base = (int64_t)to * A.Hkv + kv;
+  uint8_t* page = A.pool + base * kPage8Bytes;
+  if (tid < here) A.weights[base * kPage8 + tid] = weight;
+  if (t0 >= here) return;  // a block behind the last token stays as it was
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+    *(uint4*)(page + (t0 + 16 * (w & 1) + 8 * p + (lane >> 3)) * kDim8 + 16 * (lane & 7)) = k[p];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    *(uint4*)(page + fc::v8_at(t0 + 16 * q, d)) = make_uint4(codes[4 * q], codes[4 * q + 1], codes[4 * q + 2], codes[4 * q + 3]);
+  if ((w & 1) == 0 && lane < 2) page[fc::kPage8Scales + 2 * lane + half] = (uint8_t)(e[lane] + 127);
+}
+
+size_t carve(void* p, int32_t B, int32_t Hkv, int32_t max_len, Evict& a) {
+  fc::Carver c(p);
+  const size_t rows = (size_t)B * Hkv;
+  a.pages = (max_len + kPage8 - 1) / kPage8;
+  a.from = c.take<int32_t>(rows * (size_t)max_len);
+  a.before = c.take<int32_t>(rows * ((size_t)a.pages + 1));
+  a.flags = c.take<int32_t>(rows * ((size_t)a.pages + 1));
+  return c.used + 256;
+}
+
+bool sizes_ok(int32_t B, int32_t Hkv, int32_t max_len) {
+  return B >= 0 && B <= 65536 && Hkv >= 1 && Hkv <= 1024 && max_len >= 0 && max_len <= 0x7FFFFFFF - kPage8;
+}
+
+}  // namespace
+
+extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, int64_t q_stride, const float* lse,
+                                       int32_t n_rows, const uint8_t* pool, int32_t n_pages, const int32_t* table,
+                                       int32_t max_pages, const int32_t* len, const int32_t* new_len, const int32_t* cu,
+                                       const int32_t* src, int32_t n, int32_t B, int32_t H, int32_t Hkv, int32_t D,
+                                       int32_t max_len, hipStream_t stream) {
+  if (!sizes_ok(B, Hkv, max_len) || n_rows < 0 || n < 0 || H < Hkv || H > 8192 || H % Hkv || n_pages < 1 ||
+      n_pages > (1 << 25) - 1 || max_pages < 1 || (int64_t)max_len > (int64_t)max_pages * kPage8)
+    return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (q_stride < (int64_t)H * D || (q_stride & 7)) return FC_ERR_INVALID;
+  if (B == 0 || n_rows == 0 || n == 0 || max_len == 0) return FC_OK;
+  if (!weights || !q || !lse || !pool || !table || !len || !new_len || !cu) return FC_ERR_INVALID;
+  if (((uintptr_t)q | (uintptr_t)pool) & 15 || ((uintptr_t)weights | (uintptr_t)lse) & 3) return FC_ERR_INVALID;
+  const uint64_t seqs = 4 * (uint64_t)B;
+  if (!fc::apart({{weights, 4 * (uint64_t)n_pages * Hkv * kPage8}},
+                 {fc::rows_span(q, n_rows, q_stride, (int64_t)H * D),
+                  {lse, 4 * (uint64_t)n_rows * H},
+                  {pool, fc_paged_byte_pool_bytes(n_pages, Hkv)},
+                  {table, seqs * max_pages},
+                  {len, seqs},
+                  {new_len, seqs},
+                  {cu, seqs + 4},
+                  {src, 4 * (uint64_t)n}}))
+    return FC_ERR_INVALID;
+  const Weights a = {weights, q, q_stride, lse, pool, table, len, new_len, cu, src, n_rows, n_pages, max_pages, n, H, Hkv,
+                     max_len};
+  const uint32_t pages = fc::div_up((uint64_t)max_len, kPage8);
+  // several times 16 rows for each sequence, or too few pages for the card: its waves
+  // share them
+  const bool shared = (int64_t)n * (H / Hkv) > 8 * kTile * (int64_t)B;
+  (void)hipGetLastError();
+  if (shared)
+    hipLaunchKernelGGL(k_paged8_weights<true>, dim3(pages, B, Hkv), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(k_paged8_weights<false>, dim3(fc::div_up(pages, kWaves), B, Hkv), dim3(kThreads), 0, stream, a);
+  FC_CHECK_LAUNCH();
+  return FC_OK;
+}
+
+extern "C" size_t fc_paged_byte_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len) {
+  if (!sizes_ok(B, Hkv, max_len) || B == 0) return 0;
+  Evict a;
+  return carve(nullptr, B, Hkv, max_len, a);
+}
+
+extern "C" fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t n_pages, int32_t Hkv, int32_t D,
+                                     const int32_t* table, int32_t max_pages, const int32_t* len, const int32_t* budget,
+                                     int32_t B, int32_t max_len, int32_t first, int32_t recent, int32_t* add, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+  if (!sizes_ok(B, Hkv, max_len) || n_pages < 1 || n_pages > (1 << 25) - 1 || max_pages < 1 ||
+      (int64_t)max_len > (int64_t)max_pages * kPage8 || first < 0 || recent < 0)
+    return FC_ERR_INVALID;
+  if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
+  if (B == 0) return FC_OK;
+  if (!pool || !weights || !table || !len || !budget || !add) return FC_ERR_INVALID;
+  if ((uintptr_t)pool & 15 || (uintptr_t)weights & 3) return FC_ERR_INVALID;
+  const size_t need = fc_paged_byte_evict_workspace_bytes(B, Hkv, max_len);
+  if (!ws || ws_bytes < need) return FC_ERR_WORKSPACE;
+  if ((uintptr_t)ws & 15) return FC_ERR_INVALID;
+  const uint64_t seqs = 4 * (uint64_t)B;
+  if (!fc::apart({{pool, fc_paged_byte_pool_bytes(n_pages, Hkv)},
+                  {weights, 4 * (uint64_t)n_pages * Hkv * kPage8},
+                  {add, seqs},
+                  {ws, need}},
+                 {{table, seqs * max_pages}, {len, seqs}, {budget, seqs}}))
+    return FC_ERR_INVALID;
+  Evict a = {pool, weights, table, len, budget, add, nullptr, nullptr, nullptr, n_pages, Hkv, max_pages, max_len, 0, first,
+             recent};
+  carve(ws, B, Hkv, max_len, a);
+  (void)hipGetLastError();
+  hipLaunchKernelGGL(k_evict_select, dim3(Hkv, B), dim3(kSelThreads), 0, stream, a);
+  FC_CHECK_LAUNCH();
+  if (a.pages == 0) return FC_OK;
+  hipLaunchKernelGGL(k_evict_move, dim3(a.pages, Hkv, B), dim3(kMoveThreads), 0, stream, a);
+  FC_CHECK_LAUNCH();
+  return FC_OK;
+}
