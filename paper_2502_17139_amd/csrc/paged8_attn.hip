@@ -58,7 +58,7 @@ struct Args {
   int64_t q_stride, k_stride, v_stride;
   const uint8_t* pool;
   const int32_t *table, *prefix_len, *num_nodes, *mask;
-  int n_pages, max_pages, B, R, H, Hkv, max_len, tiles, chunks, part_pages, parts;
+  int n_pages, max_pages, B, R, H, Hkv, max_len, tiles, chunks, part_pages, parts, ordered;
   uint16_t* out;
   float* lse;
   float4* part_ml;
@@ -90,13 +90,62 @@ __device__ __forceinline__ int parts_of(int pages, int part_pages) {
   return pages <= part_pages ? 1 : (pages + part_pages - 1) / part_pages;
 }
 
+// Which of n (tree, key head) pairs, in `chunks` workgroups each, workgroup x has: an
+// XCD gets every eighth workgroup, so a pair's workgroups lie eight apart, to share its
+// pages in one L2, and pairs that follow each other, which have one tree's length, are
+// spread over all XCDs.
+struct Place {
+  int pair, chunk;
+};
+__device__ __forceinline__ Place place_of(int x, int n, int chunks) {
+  const int whole = n / kXcds * kXcds;  // pairs in rounds of eight
+  if (x < whole * chunks) return Place{x / (kXcds * chunks) * kXcds + x % kXcds, x / kXcds % chunks};
+  return Place{x / chunks, x % chunks};
+}
+
+// The tree with the r-th longest prefix, in pages; of equal ones the first is longer.  A
+// wave holds the lengths, four a lane, and finds the r-th largest bit by bit, by counting.
+constexpr int kOrdered = 4 * fc::kWave;  // trees of a launch, at most
+__device__ __forceinline__ int longest(const Args& A, int r) {
+  const int lane = fc::lane_id();
+  int pages[kOrdered / fc::kWave];
+#pragma unroll
+  for (int i = 0; i < kOrdered / fc::kWave; ++i) {
+    const int b = fc::kWave * i + lane;
+    pages[i] = b < A.B ? (clamp_len(A.prefix_len[b], A.max_len) + kPage8 - 1) / kPage8 : -1;
+  }
+  const auto count = [&](int least) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kOrdered / fc::kWave; ++i) n += (int)__popcll(fc::ballot(pages[i] >= least));
+    return n;
+  };
+  int v = 0;
+  for (int bit = 31 - __builtin_clz((A.max_len + kPage8 - 1) / kPage8 | 1); bit >= 0; --bit)
+    if (count(v | 1 << bit) > r) v |= 1 << bit;
+  r -= count(v + 1);
+#pragma unroll
+  for (int i = 0; i < kOrdered / fc::kWave; ++i) {
+    uint64_t same = fc::ballot(pages[i] == v);
+    const int n = (int)__popcll(same);
+    if (r < n) {
+      for (; r > 0; --r) same &= same - 1;
+      return fc::kWave * i + (int)__builtin_ctzll(same);
+    }
+    r -= n;
+  }
+  return 0;
+}
+
 // What a workgroup works on.
 struct Work {
   int bk, b, kv, G, M, P, n, part, parts, pg0, pg1;
   bool tree;
-  __device__ __forceinline__ bool init(const Args& A, int bk_, int part_) {
-    bk = bk_, part = part_;
-    b = bk / A.Hkv, kv = bk - b * A.Hkv;
+  __device__ __forceinline__ bool init(const Args& A, int pair, int part_) {
+    part = part_;
+    b = pair / A.Hkv, kv = pair - b * A.Hkv;
+    if (A.ordered) b = __builtin_amdgcn_readfirstlane(longest(A, b));
+    bk = b * A.Hkv + kv;
     G = A.H / A.Hkv, M = A.R * G;
     P = clamp_len(A.prefix_len[b], A.max_len);
     n = A.num_nodes ? clamp_len(A.num_nodes[b], A.R) : A.R;
@@ -275,12 +324,13 @@ __device__ __forceinline__ void page_scores(Key key, const Tile (&tile)[kWaveTil
 // Keys 16 lg + 4 t + e from `left` on do not count.
 template <int NT>
 __device__ __forceinline__ void cut(floatx4 (&s)[NT][kKTiles], int lg, int left) {
+  const int live = left - 16 * lg;  // of the lane's keys
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][t][e] = 16 * lg + 4 * t + e < left ? s[i][t][e] : -INFINITY;
+      for (int e = 0; e < 4; ++e) s[i][t][e] = 4 * t + e < live ? s[i][t][e] : -INFINITY;
 }
 // And that what their bytes hold does not matter, a weight of 0 times a NaN being
 // one, their values are 0.
@@ -301,6 +351,22 @@ __device__ __forceinline__ float key_scale(uint32_t word, int lg, int left) {
   return 32 * (lg >> 1) < left ? s : 1.0f;
 }
 __device__ __forceinline__ float value_scale(uint32_t word, int lg, int left) { return key_scale(word >> 16, lg, left); }
+
+// A page's values, with the weights of NT tiles: value(t) gives the codes of a lane's 16
+// tokens at dim 16 t + lc.
+template <int NT, typename Value>
+__device__ __forceinline__ void page_values(Value value, float scale, const bf16x2 (&p)[NT][2 * kKTiles],
+                                            Tile (&tile)[kWaveTiles]) {
+#pragma unroll
+  for (int t = 0; t < kDTiles; ++t) {
+    const uint4 c = value(t);
+    const bf16x8 a = widen(c.x, c.y, scale), b = widen(c.z, c.w, scale);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) tile[i].row.o[t] = product(a, join(p[i][0], p[i][1], p[i][2], p[i][3]), tile[i].row.o[t]);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) tile[i].row.o[t] = product(b, join(p[i][4], p[i][5], p[i][6], p[i][7]), tile[i].row.o[t]);
+  }
+}
 
 // The value rows of up to 64 of a tree's tokens lie in LDS, kRowBytes apart (32 bytes
 // more than their values, so that a transposing read meets every bank once).  Such a
@@ -398,13 +464,13 @@ __device__ __forceinline__ void whole(Row& r) {
 }
 // Waves that shared a tile's keys hand over to one of them, through LDS.
 constexpr int kRec = kTile * kDim8 + 3 * kTile;  // floats of a tile: outputs, maxima, both sums
-__device__ __forceinline__ void give(const Row& r, float* rec) {
+__device__ __forceinline__ void give(const Row& r, float m, float* rec) {
   const int lane = fc::lane_id();
 #pragma unroll
   for (int t = 0; t < kDTiles; ++t) *(floatx4*)(rec + (t * 64 + lane) * 4) = r.o[t];
   if (lane < 16) {
     float* s = rec + kTile * kDim8 + lane;
-    s[0] = r.m(), s[kTile] = r.l, s[2 * kTile] = r.x;
+    s[0] = m, s[kTile] = r.l, s[2 * kTile] = r.x;
   }
 }
 __device__ __forceinline__ void take(Row& r, float& m, const float* rec) {
@@ -445,20 +511,19 @@ __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& 
   if (A.lse && lg == 0) A.lse[at] = tr < W.n ? log_sum(m, r.x) : -INFINITY;
 }
 
-// One or two tiles of query rows (a decoded token, a short chain): the four waves go
-// through every fourth page alone, out of registers, and wait for nobody until the
-// end.  A page's keys are asked for while the one before has its weights, its values
-// while the next scores are made.
-template <int NT, bool kLse>
-__global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
+// One or two tiles of query rows (a decoded token, a short chain): a workgroup's waves
+// go through every fourth (or eighth) page alone, out of registers, and wait for
+// nobody until the end.  A page's keys are asked for while the one before has its
+// weights, its values while the next scores are made.
+template <int NT, int kAloneWaves, bool kLse>
+__global__ void __launch_bounds__(kAloneWaves* fc::kWave, 2) k_paged8_attn_alone(Args A) {
   constexpr int T = 2;  // tiles of tree rows: at most 32
-  constexpr int kTree = 16 * T * kRowBytes, kGiven = (kWaves - 1) * NT * kRec * 4;
+  constexpr int kTree = 16 * T * kRowBytes, kGiven = kAloneWaves / 2 * NT * kRec * 4;
   __shared__ __align__(16) uint8_t s_x[kTree > kGiven ? kTree : kGiven];
   const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
-  const int total = (int)gridDim.x, x = (int)blockIdx.x;
   Work W;
-  if (!W.init(A, total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x, (int)blockIdx.y)) return;
+  if (!W.init(A, place_of((int)blockIdx.x, (int)gridDim.x, 1).pair, (int)blockIdx.y)) return;
 
   uint4 k[kKTiles][2], v[kDTiles];
   uint32_t k_word = 0, v_word = 0;
@@ -466,25 +531,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
   // page numbers, 64 steps at a time in a register's lanes
   int ids = 0;
   const auto id_of = [&](int pg) {
-    const int i = ((pg - W.pg0) / kWaves) & 63;
-    if (i == 0) ids = pg + kWaves * lane < W.pg1 ? table[pg + kWaves * lane] : -1;
+    const int i = ((pg - W.pg0) / kAloneWaves) & 63;
+    if (i == 0) ids = pg + kAloneWaves * lane < W.pg1 ? table[pg + kAloneWaves * lane] : -1;
     return __builtin_amdgcn_readlane(ids, i);
   };
   const auto there = [&](int id) { return id >= 0 && id < A.n_pages; };
   const auto page_of = [&](int id) { return A.pool + ((int64_t)id * A.Hkv + W.kv) * kPage8Bytes; };
-  const int key_row = 16 * (lc >> 2) + (lc & 3);
+  // a lane's places in a page: 32 bits behind an address that all lanes share
+  const uint32_t k_at = (uint32_t)((16 * (lc >> 2) + (lc & 3)) * kDim8 + 16 * lg);
+  const uint32_t v_at = (uint32_t)(fc::kPage8V + lg * 2048 + lc * 16);
   const auto load_k = [&](int id) {
     const uint8_t* p = page_of(id);
 #pragma unroll
     for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) k[t][u] = *(const uint4*)(p + (key_row + 4 * t) * kDim8 + 64 * u + 16 * lg);
+      for (int u = 0; u < 2; ++u) k[t][u] = *(const uint4*)(p + k_at + (4 * t * kDim8 + 64 * u));
     k_word = *(const uint32_t*)(p + fc::kPage8Scales);
   };
   const auto load_v = [&](int id) {
     const uint8_t* p = page_of(id);
 #pragma unroll
-    for (int t = 0; t < kDTiles; ++t) v[t] = *(const uint4*)(p + fc::kPage8V + lg * 2048 + (16 * t + lc) * 16);
+    for (int t = 0; t < kDTiles; ++t) v[t] = *(const uint4*)(p + v_at + 256 * t);
     v_word = *(const uint32_t*)(p + fc::kPage8Scales);
   };
   int pg = W.pg0 + w, id = pg < W.pg1 ? id_of(pg) : -1;
@@ -493,7 +560,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
   for (int i = 0; i < NT; ++i) tile[i].load(W.q_row(A, kTile * i + lc), lg);
   if (there(id)) load_k(id), load_v(id);
 
-  if (W.tree && w == kWaves - 1) {  // the wave whose pages may be fewer
+  // The tree's own rows are the last wave's, whose pages may be fewer: one tile's while
+  // the first page is on its way, two tiles' after the last one, for want of registers.
+  const auto attend_tree = [&]() {
     uint64_t bad = 0;
 #pragma unroll
     for (int i = 0; i < 4 * T; ++i) {
@@ -521,10 +590,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
 #pragma unroll
       for (int i = 0; i < NT; ++i) add_marked<T>(A, W, bad, 0, p[i], see[i], tile[i].row);
     }
-  }
+  };
+  if (NT == 1 && W.tree && w == kAloneWaves - 1) attend_tree();
 
-  for (; pg < W.pg1; pg += kWaves) {
-    const int next = pg + kWaves < W.pg1 ? id_of(pg + kWaves) : -1;
+  for (; pg < W.pg1; pg += kAloneWaves) {
+    const int next = pg + kAloneWaves < W.pg1 ? id_of(pg + kAloneWaves) : -1;
     if (!there(id)) {
       id = next;
       if (there(id)) load_k(id), load_v(id);
@@ -534,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
     floatx4 s[NT][kKTiles];
     page_scores<NT>([&](int t, int u) { return k[t][u]; }, tile, s);
     const float ks = key_scale(k_word, lg, left) * score_scale(), vs = value_scale(v_word, lg, left);
-    if (there(next)) load_k(next);
+    if (NT == 1 && there(next)) load_k(next);
     if (left < kPage8) {
       cut<NT>(s, lg, left);
 #pragma unroll
@@ -542,36 +612,39 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
     }
     bf16x2 p[NT][2 * kKTiles];
     weights<kLse, NT, kKTiles>(s, ks, tile, p);
-#pragma unroll
-    for (int t = 0; t < kDTiles; ++t) {
-      const bf16x8 a = widen(v[t].x, v[t].y, vs), b = widen(v[t].z, v[t].w, vs);
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        tile[i].row.o[t] = product(a, join(p[i][0], p[i][1], p[i][2], p[i][3]), tile[i].row.o[t]);
-        tile[i].row.o[t] = product(b, join(p[i][4], p[i][5], p[i][6], p[i][7]), tile[i].row.o[t]);
-      }
-    }
+    if (NT == 2 && there(next)) load_k(next);  // the scores' registers are free
+    page_values<NT>([&](int t) { return v[t]; }, vs, p, tile);
     if (there(next)) load_v(next);
     id = next;
   }
 
+  if (NT == 2 && W.tree && w == kAloneWaves - 1) attend_tree();
+
+  // half of the waves hand over to the others, until one has all
   float* rec = (float*)s_x;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) whole(tile[i].row);
-  __syncthreads();
-  if (w > 0) {
-#pragma unroll
-    for (int i = 0; i < NT; ++i) give(tile[i].row, rec + ((w - 1) * NT + i) * kRec);
-  }
-  __syncthreads();
-  if (w > 0) return;
+  float m[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    float m = tile[i].row.m();
-#pragma unroll
-    for (int g = 0; g < kWaves - 1; ++g) take(tile[i].row, m, rec + (g * NT + i) * kRec);
-    if (kTile * i + lc < W.M) finish(A, W, tile[i].row, m, kTile * i + lc);
+    whole(tile[i].row);
+    m[i] = tile[i].row.m();
   }
+#pragma unroll
+  for (int half = kAloneWaves / 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (w >= half && w < 2 * half) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) give(tile[i].row, m[i], rec + ((w - half) * NT + i) * kRec);
+    }
+    __syncthreads();
+    if (w < half) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) take(tile[i].row, m[i], rec + (w * NT + i) * kRec);
+    }
+  }
+  if (w > 0) return;
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+    if (kTile * i + lc < W.M) finish(A, W, tile[i].row, m[i], kTile * i + lc);
 }
 
 // More tiles: a workgroup's four waves take up to eight of them through the same pages,
@@ -579,6 +652,45 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn_alone(Args A) {
 // two on their way while a third is used.  The keys' pieces of 16 bytes change places
 // by the row, so that a wave reads its 16 rows without two lanes in a bank.
 __device__ __forceinline__ int swap_of(int row) { return ((row >> 3) & 6) | ((row >> 1) & 1); }
+
+// Pages on their way into LDS: a wave issues a quarter of each.
+struct Pages {
+  const Args& A;
+  const Work& W;
+  const int32_t* table;
+  uint32_t lds0;
+  int w;
+  // page numbers and scales, 64 at a time in a register's lanes: read one by one they
+  // would be loads to wait for among the loads that are meant to stay in flight
+  int ids, words;
+  static constexpr int kLoads = kSlot / (16 * fc::kWave) / kWaves;  // of a wave and page
+  __device__ __forceinline__ Pages(const Args& a, const Work& work, uint8_t* lds, int wave)
+      : A(a), W(work), table(a.table + (int64_t)work.b * a.max_pages), lds0((uint32_t)(uintptr_t)(lds_u8*)lds), w(wave),
+        ids(0), words(0) {}
+  __device__ __forceinline__ int slot_of(int pg) const { return ((pg - W.pg0) & (kSlots - 1)) * kSlot; }
+  // Whether page pg is there, and its scales.
+  __device__ __forceinline__ bool issue(int pg, int& word) {
+    const int lane = fc::lane_id(), i = (pg - W.pg0) & 63;
+    if (i == 0) {
+      ids = pg + lane < W.pg1 ? table[pg + lane] : -1;
+      const bool there = ids >= 0 && ids < A.n_pages;
+      if (!there) ids = -1;
+      words = there ? *(const int*)(A.pool + ((int64_t)ids * A.Hkv + W.kv) * kPage8Bytes + fc::kPage8Scales) : 0;
+      asm volatile("" : "+v"(words));  // waited for here, as the queries are
+    }
+    const int id = __builtin_amdgcn_readlane(ids, i);
+    word = __builtin_amdgcn_readlane(words, i);
+    const bool there = id >= 0;  // an absent page's loads give zeros, and none of its keys counts
+    const uint8_t* page = A.pool + ((int64_t)(there ? id : 0) * A.Hkv + W.kv) * kPage8Bytes;
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const int at = (w * kLoads + l) * 1024;  // the first half of them are keys: eight rows a load
+      const int from = at < fc::kPage8V ? 16 * (lane ^ swap_of(at / kDim8 + (lane >> 3))) : 16 * lane;
+      fc::lds_load16(lds0 + (uint32_t)(slot_of(pg) + at), (uint32_t)from, fc::buffer_rsrc(page + at, there ? 1024u : 0u));
+    }
+    return there;
+  }
+};
 
 template <int NT, bool kLse>
 __device__ __forceinline__ void group_page(const uint8_t* raw, uint32_t word, int left, Tile (&tile)[kWaveTiles]) {
@@ -593,58 +705,108 @@ __device__ __forceinline__ void group_page(const uint8_t* raw, uint32_t word, in
   weights<kLse, NT, kKTiles>(s, key_scale(word, lg, left) * score_scale(), tile, p);
   const float vs = value_scale(word, lg, left);
   const uint8_t* values = raw + fc::kPage8V + lg * 2048 + lc * 16;
-#pragma unroll
-  for (int t = 0; t < kDTiles; ++t) {
-    uint4 c = *(const uint4*)(values + t * 256);
-    if (left < kPage8) c = cut_values(c, lg, left);
-    const bf16x8 a = widen(c.x, c.y, vs), b = widen(c.z, c.w, vs);
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      tile[i].row.o[t] = product(a, join(p[i][0], p[i][1], p[i][2], p[i][3]), tile[i].row.o[t]);
-      tile[i].row.o[t] = product(b, join(p[i][4], p[i][5], p[i][6], p[i][7]), tile[i].row.o[t]);
-    }
+  const auto value = [&](int t) { return *(const uint4*)(values + t * 256); };
+  if (left >= kPage8) page_values<NT>(value, vs, p, tile);
+  else page_values<NT>([&](int t) { return cut_values(value(t), lg, left); }, vs, p, tile);
+}
+
+// A part's pages, with NT tiles of this wave (0: it loads for the others alone).
+template <int NT, bool kLse>
+__device__ __forceinline__ void group_pages(Pages& pages, const uint8_t* lds, bool here0, bool here1, int word0, int word1,
+                                            Tile (&tile)[kWaveTiles]) {
+  const Work& W = pages.W;
+  bool here2 = false;  // whether page pg, pg + 1, pg + 2 is
+  int word2 = 0;
+  for (int pg = W.pg0; pg < W.pg1; ++pg) {
+    // this page is there: only the next may be on its way
+    if (pg + 1 < W.pg1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Pages::kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // for all; and the slot of the page before it is free
+    if (pg + 2 < W.pg1) here2 = pages.issue(pg + 2, word2);
+    const int left = here0 ? W.P - pg * kPage8 : 0;  // keys that exist, if below 64
+    if constexpr (NT > 0) group_page<NT, kLse>(lds + pages.slot_of(pg), (uint32_t)word0, left, tile);
+    here0 = here1, here1 = here2;
+    word0 = word1, word1 = word2;
   }
 }
 
-// 64 tree rows from j0 on, whose values lie in LDS at `values`.
-template <int NT, bool kLse>
-__device__ __forceinline__ void group_tree(const Args& A, const Work& W, int j0, const int (&row)[kWaveTiles],
-                                           uint8_t* values, uint64_t bad, Tile (&tile)[kWaveTiles]) {
-  const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
-  floatx4 s[NT][kKTiles];
-  tree_scores<NT, kKTiles>(A, W, j0, tile, s);
-  uint32_t see[NT];
+// 64 tree rows on their way through a thread's registers to LDS: row 16 i + tid / 16,
+// eight dims of its keys and values.
+struct TreeRows {
+  uint4 k[4], v[4];
+  __device__ __forceinline__ void load(const Args& A, const Work& W, int j0) {
 #pragma unroll
-  for (int i = 0; i < NT; ++i) see[i] = W.allowed<kKTiles>(A, row[i], j0, lg);
-  hide<NT, kKTiles>(s, see);
-  bf16x2 p[NT][2 * kKTiles];
-  weights<kLse, NT, kKTiles>(s, score_scale(), tile, p);
+    for (int i = 0; i < 4; ++i) {
+      const int r = j0 + 16 * i + (int)threadIdx.x / 16, c = 8 * ((int)threadIdx.x % 16);
+      k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < W.n) {
+        k[i] = *(const uint4*)(W.k_row(A, r) + c);
+        v[i] = *(const uint4*)(W.v_row(A, r) + c);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* keys, uint8_t* values, uint32_t* bad) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 16 * i + (int)threadIdx.x / 16, c = 16 * ((int)threadIdx.x % 16);
+      if (keep_finite(v[i])) atomicOr(&bad[r / 32], 1u << (r % 32));
+      *(uint4*)(keys + r * kRowBytes + c) = k[i];
+      *(uint4*)(values + r * kRowBytes + c) = v[i];
+    }
+  }
+};
+
+// 16 T tree rows from j0 on, which lie in LDS; `see`: which of them the lane's rows may.
+template <int NT, int T, bool kLse>
+__device__ __forceinline__ void group_tree(const Args& A, const Work& W, int j0, const uint32_t (&see)[kWaveTiles],
+                                           const uint8_t* keys, uint8_t* values, uint64_t bad, Tile (&tile)[kWaveTiles]) {
+  const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
+  floatx4 s[NT][T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) s[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bf16x8 k = *(const bf16x8*)(keys + (16 * t + lc) * kRowBytes + 128 * (u / 2) + 32 * lg + 16 * (u % 2));
+#pragma unroll
+      for (int i = 0; i < NT; ++i) s[i][t] = product(k, tile[i].q[u], s[i][t]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int t = 0; t < T; ++t) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[i][t]));
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int u = 0; u < 4 * T; ++u) s[i][u / 4][u % 4] = (see[i] >> u) & 1u ? s[i][u / 4][u % 4] : -INFINITY;
+  bf16x2 p[NT][2 * T];
+  weights<kLse, NT, T>(s, score_scale(), tile, p);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)values;
   lds_u8* const at = (lds_u8*)(uintptr_t)(lds0 + (uint32_t)((4 * lg + (lc >> 2)) * kRowBytes + (lc & 3) * 8));
-  tree_values<NT, kKTiles>(at, p, tile);
+  tree_values<NT, T>(at, p, tile);
   if (bad) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) add_marked<kKTiles>(A, W, bad, j0, p[i], see[i], tile[i].row);
+    for (int i = 0; i < NT; ++i) add_marked<T>(A, W, bad, j0, p[i], see[i], tile[i].row);
   }
 }
 
 template <bool kLse>
 __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
-  static_assert(kPage8 * kRowBytes <= 2 * kSlot, "tree values where the third and fourth page go");
+  static_assert(2 * kPage8 * kRowBytes <= kSlots * kSlot, "tree rows where the pages were");
   __shared__ __align__(16) uint8_t s_x[kSlots * kSlot];
   __shared__ uint32_t s_bad[2];
   const int tid = (int)threadIdx.x, lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
-  // consecutive workgroups of one XCD share a key head's pages in its L2
-  const int total = (int)gridDim.x, x = (int)blockIdx.x;
-  const int lin = total % kXcds == 0 ? (x % kXcds) * (total / kXcds) + x / kXcds : x;
-  const int chunk = lin % A.chunks;
+  const Place place = place_of((int)blockIdx.x, A.B * A.Hkv, A.chunks);
+  const int chunk = place.chunk;
   Work W;
-  if (!W.init(A, lin / A.chunks, (int)blockIdx.y)) return;
+  if (!W.init(A, place.pair, (int)blockIdx.y)) return;
   // a chunk's tiles, evenly; its waves have one or two, and which have two changes
   // from workgroup to workgroup, as a SIMD has one wave of each
   const int tile0 = (int)((int64_t)A.tiles * chunk / A.chunks), tile1 = (int)((int64_t)A.tiles * (chunk + 1) / A.chunks);
-  const int turn = (w + lin * 2) % kWaves;
+  const int turn = (w + 2 * (W.kv + chunk)) % kWaves;
   int row[kWaveTiles], mine = 0;
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
@@ -653,77 +815,51 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
     row[i] = t < tile1 ? t * kTile + lc : W.M;
   }
 
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)s_x;
-  const int32_t* table = A.table + (int64_t)W.b * A.max_pages;
-  const auto slot_of = [&](int pg) { return ((pg - W.pg0) & (kSlots - 1)) * kSlot; };
-  // page numbers and scales, 64 at a time in a register's lanes: read one by one they
-  // would be loads to wait for among the loads that are meant to stay in flight
-  int ids = 0, words = 0;
-  constexpr int kLoads = kSlot / (16 * fc::kWave) / kWaves;  // of a wave and page
-  const auto issue = [&](int pg, int& word) {
-    const int i = (pg - W.pg0) & 63;
-    if (i == 0) {
-      ids = pg + lane < W.pg1 ? table[pg + lane] : -1;
-      const bool there = ids >= 0 && ids < A.n_pages;
-      if (!there) ids = -1;
-      words = there ? *(const int*)(A.pool + ((int64_t)ids * A.Hkv + W.kv) * kPage8Bytes + fc::kPage8Scales) : 0;
-    }
-    const int id = __builtin_amdgcn_readlane(ids, i);
-    word = __builtin_amdgcn_readlane(words, i);
-    const bool there = id >= 0;  // an absent page's loads give zeros, and none of its keys counts
-    const fc::int32x4 rsrc = fc::buffer_rsrc(A.pool + ((int64_t)(there ? id : 0) * A.Hkv + W.kv) * kPage8Bytes,
-                                             there ? (uint32_t)kPage8Bytes : 0u);
-#pragma unroll
-    for (int l = 0; l < kLoads; ++l) {
-      const int at = (w * kLoads + l) * 1024;  // the first half of them are keys: eight rows a load
-      const int r = at / kDim8 + (lane >> 3), c = lane & 7;
-      const int from = at < fc::kPage8V ? r * kDim8 + 16 * (c ^ swap_of(r)) : at + 16 * lane;
-      fc::lds_load16(lds0 + (uint32_t)(slot_of(pg) + at), (uint32_t)from, rsrc);
-    }
-    return there;
-  };
-  bool here0 = false, here1 = false, here2 = false;  // whether page pg, pg + 1, pg + 2 is
-  int word0 = 0, word1 = 0, word2 = 0;
-  if (W.pg0 < W.pg1) here0 = issue(W.pg0, word0);
-  if (W.pg0 + 1 < W.pg1) here1 = issue(W.pg0 + 1, word1);
+  Pages pages(A, W, s_x, w);
+  bool here0 = false, here1 = false;
+  int word0 = 0, word1 = 0;
+  if (W.pg0 < W.pg1) here0 = pages.issue(W.pg0, word0);
+  if (W.pg0 + 1 < W.pg1) here1 = pages.issue(W.pg0 + 1, word1);
 
   Tile tile[kWaveTiles];
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) tile[i].load(W.q_row(A, row[i]), lg);
+  // Queries are waited for here: in the loop below the compiler would wait for them in
+  // every turn, and with them for the pages that are meant to stay on their way.
+#pragma unroll
+  for (int i = 0; i < kWaveTiles; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(tile[i].q[u]));
+
+  if (mine == 2) group_pages<2, kLse>(pages, s_x, here0, here1, word0, word1, tile);
+  else if (mine == 1) group_pages<1, kLse>(pages, s_x, here0, here1, word0, word1, tile);
+  else group_pages<0, kLse>(pages, s_x, here0, here1, word0, word1, tile);
 
   if (W.tree) {
-    uint8_t* const values = s_x + 2 * kSlot;
+    // 64 of its rows at a time: what is read of them, and which of them each query row
+    // may see, is asked for together, the next ones' before these are used
+    uint8_t *const keys = s_x, *const values = s_x + kPage8 * kRowBytes;
+    TreeRows rows;
+    rows.load(A, W, 0);
+    uint32_t see[kWaveTiles];
+    __syncthreads();  // the last page is used
     for (int j0 = 0; j0 < W.n; j0 += kPage8) {
+#pragma unroll
+      for (int i = 0; i < kWaveTiles; ++i) see[i] = W.allowed<kKTiles>(A, row[i], j0, lg);
       if (tid < 2) s_bad[tid] = 0;
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * i + tid / 16;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (j0 + r < W.n) v = *(const uint4*)(W.v_row(A, j0 + r) + 8 * (tid % 16));
-        if (keep_finite(v)) atomicOr(&s_bad[r / 32], 1u << (r % 32));
-        *(uint4*)(values + r * kRowBytes + 16 * (tid % 16)) = v;
-      }
+      rows.store(keys, values, s_bad);
       __syncthreads();
+      if (j0 + kPage8 < W.n) rows.load(A, W, j0 + kPage8);
       const uint64_t bad = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)s_bad[0]) |
                            (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)s_bad[1]) << 32;
-      if (mine == 2) group_tree<2, kLse>(A, W, j0, row, values, bad, tile);
-      else if (mine == 1) group_tree<1, kLse>(A, W, j0, row, values, bad, tile);
+      const bool few = W.n - j0 <= 32;  // a tree's 65th row
+      if (mine == 2 && few) group_tree<2, 2, kLse>(A, W, j0, see, keys, values, bad, tile);
+      else if (mine == 2) group_tree<2, kKTiles, kLse>(A, W, j0, see, keys, values, bad, tile);
+      else if (mine == 1 && few) group_tree<1, 2, kLse>(A, W, j0, see, keys, values, bad, tile);
+      else if (mine == 1) group_tree<1, kKTiles, kLse>(A, W, j0, see, keys, values, bad, tile);
       __syncthreads();
     }
-  }
-
-  for (int pg = W.pg0; pg < W.pg1; ++pg) {
-    // this page is there: only the next may be on its way
-    if (pg + 1 < W.pg1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // for all; and the slot of the page before it is free
-    if (pg + 2 < W.pg1) here2 = issue(pg + 2, word2);
-    const int left = here0 ? W.P - pg * kPage8 : 0;  // keys that exist, if below 64
-    if (mine == 2) group_page<2, kLse>(s_x + slot_of(pg), (uint32_t)word0, left, tile);
-    else if (mine == 1) group_page<1, kLse>(s_x + slot_of(pg), (uint32_t)word0, left, tile);
-    here0 = here1, here1 = here2;
-    word0 = word1, word1 = word2;
   }
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
@@ -813,7 +949,8 @@ __global__ void __launch_bounds__(kMergeWaves* fc::kWave) k_paged8_merge(Args A)
 
 struct Shape {
   int tiles, chunks, part_pages, parts;
-  bool alone;
+  int alone;     // waves of a workgroup whose waves take pages alone; 0: they share them
+  bool ordered;  // the longest prefixes first
 };
 
 // How a call is laid out: a workgroup for every eight tiles of query rows of a key
@@ -821,21 +958,24 @@ struct Shape {
 Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   Shape s;
   s.tiles = (R * (H / Hkv) + kTile - 1) / kTile;
-  s.alone = s.tiles <= kWaveTiles;
-  s.chunks = s.alone ? 1 : (s.tiles + kGroupTiles - 1) / kGroupTiles;
+  s.chunks = s.tiles <= kWaveTiles ? 1 : (s.tiles + kGroupTiles - 1) / kGroupTiles;
   const int64_t wgs = (int64_t)B * Hkv * s.chunks;
   const int64_t pages = ((int64_t)max_len + kPage8 - 1) / kPage8;
-  const int64_t slots = 2 * kCus;  // workgroups at once
-  int64_t each = s.alone ? 16 : 4;
+  s.alone = s.tiles > kWaveTiles ? 0 : pages >= 64 || wgs <= kCus ? 8 : 4;
+  const int64_t slots = s.alone == 8 ? kCus : 2 * kCus;  // workgroups at once
+  int64_t each = s.alone ? s.alone : 4;
   int64_t parts = (slots + (pages < 64 ? 0 : wgs - 1)) / wgs;
   if (parts > kMostParts) parts = kMostParts;
   const int64_t fit = (pages + each - 1) / each;
   if (parts > fit) parts = fit;
   if (parts < 1) parts = 1;
   each = (pages + parts - 1) / parts;
-  if (s.alone) each = (each + kWaves - 1) / kWaves * kWaves;
+  if (s.alone) each = (each + s.alone - 1) / s.alone * s.alone;
   s.part_pages = each < 1 ? 1 : (int)each;
   s.parts = pages <= s.part_pages ? 1 : (int)((pages + s.part_pages - 1) / s.part_pages);
+  // Where not all workgroups run at once, a long one that began last would be waited
+  // for alone.
+  s.ordered = B > 1 && wgs * s.parts > slots;
   return s;
 }
 
@@ -860,15 +1000,19 @@ bool sizes_ok(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
          H % Hkv == 0 && max_len >= 0 && max_len <= 0x7FFFFFFF - kPage8;
 }
 
+template <int NT, bool kLse>
+void launch_alone(const Args& a, const Shape& s, dim3 grid, hipStream_t stream) {
+  if (s.alone == 8)
+    hipLaunchKernelGGL((k_paged8_attn_alone<NT, 8, kLse>), grid, dim3(8 * fc::kWave), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_paged8_attn_alone<NT, 4, kLse>), grid, dim3(4 * fc::kWave), 0, stream, a);
+}
 template <bool kLse>
 void launch(const Args& a, const Shape& s, hipStream_t stream) {
   const dim3 grid((uint32_t)a.B * (uint32_t)a.Hkv * (uint32_t)s.chunks, (uint32_t)s.parts);
-  if (s.alone && s.tiles == 1)
-    hipLaunchKernelGGL((k_paged8_attn_alone<1, kLse>), grid, dim3(kThreads), 0, stream, a);
-  else if (s.alone)
-    hipLaunchKernelGGL((k_paged8_attn_alone<2, kLse>), grid, dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_paged8_attn<kLse>), grid, dim3(kThreads), 0, stream, a);
+  if (!s.alone) hipLaunchKernelGGL((k_paged8_attn<kLse>), grid, dim3(kThreads), 0, stream, a);
+  else if (s.tiles == 1) launch_alone<1, kLse>(a, s, grid, stream);
+  else launch_alone<2, kLse>(a, s, grid, stream);
 }
 
 }  // namespace
@@ -932,7 +1076,7 @@ extern "C" fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride
     const Args a = {q + row * q_stride, k_tree + row * k_stride, v_tree + row * v_stride, q_stride, k_stride, v_stride,
                     pool, table + (int64_t)b * max_pages, prefix_len + b, num_nodes ? num_nodes + b : nullptr,
                     mask ? mask + row * R : nullptr, n_pages, max_pages, now, R, H, Hkv, max_len, s.tiles, s.chunks,
-                    s.part_pages, s.parts, out + row * H * kDim8, lse ? lse + row * H : nullptr, part_ml, part_o};
+                    s.part_pages, s.parts, s.ordered && now <= kOrdered, out + row * H * kDim8, lse ? lse + row * H : nullptr, part_ml, part_o};
     if (lse) launch<true>(a, s, stream);
     else launch<false>(a, s, stream);
     FC_CHECK_LAUNCH();
