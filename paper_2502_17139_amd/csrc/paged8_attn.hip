@@ -305,18 +305,22 @@ __device__ __forceinline__ bf16x8 join(const bf16x2& a, const bf16x2& b, const b
 template <int NT, typename Key>
 __device__ __forceinline__ void page_scores(Key key, const Tile (&tile)[kWaveTiles], floatx4 (&s)[NT][kKTiles]) {
 #pragma unroll
-  for (int t = 0; t < kKTiles; ++t) {
+  for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
     for (int i = 0; i < NT; ++i) s[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint4 c = key(t, u);
-      const bf16x8 a = widen(c.x, c.y, 1.0f), b = widen(c.z, c.w, 1.0f);
+  for (int u = 0; u < 2; ++u) {  // no product waits for the one before
+    uint4 c[kKTiles];
 #pragma unroll
-      for (int i = 0; i < NT; ++i) s[i][t] = product(a, tile[i].q[2 * u], s[i][t]);
+    for (int t = 0; t < kKTiles; ++t) c[t] = key(t, u);
 #pragma unroll
-      for (int i = 0; i < NT; ++i) s[i][t] = product(b, tile[i].q[2 * u + 1], s[i][t]);
-    }
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < kKTiles; ++t) {
+        const bf16x8 a = h ? widen(c[t].z, c[t].w, 1.0f) : widen(c[t].x, c[t].y, 1.0f);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) s[i][t] = product(a, tile[i].q[2 * u + h], s[i][t]);
+      }
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i) settle(s[i]);

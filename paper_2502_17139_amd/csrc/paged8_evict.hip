@@ -46,119 +46,266 @@ __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
   return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
-// Sixteen values a lane to their sums over the 16 lanes of a row: lane lc gets the sum
-// of value lc.
-__device__ __forceinline__ float sum_of_own(float (&v)[16], int lc) {
+// 16 values a lane to their sums over the 16 lanes of a row: lane lc gets the sum of
+// value lc.  Lanes that differ in one bit (and in all below it, as the row's mirrors
+// have them) exchange the halves that the other keeps.
+template <int HALF, int CTRL>
+__device__ __forceinline__ void fold(float (&v)[16], int lc) {
+  const bool up = lc & HALF;
 #pragma unroll
-  for (int half = 8; half >= 1; half >>= 1) {
-    const bool up = lc & half;
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const float keep = up ? v[half + i] : v[i], send = up ? v[i] : v[half + i];
-      v[i] = keep + __shfl_xor(send, half);
-    }
+  for (int i = 0; i < HALF; ++i) {
+    const float keep = up ? v[HALF + i] : v[i], send = up ? v[i] : v[HALF + i];
+    v[i] = keep + __uint_as_float(fc::dpp_mov<CTRL>(__float_as_uint(send)));
   }
+}
+__device__ __forceinline__ float sum_of_own(float (&v)[16], int lc) {
+  fold<8, 0x140>(v, lc);  // row_mirror
+  fold<4, 0x141>(v, lc);  // row_half_mirror
+  fold<2, 0x1B>(v, lc);   // quad_perm 3 2 1 0
+  fold<1, 0xB1>(v, lc);   // quad_perm 1 0 3 2
   return v[0];
 }
 
-// A wave holds a page's keys as bf16 and goes through the sequence's rows, 16 at a
-// time, next ones on their way: S^T = K Q^T as in attention, so that lane (lg, lc) has
-// row lc's scores with keys 16 lg + 4 t + e, whose weights it adds up over the rows;
-// at the end the 16 lanes' sums are joined.  kShared: the waves of a workgroup take one
-// page, every fourth 16 rows each (prompts: many rows, few pages); otherwise a page
-// each.  Nothing is added by two workgroups, so sums have one order.
-template <bool kShared>
-__global__ void __launch_bounds__(kThreads, 2) k_paged8_weights(Weights A) {
-  __shared__ float s_sum[kWaves - 1][kPage8];
+// What a wave knows of its sequence and head.
+struct Step {
+  int len, end, G, kv, cu, n;  // n: new tokens, each with the group's G query heads as rows
+  float inv;                   // 1 / G
+  __device__ __forceinline__ Step(const Weights& A, int b, int kv_) {
+    kv = kv_, G = A.H / A.Hkv;
+    len = clamp_len(A.len[b], A.max_len), end = clamp_len(A.new_len[b], A.max_len);
+    cu = A.cu[b], n = end - len;
+    inv = 1.0f / (float)G;
+  }
+};
+// A place among a sequence's rows: a token and a head of its group, to go on from.
+struct Cursor {
+  int t, h;
+  __device__ __forceinline__ Cursor(const Step& S, int64_t row) : t((int)(row / S.G)), h((int)(row % S.G)) {}
+  __device__ __forceinline__ void operator+=(const Cursor& d) { t += d.t, h += d.h; }
+  __device__ __forceinline__ void carry(const Step& S) {
+    if (h >= S.G) h -= S.G, ++t;
+  }
+  // The row `on` (below 2^13) rows further: quotients of such numbers are exact in fp32.
+  __device__ __forceinline__ void at(const Step& S, int on, int& token, int& head) const {
+    const int x = h + on, q = (int)(((float)x + 0.5f) * S.inv);
+    token = t + q, head = x - q * S.G;
+  }
+};
+// New token t's row among the call's: what src says, whatever that is, so that nobody
+// waits for it before it is used.  A token or a place that is not there has none.
+template <bool kSrc>
+__device__ __forceinline__ int number_of(const Weights& A, const Step& S, int t) {
+  const int64_t at = (int64_t)S.cu + t;
+  const bool there = t < S.n && at >= 0 && at < A.n;
+  const int row = kSrc ? A.src[there ? at : 0] : (int)at;
+  return there ? row : -1;
+}
+// 16 rows of queries.  kAsCodes: lane (lg, lc) has dims 64 u + 16 lg + 8 h .. + 7 of row
+// lc in q[2 u + h], as 16 key codes lie; otherwise dims 32 u + 8 lg .. + 7 in q[u], so
+// that four lanes read 64 bytes of a row together.
+template <bool kAsCodes>
+struct Rows {
+  bf16x8 q[4];
+  float lse;
+  int last;  // the last key that the row sees; -1: there is no such row
+  __device__ __forceinline__ void load(const Weights& A, const Step& S, int token, int head, int number) {
+    const bool there = number >= 0 && number < A.n_rows;
+    const int row = there ? number : 0;
+    const int64_t h = S.kv * S.G + head;
+    const uint16_t* p = A.q + row * A.q_stride + h * kDim8 + (kAsCodes ? 16 : 8) * (fc::lane_id() >> 4);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = *(const bf16x8*)(p + (kAsCodes ? 64 * (u / 2) + 8 * (u % 2) : 32 * u));
+    lse = A.lse[(int64_t)row * A.H + h];
+    last = there ? S.len + token : -1;
+  }
+};
+// What 16 rows pay to a lane's keys key0 .. key0 + 4 T - 1, on top of `got`.  keys(t, u):
+// the u-th quarter of the dims of key tile t, whose row 4 a + b is key 4 T a + 4 t + b.
+template <int T, bool kAsCodes, typename Keys>
+__device__ __forceinline__ void pay(Keys keys, const Rows<kAsCodes>& x, float scale, int key0, float (&got)[4 * T]) {
+  floatx4 s[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int u = 0; u < 4; ++u)  // no product waits for the one before
+#pragma unroll
+    for (int t = 0; t < T; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys(t, u), x.q[u], s[t], 0, 0, 0);
+  // a product's result is read only some cycles after it was issued
+  static_assert(T == 4, "the wait below");
+  asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
+  const float minus = 0.0f - x.lse * kLog2e;
+  // the lane's keys that the row sees, less one; a row that saw nothing pays nothing
+  const int seen = x.lse == -INFINITY ? -1 : x.last - key0;
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, minus));
+      got[4 * t + e] += 4 * t + e <= seen ? p : 0.0f;
+    }
+}
+__device__ __forceinline__ float key_scale(uint32_t byte) {
+  return fc::scale8(byte) * (kLog2e / sqrtf((float)kDim8));
+}
+// A token's sum into its place: new tokens' weights become it.
+__device__ __forceinline__ void settle_weight(const Weights& A, const Step& S, int id, int j, float sum, bool again) {
+  float* to = A.weights + ((int64_t)id * A.Hkv + S.kv) * kPage8 + j % kPage8;
+  if (j < S.end) *to = j < S.len || again ? *to + sum : sum;
+}
+
+// Many rows (prompts): a workgroup's waves hold a page's keys as bf16 and go through the
+// sequence's rows, every eighth 16 of them each, four of those on their way; the waves'
+// sums are joined.  Nothing is added by two workgroups, so sums have one order.
+constexpr int kAhead = 4, kManyWaves = 8;
+template <bool kSrc>
+__global__ void __launch_bounds__(kManyWaves* fc::kWave, 2) k_weights_many(Weights A) {
+  constexpr int T = kKTiles;
+  __shared__ float s_sum[kManyWaves - 1][kPage8];
   const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
-  const int b = (int)blockIdx.y, kv = (int)blockIdx.z;
-  const int pg = kShared ? (int)blockIdx.x : (int)blockIdx.x * kWaves + w;
-  const int len = clamp_len(A.len[b], A.max_len), end = clamp_len(A.new_len[b], A.max_len);
-  const int G = A.H / A.Hkv;
-  const int64_t M = (int64_t)(end - len) * G;
-  if (M <= 0 || pg * kPage8 >= end) return;  // with kShared: all waves of the workgroup
+  // a head's pages lie on one XCD, whose L2 has its rows then; the first ones, which most
+  // rows see, begin first
+  const int b = (int)blockIdx.x / A.Hkv, pg = (int)blockIdx.y;
+  const Step S(A, b, (int)blockIdx.x % A.Hkv);
+  if (S.n <= 0 || pg * kPage8 >= S.end) return;  // all waves of the workgroup
   const int id = A.table[(int64_t)b * A.max_pages + pg];
   if (id < 0 || id >= A.n_pages) return;
-  const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + kv) * kPage8Bytes;
-  const int key_row = 16 * (lc >> 2) + (lc & 3);
-  bf16x8 key[kKTiles][4];
-#pragma unroll
-  for (int t = 0; t < kKTiles; ++t)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint4 c = *(const uint4*)(page + (key_row + 4 * t) * kDim8 + 64 * u + 16 * lg);
-      key[t][2 * u] = widen(c.x, c.y);
-      key[t][2 * u + 1] = widen(c.z, c.w);
-    }
-  const float scale = fc::scale8(page[fc::kPage8Scales + (lg >> 1)]) * (kLog2e / sqrtf((float)kDim8));
-  const int key0 = pg * kPage8 + 16 * lg;  // the lane's first key
-  float got[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) got[i] = 0.0f;
-
-  const int cu = A.cu[b];
-  struct Rows {
-    bf16x8 q[4];
-    float minus;  // 0 - lse, base 2
-    int last;     // the last key that the row sees; -1: it pays nothing
-  };
-  const auto load = [&](int64_t r, Rows& x) {
-    // a row past the last one: the last one, for nothing
-    const bool in = r < M;
-    const int64_t rr = in ? r : M - 1;
-    const int t = (int)(rr / G), h = kv * G + (int)(rr - (int64_t)t * G);
-    const int64_t at = (int64_t)cu + t;
-    bool ok = in && at >= 0 && at < A.n;
-    int64_t row = ok ? (A.src ? (int64_t)A.src[at] : at) : 0;
-    ok = ok && row >= 0 && row < A.n_rows;
-    if (!ok) row = 0;
-    const uint16_t* p = A.q + row * A.q_stride + (int64_t)h * kDim8 + 16 * lg;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) x.q[u] = *(const bf16x8*)(p + 64 * (u / 2) + 8 * (u % 2));
-    const float lse = A.lse[row * A.H + h];
-    x.minus = 0.0f - lse * kLog2e;
-    x.last = ok && lse != -INFINITY ? len + t : -1;
-  };
   // rows that come before the page's first key see nothing of it
-  const int64_t skip = (int64_t)pg * kPage8 - len;
-  int64_t tile = skip > 0 ? skip * G / kTile : 0;
-  const int64_t step = kShared ? kWaves : 1;
-  if (kShared) tile += w;
-  Rows x;
-  if (tile * kTile < M) load(tile * kTile + lc, x);
-  for (; tile * kTile < M; tile += step) {
-    Rows next = x;
-    if ((tile + step) * kTile < M) load((tile + step) * kTile + lc, next);
-    floatx4 s[kKTiles];
+  const int64_t skip = (int64_t)pg * kPage8 - S.len;
+  const int64_t tiles = ((int64_t)S.n * S.G + kTile - 1) / kTile;
+  int64_t tile = (skip > 0 ? skip * S.G / kTile : 0) + w;
+  constexpr int kRound = kManyWaves * kAhead * kTile;  // rows of a round of the waves
+  const Cursor round(S, kRound);
+  Cursor now(S, tile * kTile), next = now;
+  // numbers of a round's rows, a tile in each 16 lanes
+  const auto numbers = [&](const Cursor& c) {
+    int token, head;
+    c.at(S, kManyWaves * kTile * lg + lc, token, head);
+    return number_of<kSrc>(A, S, token);
+  };
+  const auto go_on = [&](Cursor& c) {
+    c += round;
+    c.carry(S);
+  };
+  Rows<false> x[kAhead];
+  const auto load = [&](const Cursor& c, int n, int i) {
+    int token, head;
+    c.at(S, kManyWaves * kTile * i + lc, token, head);
+    x[i].load(A, S, token, head, __shfl(n, 16 * i + lc));
+    asm volatile("" ::: "memory");  // asked for here and no later
+  };
+  int n_now = numbers(now);
+  go_on(next);
+  int n_next = numbers(next);
 #pragma unroll
-    for (int t = 0; t < kKTiles; ++t) {
-      s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < kAhead; ++i) load(now, n_now, i);
+  const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + S.kv) * kPage8Bytes;
+  const int key_row = 4 * T * (lc >> 2) + (lc & 3);
+  bf16x8 key[T][4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key[t][u], x.q[u], s[t], 0, 0, 0);
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint2 c = *(const uint2*)(page + (key_row + 4 * t) * kDim8 + 32 * u + 8 * lg);
+      key[t][u] = widen(c.x, c.y);
     }
-    // a product's result is read only some cycles after it was issued
-    asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
+  const float scale = key_scale(page[fc::kPage8Scales + (lg >> 1)]);
+  float got[4 * T];
+#pragma unroll
+  for (int i = 0; i < 4 * T; ++i) got[i] = 0.0f;
+  for (; tile < tiles; tile += kManyWaves * kAhead) {
+    now = next;
+    n_now = n_next;
+    go_on(next);
+    n_next = numbers(next);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      pay<T>([&](int t, int u) { return key[t][u]; }, x[i], scale, pg * kPage8 + 4 * T * lg, got);
+      asm volatile("" ::: "memory");
+      load(now, n_now, i);
+    }
+  }
+  float sum = sum_of_own(got, lc);  // of key 16 lg + lc
+  if (w > 0) s_sum[w - 1][lane] = sum;
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int g = 0; g < kManyWaves - 1; ++g) sum += s_sum[g][lane];
+  settle_weight(A, S, id, pg * kPage8 + lane, sum, false);
+}
+
+// Few rows (a token, an accepted path): a wave holds up to 64 of them and goes through
+// every fourth of its part's pages, the next one's keys on their way.  More rows are
+// more rounds of the same pages.
+constexpr int kFewTiles = 4;
+template <bool kSrc>
+__global__ void __launch_bounds__(kThreads, 2) k_weights_few(Weights A, int part_pages) {
+  const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
+  const int b = (int)blockIdx.x / A.Hkv;
+  const Step S(A, b, (int)blockIdx.x % A.Hkv);
+  const int pages = (S.end + kPage8 - 1) / kPage8;
+  const int pg0 = (int)blockIdx.y * part_pages + w;
+  const int pg1 = ((int)blockIdx.y + 1) * part_pages < pages ? ((int)blockIdx.y + 1) * part_pages : pages;
+  if (S.n <= 0 || pg0 >= pg1) return;
+  const int32_t* table = A.table + (int64_t)b * A.max_pages;
+  const uint32_t k_at = (uint32_t)((16 * (lc >> 2) + (lc & 3)) * kDim8 + 16 * lg);
+  uint4 k[kKTiles][2];
+  uint32_t word = 0;
+  const auto load_page = [&](int id) {
+    if (id < 0 || id >= A.n_pages) return;
+    const uint8_t* p = A.pool + ((int64_t)id * A.Hkv + S.kv) * kPage8Bytes;
 #pragma unroll
     for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, x.minus));
-        got[4 * t + e] += key0 + 4 * t + e <= x.last ? p : 0.0f;
-      }
-    x = next;
-  }
-  float sum = sum_of_own(got, lc);  // of key 16 lg + lc
-  if (kShared) {
-    if (w > 0) s_sum[w - 1][lane] = sum;
-    __syncthreads();
-    if (w > 0) return;
+      for (int u = 0; u < 2; ++u) k[t][u] = *(const uint4*)(p + k_at + (4 * t * kDim8 + 64 * u));
+    word = *(const uint32_t*)(p + fc::kPage8Scales);
+  };
+  constexpr int kRound = kFewTiles * kTile;
+  const int64_t rows = (int64_t)S.n * S.G;
+  const Cursor round(S, kRound);
+  Cursor c(S, 0);
+  for (int64_t r0 = 0; r0 < rows; r0 += kRound) {
+    int id = table[pg0], token, head;
+    c.at(S, lane, token, head);
+    const int mine = number_of<kSrc>(A, S, token);  // a row a lane
+    load_page(id);
+    Rows<true> x[kFewTiles];
+    const int n = rows - r0 < kRound ? (int)((rows - r0 + kTile - 1) / kTile) : kFewTiles;
 #pragma unroll
-    for (int g = 0; g < kWaves - 1; ++g) sum += s_sum[g][lane];
+    for (int i = 0; i < kFewTiles; ++i)
+      if (i < n) {
+        c.at(S, kTile * i + lc, token, head);
+        x[i].load(A, S, token, head, __shfl(mine, kTile * i + lc));
+      }
+    c += round;
+    c.carry(S);
+    for (int pg = pg0; pg < pg1; pg += kWaves) {
+      const int next = pg + kWaves < pg1 ? table[pg + kWaves] : -1;
+      if (id >= 0 && id < A.n_pages) {
+        bf16x8 key[kKTiles][4];
+#pragma unroll
+        for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            key[t][2 * u] = widen(k[t][u].x, k[t][u].y);
+            key[t][2 * u + 1] = widen(k[t][u].z, k[t][u].w);
+          }
+        const float scale = key_scale((word >> (8 * (lg >> 1))) & 255u);
+        load_page(next);
+        float got[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) got[i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kFewTiles; ++i)
+          if (i < n) pay<kKTiles>([&](int t, int u) { return key[t][u]; }, x[i], scale, pg * kPage8 + 16 * lg, got);
+        settle_weight(A, S, id, pg * kPage8 + lane, sum_of_own(got, lc), r0 > 0);  // key 16 lg + lc
+      } else {
+        load_page(next);
+      }
+      id = next;
+    }
   }
-  const int j = key0 + lc;
-  float* to = A.weights + ((int64_t)id * A.Hkv + kv) * kPage8 + lane;
-  if (j < end) *to = j < len ? *to + sum : sum;
 }
 
 // ------------------------------------------------------------------ evict --
@@ -473,14 +620,21 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
   const Weights a = {weights, q, q_stride, lse, pool, table, len, new_len, cu, src, n_rows, n_pages, max_pages, n, H, Hkv,
                      max_len};
   const uint32_t pages = fc::div_up((uint64_t)max_len, kPage8);
-  // several times 16 rows for each sequence, or too few pages for the card: its waves
-  // share them
-  const bool shared = (int64_t)n * (H / Hkv) > 8 * kTile * (int64_t)B;
   (void)hipGetLastError();
-  if (shared)
-    hipLaunchKernelGGL(k_paged8_weights<true>, dim3(pages, B, Hkv), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(k_paged8_weights<false>, dim3(fc::div_up(pages, kWaves), B, Hkv), dim3(kThreads), 0, stream, a);
+  // More rows than a wave holds twice over: pages are held, rows go by.
+  if ((int64_t)n * (H / Hkv) > 2 * kFewTiles * kTile * (int64_t)B) {
+    const dim3 grid(B * Hkv, pages), threads(kManyWaves * fc::kWave);
+    if (src) hipLaunchKernelGGL(k_weights_many<true>, grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL(k_weights_many<false>, grid, threads, 0, stream, a);
+  } else {
+    // four pages a wave, or fewer where that leaves the card idle
+    const int64_t pairs = (int64_t)B * Hkv;
+    int each = 4;
+    while (each > 1 && pairs * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
+    const dim3 grid(B * Hkv, fc::div_up(pages, (uint32_t)(each * kWaves)));
+    if (src) hipLaunchKernelGGL(k_weights_few<true>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+    else hipLaunchKernelGGL(k_weights_few<false>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+  }
   FC_CHECK_LAUNCH();
   return FC_OK;
 }
