@@ -348,7 +348,10 @@ __device__ __forceinline__ uint32_t rank_of(float w) { return w > 0.0f ? __float
 // A workgroup finds what one head of one sequence keeps: the weight of the last one to
 // stay, 11 bits at a time from the top, by counting; then, in order, which tokens are
 // above it, and of those that equal it the first ones.  A wave's lanes are a page's
-// tokens.
+// tokens, a wave's pages follow one another, and 16 of them are read together: up to
+// 16,384 tokens stay in registers, longer sequences are read again for each of the five
+// turns.
+constexpr int kTogether = 16;
 __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
   __shared__ uint32_t s_bins[kBins];
   __shared__ uint32_t s_sum[kSelWaves + 1];
@@ -365,10 +368,31 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
   int32_t* flags = A.flags + bk * (A.pages + 1);
   const int pages = (c.n + kPage8 - 1) / kPage8;
   for (int p = tid; p <= A.pages; p += kSelThreads) flags[p] = 0;
-  const auto weight = [&](int p) {
-    const int id = table[p];
-    const bool there = id >= 0 && id < A.n_pages;
-    return there ? rank_of(A.weights[((int64_t)id * A.Hkv + kv) * kPage8 + lane]) : 0u;
+  const int p0 = (int)((int64_t)pages * w / kSelWaves), p1 = (int)((int64_t)pages * (w + 1) / kSelWaves);
+  uint32_t rank[kTogether];  // of pages at .. at + 15
+  const auto load = [&](int at) {
+    // a page number a lane; what is not there has weight 0
+    int id = lane < kTogether && at + lane < p1 ? table[at + lane] : -1;
+    if (id >= A.n_pages) id = -1;
+    float x[kTogether];
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      const int page = __builtin_amdgcn_readlane(id, i);
+      x[i] = A.weights[((int64_t)(page < 0 ? 0 : page) * A.Hkv + kv) * kPage8 + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) rank[i] = __builtin_amdgcn_readlane(id, i) < 0 ? 0u : rank_of(x[i]);
+  };
+  const bool held = p1 - p0 <= kTogether;
+  if (held) load(p0);
+  // f(page, the lane's token's rank) for the wave's pages in their order
+  const auto each_page = [&](auto f) {
+    for (int at = p0; at < p1; at += kTogether) {
+      if (!held) load(at);
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i)
+        if (at + i < p1) f(at + i, rank[i]);
+    }
   };
   const int lo = c.lo, hi = c.hi;
   const uint32_t heavy = (uint32_t)c.heavy;
@@ -378,12 +402,11 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
       const int shift = level == 0 ? 20 : level == 1 ? 9 : 0, bits = level == 2 ? 9 : 11;
       for (int i = tid; i < kBins; i += kSelThreads) s_bins[i] = 0;
       __syncthreads();
-      for (int p = w; p < pages; p += kSelWaves) {
+      each_page([&](int p, uint32_t r) {
         const int t = p * kPage8 + lane;
-        const uint32_t r = weight(p);
         if (t >= lo && t < hi && (level == 0 || (r >> (shift + bits)) == found))
           atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1u)], 1u);
-      }
+      });
       __syncthreads();
       // two bins a thread, from the largest down
       const int top = kBins - 1 - 2 * tid;
@@ -397,31 +420,29 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
       __syncthreads();
     }
   }
-  // each wave's pages follow one another; first how many it has of either kind
-  const int p0 = (int)((int64_t)pages * w / kSelWaves), p1 = (int)((int64_t)pages * (w + 1) / kSelWaves);
-  const auto kinds = [&](int p, uint64_t& stays, uint64_t& equal) {
+  // how many each wave has that stay, and that do if there is room, then which they are
+  const auto kinds = [&](int p, uint32_t r, uint64_t& stays, uint64_t& equal) {
     const int t = p * kPage8 + lane;
-    const uint32_t r = weight(p);
     const bool by_weight = heavy > 0 && t >= lo && t < hi;
     stays = fc::ballot(t < lo || (t >= c.late && t < c.n) || (by_weight && r > found));
     equal = fc::ballot(by_weight && r == found);
   };
   uint32_t sure = 0, maybe = 0;
-  for (int p = p0; p < p1; ++p) {
+  each_page([&](int p, uint32_t r) {
     uint64_t stays, equal;
-    kinds(p, stays, equal);
+    kinds(p, r, stays, equal);
     sure += (uint32_t)__popcll(stays);
     maybe += (uint32_t)__popcll(equal);
-  }
+  });
   if (lane == 0) s_wave[0][w] = sure, s_wave[1][w] = maybe;
   __syncthreads();
   sure = maybe = 0;
   for (int i = 0; i < w; ++i) sure += s_wave[0][i], maybe += s_wave[1][i];
   int32_t* before = A.before + bk * (A.pages + 1);
   int32_t* from = A.from + bk * A.max_len;
-  for (int p = p0; p < p1; ++p) {
+  each_page([&](int p, uint32_t r) {
     uint64_t stays, equal;
-    kinds(p, stays, equal);
+    kinds(p, r, stays, equal);
     const uint32_t at = sure + (maybe < left ? maybe : left);
     const uint64_t below = fc::lanemask_lt();
     const bool taken = ((equal >> lane) & 1u) && maybe + (uint32_t)__popcll(equal & below) < left;
@@ -430,151 +451,211 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
     if ((all >> lane) & 1u) from[at + (uint32_t)__popcll(all & below)] = p * kPage8 + lane;
     sure += (uint32_t)__popcll(stays);
     maybe += (uint32_t)__popcll(equal);
-  }
+  });
   if (tid == 0) before[pages] = c.keep;
 }
 
 constexpr int kMoveThreads = 256;
+constexpr int kMoveAtOnce = 4 * 256;  // workgroups that run at once
 constexpr int kMoveWaves = kMoveThreads / fc::kWave;
 
-// A workgroup brings 64 tokens to one page of their new places.  They come from this
-// page and later ones; it reads them into registers, says so, waits until the pages
-// ahead of it that read from this one have said so too (two at most), and writes.
-// Pages are begun in the order of a counter, so that whoever is waited for has begun,
+// Codes as numbers that sort as their magnitudes do, 0 for a NaN.  Eight times an
+// exponent on top is a code's magnitude at that scale, as long as the code is a normal
+// number (8 or more): an exponent is three bits above the mantissa's last.
+__device__ __forceinline__ uint32_t magnitude7(uint32_t code) {
+  const uint32_t m = code & 127u;
+  return m == 127u ? 0u : m;
+}
+// What makes a token's codes those of another scale: 2^(was - now), as far as it matters
+// (below, codes become 0; above, there are none but zeros and NaN).
+__device__ __forceinline__ float ratio8(int was, int now) {
+  const int e = was - now;
+  return e < -126 ? 0.0f : fc::power8(e > 127 ? 127 : e);
+}
+
+// A workgroup brings 64 tokens to one page of their new places at a time.  They come
+// from this page and later ones; it reads them into registers, says so, waits until the
+// pages ahead of it that read from this one have said so too (two at most), and writes.
+// Pages are taken in the order of a counter, so that whoever is waited for has begun,
 // and nobody waits before it has read: the wait ends.  Two waves a block of 32: keys 16
 // bytes a lane, values a dim a lane, whose bytes lie 16 apart.
-__global__ void __launch_bounds__(kMoveThreads) k_evict_move(Evict A) {
+__global__ void __launch_bounds__(kMoveThreads, 4) k_evict_move(Evict A) {
   __shared__ int s_page;
-  __shared__ uint32_t s_top[2][kMoveWaves];
-  __shared__ int s_from[kPage8];
-  __shared__ int64_t s_base[kPage8];   // of the page that a token comes from; -1: none
-  __shared__ int s_exp[2][kPage8];     // of its keys' and values' scale
+  __shared__ int s_top[2][kMoveWaves];
   const int tid = (int)threadIdx.x, lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
-  const int kv = (int)blockIdx.y, b = (int)blockIdx.z;
+  const int kv = (int)blockIdx.x % A.Hkv, b = (int)blockIdx.x / A.Hkv;
   const Cut c(A, b);
-  if (c.keep >= c.n || (int)blockIdx.x * kPage8 >= c.keep) return;
+  if (c.keep >= c.n || c.keep == 0) return;
   const int64_t bk = (int64_t)b * A.Hkv + kv;
   const int32_t* table = A.table + (int64_t)b * A.max_pages;
-  int32_t* flags = A.flags + bk * (A.pages + 1);
-  if (tid == 0) s_page = __hip_atomic_fetch_add(&flags[A.pages], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  const int pg = __builtin_amdgcn_readfirstlane(s_page);
-  const int here = c.keep - pg * kPage8 < kPage8 ? c.keep - pg * kPage8 : kPage8;  // tokens of the page
-  const int32_t* from = A.from + bk * A.max_len + (int64_t)pg * kPage8;
-  float weight = 0.0f;
-  if (tid < kPage8) {
-    const int t = tid < here ? from[tid] : -1;
-    const int id = t >= 0 ? table[t / kPage8] : -1;
-    const bool there = id >= 0 && id < A.n_pages;
-    const int64_t base = there ? ((int64_t)id * A.Hkv + kv) : -1;
-    s_from[tid] = t % kPage8;
-    s_base[tid] = base;
-    const uint8_t* scales = A.pool + (there ? base : 0) * kPage8Bytes + fc::kPage8Scales + (there ? t % kPage8 / kBlock8 : 0);
-    s_exp[0][tid] = there ? fc::clamp_exp8((int)scales[0] - 127) : fc::kLeastExp8;
-    s_exp[1][tid] = there ? fc::clamp_exp8((int)scales[2] - 127) : fc::kLeastExp8;
-    if (there) weight = A.weights[base * kPage8 + t % kPage8];
-  }
-  __syncthreads();
-  const int half = w >> 1, t0 = half * kBlock8;  // the wave's block
-  // keys: 16 rows a wave, eight lanes each
-  uint4 k[2];
-  int k_exp[2];
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int t = t0 + 16 * (w & 1) + 8 * p + (lane >> 3);
-    const int64_t base = s_base[t];
-    k[p] = make_uint4(0u, 0u, 0u, 0u);
-    k_exp[p] = s_exp[0][t];
-    if (base >= 0) k[p] = *(const uint4*)(A.pool + base * kPage8Bytes + s_from[t] * kDim8 + 16 * (lane & 7));
-  }
-  // values: every token of the block, one dim a lane
-  const int d = 64 * (w & 1) + lane;
-  uint32_t v[kBlock8];
-#pragma unroll
-  for (int i = 0; i < kBlock8; ++i) {
-    const int64_t base = s_base[t0 + i];
-    v[i] = 0;
-    if (base >= 0) v[i] = A.pool[base * kPage8Bytes + fc::v8_at(s_from[t0 + i], d)];
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all of it is here
-  __syncthreads();
-  if (tid == 0) __hip_atomic_store(&flags[pg], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-
-  // the largest magnitudes of the block, then its codes
-  const auto magnitude = [&](float x, int e) { return fc::reach8(x * fc::power8(e)); };
-  uint32_t top[2] = {0, 0};
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const uint32_t words[4] = {k[p].x, k[p].y, k[p].z, k[p].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const fc::floatx2_8 x = hi ? __builtin_amdgcn_cvt_pk_f32_fp8((int)words[i], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)words[i], false);
-        const uint32_t a = magnitude(x[0], k_exp[p]), m = magnitude(x[1], k_exp[p]);
-        top[0] = a > top[0] ? a : top[0];
-        top[0] = m > top[0] ? m : top[0];
-      }
-  }
-#pragma unroll
-  for (int i = 0; i < kBlock8; ++i) {
-    const uint32_t a = magnitude(__builtin_amdgcn_cvt_f32_fp8((int)v[i], 0), s_exp[1][t0 + i]);
-    top[1] = a > top[1] ? a : top[1];
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int o = 1; o < fc::kWave; o <<= 1) {
-      const uint32_t x = (uint32_t)__shfl_xor((int)top[i], o);
-      top[i] = x > top[i] ? x : top[i];
-    }
-    if (lane == 0) s_top[i][w] = top[i];
-  }
-  __syncthreads();
-  int e[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t x = s_top[i][w & ~1], y = s_top[i][w | 1];
-    e[i] = fc::exponent8(x > y ? x : y);
-  }
-  const auto ratio = [&](int was, int now) { return was - now < -126 ? 0.0f : fc::power8(was - now); };
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const float f = ratio(k_exp[p], e[0]);
-    k[p] = make_uint4(fc::recode8(k[p].x, f), fc::recode8(k[p].y, f), fc::recode8(k[p].z, f), fc::recode8(k[p].w, f));
-  }
-  uint32_t codes[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float x[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      x[u] = __builtin_amdgcn_cvt_f32_fp8((int)v[4 * i + u], 0) * ratio(s_exp[1][t0 + 4 * i + u], e[1]);
-    codes[i] = fc::codes8(x[0], x[1], x[2], x[3]);
-  }
-
-  // tokens of this page stay for pages ahead: those have to be read
   const int32_t* before = A.before + bk * (A.pages + 1);
-  const int q0 = before[pg] / kPage8, q1 = (before[pg + 1] - 1) / kPage8;
-  if (tid == 0 && before[pg] < before[pg + 1]) {
-    for (int q = q0; q <= q1 && q < pg; ++q)
-      while (__hip_atomic_load(&flags[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0) __builtin_amdgcn_s_sleep(1);
+  int32_t* flags = A.flags + bk * (A.pages + 1);
+  const int pages = (c.keep + kPage8 - 1) / kPage8;
+  const int half = w >> 1, t0 = half * kBlock8;  // the wave's block
+  const uint32_t d = (uint32_t)(64 * (w & 1) + lane);
+  const auto take_page = [&]() {
+    if (tid == 0) s_page = __hip_atomic_fetch_add(&flags[A.pages], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  take_page();
+  for (;;) {
+    __syncthreads();
+    const int pg = __builtin_amdgcn_readfirstlane(s_page);
+    if (pg >= pages) return;
+    const int here = c.keep - pg * kPage8 < kPage8 ? c.keep - pg * kPage8 : kPage8;  // tokens of the page
+    // lane i (and i + 32) has token t0 + i: its place, its scales, its weight
+    const int mine = t0 + (lane & 31);
+    const int t = mine < here ? A.from[bk * A.max_len + (int64_t)pg * kPage8 + mine] : -1;
+    const int q0 = before[pg], q1 = before[pg + 1];
+    const int to = table[pg];
+    int id = t >= 0 ? table[t / kPage8] : -1;
+    if (id >= A.n_pages) id = -1;
+    const int64_t base = (int64_t)(id < 0 ? 0 : id) * A.Hkv + kv;  // what is not there reads page 0, for nothing
+    const int row = id < 0 ? 0 : t % kPage8;
+    const uint8_t* scales = A.pool + base * kPage8Bytes + fc::kPage8Scales + row / kBlock8;
+    const int k_byte = scales[0], v_byte = scales[2];
+    const float weight = A.weights[base * kPage8 + row];
+    // keys: 16 rows a wave, eight lanes each
+    const int64_t at = base * kPage8Bytes + row * kDim8;  // of the token's keys
+    uint4 k[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int64_t key = __shfl(at, 16 * (w & 1) + 8 * p + (lane >> 3));
+      k[p] = *(const uint4*)(A.pool + key + 16 * (lane & 7));
+    }
+    // values: every token of the block, one dim a lane
+    const int64_t v_at = base * kPage8Bytes + fc::v8_at(row, 0);
+    uint32_t v[kBlock8];
+#pragma unroll
+    for (int i = 0; i < kBlock8; ++i) {
+      const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v_at, i);
+      const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v_at >> 32), i);
+      v[i] = (A.pool + (((uint64_t)hi << 32) | lo))[d * fc::kQuarter8];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all of it is here
+    __syncthreads();
+    if (tid == 0) __hip_atomic_store(&flags[pg], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    take_page();  // the next one
+
+    // The largest magnitude of each block, as magnitude7 plus eight times the exponent
+    // (-1024: none).  Codes below 8 count as nothing where one above them is as large at
+    // the block's largest scale; where none is, their exact magnitudes decide.
+    constexpr int kNone = -1024;
+    const int k_exp = id < 0 ? kNone : fc::clamp_exp8(k_byte - 127), v_exp = id < 0 ? kNone : fc::clamp_exp8(v_byte - 127);
+    int k_from[2], top[2] = {0, 0}, least[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      k_from[p] = __shfl(k_exp, 16 * (w & 1) + 8 * p + (lane >> 3));
+      if (k_from[p] == kNone) k[p] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    const auto code_of = [](const uint4& x, int i) { return ((i < 4 ? x.x : i < 8 ? x.y : i < 12 ? x.z : x.w) >> (8 * (i & 3))) & 255u; };
+    const auto all_lanes = [](int x, auto join) {
+#pragma unroll
+      for (int o = 1; o < fc::kWave; o <<= 1) x = join(x, __shfl_xor(x, o));
+      return x;
+    };
+    const auto larger = [](int x, int y) { return x > y ? x : y; };
+    top[0] = top[1] = 8 * kNone;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t m = magnitude7(code_of(k[p], i));
+        most = m > most ? m : most;
+      }
+      if (most > 0) top[0] = larger(top[0], (int)most + 8 * k_from[p]);
+    }
+#pragma unroll
+    for (int i = 0; i < kBlock8; ++i) {
+      const int e = __builtin_amdgcn_readlane(v_exp, i);
+      if (e == kNone) v[i] = 0;
+      const uint32_t m = magnitude7(v[i]);
+      top[1] = larger(top[1], m > 0 ? (int)m + 8 * e : 8 * kNone);
+    }
+    // the block's largest exponents: those of its tokens, which every wave has
+    least[0] = all_lanes(k_exp, larger);
+    least[1] = all_lanes(v_exp, larger);
+    top[0] = all_lanes(top[0], larger);
+    top[1] = all_lanes(top[1], larger);
+    if (lane == 0) s_top[0][w] = top[0], s_top[1][w] = top[1];
+    __syncthreads();
+    int e[2];
+    bool exact = false;  // whether a small code's own magnitude may decide
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int x = larger(s_top[i][w & ~1], s_top[i][w | 1]);
+      // 448 is code 126
+      e[i] = x <= 8 * kNone ? fc::kLeastExp8 : fc::clamp_exp8((x - 126 + 7) >> 3);
+      exact |= x > 8 * kNone && x < 8 + 8 * least[i];
+    }
+    if (__any(exact)) {  // both waves of a block alike
+      uint32_t bits[2] = {0, 0};
+      const auto reach = [](uint32_t code, int e) { return fc::reach8(__builtin_amdgcn_cvt_f32_fp8((int)code, 0) * fc::power8(e)); };
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t m = k_from[p] == kNone ? 0u : reach(code_of(k[p], i), k_from[p]);
+          bits[0] = m > bits[0] ? m : bits[0];
+        }
+#pragma unroll
+      for (int i = 0; i < kBlock8; ++i) {
+        const int from = __builtin_amdgcn_readlane(v_exp, i);
+        const uint32_t m = from == kNone ? 0u : reach(v[i], from);
+        bits[1] = m > bits[1] ? m : bits[1];
+      }
+      top[0] = all_lanes((int)bits[0], larger);
+      top[1] = all_lanes((int)bits[1], larger);
+    }
+    __syncthreads();
+    if (lane == 0) s_top[0][w] = top[0], s_top[1][w] = top[1];
+    __syncthreads();
+    if (__any(exact)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) e[i] = fc::exponent8((uint32_t)larger(s_top[i][w & ~1], s_top[i][w | 1]));
+    }
+    // codes at another scale are rounded anew
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+      if (__any(k_from[p] != kNone && k_from[p] != e[0])) {
+        const float f = k_from[p] == kNone ? 0.0f : ratio8(k_from[p], e[0]);
+        k[p] = make_uint4(fc::recode8(k[p].x, f), fc::recode8(k[p].y, f), fc::recode8(k[p].z, f), fc::recode8(k[p].w, f));
+      }
+    uint32_t codes[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) codes[i] = v[4 * i] | v[4 * i + 1] << 8 | v[4 * i + 2] << 16 | v[4 * i + 3] << 24;
+    if (__any(v_exp != kNone && v_exp != e[1])) {
+      const float f = v_exp == kNone ? 0.0f : ratio8(v_exp, e[1]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          x[u] = __builtin_amdgcn_cvt_f32_fp8((int)v[4 * i + u], 0) *
+                 __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), 4 * i + u));
+        codes[i] = fc::codes8(x[0], x[1], x[2], x[3]);
+      }
+    }
+
+    // tokens of this page stay for pages ahead: those have to be read
+    if (tid == 0 && q0 < q1) {
+      for (int q = q0 / kPage8; q <= (q1 - 1) / kPage8 && q < pg; ++q)
+        while (__hip_atomic_load(&flags[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0) __builtin_amdgcn_s_sleep(1);
+    }
+    __syncthreads();
+    if (to < 0 || to >= A.n_pages || t0 >= here) continue;  // a block behind the last token stays as it was
+    const int64_t dest = (int64_t)to * A.Hkv + kv;
+    uint8_t* page = A.pool + dest * kPage8Bytes;
+    if ((w & 1) == 0 && lane < kBlock8 && mine < here) A.weights[dest * kPage8 + mine] = id < 0 ? 0.0f : weight;
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+      *(uint4*)(page + (t0 + 16 * (w & 1) + 8 * p + (lane >> 3)) * kDim8 + 16 * (lane & 7)) = k[p];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      *(uint4*)(page + fc::v8_at(t0 + 16 * q, (int)d)) = make_uint4(codes[4 * q], codes[4 * q + 1], codes[4 * q + 2], codes[4 * q + 3]);
+    if ((w & 1) == 0 && lane < 2) page[fc::kPage8Scales + 2 * lane + half] = (uint8_t)(e[lane] + 127);
   }
-  __syncthreads();
-  const int to = table[pg];
-  if (to < 0 || to >= A.n_pages) return;
-  const int64_t base = (int64_t)to * A.Hkv + kv;
-  uint8_t* page = A.pool + base * kPage8Bytes;
-  if (tid < here) A.weights[base * kPage8 + tid] = weight;
-  if (t0 >= here) return;  // a block behind the last token stays as it was
-#pragma unroll
-  for (int p = 0; p < 2; ++p)
-    *(uint4*)(page + (t0 + 16 * (w & 1) + 8 * p + (lane >> 3)) * kDim8 + 16 * (lane & 7)) = k[p];
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-    *(uint4*)(page + fc::v8_at(t0 + 16 * q, d)) = make_uint4(codes[4 * q], codes[4 * q + 1], codes[4 * q + 2], codes[4 * q + 3]);
-  if ((w & 1) == 0 && lane < 2) page[fc::kPage8Scales + 2 * lane + half] = (uint8_t)(e[lane] + 127);
 }
 
 size_t carve(void* p, int32_t B, int32_t Hkv, int32_t max_len, Evict& a) {
@@ -673,7 +754,10 @@ extern "C" fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t 
   hipLaunchKernelGGL(k_evict_select, dim3(Hkv, B), dim3(kSelThreads), 0, stream, a);
   FC_CHECK_LAUNCH();
   if (a.pages == 0) return FC_OK;
-  hipLaunchKernelGGL(k_evict_move, dim3(a.pages, Hkv, B), dim3(kMoveThreads), 0, stream, a);
+  // As many workgroups for each pair as the card takes at once, or one a page.
+  const uint32_t each = fc::div_up(kMoveAtOnce, (uint64_t)B * Hkv);
+  hipLaunchKernelGGL(k_evict_move, dim3((uint32_t)B * (uint32_t)Hkv, each < (uint32_t)a.pages ? each : (uint32_t)a.pages),
+                     dim3(kMoveThreads), 0, stream, a);
   FC_CHECK_LAUNCH();
   return FC_OK;
 }

@@ -996,3 +996,29 @@ def test_refusals_on_the_gpu():
     with pytest.raises(ValueError, match="lse"):
         fc.fc_paged_byte_weights(w, s["q"], torch.zeros((2, 9, 4), device="cuda"), s["pool"], s["table"], n, n,
                              dev(np.zeros(3, np.int32)))
+
+
+def test_evictions_of_far_scales():
+    """Tokens of blocks whose scales lie far apart meet in one: the largest decides, small
+    codes become smaller or nothing; blocks of nothing but the least codes, of zeros, and
+    of NaN."""
+    rng = np.random.default_rng(27)
+    n, Hkv = 512, 2
+    powers = np.repeat(rng.integers(-110, 100, n // 32), 32)
+    kinds = [2.0 ** powers, 2.0 ** np.repeat([0, 3, -9, 1], n // 4), np.zeros(n), np.full(n, np.nan)]
+    for i, scale in enumerate(kinds):
+        k, v = (torch.from_numpy(rng.standard_normal((n, Hkv, D)) * scale[:, None, None]).to(BF) for _ in "kv")
+        if i == 1:  # every block has one large row, which leaves; the others' codes are below 8
+            k[::32], v[::32] = k[::32] * 2 ** 17, v[::32] * 2 ** 17
+        pool = torch.zeros((n // 64, Hkv, fc.FC_PAGE8_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+        fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(np.arange(n, dtype=np.int32)))
+        w = rng.uniform(0.1, 1, (n // 64, Hkv, 64)).astype(np.float32)
+        w[:, :, ::32] = 0
+        table = np.arange(n // 64, dtype=np.int32)[None]
+        say(f"evict of far scales, kind {i}")
+        for budget in (496, 300, 33):
+            got, gw = pool.clone(), dev(w)
+            want, ww, _ = o8.evict(host(pool), w, table, [n], [budget])
+            fc.fc_paged_byte_evict(got, gw, dev(table), dev(np.array([n], np.int32)), dev(np.array([budget], np.int32)))
+            same_pool(got, want, (i, budget))
+            assert np.array_equal(host(gw), ww)
