@@ -38,6 +38,7 @@ struct Weights {
   const uint8_t* pool;
   const int32_t *table, *len, *new_len, *cu, *src;
   int n_rows, n_pages, max_pages, n, H, Hkv, max_len;
+  int y0;  // pages, or parts, before this launch's
 };
 
 __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kManyWaves* fc::kWave, 2) k_weights_many(Weigh
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
   // a head's pages lie on one XCD, whose L2 has its rows then; the first ones, which most
   // rows see, begin first
-  const int b = (int)blockIdx.x / A.Hkv, pg = (int)blockIdx.y;
+  const int b = (int)blockIdx.x / A.Hkv, pg = A.y0 + (int)blockIdx.y;
   const Step S(A, b, (int)blockIdx.x % A.Hkv);
   if (S.n <= 0 || pg * kPage8 >= S.end) return;  // all waves of the workgroup
   const int id = A.table[(int64_t)b * A.max_pages + pg];
@@ -245,8 +246,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_weights_few(Weights A, int part
   const int b = (int)blockIdx.x / A.Hkv;
   const Step S(A, b, (int)blockIdx.x % A.Hkv);
   const int pages = (S.end + kPage8 - 1) / kPage8;
-  const int pg0 = (int)blockIdx.y * part_pages + w;
-  const int pg1 = ((int)blockIdx.y + 1) * part_pages < pages ? ((int)blockIdx.y + 1) * part_pages : pages;
+  const int part = A.y0 + (int)blockIdx.y;
+  const int pg0 = part * part_pages + w;
+  const int pg1 = (part + 1) * part_pages < pages ? (part + 1) * part_pages : pages;
   if (S.n <= 0 || pg0 >= pg1) return;
   const int32_t* table = A.table + (int64_t)b * A.max_pages;
   const uint32_t k_at = (uint32_t)((16 * (lc >> 2) + (lc & 3)) * kDim8 + 16 * lg);
@@ -322,7 +324,10 @@ struct Evict {
   int32_t* from;    // [B][Hkv][max_len] token that moves to each place
   int32_t* before;  // [B][Hkv][pages + 1] tokens that stay, ahead of each page
   int32_t* flags;   // [B][Hkv][pages + 1] pages whose tokens are read; the last: pages begun
-  int n_pages, Hkv, max_pages, max_len, pages, first, recent;
+  uint32_t* bins;   // [B][Hkv][3][kBins] and [B][Hkv][parts][2], where there are parts:
+  uint32_t* kinds;  // how many tokens of each part stay, and how many do if there is room
+  int n_pages, Hkv, max_pages, max_len, pages, parts, first, recent;
+  int y0;  // parts before this launch's
 };
 
 // How a sequence is cut: its length, how many stay, the tokens that do by their place
@@ -345,34 +350,31 @@ struct Cut {
 // A weight as a number that sorts as it does: 0 for what is not above 0.
 __device__ __forceinline__ uint32_t rank_of(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
 
-// A workgroup finds what one head of one sequence keeps: the weight of the last one to
-// stay, 11 bits at a time from the top, by counting; then, in order, which tokens are
-// above it, and of those that equal it the first ones.  A wave's lanes are a page's
-// tokens, a wave's pages follow one another, and 16 of them are read together: up to
-// 16,384 tokens stay in registers, longer sequences are read again for each of the five
-// turns.
+// What one head of one sequence keeps: the weight of the last one to stay is found 11
+// bits at a time from the top, by counting; then, in order, which tokens are above it,
+// and of those that equal it the first ones.  A wave's lanes are a page's tokens, a wave's
+// pages follow one another, 16 of them in registers.  One workgroup has up to 256 pages
+// and does it all; longer sequences are parts of as many, counted together in memory by
+// one launch for each turn (the 131,000 tokens of 8 heads that eight workgroups alone
+// read five times over: 186 us).
 constexpr int kTogether = 16;
-__global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
-  __shared__ uint32_t s_bins[kBins];
-  __shared__ uint32_t s_sum[kSelWaves + 1];
-  __shared__ uint32_t s_bin, s_left;
-  __shared__ uint32_t s_wave[2][kSelWaves];
-  const int tid = (int)threadIdx.x, lane = fc::lane_id();
-  const int w = __builtin_amdgcn_readfirstlane(tid / fc::kWave);
-  const int kv = (int)blockIdx.x, b = (int)blockIdx.y;
-  const Cut c(A, b);
-  if (kv == 0 && tid == 0) A.add[b] = c.keep - c.n;
-  if (c.keep >= c.n || c.keep == 0) return;
-  const int64_t bk = (int64_t)b * A.Hkv + kv;
-  const int32_t* table = A.table + (int64_t)b * A.max_pages;
-  int32_t* flags = A.flags + bk * (A.pages + 1);
-  const int pages = (c.n + kPage8 - 1) / kPage8;
-  for (int p = tid; p <= A.pages; p += kSelThreads) flags[p] = 0;
-  const int p0 = (int)((int64_t)pages * w / kSelWaves), p1 = (int)((int64_t)pages * (w + 1) / kSelWaves);
-  uint32_t rank[kTogether];  // of pages at .. at + 15
-  const auto load = [&](int at) {
+constexpr int kPartPages = kSelWaves * kTogether;
+
+struct Select {
+  const Evict& A;
+  const Cut& c;
+  const int32_t* table;
+  int kv, lane, w, p0, p1;
+  uint32_t found, left;  // the bits of the last one to stay, and how many of those that share them do
+  uint32_t rank[kTogether];
+  __device__ __forceinline__ Select(const Evict& a, const Cut& cut, int b, int kv_, int part)
+      : A(a), c(cut), table(a.table + (int64_t)b * a.max_pages), kv(kv_), lane(fc::lane_id()),
+        w(__builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave)), found(0), left((uint32_t)cut.heavy) {
+    const int pages = (c.n + kPage8 - 1) / kPage8, q0 = part * kPartPages;
+    const int n = pages - q0 < kPartPages ? pages - q0 : kPartPages;
+    p0 = q0 + n * w / kSelWaves, p1 = q0 + n * (w + 1) / kSelWaves;
     // a page number a lane; what is not there has weight 0
-    int id = lane < kTogether && at + lane < p1 ? table[at + lane] : -1;
+    int id = lane < kTogether && p0 + lane < p1 ? table[p0 + lane] : -1;
     if (id >= A.n_pages) id = -1;
     float x[kTogether];
 #pragma unroll
@@ -382,77 +384,151 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
     }
 #pragma unroll
     for (int i = 0; i < kTogether; ++i) rank[i] = __builtin_amdgcn_readlane(id, i) < 0 ? 0u : rank_of(x[i]);
-  };
-  const bool held = p1 - p0 <= kTogether;
-  if (held) load(p0);
-  // f(page, the lane's token's rank) for the wave's pages in their order
-  const auto each_page = [&](auto f) {
-    for (int at = p0; at < p1; at += kTogether) {
-      if (!held) load(at);
-#pragma unroll
-      for (int i = 0; i < kTogether; ++i)
-        if (at + i < p1) f(at + i, rank[i]);
-    }
-  };
-  const int lo = c.lo, hi = c.hi;
-  const uint32_t heavy = (uint32_t)c.heavy;
-  uint32_t found = 0, left = heavy;  // the bits of the last one to stay, and how many of those that share them do
-  if (heavy > 0) {
-    for (int level = 0; level < 3; ++level) {
-      const int shift = level == 0 ? 20 : level == 1 ? 9 : 0, bits = level == 2 ? 9 : 11;
-      for (int i = tid; i < kBins; i += kSelThreads) s_bins[i] = 0;
-      __syncthreads();
-      each_page([&](int p, uint32_t r) {
-        const int t = p * kPage8 + lane;
-        if (t >= lo && t < hi && (level == 0 || (r >> (shift + bits)) == found))
-          atomicAdd(&s_bins[(r >> shift) & ((1u << bits) - 1u)], 1u);
-      });
-      __syncthreads();
-      // two bins a thread, from the largest down
-      const int top = kBins - 1 - 2 * tid;
-      const uint32_t x = s_bins[top], y = s_bins[top - 1];
-      const uint32_t ahead = fc::block_excl_sum<uint32_t>(x + y, s_sum, nullptr);
-      if (ahead < left && left <= ahead + x) s_bin = (uint32_t)top, s_left = left - ahead;
-      else if (ahead + x < left && left <= ahead + x + y) s_bin = (uint32_t)top - 1, s_left = left - ahead - x;
-      __syncthreads();
-      found = found << bits | s_bin;
-      left = s_left;
-      __syncthreads();
-    }
   }
-  // how many each wave has that stay, and that do if there is room, then which they are
-  const auto kinds = [&](int p, uint32_t r, uint64_t& stays, uint64_t& equal) {
+  // f(page, the lane's token's rank) for the wave's pages in their order
+  template <typename F>
+  __device__ __forceinline__ void each_page(F f) {
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i)
+      if (p0 + i < p1) f(p0 + i, rank[i]);
+  }
+  __device__ __forceinline__ static int shift(int level) { return level == 0 ? 20 : level == 1 ? 9 : 0; }
+  __device__ __forceinline__ static int bits(int level) { return level == 2 ? 9 : 11; }
+  // The tokens that share the bits found so far, by their next bits.
+  __device__ __forceinline__ void count(int level, uint32_t* bins) {
+    for (int i = (int)threadIdx.x; i < kBins; i += kSelThreads) bins[i] = 0;
+    __syncthreads();
+    each_page([&](int p, uint32_t r) {
+      const int t = p * kPage8 + lane;
+      if (t >= c.lo && t < c.hi && (level == 0 || (r >> (shift(level) + bits(level))) == found))
+        atomicAdd(&bins[(r >> shift(level)) & ((1u << bits(level)) - 1u)], 1u);
+    });
+    __syncthreads();
+  }
+  // From such counts (x and y: this thread's two, from the largest down), the next bits.
+  __device__ __forceinline__ void narrow(int level, uint32_t x, uint32_t y, uint32_t* sum, uint32_t* found_left) {
+    const uint32_t top = kBins - 1 - 2 * threadIdx.x;
+    const uint32_t ahead = fc::block_excl_sum<uint32_t>(x + y, sum, nullptr);
+    if (ahead < left && left <= ahead + x) found_left[0] = top, found_left[1] = left - ahead;
+    else if (ahead + x < left && left <= ahead + x + y) found_left[0] = top - 1, found_left[1] = left - ahead - x;
+    __syncthreads();
+    found = found << bits(level) | found_left[0];
+    left = found_left[1];
+    __syncthreads();
+  }
+  // Tokens of a page that stay, and that do if there is room.
+  __device__ __forceinline__ void kinds(int p, uint32_t r, uint64_t& stays, uint64_t& equal) const {
     const int t = p * kPage8 + lane;
-    const bool by_weight = heavy > 0 && t >= lo && t < hi;
-    stays = fc::ballot(t < lo || (t >= c.late && t < c.n) || (by_weight && r > found));
+    const bool by_weight = c.heavy > 0 && t >= c.lo && t < c.hi;
+    stays = fc::ballot(t < c.lo || (t >= c.late && t < c.n) || (by_weight && r > found));
     equal = fc::ballot(by_weight && r == found);
-  };
+  }
+  // How many each wave has of either kind, into s_wave; with those before the workgroup's,
+  // how many come before this wave's.
+  __device__ __forceinline__ void count_kinds(uint32_t (*s_wave)[kSelWaves], uint32_t& sure, uint32_t& maybe) {
+    uint32_t a = 0, e = 0;
+    each_page([&](int p, uint32_t r) {
+      uint64_t stays, equal;
+      kinds(p, r, stays, equal);
+      a += (uint32_t)__popcll(stays);
+      e += (uint32_t)__popcll(equal);
+    });
+    if (lane == 0) s_wave[0][w] = a, s_wave[1][w] = e;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) sure += s_wave[0][i], maybe += s_wave[1][i];
+  }
+  __device__ __forceinline__ void write(int32_t* before, int32_t* from, uint32_t sure, uint32_t maybe) {
+    each_page([&](int p, uint32_t r) {
+      uint64_t stays, equal;
+      kinds(p, r, stays, equal);
+      const uint32_t at = sure + (maybe < left ? maybe : left);
+      const uint64_t below = fc::lanemask_lt();
+      const bool taken = ((equal >> lane) & 1u) && maybe + (uint32_t)__popcll(equal & below) < left;
+      const uint64_t all = stays | fc::ballot(taken);
+      if (lane == 0) before[p] = (int32_t)at;
+      if ((all >> lane) & 1u) from[at + (uint32_t)__popcll(all & below)] = p * kPage8 + lane;
+      sure += (uint32_t)__popcll(stays);
+      maybe += (uint32_t)__popcll(equal);
+    });
+  }
+};
+
+__global__ void __launch_bounds__(kSelThreads) k_evict_select(Evict A) {
+  __shared__ uint32_t s_bins[kBins];
+  __shared__ uint32_t s_sum[kSelWaves + 1], s_found[2], s_wave[2][kSelWaves];
+  const int tid = (int)threadIdx.x, kv = (int)blockIdx.x % A.Hkv, b = (int)blockIdx.x / A.Hkv;
+  const Cut c(A, b);
+  if (kv == 0 && tid == 0) A.add[b] = c.keep - c.n;
+  if (c.keep >= c.n || c.keep == 0) return;
+  const int64_t bk = (int64_t)b * A.Hkv + kv;
+  int32_t* flags = A.flags + bk * (A.pages + 1);
+  for (int p = tid; p <= A.pages; p += kSelThreads) flags[p] = 0;
+  Select s(A, c, b, kv, 0);
+  if (c.heavy > 0)
+    for (int level = 0; level < 3; ++level) {
+      s.count(level, s_bins);
+      const int top = kBins - 1 - 2 * tid;
+      s.narrow(level, s_bins[top], s_bins[top - 1], s_sum, s_found);
+    }
   uint32_t sure = 0, maybe = 0;
-  each_page([&](int p, uint32_t r) {
-    uint64_t stays, equal;
-    kinds(p, r, stays, equal);
-    sure += (uint32_t)__popcll(stays);
-    maybe += (uint32_t)__popcll(equal);
-  });
-  if (lane == 0) s_wave[0][w] = sure, s_wave[1][w] = maybe;
-  __syncthreads();
-  sure = maybe = 0;
-  for (int i = 0; i < w; ++i) sure += s_wave[0][i], maybe += s_wave[1][i];
+  s.count_kinds(s_wave, sure, maybe);
   int32_t* before = A.before + bk * (A.pages + 1);
-  int32_t* from = A.from + bk * A.max_len;
-  each_page([&](int p, uint32_t r) {
-    uint64_t stays, equal;
-    kinds(p, r, stays, equal);
-    const uint32_t at = sure + (maybe < left ? maybe : left);
-    const uint64_t below = fc::lanemask_lt();
-    const bool taken = ((equal >> lane) & 1u) && maybe + (uint32_t)__popcll(equal & below) < left;
-    const uint64_t all = stays | fc::ballot(taken);
-    if (lane == 0) before[p] = (int32_t)at;
-    if ((all >> lane) & 1u) from[at + (uint32_t)__popcll(all & below)] = p * kPage8 + lane;
-    sure += (uint32_t)__popcll(stays);
-    maybe += (uint32_t)__popcll(equal);
-  });
-  if (tid == 0) before[pages] = c.keep;
+  s.write(before, A.from + bk * A.max_len, sure, maybe);
+  if (tid == 0) before[(c.n + kPage8 - 1) / kPage8] = c.keep;
+}
+
+// The same in turns, a workgroup for each part: 0 clears what is counted in memory, 1 to
+// 3 count bits, 4 counts what stays, 5 writes it down.  Sums of whole numbers, so the
+// order of the atomic additions does not matter.
+template <int TURN>
+__global__ void __launch_bounds__(kSelThreads) k_evict_turn(Evict A) {
+  __shared__ uint32_t s_bins[kBins];
+  __shared__ uint32_t s_sum[kSelWaves + 1], s_found[2], s_wave[2][kSelWaves];
+  const int tid = (int)threadIdx.x, kv = (int)blockIdx.x % A.Hkv, b = (int)blockIdx.x / A.Hkv;
+  const int part = A.y0 + (int)blockIdx.y;
+  const Cut c(A, b);
+  if (TURN == 0 && kv == 0 && part == 0 && tid == 0) A.add[b] = c.keep - c.n;
+  const int pages = (c.n + kPage8 - 1) / kPage8;
+  if (c.keep >= c.n || c.keep == 0 || part * kPartPages >= pages) return;
+  const int64_t bk = (int64_t)b * A.Hkv + kv;
+  uint32_t* bins = A.bins + bk * 3 * kBins;
+  uint32_t* of_part = A.kinds + bk * A.parts * 2;
+  if (TURN == 0) {
+    int32_t* flags = A.flags + bk * (A.pages + 1);
+    for (int p = part * kPartPages + tid; p <= A.pages && p < (part + 1) * kPartPages; p += kSelThreads) flags[p] = 0;
+    if (part == 0) {
+      for (int i = tid; i < 3 * kBins; i += kSelThreads) bins[i] = 0;
+      if (tid == 0) flags[A.pages] = 0;
+    }
+    return;
+  }
+  if (TURN <= 3 && c.heavy == 0) return;
+  Select s(A, c, b, kv, part);
+  if (c.heavy > 0)
+    for (int level = 0; level < TURN - 1 && level < 3; ++level) {
+      const uint32_t* now = bins + level * kBins + kBins - 1 - 2 * tid;
+      s.narrow(level, now[0], now[-1], s_sum, s_found);
+    }
+  if (TURN <= 3) {
+    s.count(TURN - 1, s_bins);
+    for (int i = tid; i < kBins; i += kSelThreads)
+      if (s_bins[i]) atomicAdd(&bins[(TURN - 1) * kBins + i], s_bins[i]);
+    return;
+  }
+  uint32_t sure = 0, maybe = 0;
+  if (TURN == 4) {
+    s.count_kinds(s_wave, sure, maybe);
+    if (tid == kSelThreads - 1) {
+      of_part[2 * part] = sure + s_wave[0][kSelWaves - 1];
+      of_part[2 * part + 1] = maybe + s_wave[1][kSelWaves - 1];
+    }
+    return;
+  }
+  for (int i = 0; i < part; ++i) sure += of_part[2 * i], maybe += of_part[2 * i + 1];
+  s.count_kinds(s_wave, sure, maybe);
+  int32_t* before = A.before + bk * (A.pages + 1);
+  s.write(before, A.from + bk * A.max_len, sure, maybe);
+  if (part == 0 && tid == 0) before[pages] = c.keep;
 }
 
 constexpr int kMoveThreads = 256;
@@ -658,6 +734,18 @@ __global__ void __launch_bounds__(kMoveThreads, 4) k_evict_move(Evict A) {
   }
 }
 
+// A launch takes fewer than 2^32 threads in a dimension, and 65,536 workgroups in the
+// second: longer calls are several.
+constexpr uint32_t kMostY = 1 << 15;
+template <int TURN>
+void in_turn(Evict a, uint32_t pairs, hipStream_t stream) {
+  for (uint32_t y = 0; y < (uint32_t)a.parts; y += kMostY) {
+    a.y0 = (int)y;
+    const uint32_t parts = (uint32_t)a.parts - y;
+    hipLaunchKernelGGL(k_evict_turn<TURN>, dim3(pairs, parts < kMostY ? parts : kMostY), dim3(kSelThreads), 0, stream, a);
+  }
+}
+
 size_t carve(void* p, int32_t B, int32_t Hkv, int32_t max_len, Evict& a) {
   fc::Carver c(p);
   const size_t rows = (size_t)B * Hkv;
@@ -665,7 +753,15 @@ size_t carve(void* p, int32_t B, int32_t Hkv, int32_t max_len, Evict& a) {
   a.from = c.take<int32_t>(rows * (size_t)max_len);
   a.before = c.take<int32_t>(rows * ((size_t)a.pages + 1));
   a.flags = c.take<int32_t>(rows * ((size_t)a.pages + 1));
+  a.parts = (a.pages + kPartPages - 1) / kPartPages;
+  a.bins = a.parts > 1 ? c.take<uint32_t>(rows * 3 * kBins) : nullptr;
+  a.kinds = a.parts > 1 ? c.take<uint32_t>(rows * 2 * (size_t)a.parts) : nullptr;
   return c.used + 256;
+}
+
+int32_t sequences_at_once(int32_t B, int32_t Hkv) {
+  const int32_t most = (1 << 20) / Hkv;  // Hkv is 1,024 at most
+  return B < most ? B : most;
 }
 
 bool sizes_ok(int32_t B, int32_t Hkv, int32_t max_len) {
@@ -698,25 +794,28 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
                   {cu, seqs + 4},
                   {src, 4 * (uint64_t)n}}))
     return FC_ERR_INVALID;
-  const Weights a = {weights, q, q_stride, lse, pool, table, len, new_len, cu, src, n_rows, n_pages, max_pages, n, H, Hkv,
-                     max_len};
   const uint32_t pages = fc::div_up((uint64_t)max_len, kPage8);
+  // More rows than a wave holds twice over: pages are held, rows go by.  Otherwise four
+  // pages a wave, or fewer where that leaves the card idle.
+  const bool many = (int64_t)n * (H / Hkv) > 2 * kFewTiles * kTile * (int64_t)B;
+  int each = 4;
+  while (each > 1 && (int64_t)B * Hkv * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
+  const uint32_t parts = many ? pages : fc::div_up(pages, each * kWaves);
+  const int32_t at_once = sequences_at_once(B, Hkv);
   (void)hipGetLastError();
-  // More rows than a wave holds twice over: pages are held, rows go by.
-  if ((int64_t)n * (H / Hkv) > 2 * kFewTiles * kTile * (int64_t)B) {
-    const dim3 grid(B * Hkv, pages), threads(kManyWaves * fc::kWave);
-    if (src) hipLaunchKernelGGL(k_weights_many<true>, grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL(k_weights_many<false>, grid, threads, 0, stream, a);
-  } else {
-    // four pages a wave, or fewer where that leaves the card idle
-    const int64_t pairs = (int64_t)B * Hkv;
-    int each = 4;
-    while (each > 1 && pairs * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
-    const dim3 grid(B * Hkv, fc::div_up(pages, (uint32_t)(each * kWaves)));
-    if (src) hipLaunchKernelGGL(k_weights_few<true>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
-    else hipLaunchKernelGGL(k_weights_few<false>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+  for (int32_t b = 0; b < B; b += at_once) {
+    const uint32_t pairs = (uint32_t)(B - b < at_once ? B - b : at_once) * (uint32_t)Hkv;
+    for (uint32_t y = 0; y < parts; y += kMostY) {
+      const Weights a = {weights, q, q_stride, lse, pool, table + (int64_t)b * max_pages, len + b, new_len + b, cu + b, src,
+                         n_rows, n_pages, max_pages, n, H, Hkv, max_len, (int)y};
+      const dim3 grid(pairs, parts - y < kMostY ? parts - y : kMostY);
+      if (many && src) hipLaunchKernelGGL(k_weights_many<true>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a);
+      else if (many) hipLaunchKernelGGL(k_weights_many<false>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a);
+      else if (src) hipLaunchKernelGGL(k_weights_few<true>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+      else hipLaunchKernelGGL(k_weights_few<false>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+      FC_CHECK_LAUNCH();
+    }
   }
-  FC_CHECK_LAUNCH();
   return FC_OK;
 }
 
@@ -747,17 +846,35 @@ extern "C" fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t 
                   {ws, need}},
                  {{table, seqs * max_pages}, {len, seqs}, {budget, seqs}}))
     return FC_ERR_INVALID;
-  Evict a = {pool, weights, table, len, budget, add, nullptr, nullptr, nullptr, n_pages, Hkv, max_pages, max_len, 0, first,
-             recent};
+  Evict a = {pool, weights, table, len, budget, add, nullptr, nullptr, nullptr, nullptr, nullptr, n_pages, Hkv, max_pages,
+             max_len, 0, 0, first, recent, 0};
   carve(ws, B, Hkv, max_len, a);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(k_evict_select, dim3(Hkv, B), dim3(kSelThreads), 0, stream, a);
-  FC_CHECK_LAUNCH();
-  if (a.pages == 0) return FC_OK;
-  // As many workgroups for each pair as the card takes at once, or one a page.
-  const uint32_t each = fc::div_up(kMoveAtOnce, (uint64_t)B * Hkv);
-  hipLaunchKernelGGL(k_evict_move, dim3((uint32_t)B * (uint32_t)Hkv, each < (uint32_t)a.pages ? each : (uint32_t)a.pages),
-                     dim3(kMoveThreads), 0, stream, a);
-  FC_CHECK_LAUNCH();
+  const int32_t at_once = sequences_at_once(B, Hkv);
+  for (int32_t b = 0; b < B; b += at_once) {
+    const uint32_t pairs = (uint32_t)(B - b < at_once ? B - b : at_once) * (uint32_t)Hkv;
+    const int64_t before = (int64_t)b * Hkv;
+    Evict now = a;
+    now.table += (int64_t)b * max_pages, now.len += b, now.budget += b, now.add += b;
+    now.from += before * max_len, now.before += before * (a.pages + 1), now.flags += before * (a.pages + 1);
+    if (a.parts <= 1) {
+      hipLaunchKernelGGL(k_evict_select, dim3(pairs), dim3(kSelThreads), 0, stream, now);
+    } else {
+      now.bins += before * 3 * kBins, now.kinds += before * 2 * a.parts;
+      in_turn<0>(now, pairs, stream);
+      in_turn<1>(now, pairs, stream);
+      in_turn<2>(now, pairs, stream);
+      in_turn<3>(now, pairs, stream);
+      in_turn<4>(now, pairs, stream);
+      in_turn<5>(now, pairs, stream);
+    }
+    FC_CHECK_LAUNCH();
+    if (a.pages == 0) continue;
+    // As many workgroups for each pair as the card takes at once, or one a page.
+    const uint32_t each = fc::div_up(kMoveAtOnce, pairs);
+    hipLaunchKernelGGL(k_evict_move, dim3(pairs, each < (uint32_t)a.pages ? each : (uint32_t)a.pages), dim3(kMoveThreads), 0,
+                       stream, now);
+    FC_CHECK_LAUNCH();
+  }
   return FC_OK;
 }

@@ -1022,3 +1022,74 @@ def test_evictions_of_far_scales():
             fc.fc_paged_byte_evict(got, gw, dev(table), dev(np.array([n], np.int32)), dev(np.array([budget], np.int32)))
             same_pool(got, want, (i, budget))
             assert np.array_equal(host(gw), ww)
+
+
+@pytest.mark.parametrize("n,budget,first,recent", [(16_385, 9_000, 0, 0), (40_000, 17_000, 5, 300), (33_000, 32_999, 4, 0),
+                                                   (50_000, 700, 900, 600)])
+def test_evictions_in_parts(n, budget, first, recent):
+    """More tokens than one workgroup weighs: counted in parts, with equal weights across
+    their borders, beside a short sequence and one that stays."""
+    rng = np.random.default_rng(n)
+    lens, budgets = [300, n, 64], [120, budget, 64]
+    pages = [-(-x // 64) for x in lens]
+    perm = rng.permutation(sum(pages) + 3).astype(np.int32)
+    table, at = np.full((3, max(pages)), -1, np.int32), 0
+    for b, m in enumerate(pages):
+        table[b, :m] = perm[at:at + m]
+        at += m
+    torch.manual_seed(n)
+    pool = fc.paged_byte_pool(len(perm), 1, "cuda")
+    x = torch.randn((64 * len(perm), 1, D), device="cuda").to(BF)
+    fc.fc_paged_byte_write(pool, x, x.flip(0), torch.arange(64 * len(perm), dtype=torch.int32, device="cuda"))
+    for weights in (rng.uniform(0, 1, (len(perm), 1, 64)), rng.integers(0, 3, (len(perm), 1, 64))):
+        w = weights.astype(np.float32)
+        say(f"evict in parts {n} to {budget}")
+        want, ww, add = o8.evict(host(pool), w, table, lens, budgets, first, recent)
+        got, gw = pool.clone(), dev(w)
+        got_add = fc.fc_paged_byte_evict(got, gw, dev(table), dev(np.array(lens, np.int32)), dev(np.array(budgets, np.int32)),
+                                         first=first, recent=recent)
+        assert np.array_equal(host(got_add), add) and np.array_equal(host(gw), ww)
+        same_pool(got, want)
+
+
+def test_more_sequences_and_pages_than_one_launch_takes():
+    """Pairs past 2^20 and tables of 2^17 pages: weights and evictions are those of calls
+    with fewer sequences, and of narrower tables."""
+    rng = np.random.default_rng(28)
+    B, Hkv = 33_000, 32
+    pool = make_pool(rng, B // 500, Hkv)
+    pool = pool.repeat(500, 1, 1)[:B].contiguous()
+    table = torch.randperm(B, device="cuda").int()[:, None].contiguous()
+    n, cu = torch.full((B,), 40, dtype=torch.int32, device="cuda"), torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    q, lse = bf16(rng, B, Hkv, D).cuda(), torch.rand((B, Hkv), device="cuda") * 4
+    budget = torch.randint(0, 41, (B,), dtype=torch.int32, device="cuda")
+    w = torch.rand((B, Hkv, 64), device="cuda")
+    a, b = (pool.clone(), w.clone()), (pool, w)
+    say("more pairs than a launch takes")
+    fc.fc_paged_byte_weights(a[1], q, lse, a[0], table, n - 1, n, cu)
+    add = fc.fc_paged_byte_evict(*a, table, n, budget)
+    for i in range(0, B, 11_000):
+        s = slice(i, i + 11_000)
+        fc.fc_paged_byte_weights(b[1], q, lse, b[0], table[s], n[s] - 1, n[s], cu[i:i + 11_001].contiguous())
+    for i in range(0, B, 11_000):
+        s = slice(i, i + 11_000)
+        assert torch.equal(add[s], fc.fc_paged_byte_evict(*b, table[s], n[s], budget[s]))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    del a, b, pool, w
+    wide = torch.full((1, 2 ** 17 + 3), -1, dtype=torch.int32, device="cuda")
+    wide[0, :5] = torch.arange(5, device="cuda")
+    pool, w = make_pool(rng, 5, 1), torch.rand((5, 1, 64), device="cuda")
+    n = torch.tensor([300], dtype=torch.int32, device="cuda")
+    got = []
+    say("wide tables")
+    for t in (wide, wide[:, :5].contiguous()):
+        for rows in (2, 200):
+            p, x = pool.clone(), w.clone()
+            q, lse = bf16(np.random.default_rng(rows), rows, 3, D).cuda(), torch.ones((rows, 3), device="cuda")
+            fc.fc_paged_byte_weights(x, q, lse, p, t, n - rows, n, torch.tensor([0, rows], dtype=torch.int32, device="cuda"))
+            out = fc.fc_paged_byte_attention(q[None, :2], pool.new_zeros((1, 2, 1, 256)).view(BF), q[None, :2, :1].contiguous(), p, t, n)
+            fc.fc_paged_byte_evict(p, x, t, n, n - 77, recent=9)
+            got.append((p, x, out))
+    for x, y in zip(got[:2], got[2:]):
+        assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+        assert (x[2].float() - y[2].float()).abs().max() < 0.03      # other parts: a weight's rounding
