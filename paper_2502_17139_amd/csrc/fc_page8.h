@@ -64,4 +64,25 @@ __device__ __forceinline__ uint32_t recode8(uint32_t w, float inv) {
   return codes8(lo[0] * inv, lo[1] * inv, hi[0] * inv, hi[1] * inv);
 }
 
+// Most calls need less: with only finite numbers and a scale between the ends, no
+// quotient passes 448, and the conversion of two bfloat16 numbers at a time is the same
+// codes.  (Its quotient by a power of two is exact before it rounds.)
+typedef unsigned short ushort2_8 __attribute__((ext_vector_type(2)));
+typedef short short2_8 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_8 __attribute__((ext_vector_type(2)));
+// The larger magnitudes of two pairs of bfloat16 bits, infinities and NaN above all.
+__device__ __forceinline__ uint32_t tops8(uint32_t top, uint32_t pair) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2_8, top),
+                                                                __builtin_bit_cast(ushort2_8, pair & 0x7FFF7FFFu)));
+}
+__device__ __forceinline__ uint32_t codes8(uint32_t pair0, uint32_t pair1, float scale) {
+  const short2_8 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(short2_8{0, 0}, __builtin_bit_cast(bf16x2_8, pair0), scale, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2_8, pair1), scale, true));
+}
+// Four codes of two pairs by the longer way.
+__device__ __forceinline__ uint32_t codes8_any(uint32_t pair0, uint32_t pair1, float inv) {
+  return codes8(to_code8(__uint_as_float(pair0 << 16), inv), to_code8(__uint_as_float(pair0 & 0xFFFF0000u), inv),
+                to_code8(__uint_as_float(pair1 << 16), inv), to_code8(__uint_as_float(pair1 & 0xFFFF0000u), inv));
+}
+
 }  // namespace fc

@@ -32,14 +32,14 @@ struct Write {
   int n_pages, Hkv, window;
 };
 
-// Magnitudes of a wave's rows, joined: all lanes get the largest.
-__device__ __forceinline__ uint32_t wave_top(uint32_t m) {
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// The largest magnitude of a wave's pairs (bfloat16 bits), the same in all lanes.
+__device__ __forceinline__ uint32_t wave_top(uint32_t pair) {
+  uint32_t m = larger(pair & 0xFFFFu, pair >> 16);
 #pragma unroll
-  for (int o = 1; o < fc::kWave; o <<= 1) {
-    const uint32_t x = (uint32_t)__shfl_xor((int)m, o);
-    m = x > m ? x : m;
-  }
-  return m;
+  for (int o = 1; o < fc::kWave; o <<= 1) m = larger(m, (uint32_t)__shfl_xor((int)m, o));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
 }
 
 // What a block's scale becomes, and what its other rows' codes are multiplied by.
@@ -133,35 +133,46 @@ __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
           raw[p][1] = at[1];
         }
       }
-      uint32_t top = 0;
+      uint32_t tops = 0;
 #pragma unroll
       for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float v[8];
-          fc::unpack8(raw[p][u], v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t m = fc::reach8(v[e]);
-            top = m > top ? m : top;
-          }
+          tops = fc::tops8(tops, raw[p][u].x);
+          tops = fc::tops8(tops, raw[p][u].y);
+          tops = fc::tops8(tops, raw[p][u].z);
+          tops = fc::tops8(tops, raw[p][u].w);
         }
-      const Scaled s = rescale(wave_top(top), byte, fresh);
+      uint32_t top = wave_top(tops);
+      const bool odd = top >= 0x7F80u;
+      if (odd) {  // the largest finite one
+        top = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            float v[8];
+            fc::unpack8(raw[p][u], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = larger(top, fc::reach8(v[e]) >> 16);
+          }
+        top = wave_top(top);
+      }
+      const Scaled s = rescale(top << 16, byte, fresh);
+      const bool plain = !odd && s.e > fc::kLeastExp8 && s.e < fc::kMostExp8;
+      const float scale_of = fc::power8(s.e);
       uint8_t* to = page + half * (kBlock8 * kDim8) + (lane >> 3) * kDim8 + 16 * c;
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         uint4* at = (uint4*)(to + p * 8 * kDim8);
         if (live[p]) {
           uint32_t o[4];
+          const uint32_t in[8] = {raw[p][0].x, raw[p][0].y, raw[p][0].z, raw[p][0].w,
+                                  raw[p][1].x, raw[p][1].y, raw[p][1].z, raw[p][1].w};
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            float v[8];
-            fc::unpack8(raw[p][u], v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fc::to_code8(v[e], s.inv);
-            o[2 * u] = fc::codes8(v[0], v[1], v[2], v[3]);
-            o[2 * u + 1] = fc::codes8(v[4], v[5], v[6], v[7]);
-          }
+          for (int i4 = 0; i4 < 4; ++i4)
+            o[i4] = plain ? fc::codes8(in[2 * i4], in[2 * i4 + 1], scale_of)
+                          : fc::codes8_any(in[2 * i4], in[2 * i4 + 1], s.inv);
           *at = make_uint4(o[0], o[1], o[2], o[3]);
         } else if (fresh) {
           *at = make_uint4(0u, 0u, 0u, 0u);
@@ -193,14 +204,21 @@ __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
           old[q][d] = make_uint4(0u, 0u, 0u, 0u);
           if (merge) old[q][d] = *(const uint4*)(to + q * (kQuarter8 * kDim8) + d * kQuarter8);
         }
-      uint32_t top = 0;
+      uint32_t tops = 0;
 #pragma unroll
-      for (int r = 0; r < kBlock8; ++r) {
-        const uint32_t a = fc::reach8(__uint_as_float(raw[r] << 16)), b = fc::reach8(__uint_as_float(raw[r] & 0xFFFF0000u));
-        top = a > top ? a : top;
-        top = b > top ? b : top;
+      for (int r = 0; r < kBlock8; ++r) tops = fc::tops8(tops, raw[r]);
+      uint32_t top = wave_top(tops);
+      const bool odd = top >= 0x7F80u;
+      if (odd) {
+        top = 0;
+#pragma unroll
+        for (int r = 0; r < kBlock8; ++r)
+          top = larger(top, larger(fc::reach8(__uint_as_float(raw[r] << 16)), fc::reach8(__uint_as_float(raw[r] & 0xFFFF0000u))) >> 16);
+        top = wave_top(top);
       }
-      const Scaled s = rescale(wave_top(top), byte, fresh);
+      const Scaled s = rescale(top << 16, byte, fresh);
+      const bool plain = !odd && s.e > fc::kLeastExp8 && s.e < fc::kMostExp8;
+      const float scale_of = fc::power8(s.e);
 #pragma unroll
       for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -209,17 +227,15 @@ __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
           const uint32_t was[4] = {old[q][d].x, old[q][d].y, old[q][d].z, old[q][d].w};
 #pragma unroll
           for (int i4 = 0; i4 < 4; ++i4) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t bits = raw[16 * q + 4 * i4 + e];
-              v[e] = fc::to_code8(__uint_as_float(d ? bits & 0xFFFF0000u : bits << 16), s.inv);
-            }
+            const uint32_t* in = raw + 16 * q + 4 * i4;
+            const uint32_t half0 = d ? (in[0] >> 16) | (in[1] & 0xFFFF0000u) : (in[0] & 0xFFFFu) | in[1] << 16;
+            const uint32_t half1 = d ? (in[2] >> 16) | (in[3] & 0xFFFF0000u) : (in[2] & 0xFFFFu) | in[3] << 16;
+            const uint32_t code = plain ? fc::codes8(half0, half1, scale_of) : fc::codes8_any(half0, half1, s.inv);
             const uint32_t nibble = (have >> (16 * q + 4 * i4)) & 15u;
             const uint32_t keep = ((nibble & 1u) | (nibble & 2u) << 7 | (nibble & 4u) << 14 | (nibble & 8u) << 21) * 255u;
             uint32_t rest = was[i4];
             if (s.recode) rest = fc::recode8(rest, s.again);
-            o[i4] = (fc::codes8(v[0], v[1], v[2], v[3]) & keep) | (rest & ~keep);
+            o[i4] = (code & keep) | (rest & ~keep);
           }
           *(uint4*)(to + q * (kQuarter8 * kDim8) + d * kQuarter8) = make_uint4(o[0], o[1], o[2], o[3]);
         }
@@ -253,38 +269,48 @@ __global__ void __launch_bounds__(kReadThreads) k_paged8_read(const uint8_t* __r
   int sl = lane < kReadRows && i0 + lane < n ? slot[i0 + lane] : -1;
   if (sl >= n_pages * kPage8) sl = -1;
   for (int h = (int)blockIdx.y * kReadWaves + w; h < Hkv; h += (int)gridDim.y * kReadWaves) {
-    const int c = lane & 15;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int e = 4 * p + (lane >> 4), s = __shfl(sl, e);
-      if (s < 0) continue;
-      const int t = s % kPage8;
-      const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
-      const uint2 x = *(const uint2*)(page + fc::k8_at(t, 8 * c));
-      const float f = fc::scale8(page[fc::kPage8Scales + t / kBlock8]);
-      *(uint4*)(k + ((i0 + e) * Hkv + h) * kDim8 + 8 * c) =
-          make_uint4(pair8(x.x, f, false), pair8(x.x, f, true), pair8(x.y, f, false), pair8(x.y, f, true));
-    }
     int at = -1;  // the quarter in registers
     uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-    float f = 0.0f;
+    uint32_t byte = 0;
+    const auto quarter = [&](int s) {
+      at = s / kQuarter8;
+      const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
+      const uint4* from = (const uint4*)(page + fc::v8_at(s % kPage8 & ~(kQuarter8 - 1), 2 * lane));
+      a = from[0];
+      b = from[1];
+      byte = page[fc::kPage8Scales + 2 + s % kPage8 / kBlock8];
+    };
+    const int c = lane & 15;
+    int from[4];
+    uint2 x[4];
+    uint32_t bytes[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      from[p] = __shfl(sl, 4 * p + (lane >> 4));
+      const int s = from[p] < 0 ? 0 : from[p], t = s % kPage8;  // row 0 for nothing
+      const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
+      x[p] = *(const uint2*)(page + fc::k8_at(t, 8 * c));
+      bytes[p] = page[fc::kPage8Scales + t / kBlock8];
+    }
+    const int s0 = __builtin_amdgcn_readfirstlane(sl);
+    if (s0 >= 0) quarter(s0);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      if (from[p] < 0) continue;
+      const float f = fc::scale8(bytes[p]);
+      *(uint4*)(k + ((i0 + 4 * p + (lane >> 4)) * Hkv + h) * kDim8 + 8 * c) =
+          make_uint4(pair8(x[p].x, f, false), pair8(x[p].x, f, true), pair8(x[p].y, f, false), pair8(x[p].y, f, true));
+    }
     for (int e = 0; e < kReadRows; ++e) {
       const int s = __builtin_amdgcn_readlane(sl, e);
       if (s < 0) continue;
       const int t = s % kPage8;
-      if (s / kQuarter8 != at) {
-        at = s / kQuarter8;
-        const uint8_t* page = pool + ((int64_t)(s / kPage8) * Hkv + h) * kPage8Bytes;
-        const uint4* from = (const uint4*)(page + fc::v8_at(t & ~(kQuarter8 - 1), 2 * lane));
-        a = from[0];
-        b = from[1];
-        f = fc::scale8(page[fc::kPage8Scales + 2 + t / kBlock8]);
-      }
+      if (s / kQuarter8 != at) quarter(s);
       const int u = t % kQuarter8;
       const uint32_t wa = u < 8 ? (u < 4 ? a.x : a.y) : (u < 12 ? a.z : a.w);
       const uint32_t wb = u < 8 ? (u < 4 ? b.x : b.y) : (u < 12 ? b.z : b.w);
       const uint32_t both = ((wa >> (8 * (u & 3))) & 255u) | (((wb >> (8 * (u & 3))) & 255u) << 8);
-      *(uint32_t*)(v + ((i0 + e) * Hkv + h) * kDim8 + 2 * lane) = pair8(both, f, false);
+      *(uint32_t*)(v + ((i0 + e) * Hkv + h) * kDim8 + 2 * lane) = pair8(both, fc::scale8(byte), false);
     }
   }
 }
