@@ -1093,3 +1093,28 @@ def test_more_sequences_and_pages_than_one_launch_takes():
     for x, y in zip(got[:2], got[2:]):
         assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
         assert (x[2].float() - y[2].float()).abs().max() < 0.03      # other parts: a weight's rounding
+
+
+@pytest.mark.parametrize("B,R,H,Hkv", [(140, 9, 16, 4), (270, 9, 8, 2), (300, 1, 8, 2), (130, 2, 16, 8)])
+@pytest.mark.parametrize("how", ["mixed", "same", "none", "one"])
+def test_attention_of_more_workgroups_than_run_at_once(B, R, H, Hkv, how):
+    """Trees taken longest first, with ties, with empty prefixes, and with more of them
+    than are put in order: each is still answered once."""
+    rng = np.random.default_rng(B + R)
+    lens = {"mixed": rng.integers(0, 260, B), "same": np.full(B, 130), "none": np.zeros(B, int),
+            "one": np.where(np.arange(B) == B // 2, 300, 0)}[how].tolist()
+    say(f"attention of many {B},{R},{H},{Hkv} {how}")
+    pool = make_pool(rng, 50, Hkv)
+    attend(rng, B, R, H, Hkv, lens, pool=pool, width=5, tree=trees(rng, B, R) if how == "mixed" else None)
+
+
+@pytest.mark.parametrize("H,Hkv,lens,adds", [
+    (3, 1, [200], [700]),            # 2,100 rows, three heads: rounds end inside a token
+    (5, 1, [0, 640], [300, 1]),      # one sequence of many rows, one of a token
+    (7, 1, [63], [129]), (40, 2, [5], [110]), (12, 4, [1000, 3], [40, 300]),
+])
+def test_weights_of_long_prompts_and_odd_heads(H, Hkv, lens, adds):
+    rng = np.random.default_rng(H + sum(adds))
+    say(f"weights of prompts H={H} Hkv={Hkv} lens={lens} adds={adds}")
+    weigh(rng, H, Hkv, lens, adds)
+    weigh(rng, H, Hkv, lens, adds, n_src=sum(adds) + 5)
