@@ -11,6 +11,8 @@
 
 namespace {
 
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
 using fc::kBlock8;
 using fc::kDim8;
 using fc::kPage8;
@@ -101,10 +103,8 @@ __device__ __forceinline__ int number_of(const Weights& A, const Step& S, int t)
   const int row = kSrc ? A.src[there ? at : 0] : (int)at;
   return there ? row : -1;
 }
-// 16 rows of queries.  kAsCodes: lane (lg, lc) has dims 64 u + 16 lg + 8 h .. + 7 of row
-// lc in q[2 u + h], as 16 key codes lie; otherwise dims 32 u + 8 lg .. + 7 in q[u], so
-// that four lanes read 64 bytes of a row together.
-template <bool kAsCodes>
+// 16 rows of queries: lane (lg, lc) has dims 64 u + 16 lg + 8 h .. + 7 of row lc in
+// q[2 u + h], as 16 key codes lie.
 struct Rows {
   bf16x8 q[4];
   float lse;
@@ -113,37 +113,40 @@ struct Rows {
     const bool there = number >= 0 && number < A.n_rows;
     const int row = there ? number : 0;
     const int64_t h = S.kv * S.G + head;
-    const uint16_t* p = A.q + row * A.q_stride + h * kDim8 + (kAsCodes ? 16 : 8) * (fc::lane_id() >> 4);
+    const uint16_t* p = A.q + row * A.q_stride + h * kDim8 + 16 * (fc::lane_id() >> 4);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) q[u] = *(const bf16x8*)(p + (kAsCodes ? 64 * (u / 2) + 8 * (u % 2) : 32 * u));
+    for (int u = 0; u < 4; ++u) q[u] = *(const bf16x8*)(p + 64 * (u / 2) + 8 * (u % 2));
     lse = A.lse[(int64_t)row * A.H + h];
     last = there ? S.len + token : -1;
   }
 };
-// What 16 rows pay to a lane's keys key0 .. key0 + 4 T - 1, on top of `got`.  keys(t, u):
-// the u-th quarter of the dims of key tile t, whose row 4 a + b is key 4 T a + 4 t + b.
-template <int T, bool kAsCodes, typename Keys>
-__device__ __forceinline__ void pay(Keys keys, const Rows<kAsCodes>& x, float scale, int key0, float (&got)[4 * T]) {
+// What 16 rows pay to a lane's 4 T keys, on top of `got`.  keys(t, u): the u-th quarter
+// of the dims of key tile t, whose row 4 a + b is key 4 T a + 4 t + b.  minus: the row's
+// logarithm, base 2, turned around; seen: the last of the lane's keys that the row sees.
+template <int T, typename Keys>
+__device__ __forceinline__ void pay(Keys keys, const bf16x8 (&q)[4], float scale, float minus, int seen, float (&got)[4 * T]) {
   floatx4 s[T];
 #pragma unroll
   for (int t = 0; t < T; ++t) s[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int u = 0; u < 4; ++u)  // no product waits for the one before
 #pragma unroll
-    for (int t = 0; t < T; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys(t, u), x.q[u], s[t], 0, 0, 0);
+    for (int t = 0; t < T; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys(t, u), q[u], s[t], 0, 0, 0);
   // a product's result is read only some cycles after it was issued
-  static_assert(T == 4, "the wait below");
-  asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
-  const float minus = 0.0f - x.lse * kLog2e;
-  // the lane's keys that the row sees, less one; a row that saw nothing pays nothing
-  const int seen = x.lse == -INFINITY ? -1 : x.last - key0;
+  static_assert(T == 4 || T == 2, "the wait below");
+  if constexpr (T == 4) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
+  else asm volatile("s_nop 7\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1]));
+  const auto add = [&](bool all) {
 #pragma unroll
-  for (int t = 0; t < T; ++t)
+    for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, minus));
-      got[4 * t + e] += 4 * t + e <= seen ? p : 0.0f;
-    }
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, minus));
+        got[4 * t + e] += all || 4 * t + e <= seen ? p : 0.0f;
+      }
+  };
+  if (T == 2 && fc::ballot(seen < 4 * T - 1) == 0) add(true);
+  else add(false);
 }
 __device__ __forceinline__ float key_scale(uint32_t byte) {
   return fc::scale8(byte) * (kLog2e / sqrtf((float)kDim8));
@@ -154,54 +157,56 @@ __device__ __forceinline__ void settle_weight(const Weights& A, const Step& S, i
   if (j < S.end) *to = j < S.len || again ? *to + sum : sum;
 }
 
-// Many rows (prompts): a workgroup's waves hold a page's keys as bf16 and go through the
-// sequence's rows, every eighth 16 of them each, four of those on their way; the waves'
-// sums are joined.  Nothing is added by two workgroups, so sums have one order.
-constexpr int kAhead = 4, kManyWaves = 8;
+// One wave loads 64 x 16 (or 64 x 4) bytes into LDS, lane L's behind lane L - 1's.
+// Counted by vmcnt like any load; the compiler does not know of it.
+__device__ __forceinline__ void to_lds16(uint32_t lds, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(from)
+               : "memory");
+}
+__device__ __forceinline__ void to_lds4(uint32_t lds, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(from)
+               : "memory");
+}
+
+// Many rows (prompts): a workgroup's waves hold half a page's keys as bf16 and go through
+// the sequence's rows, every eighth 16 of them each; the waves' sums are joined.  Nothing
+// is added by two workgroups, so sums have one order.  Rows come through LDS, whole ones
+// at a time: as a product takes them, 16 lanes would ask for 16 lines at once.
+constexpr int kManyWaves = 8, kManyTiles = 2, kHalf = 16 * kManyTiles;
+constexpr int kRing = 2, kRoundTiles = 4;  // tiles on their way, tiles whose rows lanes look after
+constexpr int kTileBytes = kTile * kDim8 * 2;
+constexpr int kCus = 256;
+struct ManyShared {
+  alignas(16) uint8_t rows[kManyWaves][kRing][kTileBytes];
+  float lse[kManyWaves][fc::kWave];
+  int number[kManyWaves][fc::kWave];
+  float sum[kManyWaves - 1][fc::kWave];
+};
 template <bool kSrc>
-__global__ void __launch_bounds__(kManyWaves* fc::kWave, 2) k_weights_many(Weights A) {
-  constexpr int T = kKTiles;
-  __shared__ float s_sum[kManyWaves - 1][kPage8];
+__global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weights A, int pieces) {
+  constexpr int T = kManyTiles;
+  __shared__ ManyShared sh;
   const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
-  // a head's pages lie on one XCD, whose L2 has its rows then; the first ones, which most
-  // rows see, begin first
-  const int b = (int)blockIdx.x / A.Hkv, pg = A.y0 + (int)blockIdx.y;
+  // A head's pages lie on one XCD, whose L2 has its rows then.  The first pages are seen
+  // by most rows: the heaviest workgroup of a card full begins with the lightest of the
+  // next one, so that a CU which gets both has no more to do than the others.
+  const int full = gridDim.x < kCus ? kCus / (int)gridDim.x : 1, y = A.y0 + (int)blockIdx.y, y0 = y / full * full;
+  const int piece = (y / full) % 2 ? y0 + (y0 + full < pieces ? full : pieces - y0) - 1 - (y - y0) : y;
+  const int b = (int)blockIdx.x / A.Hkv, key0 = piece * kHalf;
   const Step S(A, b, (int)blockIdx.x % A.Hkv);
-  if (S.n <= 0 || pg * kPage8 >= S.end) return;  // all waves of the workgroup
-  const int id = A.table[(int64_t)b * A.max_pages + pg];
+  if (S.n <= 0 || key0 >= S.end) return;  // all waves of the workgroup
+  const int id = A.table[(int64_t)b * A.max_pages + piece / 2];
   if (id < 0 || id >= A.n_pages) return;
-  // rows that come before the page's first key see nothing of it
-  const int64_t skip = (int64_t)pg * kPage8 - S.len;
+  // rows that come before the first key see nothing
+  const int64_t skip = (int64_t)key0 - S.len;
   const int64_t tiles = ((int64_t)S.n * S.G + kTile - 1) / kTile;
   int64_t tile = (skip > 0 ? skip * S.G / kTile : 0) + w;
-  constexpr int kRound = kManyWaves * kAhead * kTile;  // rows of a round of the waves
-  const Cursor round(S, kRound);
-  Cursor now(S, tile * kTile), next = now;
-  // numbers of a round's rows, a tile in each 16 lanes
-  const auto numbers = [&](const Cursor& c) {
-    int token, head;
-    c.at(S, kManyWaves * kTile * lg + lc, token, head);
-    return number_of<kSrc>(A, S, token);
-  };
-  const auto go_on = [&](Cursor& c) {
-    c += round;
-    c.carry(S);
-  };
-  Rows<false> x[kAhead];
-  const auto load = [&](const Cursor& c, int n, int i) {
-    int token, head;
-    c.at(S, kManyWaves * kTile * i + lc, token, head);
-    x[i].load(A, S, token, head, __shfl(n, 16 * i + lc));
-    asm volatile("" ::: "memory");  // asked for here and no later
-  };
-  int n_now = numbers(now);
-  go_on(next);
-  int n_next = numbers(next);
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) load(now, n_now, i);
+  static_assert(kRoundTiles * kTile == fc::kWave, "a lane for each of a wave's rows");
+  const Cursor round(S, kManyWaves * kRoundTiles * kTile);
+  Cursor at(S, tile * kTile);
   const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + S.kv) * kPage8Bytes;
-  const int key_row = 4 * T * (lc >> 2) + (lc & 3);
+  const int key_row = piece % 2 * kHalf + 4 * T * (lc >> 2) + (lc & 3);
   bf16x8 key[T][4];
 #pragma unroll
   for (int t = 0; t < T; ++t)
@@ -210,29 +215,94 @@ __global__ void __launch_bounds__(kManyWaves* fc::kWave, 2) k_weights_many(Weigh
       const uint2 c = *(const uint2*)(page + (key_row + 4 * t) * kDim8 + 32 * u + 8 * lg);
       key[t][u] = widen(c.x, c.y);
     }
-  const float scale = key_scale(page[fc::kPage8Scales + (lg >> 1)]);
+  static_assert(kHalf == fc::kBlock8, "one scale");
+  const float scale = key_scale(page[fc::kPage8Scales + piece % 2]);
+  // Each lane looks after one of a round's rows: its number is asked for first, from that
+  // follow its place and its logarithm.
+  const uint32_t lds_rows = (uint32_t)(uintptr_t)(lds_u8*)sh.rows[w], lds_lse = (uint32_t)(uintptr_t)(lds_u8*)sh.lse[w],
+                 lds_number = (uint32_t)(uintptr_t)(lds_u8*)sh.number[w];
+  int token, head, number;  // of the row after the one looked at
+  bool there;
+  const auto ask = [&] {
+    at.at(S, kManyWaves * kTile * lg + lc, token, head);
+    const int64_t i = (int64_t)S.cu + token;
+    there = token < S.n && i >= 0 && i < A.n, number = (int)i;
+    if (kSrc) to_lds4(lds_number, A.src + (there ? i : 0));
+    at += round;
+    at.carry(S);
+  };
+  int64_t place;
+  int last;  // the last key that the row sees; -1: there is no such row
+  const auto look = [&] {
+    if (kSrc) number = sh.number[w][lane];
+    const bool is = there && number >= 0 && number < A.n_rows;
+    const int row = is ? number : 0, h = S.kv * S.G + head;
+    place = row * A.q_stride + (int64_t)h * kDim8;
+    last = is ? S.len + token : -1;
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(last) : : "memory");  // the number is read
+    to_lds4(lds_lse, A.lse + (int64_t)row * A.H + h);
+  };
+  // Four rows at a time, 16 lanes each; a row's r-th 16 bytes lie at r ^ row, so that 16
+  // rows' are read from all banks at once.
+  const auto load = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 4 * u + lg;
+      const int64_t from = (int64_t)(uint32_t)__shfl((int)(uint32_t)place, kTile * i + r) |
+                           (int64_t)__shfl((int)(place >> 32), kTile * i + r) << 32;
+      to_lds16(lds_rows + (uint32_t)(i % kRing * kTileBytes + u * 1024), A.q + from + 8 * (lc ^ r));
+    }
+  };
+  ask();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  look();
+  ask();
+  load(0);
+  load(1);
   float got[4 * T];
 #pragma unroll
   for (int i = 0; i < 4 * T; ++i) got[i] = 0.0f;
-  for (; tile < tiles; tile += kManyWaves * kAhead) {
-    now = next;
-    n_now = n_next;
-    go_on(next);
-    n_next = numbers(next);
+  const int own0 = key0 + 4 * T * lg;
+  int next_last = last;
+  for (; tile < tiles; tile += kManyWaves * kRoundTiles) {
+    float minus = 0.0f;
+    int sees = -1;
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      pay<T>([&](int t, int u) { return key[t][u]; }, x[i], scale, pg * kPage8 + 4 * T * lg, got);
-      asm volatile("" ::: "memory");
-      load(now, n_now, i);
+    for (int i = 0; i < kRoundTiles; ++i) {
+      // Behind tile i's loads: the next tile's, and what `look` and `ask` loaded.
+      if (i == kRoundTiles - 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSrc ? 6 : 5) : "memory");
+      else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      if (i == 0) {
+        const float lse = sh.lse[w][lane];
+        minus = 0.0f - lse * kLog2e;
+        sees = lse == -INFINITY ? -1 : next_last;  // a row that saw nothing pays nothing
+      }
+      bf16x8 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        x[u] = *(const bf16x8*)(sh.rows[w][i % kRing] + lc * (kDim8 * 2) + (((4 * u + lg) ^ lc) * 16));
+      asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]) : : "memory");
+      if (i == kRoundTiles - kRing) {
+        look();
+        ask();
+        next_last = last;
+      }
+      load((i + kRing) % kRoundTiles);
+      pay<T>([&](int t, int u) { return key[t][u]; }, x, scale, __shfl(minus, kTile * i + lc),
+             __shfl(sees, kTile * i + lc) - own0, got);
     }
   }
-  float sum = sum_of_own(got, lc);  // of key 16 lg + lc
-  if (w > 0) s_sum[w - 1][lane] = sum;
-  __syncthreads();
-  if (w > 0) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing on its way into LDS that others may get
+  float v[16];
 #pragma unroll
-  for (int g = 0; g < kManyWaves - 1; ++g) sum += s_sum[g][lane];
-  settle_weight(A, S, id, pg * kPage8 + lane, sum, false);
+  for (int i = 0; i < 16; ++i) v[i] = i < 4 * T ? got[i] : 0.0f;
+  float sum = sum_of_own(v, lc);  // of key 8 lg + lc, lc < 8
+  if (w > 0) sh.sum[w - 1][lane] = sum;
+  __syncthreads();
+  if (w > 0 || lc >= 4 * T) return;
+#pragma unroll
+  for (int g = 0; g < kManyWaves - 1; ++g) sum += sh.sum[g][lane];
+  settle_weight(A, S, id, own0 + lc, sum, false);
 }
 
 // Few rows (a token, an accepted path): a wave holds up to 64 of them and goes through
@@ -272,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_weights_few(Weights A, int part
     c.at(S, lane, token, head);
     const int mine = number_of<kSrc>(A, S, token);  // a row a lane
     load_page(id);
-    Rows<true> x[kFewTiles];
+    Rows x[kFewTiles];
     const int n = rows - r0 < kRound ? (int)((rows - r0 + kTile - 1) / kTile) : kFewTiles;
 #pragma unroll
     for (int i = 0; i < kFewTiles; ++i)
@@ -300,7 +370,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_weights_few(Weights A, int part
         for (int i = 0; i < 16; ++i) got[i] = 0.0f;
 #pragma unroll
         for (int i = 0; i < kFewTiles; ++i)
-          if (i < n) pay<kKTiles>([&](int t, int u) { return key[t][u]; }, x[i], scale, pg * kPage8 + 16 * lg, got);
+          if (i < n)
+            pay<kKTiles>([&](int t, int u) { return key[t][u]; }, x[i].q, scale, 0.0f - x[i].lse * kLog2e,
+                         // a row that saw nothing pays nothing
+                         x[i].lse == -INFINITY ? -1 : x[i].last - (pg * kPage8 + 16 * lg), got);
         settle_weight(A, S, id, pg * kPage8 + lane, sum_of_own(got, lc), r0 > 0);  // key 16 lg + lc
       } else {
         load_page(next);
@@ -800,7 +873,7 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
   const bool many = (int64_t)n * (H / Hkv) > 2 * kFewTiles * kTile * (int64_t)B;
   int each = 4;
   while (each > 1 && (int64_t)B * Hkv * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
-  const uint32_t parts = many ? pages : fc::div_up(pages, each * kWaves);
+  const uint32_t parts = many ? pages * (kPage8 / kHalf) : fc::div_up(pages, each * kWaves);
   const int32_t at_once = sequences_at_once(B, Hkv);
   (void)hipGetLastError();
   for (int32_t b = 0; b < B; b += at_once) {
@@ -809,8 +882,8 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
       const Weights a = {weights, q, q_stride, lse, pool, table + (int64_t)b * max_pages, len + b, new_len + b, cu + b, src,
                          n_rows, n_pages, max_pages, n, H, Hkv, max_len, (int)y};
       const dim3 grid(pairs, parts - y < kMostY ? parts - y : kMostY);
-      if (many && src) hipLaunchKernelGGL(k_weights_many<true>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a);
-      else if (many) hipLaunchKernelGGL(k_weights_many<false>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a);
+      if (many && src) hipLaunchKernelGGL(k_weights_many<true>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a, (int)parts);
+      else if (many) hipLaunchKernelGGL(k_weights_many<false>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a, (int)parts);
       else if (src) hipLaunchKernelGGL(k_weights_few<true>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
       else hipLaunchKernelGGL(k_weights_few<false>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
       FC_CHECK_LAUNCH();
