@@ -40,7 +40,7 @@ struct Weights {
   const uint8_t* pool;
   const int32_t *table, *len, *new_len, *cu, *src;
   int n_rows, n_pages, max_pages, n, H, Hkv, max_len;
-  int y0;  // pages, or parts, before this launch's
+  int y0;  // parts before this launch's
 };
 
 __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b) {
@@ -175,7 +175,7 @@ __device__ __forceinline__ void to_lds4(uint32_t lds, const void* from) {
 constexpr int kManyWaves = 8, kManyTiles = 2, kHalf = 16 * kManyTiles;
 constexpr int kRing = 2, kRoundTiles = 4;  // tiles on their way, tiles whose rows lanes look after
 constexpr int kTileBytes = kTile * kDim8 * 2;
-constexpr int kCus = 256;
+constexpr int kCus = 256, kXcds = 8;
 struct ManyShared {
   alignas(16) uint8_t rows[kManyWaves][kRing][kTileBytes];
   float lse[kManyWaves][fc::kWave];
@@ -183,21 +183,24 @@ struct ManyShared {
   float sum[kManyWaves - 1][fc::kWave];
 };
 template <bool kSrc>
-__global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weights A, int pieces) {
+__global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weights A, int pairs, int pieces) {
   constexpr int T = kManyTiles;
   __shared__ ManyShared sh;
   const int lane = fc::lane_id(), lg = lane >> 4, lc = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
-  // A head's pages lie on one XCD, whose L2 has its rows then.  The first pages are seen
-  // by most rows: the heaviest workgroup of a card full begins with the lightest of the
-  // next one, so that a CU which gets both has no more to do than the others.
-  const int full = gridDim.x < kCus ? kCus / (int)gridDim.x : 1, y = A.y0 + (int)blockIdx.y, y0 = y / full * full;
-  const int piece = (y / full) % 2 ? y0 + (y0 + full < pieces ? full : pieces - y0) - 1 - (y - y0) : y;
-  const int b = (int)blockIdx.x / A.Hkv, key0 = piece * kHalf;
-  const Step S(A, b, (int)blockIdx.x % A.Hkv);
+  // A sequence's and head's workgroups follow one another, on one XCD if heads can be
+  // dealt out like that: its L2 has the rows then.  The first keys are seen by most rows:
+  // every other card full goes backwards, so that a CU which gets one workgroup of each
+  // has no more to do than the others.
+  const bool dealt = pairs % kXcds == 0;
+  const int full = dealt ? kCus / kXcds : kCus, all = dealt ? pairs / kXcds * pieces : pairs * pieces;
+  int at_pair = dealt ? (int)blockIdx.x % kXcds : 0, k = dealt ? (int)blockIdx.x / kXcds : (int)blockIdx.x;
+  const int k0 = k / full * full;
+  if (k / full % 2) k = k0 + (all - k0 < full ? all - k0 : full) - 1 - (k - k0);
+  at_pair += k / pieces * (dealt ? kXcds : 1);
+  const int piece = k % pieces, b = at_pair / A.Hkv, key0 = piece * kHalf;
+  const Step S(A, b, at_pair % A.Hkv);
   if (S.n <= 0 || key0 >= S.end) return;  // all waves of the workgroup
-  const int id = A.table[(int64_t)b * A.max_pages + piece / 2];
-  if (id < 0 || id >= A.n_pages) return;
   // rows that come before the first key see nothing
   const int64_t skip = (int64_t)key0 - S.len;
   const int64_t tiles = ((int64_t)S.n * S.G + kTile - 1) / kTile;
@@ -205,18 +208,6 @@ __global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weigh
   static_assert(kRoundTiles * kTile == fc::kWave, "a lane for each of a wave's rows");
   const Cursor round(S, kManyWaves * kRoundTiles * kTile);
   Cursor at(S, tile * kTile);
-  const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + S.kv) * kPage8Bytes;
-  const int key_row = piece % 2 * kHalf + 4 * T * (lc >> 2) + (lc & 3);
-  bf16x8 key[T][4];
-#pragma unroll
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const uint2 c = *(const uint2*)(page + (key_row + 4 * t) * kDim8 + 32 * u + 8 * lg);
-      key[t][u] = widen(c.x, c.y);
-    }
-  static_assert(kHalf == fc::kBlock8, "one scale");
-  const float scale = key_scale(page[fc::kPage8Scales + piece % 2]);
   // Each lane looks after one of a round's rows: its number is asked for first, from that
   // follow its place and its logarithm.
   const uint32_t lds_rows = (uint32_t)(uintptr_t)(lds_u8*)sh.rows[w], lds_lse = (uint32_t)(uintptr_t)(lds_u8*)sh.lse[w],
@@ -254,11 +245,25 @@ __global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weigh
     }
   };
   ask();
+  const int id = A.table[(int64_t)b * A.max_pages + piece / 2];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (id < 0 || id >= A.n_pages) return;
   look();
   ask();
   load(0);
   load(1);
+  const uint8_t* page = A.pool + ((int64_t)id * A.Hkv + S.kv) * kPage8Bytes;
+  const int key_row = piece % 2 * kHalf + 4 * T * (lc >> 2) + (lc & 3);
+  bf16x8 key[T][4];
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint2 c = *(const uint2*)(page + (key_row + 4 * t) * kDim8 + 32 * u + 8 * lg);
+      key[t][u] = widen(c.x, c.y);
+    }
+  static_assert(kHalf == fc::kBlock8, "one scale");
+  const float scale = key_scale(page[fc::kPage8Scales + piece % 2]);
   float got[4 * T];
 #pragma unroll
   for (int i = 0; i < 4 * T; ++i) got[i] = 0.0f;
@@ -810,6 +815,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) k_evict_move(Evict A) {
 // A launch takes fewer than 2^32 threads in a dimension, and 65,536 workgroups in the
 // second: longer calls are several.
 constexpr uint32_t kMostY = 1 << 15;
+constexpr int64_t kMostMany = 1 << 22;  // workgroups of 512 threads
 template <int TURN>
 void in_turn(Evict a, uint32_t pairs, hipStream_t stream) {
   for (uint32_t y = 0; y < (uint32_t)a.parts; y += kMostY) {
@@ -868,24 +874,39 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
                   {src, 4 * (uint64_t)n}}))
     return FC_ERR_INVALID;
   const uint32_t pages = fc::div_up((uint64_t)max_len, kPage8);
-  // More rows than a wave holds twice over: pages are held, rows go by.  Otherwise four
-  // pages a wave, or fewer where that leaves the card idle.
-  const bool many = (int64_t)n * (H / Hkv) > 2 * kFewTiles * kTile * (int64_t)B;
+  // Held rows go through the pages in rounds of 64, P pages of all heads together at
+  // 5.5 + 0.002 P us a round.  Held pages cost 9 + 0.034 P us to begin with (a workgroup
+  // waits three times before its first product), and rows past the first 500 0.0018 P us
+  // for each 64.  Both measured: 32 heads on 8, 1 sequence of 2,000 tokens, 264 pages: 256
+  // rows 23 and 18 us, 2,048 rows 118 and 37; 8 sequences, 2,112 pages: 256 rows 43 and
+  // 81, 512 rows 85 and 82, 1,024 rows 183 and 117; 48 sequences, 12,700 pages: 512 rows
+  // 235 and 436, 1,024 rows 482 and 617.
+  const int64_t all_pages = (int64_t)B * Hkv * pages;
+  const bool many = all_pages * (kPage8 / kHalf) <= kMostMany &&
+                    25 * (int64_t)n * (H / Hkv) >= 4 * (int64_t)B * (all_pages + 700);
+  // Four pages a wave, or fewer where that leaves the card idle.
   int each = 4;
   while (each > 1 && (int64_t)B * Hkv * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
-  const uint32_t parts = many ? pages * (kPage8 / kHalf) : fc::div_up(pages, each * kWaves);
-  const int32_t at_once = sequences_at_once(B, Hkv);
   (void)hipGetLastError();
+  const auto now = [&](int32_t b, int y0) {
+    return Weights{weights, q, q_stride, lse, pool, table + (int64_t)b * max_pages, len + b, new_len + b, cu + b, src,
+                   n_rows, n_pages, max_pages, n, H, Hkv, max_len, y0};
+  };
+  if (many) {
+    const uint32_t pieces = pages * (kPage8 / kHalf), pairs = (uint32_t)B * (uint32_t)Hkv;
+    const auto kernel = src ? k_weights_many<true> : k_weights_many<false>;
+    hipLaunchKernelGGL(kernel, dim3(pairs * pieces), dim3(kManyWaves * fc::kWave), 0, stream, now(0, 0), (int)pairs, (int)pieces);
+    FC_CHECK_LAUNCH();
+    return FC_OK;
+  }
+  const uint32_t parts = fc::div_up(pages, each * kWaves);
+  const int32_t at_once = sequences_at_once(B, Hkv);
   for (int32_t b = 0; b < B; b += at_once) {
     const uint32_t pairs = (uint32_t)(B - b < at_once ? B - b : at_once) * (uint32_t)Hkv;
     for (uint32_t y = 0; y < parts; y += kMostY) {
-      const Weights a = {weights, q, q_stride, lse, pool, table + (int64_t)b * max_pages, len + b, new_len + b, cu + b, src,
-                         n_rows, n_pages, max_pages, n, H, Hkv, max_len, (int)y};
-      const dim3 grid(pairs, parts - y < kMostY ? parts - y : kMostY);
-      if (many && src) hipLaunchKernelGGL(k_weights_many<true>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a, (int)parts);
-      else if (many) hipLaunchKernelGGL(k_weights_many<false>, grid, dim3(kManyWaves * fc::kWave), 0, stream, a, (int)parts);
-      else if (src) hipLaunchKernelGGL(k_weights_few<true>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
-      else hipLaunchKernelGGL(k_weights_few<false>, grid, dim3(kThreads), 0, stream, a, each * kWaves);
+      const auto kernel = src ? k_weights_few<true> : k_weights_few<false>;
+      hipLaunchKernelGGL(kernel, dim3(pairs, parts - y < kMostY ? parts - y : kMostY), dim3(kThreads), 0, stream,
+                         now(b, (int)y), each * kWaves);
       FC_CHECK_LAUNCH();
     }
   }
