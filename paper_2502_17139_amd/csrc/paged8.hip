@@ -66,7 +66,10 @@ __device__ __forceinline__ Scaled rescale(uint32_t top, uint32_t byte, bool fres
 // they are, values dim by dim.  A block that the run begins (its first row is among
 // the run's) is written whole, with zeros in the rows that are not there yet; in
 // others the key rows alone and all of the values, whose 16-byte pieces hold other
-// tokens too, unless the scale rises and all codes are rounded anew.
+// tokens too, unless the scale rises and all codes are rounded anew.  Read are 512 bytes a
+// token and key head, written 258: prompts of 22,700 tokens, 32 key heads, 190 us where a
+// copy of as many bytes takes 113.  140 registers leave three waves a SIMD; held to 128
+// or 96 they spill (227 and 302 us).
 __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
   const int lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
@@ -259,7 +262,10 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w, float s, bool high) {
 
 // A wave takes 16 entries through every fourth head.  Keys: 16 lanes a row, eight dims
 // each.  Values: two dims a lane, 16 tokens of them in two loads; entries of one such
-// quarter that follow one another, as the tokens of a sequence do, share the loads.
+// quarter that follow one another, as the tokens of a sequence do, share the loads.  Bound
+// by what is written, 512 bytes a token and key head: 22,700 tokens of 32 key heads 137 us,
+// 4.1 TB/s of a copy's 4.95.  All loads are asked for before the first result is written
+// (159 us one after another); four dims a lane, half as many tokens each, was 232.
 __global__ void __launch_bounds__(kReadThreads) k_paged8_read(const uint8_t* __restrict__ pool, int n_pages, int Hkv,
                                                               const int32_t* __restrict__ slot, int64_t first, int64_t n,
                                                               uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
@@ -349,9 +355,12 @@ extern "C" fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t
                  {fc::rows_span(k, n_src, k_stride, Hkv * D), fc::rows_span(v, n_src, v_stride, Hkv * D),
                   {slot, numbers}, {src, numbers}}))
     return FC_ERR_INVALID;
-  // A window of 32 entries begins one run or two of a prompt's; single tokens, each a
-  // run of its own, are spread further.
-  const int window = n >= 8192 ? kMostWindow : n >= 1024 ? 8 : 1;
+  // A window of 32 entries begins one run or two of a prompt's; single tokens, each a run
+  // of its own, are spread further.  Windows of 1, 8 and 32, 8 key heads: 320 single
+  // tokens 11, 30 and 113 us, 320 of a prompt 12.5, 9 and 9; 1,024: 27, 33 and 114, and
+  // 37, 9 and 9; 4,096: 95, 115 and 138, and 114, 24 and 9; 65,536 of a prompt 1,867, 261
+  // and 90.  So many single tokens at once are rarer than prompts.
+  const int window = n >= 2048 ? kMostWindow : n >= 1024 ? 8 : 1;
   Write a = {pool, {k, v}, {k_stride, v_stride}, slot, src, 0, n, n_src, n_pages, Hkv, window};
   const int64_t groups = fc::div_up((uint64_t)n, (uint64_t)window);
   const uint32_t y = over_heads(groups, (2 * (int64_t)Hkv + kWriteWaves - 1) / kWriteWaves);

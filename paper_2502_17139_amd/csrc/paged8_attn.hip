@@ -518,7 +518,9 @@ __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& 
 // One or two tiles of query rows (a decoded token, a short chain): a workgroup's waves
 // go through every fourth (or eighth) page alone, out of registers, and wait for
 // nobody until the end.  A page's keys are asked for while the one before has its
-// weights, its values while the next scores are made.
+// weights, its values while the next scores are made.  Bound by memory, 16.5 KB a page
+// and head: 131,000 tokens of 8 key heads 43 us and 5 for the join, 5.7 TB/s; 64 sequences
+// of up to 8,192 tokens 77 us, 4.7 TB/s; 3,000 tokens 10 and 4 us, a chain of round trips.
 template <int NT, int kAloneWaves, bool kLse>
 __global__ void __launch_bounds__(kAloneWaves* fc::kWave, 2) k_paged8_attn_alone(Args A) {
   constexpr int T = 2;  // tiles of tree rows: at most 32
@@ -796,6 +798,10 @@ __device__ __forceinline__ void group_tree(const Args& A, const Work& W, int j0,
   }
 }
 
+// More tiles: a workgroup's waves share pages, four of them on their way through LDS, and
+// have one or two tiles each.  Bound by what a wave does in turn - scores, weights, values
+// - with two waves a SIMD: 48 trees of 65 rows over up to 4,096 tokens, 32 heads on 8,
+// 160 us where the products' rate allows 64; of 4,096 tokens each 390; without a prefix 55.
 template <bool kLse>
 __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
   static_assert(2 * kPage8 * kRowBytes <= kSlots * kSlot, "tree rows where the pages were");
@@ -958,13 +964,17 @@ struct Shape {
 };
 
 // How a call is laid out: a workgroup for every eight tiles of query rows of a key
-// head, parts of the pages where that leaves the chip idle.
+// head, parts of the pages where that leaves the chip idle (131,000 tokens, one query row:
+// in 1 part 612 us, 8 91, 16 53, 32 48; a tree of 65 rows over 3,000 tokens: 83, 30, 33).
 Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   Shape s;
   s.tiles = (R * (H / Hkv) + kTile - 1) / kTile;
   s.chunks = s.tiles <= kWaveTiles ? 1 : (s.tiles + kGroupTiles - 1) / kGroupTiles;
   const int64_t wgs = (int64_t)B * Hkv * s.chunks;
   const int64_t pages = ((int64_t)max_len + kPage8 - 1) / kPage8;
+  // Eight waves where prefixes are long or workgroups few, one workgroup to a CU (32 heads
+  // on 8, single tokens: 64 sequences of up to 8,192 tokens 77 us, with four waves 107;
+  // 128 of up to 1,000 tokens 42 with eight, 27 with four; 64 of up to 2,048 28 and 27).
   s.alone = s.tiles > kWaveTiles ? 0 : pages >= 64 || wgs <= kCus ? 8 : 4;
   const int64_t slots = s.alone == 8 ? kCus : 2 * kCus;  // workgroups at once
   int64_t each = s.alone ? s.alone : 4;
@@ -978,7 +988,8 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   s.part_pages = each < 1 ? 1 : (int)each;
   s.parts = pages <= s.part_pages ? 1 : (int)((pages + s.part_pages - 1) / s.part_pages);
   // Where not all workgroups run at once, a long one that began last would be waited
-  // for alone.
+  // for alone (64 sequences of up to 8,192 tokens: 77 us, as they come 93; 48 trees of 65
+  // rows over up to 4,096: 153 and 221; of equal lengths no difference).
   s.ordered = B > 1 && wgs * s.parts > slots;
   return s;
 }

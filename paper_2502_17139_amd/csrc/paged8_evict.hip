@@ -171,7 +171,12 @@ __device__ __forceinline__ void to_lds4(uint32_t lds, const void* from) {
 // Many rows (prompts): a workgroup's waves hold half a page's keys as bf16 and go through
 // the sequence's rows, every eighth 16 of them each; the waves' sums are joined.  Nothing
 // is added by two workgroups, so sums have one order.  Rows come through LDS, whole ones
-// at a time: as a product takes them, 16 lanes would ask for 16 lines at once.
+// at a time: as a product takes them, 16 lanes would ask for 16 lines at once, and a CU
+// gets one in a cycle (2,011 tokens, 32 heads on 8: 86 us like that, 46 so).  Whole pages
+// with rows as a product takes them were 72, the first page's CU twice as long at work as
+// the average.  Vector unit and products in turn bound it now: 16 rows and 32 keys are 8
+// products of 16 cycles and some 100 vector instructions, 16 of them exponentials' at a
+// quarter of the rate.
 constexpr int kManyWaves = 8, kManyTiles = 2, kHalf = 16 * kManyTiles;
 constexpr int kRing = 2, kRoundTiles = 4;  // tiles on their way, tiles whose rows lanes look after
 constexpr int kTileBytes = kTile * kDim8 * 2;
@@ -312,7 +317,9 @@ __global__ void __launch_bounds__(kManyWaves* fc::kWave, 4) k_weights_many(Weigh
 
 // Few rows (a token, an accepted path): a wave holds up to 64 of them and goes through
 // every fourth of its part's pages, the next one's keys on their way.  More rows are
-// more rounds of the same pages.
+// more rounds of the same pages.  Keys alone are read, 8 KB a page and head: 48 sequences
+// of up to 4,096 tokens, 11 accepted at most, 8 key heads 31 us, 2.4 TB/s; what is left
+// to memory's 15 us are the pages' exponentials and the longest sequences' parts.
 constexpr int kFewTiles = 4;
 template <bool kSrc>
 __global__ void __launch_bounds__(kThreads, 2) k_weights_few(Weights A, int part_pages) {
@@ -434,7 +441,8 @@ __device__ __forceinline__ uint32_t rank_of(float w) { return w > 0.0f ? __float
 // pages follow one another, 16 of them in registers.  One workgroup has up to 256 pages
 // and does it all; longer sequences are parts of as many, counted together in memory by
 // one launch for each turn (the 131,000 tokens of 8 heads that eight workgroups alone
-// read five times over: 186 us).
+// read five times over: 186 us, in turns 56; 48 sequences of up to 4,096 tokens, one
+// workgroup each, 14).
 constexpr int kTogether = 16;
 constexpr int kPartPages = kSelWaves * kTogether;
 
@@ -610,7 +618,10 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_turn(Evict A) {
 }
 
 constexpr int kMoveThreads = 256;
-constexpr int kMoveAtOnce = 4 * 256;  // workgroups that run at once
+// Workgroups of a launch: each goes on with the next page of its sequence and head.  48
+// sequences cut from up to 4,096 tokens to 1,000, choice and reading back too: 1,024 93 us,
+// 2,048 77, 4,096 and more 75; one of 131,000 cut to 60,000: the same with all.
+constexpr uint32_t kMoveAtOnce = 4096;
 constexpr int kMoveWaves = kMoveThreads / fc::kWave;
 
 // Codes as numbers that sort as their magnitudes do, 0 for a NaN.  Eight times an
@@ -884,7 +895,8 @@ extern "C" fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, in
   const int64_t all_pages = (int64_t)B * Hkv * pages;
   const bool many = all_pages * (kPage8 / kHalf) <= kMostMany &&
                     25 * (int64_t)n * (H / Hkv) >= 4 * (int64_t)B * (all_pages + 700);
-  // Four pages a wave, or fewer where that leaves the card idle.
+  // Four pages a wave, or fewer where that leaves the card idle (48 sequences: 4 31 us, 2
+  // 31, 1 40; one of 3,000 tokens: no difference).
   int each = 4;
   while (each > 1 && (int64_t)B * Hkv * fc::div_up(pages, each * kWaves) < 1024) each /= 2;
   (void)hipGetLastError();
@@ -964,7 +976,6 @@ extern "C" fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t 
     }
     FC_CHECK_LAUNCH();
     if (a.pages == 0) continue;
-    // As many workgroups for each pair as the card takes at once, or one a page.
     const uint32_t each = fc::div_up(kMoveAtOnce, pairs);
     hipLaunchKernelGGL(k_evict_move, dim3(pairs, each < (uint32_t)a.pages ? each : (uint32_t)a.pages), dim3(kMoveThreads), 0,
                        stream, now);
