@@ -709,15 +709,15 @@ size_t fc_paged_byte_pool_bytes(int32_t n_pages, int32_t Hkv);
  * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise); Hkv <= 1024.  The pool
  * shares no bytes with the other arguments (FC_ERR_INVALID).
  */
-fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k, int64_t k_stride,
-                          const uint16_t* v, int64_t v_stride, int32_t n_src, const int32_t* slot, const int32_t* src,
-                          int32_t n, hipStream_t stream);
+fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k,
+                              int64_t k_stride, const uint16_t* v, int64_t v_stride, int32_t n_src, const int32_t* slot,
+                              const int32_t* src, int32_t n, hipStream_t stream);
 
 /*
  * Rows of the pool as bf16 (exact: every held value is one): as fc_paged_read.
  */
-fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot, int32_t n,
-                         uint16_t* k, uint16_t* v, hipStream_t stream);
+fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot,
+                             int32_t n, uint16_t* k, uint16_t* v, hipStream_t stream);
 
 /*
  * fc_paged_attention over the 8-bit cache, with queries and keys that are rotated
@@ -741,11 +741,11 @@ fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, 
  */
 size_t fc_paged_byte_attention_workspace_bytes(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len);
 fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,
-                              const uint16_t* v_tree, int64_t v_stride, const uint8_t* pool, int32_t n_pages,
-                              const int32_t* table, int32_t max_pages, const int32_t* prefix_len,
-                              const int32_t* num_nodes, const int32_t* mask, int32_t B, int32_t R, int32_t H,
-                              int32_t Hkv, int32_t D, int32_t max_len, uint16_t* out, float* lse, void* ws,
-                              size_t ws_bytes, hipStream_t stream);
+                                  const uint16_t* v_tree, int64_t v_stride, const uint8_t* pool, int32_t n_pages,
+                                  const int32_t* table, int32_t max_pages, const int32_t* prefix_len,
+                                  const int32_t* num_nodes, const int32_t* mask, int32_t B, int32_t R, int32_t H,
+                                  int32_t Hkv, int32_t D, int32_t max_len, uint16_t* out, float* lse, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
 
 /*
  * The attention that a step's rows pay to the cached tokens, counted for each key
@@ -771,9 +771,10 @@ fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uin
  * 8192, H % Hkv == 0, D = FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).
  */
 fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, int64_t q_stride, const float* lse, int32_t n_rows,
-                            const uint8_t* pool, int32_t n_pages, const int32_t* table, int32_t max_pages,
-                            const int32_t* len, const int32_t* new_len, const int32_t* cu, const int32_t* src, int32_t n,
-                            int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_len, hipStream_t stream);
+                                const uint8_t* pool, int32_t n_pages, const int32_t* table, int32_t max_pages,
+                                const int32_t* len, const int32_t* new_len, const int32_t* cu, const int32_t* src,
+                                int32_t n, int32_t B, int32_t H, int32_t Hkv, int32_t D, int32_t max_len,
+                                hipStream_t stream);
 
 /*
  * Cuts sequences to budget[b] tokens: those that got least attention leave the cache,
@@ -801,9 +802,10 @@ fc_status fc_paged_byte_weights(float* weights, const uint16_t* q, int64_t q_str
  * (FC_ERR_UNSUPPORTED otherwise).
  */
 size_t fc_paged_byte_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_len);
-fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* table,
-                          int32_t max_pages, const int32_t* len, const int32_t* budget, int32_t B, int32_t max_len,
-                          int32_t first, int32_t recent, int32_t* add, void* ws, size_t ws_bytes, hipStream_t stream);
+fc_status fc_paged_byte_evict(uint8_t* pool, float* weights, int32_t n_pages, int32_t Hkv, int32_t D,
+                              const int32_t* table, int32_t max_pages, const int32_t* len, const int32_t* budget,
+                              int32_t B, int32_t max_len, int32_t first, int32_t recent, int32_t* add, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Decode-trace replay                                                       */

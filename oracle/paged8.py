@@ -219,8 +219,10 @@ def weights(w, q, lse, pool, table, length, new_length, cu, src=None, max_len=No
                     s = seen @ q[r, h] * c
                     p = 2.0 ** (s - lse[r, h] * LOG2E)
                     d = SUM * c * (np.abs(seen) @ np.abs(q[r, h])) + 2.0 ** -22 * (np.abs(s) + np.abs(lse[r, h]) * LOG2E + 1)
+                    e = p * (2.0 ** d - 1)
                 got[:P + t + 1, g] += p
-                off[:P + t + 1, g] += p * (2.0 ** d - 1)
+                # 2^(s - inf) is 0 whatever the rounding of a finite s: nothing is off
+                off[:P + t + 1, g] += 0.0 if lse[r, h] == np.inf else e
         sums = (E - P) * (H // Hkv) * 2.0 ** -23
         for j in np.flatnonzero(there):
             at = (table[b][j // PAGE], slice(None), j % PAGE)

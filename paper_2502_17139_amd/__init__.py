@@ -962,7 +962,7 @@ def fc_paged_byte_pool_bytes(n_pages: int, Hkv: int) -> int:
 
 
 def fc_paged_byte_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor,
-                    src: torch.Tensor | None = None, stream=None) -> None:
+                        src: torch.Tensor | None = None, stream=None) -> None:
     """Rounds rows of k (rotated already) and v (bf16 [rows][Hkv][D] or
     [B][R][Hkv][D], rows at any even distance) to 8 bits into the pool: row src[i]
     (or i) to slot[i].  Slots in one block of 32 tokens follow one another, as
@@ -1006,10 +1006,11 @@ def fc_paged_byte_attention_workspace_bytes(B: int, R: int, H: int, Hkv: int, ma
     return int(lib().fc_paged_byte_attention_workspace_bytes(B, R, H, Hkv, max_len))
 
 
-def fc_paged_byte_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pool: torch.Tensor,
-                        table: torch.Tensor, prefix_len: torch.Tensor, tree: dict | None = None,
-                        max_len: int | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                        stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+def fc_paged_byte_attention(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
+                            pool: torch.Tensor, table: torch.Tensor, prefix_len: torch.Tensor,
+                            tree: dict | None = None, max_len: int | None = None,
+                            out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                            stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """fc_paged_attention over the 8-bit cache, with queries and keys that are
     rotated already (fc_norm_rotate): bf16 q [B][R][H][D], k/v_tree [B][R][Hkv][D]
     (rows at any even distance); of a tree num_nodes and mask are read.  Returns
@@ -1054,9 +1055,11 @@ def _token_weights(weights: torch.Tensor, n_pages: int, Hkv: int) -> None:
     _expect("weights", weights, torch.float32, (n_pages, Hkv, FC_PAGE_TOKENS))
 
 
-def fc_paged_byte_weights(weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, pool: torch.Tensor,
-                      table: torch.Tensor, length: torch.Tensor, new_length: torch.Tensor, cu: torch.Tensor,
-                      src: torch.Tensor | None = None, max_len: int | None = None, stream=None) -> None:
+def fc_paged_byte_weights(weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor,
+                          pool: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                          new_length: torch.Tensor, cu: torch.Tensor,
+                          src: torch.Tensor | None = None, max_len: int | None = None,
+                          stream=None) -> None:
     """The attention that the rows of a step's new tokens pay to every cached
     token, added to weights (fp32 [n_pages][Hkv][64]; new tokens': set): q (bf16
     [rows][H][D] or [B][R][H][D]) and lse (fp32, the same but for D) as
@@ -1092,9 +1095,10 @@ def fc_paged_byte_evict_workspace_bytes(B: int, Hkv: int, max_len: int) -> int:
     return int(lib().fc_paged_byte_evict_workspace_bytes(B, Hkv, max_len))
 
 
-def fc_paged_byte_evict(pool: torch.Tensor, weights: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
-                    budget: torch.Tensor, first: int = 0, recent: int = 0, max_len: int | None = None,
-                    add: torch.Tensor | None = None, stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+def fc_paged_byte_evict(pool: torch.Tensor, weights: torch.Tensor, table: torch.Tensor,
+                        length: torch.Tensor, budget: torch.Tensor, first: int = 0, recent: int = 0,
+                        max_len: int | None = None, add: torch.Tensor | None = None, stream=None,
+                        workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Cuts sequences to budget[b] tokens: each key head keeps the last `recent`,
     the first `first`, and of the others those of most weight, in their order.
     Returns add [B], what each sequence loses: with the same length fc_paged_plan

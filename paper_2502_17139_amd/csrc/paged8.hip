@@ -20,7 +20,10 @@ using fc::kQuarter8;
 
 constexpr int kWriteThreads = 256;
 constexpr int kWriteWaves = kWriteThreads / fc::kWave;
-constexpr int kMostWindow = 32;  // entries whose runs a workgroup looks after
+// Entries whose runs a workgroup looks after: those of one block, or as many single ones.
+// (Smaller windows of a prompt hold no run's start but every fourth or 32nd, which lie on
+// one XCD then: 512 entries, 32 key heads, 70 us in windows of one, 9 so.)
+constexpr int kWindow = 32;
 
 struct Write {
   uint8_t* pool;
@@ -29,7 +32,7 @@ struct Write {
   const int32_t *slot, *src;
   int64_t first, n;      // entries [0, n) exist; this launch's begin at `first`
   int64_t n_src;
-  int n_pages, Hkv, window;
+  int n_pages, Hkv;
 };
 
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -67,20 +70,20 @@ __device__ __forceinline__ Scaled rescale(uint32_t top, uint32_t byte, bool fres
 // the run's) is written whole, with zeros in the rows that are not there yet; in
 // others the key rows alone and all of the values, whose 16-byte pieces hold other
 // tokens too, unless the scale rises and all codes are rounded anew.  Read are 512 bytes a
-// token and key head, written 258: prompts of 22,700 tokens, 32 key heads, 190 us where a
+// token and key head, written 258: prompts of 22,790 tokens, 32 key heads, 171 us where a
 // copy of as many bytes takes 113.  140 registers leave three waves a SIMD; held to 128
-// or 96 they spill (227 and 302 us).
+// or 96 they spill (227 and 302 us against 190 in a state before this).
 __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
   const int lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
-  const int64_t i0 = A.first + (int64_t)blockIdx.x * A.window;
+  const int64_t i0 = A.first + (int64_t)blockIdx.x * kWindow;
   const int blocks = A.n_pages * (kPage8 / kBlock8);
   const auto block_at = [&](int64_t i) {  // of entry i; -1: none
     const int b = A.slot[i] >> 5;
     return b >= 0 && b < blocks ? b : -1;
   };
   const int64_t mine = i0 + lane;
-  const bool in = lane < A.window && mine < A.n;
+  const bool in = lane < kWindow && mine < A.n;
   const int b_mine = in ? block_at(mine) : -1;
   const int b_before = in && mine > 0 ? block_at(mine - 1) : -1;
   const uint64_t leads = fc::ballot(b_mine >= 0 && b_mine != b_before);
@@ -263,9 +266,10 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w, float s, bool high) {
 // A wave takes 16 entries through every fourth head.  Keys: 16 lanes a row, eight dims
 // each.  Values: two dims a lane, 16 tokens of them in two loads; entries of one such
 // quarter that follow one another, as the tokens of a sequence do, share the loads.  Bound
-// by what is written, 512 bytes a token and key head: 22,700 tokens of 32 key heads 137 us,
-// 4.1 TB/s of a copy's 4.95.  All loads are asked for before the first result is written
-// (159 us one after another); four dims a lane, half as many tokens each, was 232.
+// by what is written, 512 bytes a token and key head: 22,790 tokens of 32 key heads 117 us,
+// 4.8 TB/s of a copy's 4.95.  All loads are asked for before the first result is written
+// (137 us in a state before this, one after another 159; four dims a lane, half as many
+// tokens each, 232).
 __global__ void __launch_bounds__(kReadThreads) k_paged8_read(const uint8_t* __restrict__ pool, int n_pages, int Hkv,
                                                               const int32_t* __restrict__ slot, int64_t first, int64_t n,
                                                               uint16_t* __restrict__ k, uint16_t* __restrict__ v) {
@@ -325,9 +329,12 @@ bool pool_ok(const void* pool, int32_t n_pages, int32_t Hkv) {
   return pool && !((uintptr_t)pool & 15) && fc_paged_byte_pool_bytes(n_pages, Hkv) > 0;
 }
 
-// Workgroups over a call's heads: enough that a short call fills the card.
+// Workgroups over a group's tasks: 16 a CU in all, several times what runs at once, so that
+// heavy ones are not waited for.  4, 8, 16 and 32 a CU: 22,790 tokens of ragged prompts, 32
+// key heads, written and read 329, 305, 286 and 283 us; 65,536 of one prompt, 8 key heads,
+// written 89, 89, 93 and 93; 1,024 single tokens 32, 29, 29 and 29.
 uint32_t over_heads(int64_t groups, int64_t tasks) {
-  const int64_t want = (4 * 256 + groups - 1) / groups;
+  const int64_t want = (16 * 256 + groups - 1) / groups;
   return (uint32_t)(want < 1 ? 1 : want > tasks ? tasks : want);
 }
 
@@ -342,8 +349,8 @@ extern "C" size_t fc_paged_byte_pool_bytes(int32_t n_pages, int32_t Hkv) {
 }
 
 extern "C" fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const uint16_t* k,
-                                     int64_t k_stride, const uint16_t* v, int64_t v_stride, int32_t n_src,
-                                     const int32_t* slot, const int32_t* src, int32_t n, hipStream_t stream) {
+                                         int64_t k_stride, const uint16_t* v, int64_t v_stride, int32_t n_src,
+                                         const int32_t* slot, const int32_t* src, int32_t n, hipStream_t stream) {
   if (!pool_ok(pool, n_pages, Hkv) || n < 0 || n_src < 0) return FC_ERR_INVALID;
   if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
   if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D || ((k_stride | v_stride) & 7)) return FC_ERR_INVALID;
@@ -355,18 +362,12 @@ extern "C" fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t
                  {fc::rows_span(k, n_src, k_stride, Hkv * D), fc::rows_span(v, n_src, v_stride, Hkv * D),
                   {slot, numbers}, {src, numbers}}))
     return FC_ERR_INVALID;
-  // A window of 32 entries begins one run or two of a prompt's; single tokens, each a run
-  // of its own, are spread further.  Windows of 1, 8 and 32, 8 key heads: 320 single
-  // tokens 11, 30 and 113 us, 320 of a prompt 12.5, 9 and 9; 1,024: 27, 33 and 114, and
-  // 37, 9 and 9; 4,096: 95, 115 and 138, and 114, 24 and 9; 65,536 of a prompt 1,867, 261
-  // and 90.  So many single tokens at once are rarer than prompts.
-  const int window = n >= 2048 ? kMostWindow : n >= 1024 ? 8 : 1;
-  Write a = {pool, {k, v}, {k_stride, v_stride}, slot, src, 0, n, n_src, n_pages, Hkv, window};
-  const int64_t groups = fc::div_up((uint64_t)n, (uint64_t)window);
-  const uint32_t y = over_heads(groups, (2 * (int64_t)Hkv + kWriteWaves - 1) / kWriteWaves);
+  Write a = {pool, {k, v}, {k_stride, v_stride}, slot, src, 0, n, n_src, n_pages, Hkv};
+  const int64_t groups = fc::div_up((uint64_t)n, kWindow);
+  const uint32_t y = over_heads(groups, ((int64_t)kWindow * 2 * Hkv + kWriteWaves - 1) / kWriteWaves);
   (void)hipGetLastError();
   for (int64_t g = 0; g < groups; g += kMostGroups) {
-    a.first = g * window;
+    a.first = g * kWindow;
     const uint32_t now = (uint32_t)(groups - g < kMostGroups ? groups - g : kMostGroups);
     hipLaunchKernelGGL(k_paged8_write, dim3(now, y), dim3(kWriteThreads), 0, stream, a);
     FC_CHECK_LAUNCH();
@@ -374,8 +375,8 @@ extern "C" fc_status fc_paged_byte_write(uint8_t* pool, int32_t n_pages, int32_t
   return FC_OK;
 }
 
-extern "C" fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D, const int32_t* slot,
-                                    int32_t n, uint16_t* k, uint16_t* v, hipStream_t stream) {
+extern "C" fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, int32_t D,
+                                        const int32_t* slot, int32_t n, uint16_t* k, uint16_t* v, hipStream_t stream) {
   if (!pool_ok(pool, n_pages, Hkv) || n < 0) return FC_ERR_INVALID;
   if (D != FC_TREE_ATTN_HEAD_DIM) return FC_ERR_UNSUPPORTED;
   if (n == 0) return FC_OK;

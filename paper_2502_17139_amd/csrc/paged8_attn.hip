@@ -1040,12 +1040,13 @@ extern "C" size_t fc_paged_byte_attention_workspace_bytes(int32_t B, int32_t R, 
   return s.parts > 1 ? carve(nullptr, (int64_t)trees_at_once(B, R, H, Hkv, s) * H * R * s.parts, &ml, &o) : 0;
 }
 
-extern "C" fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree, int64_t k_stride,
-                                         const uint16_t* v_tree, int64_t v_stride, const uint8_t* pool, int32_t n_pages,
-                                         const int32_t* table, int32_t max_pages, const int32_t* prefix_len,
-                                         const int32_t* num_nodes, const int32_t* mask, int32_t B, int32_t R, int32_t H,
-                                         int32_t Hkv, int32_t D, int32_t max_len, uint16_t* out, float* lse, void* ws,
-                                         size_t ws_bytes, hipStream_t stream) {
+extern "C" fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uint16_t* k_tree,
+                                             int64_t k_stride, const uint16_t* v_tree, int64_t v_stride,
+                                             const uint8_t* pool, int32_t n_pages, const int32_t* table,
+                                             int32_t max_pages, const int32_t* prefix_len, const int32_t* num_nodes,
+                                             const int32_t* mask, int32_t B, int32_t R, int32_t H, int32_t Hkv,
+                                             int32_t D, int32_t max_len, uint16_t* out, float* lse, void* ws,
+                                             size_t ws_bytes, hipStream_t stream) {
   if (!sizes_ok(B, R, H, Hkv, max_len) || n_pages < 1 || n_pages > (1 << 25) - 1 || max_pages < 1 ||
       (int64_t)max_len > (int64_t)max_pages * kPage8)
     return FC_ERR_INVALID;

@@ -1122,3 +1122,27 @@ def test_weights_of_long_prompts_and_odd_heads(H, Hkv, lens, adds):
     say(f"weights of prompts H={H} Hkv={Hkv} lens={lens} adds={adds}")
     weigh(rng, H, Hkv, lens, adds)
     weigh(rng, H, Hkv, lens, adds, n_src=sum(adds) + 5)
+
+
+def test_weights_of_prompts_with_rows_and_pages_missing():
+    """Enough rows that half pages are held: rows outside of what there is, rows that
+    attended to nothing, logarithms that are none, absent pages, a longest length,
+    blocks nobody began, a key that is a NaN."""
+    rng = np.random.default_rng(12)
+    say("weights of prompts, parts missing")
+    for shift in (-3, 40):
+        weigh(rng, 4, 2, [70, 5], [190, 260], shift=shift)
+    for value in (-np.inf, np.inf, np.nan):
+        odd = lambda n: np.where(rng.random((n, 4)) < 0.2, value, rng.uniform(0, 8, (n, 4))).astype(np.float32)  # noqa: E731,B023
+        weigh(rng, 4, 2, [70, 5], [190, 260], lse=odd)
+    weigh(rng, 4, 2, [70, 200], [190, 100], max_len=160)
+    table = np.array([[0, -1, 2, 7, 6], [3, 99, 4, 5, -1]], np.int32)
+    weigh(rng, 4, 2, [30, 70], [280, 200], table=table, pool=make_pool(rng, 8, 2))
+    weigh(rng, 4, 2, [70, 5, 300, 0], [400, 0, -20, 300])
+    pool = make_pool(rng, 6, 1)
+    table = np.array([[1, 2, 4, 3, 5]], np.int32)
+    pool[5, 0, 10 * 128:64 * 128] = 127
+    pool[5, 0, o8.SCALES + 1] = 255
+    pool[1, 0, 7 * 128 + 5] = 127
+    got = weigh(rng, 3, 1, [6], [260], table=table, pool=pool)
+    assert np.isnan(got[1, 0, 7]) and np.isnan(got).sum() == 1
