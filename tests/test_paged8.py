@@ -1146,3 +1146,23 @@ def test_weights_of_prompts_with_rows_and_pages_missing():
     pool[1, 0, 7 * 128 + 5] = 127
     got = weigh(rng, 3, 1, [6], [260], table=table, pool=pool)
     assert np.isnan(got[1, 0, 7]) and np.isnan(got).sum() == 1
+
+
+def test_tables_of_millions_of_pages():
+    """More parts of a sequence's place than one launch takes in a dimension: the same
+    weights and cuts as by a narrow table."""
+    rng = np.random.default_rng(31)
+    say("weights of wide tables")
+    weigh(rng, 3, 1, [290], [10], width=2 ** 19 + 100)
+    pool, w = make_pool(rng, 700, 1), torch.rand((700, 1, 64), device="cuda")
+    n = torch.tensor([700 * 64 - 5], dtype=torch.int32, device="cuda")
+    wide = torch.full((1, 2 ** 23 + 300), -1, dtype=torch.int32, device="cuda")
+    wide[0, :700] = torch.randperm(700, device="cuda")
+    got = []
+    say("an eviction by a wide table")
+    for t in (wide, wide[:, :700].contiguous()):
+        p, x = pool.clone(), w.clone()
+        got.append((p, x, fc.fc_paged_byte_evict(p, x, t, n, n // 2, first=4, recent=9)))
+        torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
