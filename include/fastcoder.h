@@ -764,8 +764,10 @@ fc_status fc_paged_byte_attention(const uint16_t* q, int64_t q_stride, const uin
  *
  * q [n_rows][H][D] bf16, rows q_stride elements apart (a multiple of 8), 16-byte
  * aligned.  len and new_len are clamped to [0, max_len]; rows whose number lies
- * outside [0, n_rows), or whose place outside [0, n), pay nothing.  Table entries
- * outside the pool count as absent keys.  The pages of a call's sequences have to
+ * outside [0, n_rows), or whose place outside [0, n), pay nothing.  With n_rows or n
+ * 0 nothing is launched, and new tokens' weights, too, are left as they were (a call
+ * with one row that no entry of src names makes them 0).  Table entries outside the
+ * pool count as absent keys.  The pages of a call's sequences have to
  * differ.  Sums are fp32, in an order that depends on the sizes alone.  weights shares
  * no bytes with the other arguments (FC_ERR_INVALID).  B <= 65536, Hkv <= 1024, H <=
  * 8192, H % Hkv == 0, D = FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise).

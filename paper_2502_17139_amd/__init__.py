@@ -305,10 +305,14 @@ def _scratch(size: int, device, stream) -> torch.Tensor:
     they run."""
     if stream is None:
         return _empty(size, torch.uint8, device)
-    if not isinstance(stream, torch.cuda.Stream):  # anything with a raw stream
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         return _empty(size, torch.uint8, device)
+
+
+def _torch_stream(stream, device) -> torch.cuda.Stream:
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(stream.cuda_stream, device=device)  # anything with a raw stream
 
 
 # ---------------------------------------------------------------- index ----
@@ -708,6 +712,13 @@ class _Launch:
         size = math.prod(shape) * dtype.itemsize
         return _scratch(size, self.device, self.stream).view(dtype).view(shape)
 
+    def full(self, shape, value, dtype) -> torch.Tensor:
+        t = self.empty(shape, dtype)
+        if self.stream is None:
+            return t.fill_(value)
+        with torch.cuda.stream(_torch_stream(self.stream, self.device)):
+            return t.fill_(value)
+
 
 def _rows(name: str, t: torch.Tensor, heads: int | None = None) -> int:
     """Elements between the rows of [rows][heads][D] or [B][R][heads][D]: whole
@@ -1064,8 +1075,8 @@ def fc_paged_byte_weights(weights: torch.Tensor, q: torch.Tensor, lse: torch.Ten
     token, added to weights (fp32 [n_pages][Hkv][64]; new tokens': set): q (bf16
     [rows][H][D] or [B][R][H][D]) and lse (fp32, the same but for D) as
     fc_paged_byte_attention took and gave them, length before the step, new_length, cu
-    and src from its plan (src None: rows follow one another).  After
-    fc_paged_byte_write."""
+    and src from its plan (src None: rows follow one another; new tokens of calls
+    without rows weigh 0).  After fc_paged_byte_write."""
     if table.dim() != 2:
         raise ValueError("table [B][max_pages] expected")
     n_pages, Hkv = _pool8(pool)
@@ -1084,6 +1095,13 @@ def fc_paged_byte_weights(weights: torch.Tensor, q: torch.Tensor, lse: torch.Ten
         max_len = max_pages * FC_PAGE_TOKENS
     _in_32_bits(max_len=max_len, B=B, max_pages=max_pages, rows=n_rows, src=n)
     with _Launch(stream, (weights, q, lse, pool, table, length, new_length, cu, src)) as on:
+        if n == 0 or n_rows == 0:
+            # The library leaves everything as it is when there are no rows.  One that no
+            # token has makes the new tokens' weights what nobody pays, 0.
+            if n_rows == 0:
+                n_rows, qs = 1, H * FC_TREE_ATTN_HEAD_DIM
+                q, lse = on.empty((1, qs), torch.bfloat16), on.empty((1, H), torch.float32)
+            n, src = 1, on.full((1,), -1, i32)
         w, lse_at, pool_at, table_at, len_at, new_at, cu_at = _ptrs((weights, lse, pool, table, length, new_length, cu))
         _check("fc_paged_byte_weights", lib().fc_paged_byte_weights(
             w, q.data_ptr(), qs, lse_at, n_rows, pool_at, n_pages, table_at, max_pages, len_at, new_at, cu_at, _ptr(src),
