@@ -730,8 +730,9 @@ fc_status fc_paged_byte_read(const uint8_t* pool, int32_t n_pages, int32_t Hkv, 
  *
  * Queries, keys and values enter their products exactly; softmax weights are rounded
  * to bf16, sums are fp32.  What is not finite among the keys and values that a row
- * attends to, or in its query, shows in its result; absent, masked and later tokens do
- * not count, whatever they hold.  Values of a magnitude of 2^78 or more may overflow
+ * attends to, or in its query, shows in its result (a key of score -infinity has weight
+ * 0; a row with no others is NaN, and so is its logarithm); absent, masked and later
+ * tokens do not count, whatever they hold.  Values of a magnitude of 2^78 or more may overflow
  * the sums.
  *
  * ws holds fc_paged_byte_attention_workspace_bytes(...) bytes, 16-byte aligned (may be NULL

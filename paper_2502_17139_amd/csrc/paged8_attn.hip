@@ -186,6 +186,17 @@ struct Work {
     for (int u = 0; u < 4 * T; ++u) bits |= (uint32_t)(m[u] == 1 && j0 + 16 * (u / 4) + 4 * lg + u % 4 < n) << u;
     return bits;
   }
+  // Whether any page of this part is there.
+  __device__ __forceinline__ bool any_page(const Args& A) const {
+    const int lane = fc::lane_id();
+    const int32_t* of = A.table + (int64_t)b * A.max_pages;
+    bool any = false;
+    for (int pg = pg0; pg < pg1 && !any; pg += fc::kWave) {
+      const int id = pg + lane < pg1 ? of[pg + lane] : -1;
+      any = fc::ballot(id >= 0 && id < A.n_pages) != 0;
+    }
+    return any;
+  }
 };
 
 // A query row's outputs (lane (lg, lc): dims 16 t + 4 lg + e of row lc), its running
@@ -489,8 +500,28 @@ __device__ __forceinline__ void take(Row& r, float& m, const float* rec) {
 #pragma unroll
   for (int t = 0; t < kDTiles; ++t) r.o[t] = r.o[t] * a1 + *(const floatx4*)(rec + (t * 64 + lane) * 4) * a2;
 }
+// A row whose weights add up to nothing saw no key, or none but of scores of -infinity
+// (an infinity in its query, a product past fp32).  Those are no keys beside others, but
+// alone their softmax is a NaN: such a row's maximum is the lowest number, which any
+// other key's weights leave without effect when rows are put together.  Whether it saw
+// one is looked for here, where it is rare; of the tree's rows `saw` has the lane's.
+constexpr float kLowest = -3.402823466e38f;
+template <typename Saw>
+__device__ __forceinline__ float maximum_of(const Args& A, const Work& W, const Row& r, float m, int row, Saw saw) {
+  const bool nothing = row < W.M && r.l == 0.0f;
+  if (!__any(nothing)) return m;
+  int sees = saw();
+  sees |= __shfl_xor(sees, 16);
+  sees |= __shfl_xor(sees, 32);
+  sees |= W.any_page(A);
+  return nothing && sees ? kLowest : m;
+}
+// 1 over a row's sum: 0 for a row without a key; infinite, so that its outputs of 0
+// become NaN, for one of scores of -infinity alone.
+__device__ __forceinline__ float inverse(float m, float l) { return l == 0.0f && m == -INFINITY ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float log_sum(float m, float x) {
-  return x == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(x)) * kLn2;  // base 2; a row of NaN alone has no m
+  if (x == 0.0f) return m == -INFINITY ? m : __builtin_nanf("");
+  return (m + __builtin_amdgcn_logf(x)) * kLn2;  // base 2; a row of NaN alone has no m
 }
 __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& r, float m, int row) {
   const int lg = fc::lane_id() >> 4;
@@ -503,7 +534,7 @@ __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& 
   }
   // a row without a key has weight 0; a NaN stays one
   const int tr = row / W.G;
-  const float inv = tr < W.n && r.l != 0.0f ? 1.0f / r.l : 0.0f;
+  const float inv = tr < W.n ? inverse(m, r.l) : 0.0f;
   const int64_t at = ((int64_t)W.b * A.R + tr) * A.H + W.kv * W.G + (row - tr * W.G);
 #pragma unroll
   for (int t = 0; t < kDTiles; ++t) {
@@ -649,8 +680,11 @@ __global__ void __launch_bounds__(kAloneWaves* fc::kWave, 2) k_paged8_attn_alone
   }
   if (w > 0) return;
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
-    if (kTile * i + lc < W.M) finish(A, W, tile[i].row, m[i], kTile * i + lc);
+  for (int i = 0; i < NT; ++i) {
+    const int row = kTile * i + lc;
+    m[i] = maximum_of(A, W, tile[i].row, m[i], row, [&] { return W.tree && W.allowed<T>(A, row, 0, lg) != 0; });
+    if (row < W.M) finish(A, W, tile[i].row, m[i], row);
+  }
 }
 
 // More tiles: a workgroup's four waves take up to eight of them through the same pages,
@@ -845,6 +879,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
   else if (mine == 1) group_pages<1, kLse>(pages, s_x, here0, here1, word0, word1, tile);
   else group_pages<0, kLse>(pages, s_x, here0, here1, word0, word1, tile);
 
+  bool saw[kWaveTiles] = {false, false};  // whether the lane's rows saw any of the tree's
   if (W.tree) {
     // 64 of its rows at a time: what is read of them, and which of them each query row
     // may see, is asked for together, the next ones' before these are used
@@ -855,7 +890,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
     __syncthreads();  // the last page is used
     for (int j0 = 0; j0 < W.n; j0 += kPage8) {
 #pragma unroll
-      for (int i = 0; i < kWaveTiles; ++i) see[i] = W.allowed<kKTiles>(A, row[i], j0, lg);
+      for (int i = 0; i < kWaveTiles; ++i) {
+        see[i] = W.allowed<kKTiles>(A, row[i], j0, lg);
+        saw[i] |= see[i] != 0;
+      }
       if (tid < 2) s_bad[tid] = 0;
       __syncthreads();
       rows.store(keys, values, s_bad);
@@ -874,7 +912,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
     whole(tile[i].row);
-    if (row[i] < W.M) finish(A, W, tile[i].row, tile[i].row.m(), row[i]);
+    const float m = maximum_of(A, W, tile[i].row, tile[i].row.m(), row[i], [&] { return saw[i]; });
+    if (row[i] < W.M) finish(A, W, tile[i].row, m, row[i]);
   }
 }
 
@@ -949,7 +988,7 @@ __global__ void __launch_bounds__(kMergeWaves* fc::kWave) k_paged8_merge(Args A)
   if (lane >= 16) return;
   const int i = r / G;
   const int64_t to = ((int64_t)b * A.R + i) * A.H + kv * G + (r - i * G);
-  const float inv = i < n && l != 0.0f ? 1.0f / l : 0.0f;
+  const float inv = i < n ? inverse(m, l) : 0.0f;
   bf16x8 res;
 #pragma unroll
   for (int e = 0; e < 8; ++e) res[e] = inv == 0.0f ? (__bf16)0.0f : (__bf16)(acc[e] * inv);

@@ -18,6 +18,90 @@ from test_paged import bf16, f64, on_gpu, trees  # noqa: E402
 from test_paged8 import BF, D, INF, _norm, attend, make_pool, same_pool  # noqa: E402
 
 
+# ------------------------------------------------------------- attention --
+
+def _one_sided(rng, n_pages, Hkv, dim, sign):
+    """Pages of random rows whose `dim` has one sign everywhere, and is not 0."""
+    k, v = (bf16(rng, 64 * n_pages, Hkv, D) for _ in "kv")
+    k[..., dim] = sign * (k[..., dim].abs() + 1)
+    pool = torch.zeros((n_pages, Hkv, fc.FC_PAGE8_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(np.arange(64 * n_pages, dtype=np.int32)))
+    return pool
+
+
+@pytest.mark.parametrize("R,H,Hkv,lens", [
+    (1, 1, 1, [1]), (1, 8, 2, [130, 0]), (4, 8, 2, [70, 200]), (9, 4, 1, [64, 33]), (30, 1, 1, [100]),   # pages a wave
+    (1, 4, 1, [3001]), (7, 4, 1, [1300, 5]), (20, 2, 1, [2500]),                                        # in parts
+    (65, 4, 2, [100, 0]), (70, 2, 1, [64]), (130, 1, 1, [200]), (65, 2, 1, [2049]),                     # through LDS
+], ids=lambda x: str(x).replace(" ", ""))
+@pytest.mark.parametrize("value", [INF, -INF])
+def test_rows_whose_scores_are_all_minus_infinity(R, H, Hkv, lens, value):
+    """An infinity in a query whose scores all become -infinity shows in its row, and in
+    no other; a row that may see nothing is 0 whatever its query holds."""
+    rng = np.random.default_rng(R + H + sum(lens))
+    B, dim, sign = len(lens), 3, -np.sign(value)
+    pool = _one_sided(rng, 5, Hkv, dim, sign)
+    q, kt = bf16(rng, B, R, H, D), bf16(rng, B, R, Hkv, D)
+    kt[..., dim] = sign * (kt[..., dim].abs() + 1)
+    q[:, 0, 0, dim] = value
+    q[:, R - 1, H - 1, dim] = value
+    q[:, R // 2, H // 2, dim] = value
+    table = rng.integers(0, 5, (B, -(-max(lens) // 64))).astype(np.int32)
+    say(f"scores of -infinity R={R} H={H} lens={lens} {value}")
+    got = attend(rng, B, R, H, Hkv, lens, pool=pool, table=table, q=q, kt=kt, max_len=max(lens))
+    assert np.isnan(got[:, 0, 0]).all() and np.isnan(got[:, R - 1, H - 1]).all()
+    assert np.isnan(got).any(-1).sum() <= 3 * B
+    t = trees(rng, B, R)
+    t["mask"][:, R // 2] = 0
+    attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=table, q=q, kt=kt, max_len=max(lens))
+    # nothing but absent pages, and masks that leave a row nothing
+    got = attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=np.full_like(table, -1), q=q, kt=kt, max_len=max(lens))
+    assert (got[:, R // 2] == 0).all()
+    t["num_nodes"][:] = R // 2
+    attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=table, q=q, kt=kt, max_len=max(lens))
+
+
+@pytest.mark.parametrize("R,H,n", [(1, 2, 300), (1, 2, 3001), (20, 1, 3001), (20, 2, 3001), (65, 2, 300), (65, 1, 2500)])
+def test_keys_of_score_minus_infinity_beside_others(R, H, n):
+    """Pages, tree rows, or both whose scores are -infinity count for nothing beside keys
+    of finite scores, wherever they lie: as if they were absent or masked."""
+    rng = np.random.default_rng(R + n)
+    width = -(-n // 64)
+    k, v = bf16(rng, 64 * 6, 1, D), bf16(rng, 64 * 6, 1, D)
+    k[..., 3] = 0
+    k[:192, :, 3] = -2.0 ** 70          # pages 0 to 2; times 2^70 less than fp32 holds
+    pool = torch.zeros((6, 1, fc.FC_PAGE8_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(np.arange(384, dtype=np.int32)))
+    q, kt, vt = bf16(rng, 1, R, H, D), bf16(rng, 1, R, 1, D), bf16(rng, 1, R, 1, D)
+    q[..., 3] = 2.0 ** 70
+    kt[..., 3] = 0
+    low = kt.clone()
+    low[..., 3] = -INF
+    t = dict(trees(rng, 1, R))
+    alone = {**t, "mask": np.zeros_like(t["mask"])}
+    plen, page = np.array([n], np.int32), rng.integers(3, 6, width)
+    for name, finite in (("all but one", np.arange(width) == width // 2), ("the first", np.arange(width) == 0),
+                         ("the last", np.arange(width) == width - 1), ("every other", np.arange(width) % 2 == 0),
+                         ("the second half", np.arange(width) >= width // 2)):
+        say(f"-infinity beside others R={R} n={n}: finite pages are {name}")
+        table = np.where(finite, page, page - 3).astype(np.int32)[None]
+        there = np.where(finite, page, -1).astype(np.int32)[None]
+        for keys, tree in ((low, t), (kt, t), (kt, alone)):
+            got, want = [], []
+            for tab, tr, to in ((table, tree, got), (there, alone if keys is low else tree, want)):
+                lse = torch.empty((1, R, H), device="cuda")
+                to += [fc.fc_paged_byte_attention(q.cuda(), keys.cuda(), vt.cuda(), pool, dev(tab), dev(plen), tree=on_gpu(tr),
+                                                  lse=lse), lse]
+            assert not torch.isnan(want[0]).any() and want[0].any()
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # the tree's rows alone are finite
+    say(f"-infinity beside others R={R} n={n}: finite are the tree's rows")
+    table = (page - 3).astype(np.int32)[None]
+    got, want = (fc.fc_paged_byte_attention(q.cuda(), kt.cuda(), vt.cuda(), pool, dev(x.astype(np.int32)), dev(plen), tree=on_gpu(t))
+                 for x in (table, np.full_like(table, -1)))
+    assert torch.equal(got, want) and got.any() and not torch.isnan(got).any()
+
+
 # ---------------------------------------------------------------- weights --
 
 @pytest.mark.parametrize("H,Hkv,lens,adds", [(4, 2, [70, 5, 90, 0], [9, 0, -20, 1]), (1, 1, [0], [1]), (8, 2, [30], [300])])
