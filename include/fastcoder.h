@@ -702,10 +702,11 @@ size_t fc_paged_byte_pool_bytes(int32_t n_pages, int32_t Hkv);
 
 /*
  * Rounds rows of keys and values to 8 bits and places them: row src[i] of k and v
- * (row i without src) goes to slot[i].  k, v: as for fc_paged_write.  Entries whose
- * slots lie in one block have to follow one another (as fc_paged_plan gives them),
- * and slots have to differ: what the blocks hold is left open otherwise.  An entry
- * with a slot outside the pool or a row outside [0, n_src) is skipped.  D must be
+ * (row i without src) goes to slot[i].  k, v: as for fc_paged_write.  An entry with a
+ * slot outside the pool or a row outside [0, n_src) is skipped.  Of the others, those
+ * whose slots lie in one block have to follow one another (as fc_paged_plan gives
+ * them; skipped ones may lie between), and slots have to differ: what the blocks hold
+ * is left open otherwise.  D must be
  * FC_TREE_ATTN_HEAD_DIM (FC_ERR_UNSUPPORTED otherwise); Hkv <= 1024.  The pool
  * shares no bytes with the other arguments (FC_ERR_INVALID).
  */

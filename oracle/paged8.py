@@ -80,20 +80,21 @@ def _put(page, part, rows, x, e) -> None:
 
 
 def write(pool: np.ndarray, k, v, slot, src=None) -> np.ndarray:
-    """The pool after rows of k and v [n_src][Hkv][128] are placed, a run of entries of one block at a time."""
+    """The pool after rows of k and v [n_src][Hkv][128] are placed, a run of entries of one block at a
+    time; entries that are skipped end none."""
     pool = pool.copy()
     n_pages, Hkv = pool.shape[:2]
     slot = np.asarray(slot).astype(np.int64)
+    src = np.arange(len(slot)) if src is None else np.asarray(src).astype(np.int64)
+    placed = (slot >= 0) & (slot < PAGE * n_pages) & (src >= 0) & (src < len(k))
+    slot, src = slot[placed], src[placed]
     i = 0
     while i < len(slot):
         block, j = slot[i] // BLOCK, i
         while j < len(slot) and slot[j] // BLOCK == block:
             j += 1
-        rows = [(int(slot[x]) % BLOCK, x if src is None else int(src[x])) for x in range(i, j)]
+        rows = [(int(slot[x]) % BLOCK, int(src[x])) for x in range(i, j)]
         i = j
-        rows = [(t, r) for t, r in rows if 0 <= r < len(k)]
-        if not rows or not 0 <= block < 2 * n_pages:
-            continue
         at, half = np.array([t for t, _ in rows]), int(block % 2)
         from_ = [r for _, r in rows]
         for h in range(Hkv):

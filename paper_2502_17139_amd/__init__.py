@@ -977,7 +977,8 @@ def fc_paged_byte_write(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sl
     """Rounds rows of k (rotated already) and v (bf16 [rows][Hkv][D] or
     [B][R][Hkv][D], rows at any even distance) to 8 bits into the pool: row src[i]
     (or i) to slot[i].  Slots in one block of 32 tokens follow one another, as
-    fc_paged_plan gives them."""
+    fc_paged_plan gives them, but for entries that are skipped: slots outside the
+    pool, rows that are not there."""
     n_pages, Hkv = _pool8(pool)
     ks, vs = _rows("k", k, Hkv), _rows("v", v, Hkv)
     if k.shape != v.shape:

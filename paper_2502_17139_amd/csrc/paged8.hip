@@ -63,60 +63,123 @@ __device__ __forceinline__ Scaled rescale(uint32_t top, uint32_t byte, bool fres
   return s;
 }
 
-// The entries of one block, which follow one another, are a run; a wave takes a run's
-// keys or values of one head, so that a block has one writer.  It reads the rows, has
-// their largest magnitude by exchange within the wave, and writes codes: key rows as
-// they are, values dim by dim.  A block that the run begins (its first row is among
-// the run's) is written whole, with zeros in the rows that are not there yet; in
-// others the key rows alone and all of the values, whose 16-byte pieces hold other
-// tokens too, unless the scale rises and all codes are rounded anew.  Read are 512 bytes a
-// token and key head, written 258: prompts of 22,790 tokens, 32 key heads, 171 us where a
-// copy of as many bytes takes 113.  140 registers leave three waves a SIMD; held to 128
-// or 96 they spill (227 and 302 us against 190 in a state before this).
+// Entries as a wave looks at them, one a lane.
+struct Entries {
+  const Write& A;
+  int blocks;
+  __device__ __forceinline__ explicit Entries(const Write& a) : A(a), blocks(a.n_pages * (kPage8 / kBlock8)) {}
+  __device__ __forceinline__ int block_of(int slot) const {
+    const int b = slot >> 5;
+    return b >= 0 && b < blocks ? b : -1;
+  }
+  // Entry i's block; -1: it is skipped, or there is none.
+  __device__ __forceinline__ int look(int64_t i, int& slot, int& row) const {
+    const bool in = i >= 0 && i < A.n;
+    slot = in ? A.slot[i] : -1;
+    row = in ? (A.src ? A.src[i] : (int)i) : -1;
+    return row >= 0 && row < A.n_src ? block_of(slot) : -1;
+  }
+  // Which of 64 entries from i on have slots in the pool, for kStep such groups that lie
+  // `way` apart: what is skipped may be thousands of entries.
+  static constexpr int kStep = 8;
+  __device__ __forceinline__ void in_pool(int64_t i, int way, uint64_t (&m)[kStep]) const {
+    int slot[kStep];
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      const int64_t at = i + way * u + fc::lane_id();
+      slot[u] = at >= 0 && at < A.n ? A.slot[at] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) m[u] = fc::ballot(block_of(slot[u]) >= 0);
+  }
+  // The first entry from i on whose slot is in the pool, or one past the last.
+  __device__ __forceinline__ int64_t next(int64_t i) const {
+    for (; i < A.n; i += kStep * fc::kWave) {
+      uint64_t m[kStep];
+      in_pool(i, fc::kWave, m);
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (m[u]) return i + fc::kWave * u + __builtin_ctzll(m[u]);
+    }
+    return A.n;
+  }
+  // The block of the last entry before i that is not skipped; -1: there is none.
+  __device__ __forceinline__ int block_before(int64_t i) const {
+    while (i > 0) {
+      uint64_t m[kStep];
+      in_pool(i - fc::kWave, -fc::kWave, m);
+      int u = 0;
+      while (u < kStep && !m[u]) ++u;
+      i -= fc::kWave * u;
+      if (u == kStep) continue;
+      int slot, row;
+      const int b = look(i - fc::kWave + fc::lane_id(), slot, row);
+      const uint64_t live = fc::ballot(b >= 0);
+      if (live) return __builtin_amdgcn_readlane(b, 63 - __builtin_clzll(live));
+      i -= fc::kWave;
+    }
+    return -1;
+  }
+};
+
+// The entries of one block, which follow one another but for skipped ones, are a run; a
+// wave takes a run's keys or values of one head, so that a block has one writer.  It
+// reads the rows, has their largest magnitude by exchange within the wave, and writes
+// codes: key rows as they are, values dim by dim.  A block that the run begins (its
+// first row is among the run's) is written whole, with zeros in the rows that are not
+// there yet; in others the key rows alone and all of the values, whose 16-byte pieces
+// hold other tokens too, unless the scale rises and all codes are rounded anew.  Read are
+// 512 bytes a token and key head, written 258: prompts of 22,790 tokens, 32 key heads,
+// 162 us where a copy of as many bytes takes 113.  104 registers leave four waves a SIMD.
 __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
   const int lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
   const int64_t i0 = A.first + (int64_t)blockIdx.x * kWindow;
-  const int blocks = A.n_pages * (kPage8 / kBlock8);
-  const auto block_at = [&](int64_t i) {  // of entry i; -1: none
-    const int b = A.slot[i] >> 5;
-    return b >= 0 && b < blocks ? b : -1;
-  };
-  const int64_t mine = i0 + lane;
-  const bool in = lane < kWindow && mine < A.n;
-  const int b_mine = in ? block_at(mine) : -1;
-  const int b_before = in && mine > 0 ? block_at(mine - 1) : -1;
-  const uint64_t leads = fc::ballot(b_mine >= 0 && b_mine != b_before);
+  const Entries E(A);
+  // lanes 32 on have the window's entries, the others those before; a run begins where the
+  // last one before that is not skipped is of another block
+  int b_mine, b_before;
+  uint64_t leads;
+  {
+    int slot, row;
+    b_mine = E.look(i0 - kWindow + lane, slot, row);
+    const uint64_t live = fc::ballot(b_mine >= 0), below = live & fc::lanemask_lt();
+    if (!(live >> kWindow)) return;
+    b_before = __shfl(b_mine, below ? 63 - __builtin_clzll(below) : 0);
+    if (!(live << kWindow) && i0 > kWindow) {  // none of those before
+      const int b = E.block_before(i0 - kWindow);
+      if (!below) b_before = b;
+    } else if (!below) {
+      b_before = -1;
+    }
+    leads = fc::ballot(lane >= kWindow && b_mine >= 0 && b_mine != b_before);
+  }
   const int each = 2 * A.Hkv, tasks = (int)__popcll(leads) * each;
   for (int task = (int)blockIdx.y * kWriteWaves + w; task < tasks; task += (int)gridDim.y * kWriteWaves) {
     uint64_t left = leads;
     for (int skip = task / each; skip > 0; --skip) left &= left - 1;
-    const int64_t i = i0 + __builtin_ctzll(left);
+    const int lead = __builtin_ctzll(left), block = __builtin_amdgcn_readlane(b_mine, lead);
     const int part = task % each, is_v = part >= A.Hkv, h = is_v ? part - A.Hkv : part;
-    // the run: up to 32 entries, a lane each
-    const bool could = lane < kBlock8 && i + lane < A.n;
-    const int slot = could ? A.slot[i + lane] : -1;
-    const int64_t row = could ? (A.src ? (int64_t)A.src[i + lane] : i + lane) : -1;
-    const int block = __builtin_amdgcn_readfirstlane(slot) >> 5;
-    const uint64_t others = fc::ballot(lane >= kBlock8 || !could || (slot >> 5) != block);
-    const int run = others ? (int)__builtin_ctzll(others) : kBlock8;
-    const bool there = lane < run && row >= 0 && row < A.n_src;
-    const int t = slot & (kBlock8 - 1);
-    uint32_t have = 0;  // rows of the block that are written
-    {
-      uint32_t bit = there ? 1u << t : 0u;
-#pragma unroll
-      for (int o = 1; o < kBlock8; o <<= 1) bit |= (uint32_t)__shfl_xor((int)bit, o);
-      have = (uint32_t)__builtin_amdgcn_readfirstlane((int)bit);
-    }
-    if (!have) continue;
-    const bool fresh = have & 1u;
-    // where each row of the block comes from: lane t has row t's
+    // The run, 64 entries at a time: where each row of the block comes from (lane t has
+    // row t's), and which are written.
     int from = -1;
-    for (int e = 0; e < run; ++e) {
-      const int te = __builtin_amdgcn_readlane(t, e), re = __builtin_amdgcn_readlane(there ? (int)row : -1, e);
-      if (lane == te && re >= 0) from = re;
+    uint32_t have = 0;
+    for (int64_t i = i0 - kWindow + lead; i < A.n && have != 0xFFFFFFFFu; i = E.next(i)) {
+      int slot, row;
+      const int b = E.look(i + lane, slot, row);
+      const uint64_t others = fc::ballot(b >= 0 && b != block);
+      uint64_t run = fc::ballot(b == block);
+      if (others) run &= (1ull << __builtin_ctzll(others)) - 1;
+      for (; run; run &= run - 1) {
+        const int e = __builtin_ctzll(run);
+        const int te = __builtin_amdgcn_readlane(slot, e) & (kBlock8 - 1), re = __builtin_amdgcn_readlane(row, e);
+        if (lane == te) from = re;
+        have |= 1u << te;
+      }
+      if (others) break;
+      i += fc::kWave;
     }
+    const bool fresh = have & 1u;
     uint8_t* page = A.pool + ((int64_t)(block >> 1) * A.Hkv + h) * kPage8Bytes;
     const int half = block & 1;
     uint8_t* scale = page + fc::kPage8Scales + 2 * is_v + half;

@@ -120,3 +120,15 @@ def test_norm_rotates_as_rope_does():
         assert np.allclose(y[:, h], oracle.rope(n[:, h], pos, 10000.0))
     assert np.allclose((y ** 2).sum(-1), (n ** 2).sum(-1))
     assert np.allclose(o8.norm_rotate(x, None, None, rope_base=0.0)[0], x)
+
+
+def test_writes_pass_over_skipped_entries():
+    """A run of a block's entries is one whatever is skipped inside it."""
+    rng = np.random.default_rng(5)
+    pool = rng.integers(0, 256, (2, 1, o8.PAGE_BYTES)).astype(np.uint8)
+    k, v = _rows(rng, 6, 1, 3.0), _rows(rng, 6, 1)
+    k[3] *= 100
+    for slot, src in (([0, -1, 1, 2], None), ([0, 128, 1, 2], None), ([0, 64, 1, 2], [0, -1, 2, 3]), ([0, 2, 1, 2], [0, 6, 2, 3])):
+        src = np.arange(4) if src is None else np.array(src)
+        want = o8.write(pool, k, v, [0, 1, 2], [0, 2, 3])
+        assert np.array_equal(o8.write(pool, k, v, slot, src), want)

@@ -146,3 +146,78 @@ def test_weights_of_calls_without_rows(H, Hkv, lens, adds, rows, entries):
         torch.cuda.synchronize()
         assert torch.equal(again, got), i
         del busy
+
+
+# ------------------------------------------------------------------ write --
+
+@pytest.mark.parametrize("gap", [1, 2, 31, 32, 33, 63, 64, 65, 200, 600, 5000])
+@pytest.mark.parametrize("kind", ["slots", "rows", "slots and rows", "a block's first slot", "another block's"])
+def test_skipped_entries_inside_a_block(gap, kind):
+    """Entries of one block with skipped ones among them - outside the pool, of a row that
+    is not there, or both, one or thousands - are one run, wherever it begins and ends."""
+    rng = np.random.default_rng(gap)
+    Hkv, n_pages = 3, 6
+    say(f"skipped entries, {gap} of {kind}")
+    for first in (0, 5):                                       # the block's first row is written, or not
+        for lead in (0, 1, 29, 31, 32, 40, 70):                # entries of other blocks before it
+            rows = first + rng.permutation(32 - first)[:rng.integers(2, 33 - first)]
+            if first == 0 and lead % 2:
+                rows = rows[::-1]
+            at = np.sort(rng.integers(0, len(rows) + 1, 3))    # where skipped ones lie
+            slot, live = [64 + x for x in range(32)][:lead] + [128 + x for x in range(lead - 32)], []
+            live += [True] * len(slot)
+            for i, t in enumerate(rows):
+                for _ in range(int((at == i).sum())):
+                    slot += [-7] * gap
+                    live += [False] * gap
+                slot.append(32 + int(t))
+                live.append(True)
+            slot += [-1] * (gap if lead % 3 else 0) + [192, 193]
+            live += [False] * (gap if lead % 3 else 0) + [True, True]
+            slot, live = np.array(slot), np.array(live)
+            n = len(slot)
+            src, bad = rng.integers(0, 100, n), ~live
+            if kind == "slots":
+                slot[bad] = rng.choice([-1, -2 ** 31, 2 ** 31 - 1, 64 * n_pages], bad.sum())
+            else:
+                src[bad] = rng.choice([-1, 100, -2 ** 31, 2 ** 31 - 1], bad.sum())
+                if kind == "slots and rows":
+                    slot[bad] = rng.choice([-1, 33, 64 * n_pages + 5], bad.sum())
+                elif kind == "a block's first slot":
+                    slot[bad] = 32
+                elif kind == "another block's":
+                    slot[bad] = rng.choice([5, 64, 300], bad.sum())
+                else:
+                    slot[bad] = 32 + rng.integers(0, 32, bad.sum())
+            k, v = bf16(rng, 100, Hkv, D), bf16(rng, 100, Hkv, D, scale=30.0)
+            pool = make_pool(rng, n_pages, Hkv)
+            want = o8.write(host(pool), f64(k), f64(v), slot, src)
+            fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(slot.astype(np.int32)), src=dev(src.astype(np.int32)))
+            same_pool(pool, want, (first, lead))
+
+
+def test_skipped_entries_of_whole_calls():
+    """A padded batch: every sequence's rows in a place of their own, most of them skipped;
+    calls of nothing but skipped entries; rows that follow one another without src."""
+    rng = np.random.default_rng(3)
+    B, R, Hkv, n_pages = 40, 65, 2, 60
+    pool = make_pool(rng, n_pages, Hkv)
+    slot = np.full((B, R), -1)
+    for b in range(B):
+        on = np.sort(rng.permutation(R)[:rng.integers(0, 9)])
+        slot[b, on] = 64 * b + 30 + np.arange(len(on)) - (28 if b % 3 == 0 else 0)
+    slot = slot.reshape(-1)
+    k, v = bf16(rng, B * R, Hkv, D), bf16(rng, B * R, Hkv, D, scale=20.0)
+    say("skipped entries of a padded batch")
+    want = o8.write(host(pool), f64(k), f64(v), slot)
+    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(slot.astype(np.int32)))
+    same_pool(pool, want)
+    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), torch.full((100_000,), -1, dtype=torch.int32, device="cuda"))
+    same_pool(pool, want)
+    say("skipped entries, a hundred thousand around each of a few")
+    slot = np.full(400_000, -1)
+    slot[[7, 100_000, 200_001, 200_002, 399_999]] = [64, 70, 65, 130, 128]
+    src = rng.integers(0, B * R, len(slot))
+    want = o8.write(host(pool), f64(k), f64(v), slot, src)
+    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(slot.astype(np.int32)), src=dev(src.astype(np.int32)))
+    same_pool(pool, want)
