@@ -232,10 +232,11 @@ struct Tile {
 // rounding and a share of a sum for two, and no maximum: m is the maximum of what the
 // row saw when it was last scaled.  A factor common to a row's weights costs no
 // accuracy, bf16 and fp32 having the same exponents, as long as sums do not overflow:
-// a step adds less than 2^24 times the largest value, and 2^31 tokens are 2^25 steps.
-// A step whose weights add up to 2^24 or more (or to a NaN) is taken again with m
-// raised to its maximum, and so is a row's first.
-constexpr float kMostWeight = 16777216.0f;  // 2^24
+// each of the four lanes that share a row and a page adds less than 2^22 times the
+// largest value, and 2^31 tokens are 2^25 pages: 2^49 in all, so values below 2^78 stay
+// in.  A step in which a lane's weights add up to 2^22 or more (or to a NaN) is taken
+// again with m raised to its maximum, and so is a row's first.
+constexpr float kMostWeight = 4194304.0f;  // 2^22
 
 template <bool kLse, int T>
 __device__ __forceinline__ float weigh(const floatx4 (&s)[T], float scale, float minus_m, bf16x2 (&p)[2 * T], float& x) {

@@ -102,6 +102,34 @@ def test_keys_of_score_minus_infinity_beside_others(R, H, n):
     assert torch.equal(got, want) and got.any() and not torch.isnan(got).any()
 
 
+@pytest.mark.parametrize("q0,q1", [(9.6875, 0.3125), (8.6875, 0.640625)])
+def test_sums_of_large_values_over_the_longest_prefix(q0, q1):
+    """Values just below 2^78 over as many tokens as a table may hold, with weights that
+    are many times a row's first: 1.75 * 2^19 and 1.75 * 2^17 (rounded to bf16) where the
+    first page's are 1.  Their sum reaches 2^128 unless the row is scaled down on its way."""
+    n, value = 2 ** 31 - 65, 1.5 * 2.0 ** 77
+    pages = -(-n // 64)
+    k = torch.zeros((128, 1, D))
+    k[64:, 0, 0], k[64:, 0, 1] = 16, 1
+    pool = torch.zeros((2, 1, fc.FC_PAGE8_HEAD_BYTES), dtype=torch.uint8, device="cuda")
+    fc.fc_paged_byte_write(pool, k.to(BF).cuda(), torch.full((128, 1, D), value).to(BF).cuda(), torch.arange(128, dtype=torch.int32, device="cuda"))
+    # each of a workgroup's eight waves begins with a page of the small weights, in each of
+    # the 128 parts of 2^18 pages that a prefix of this length is cut into
+    table = (torch.arange(pages, dtype=torch.int32, device="cuda") % 2 ** 18 >= 8).int()[None]
+    q = torch.zeros((1, 1, 1, D))
+    q[..., 0], q[..., 1] = q0, q1
+    vt, lse = torch.full((1, 1, 1, D), value).to(BF).cuda(), torch.empty((1, 1, 1), device="cuda")
+    say(f"sums of large values, score {16 * q0 + q1}")
+    got = fc.fc_paged_byte_attention(q.to(BF).cuda(), torch.zeros_like(vt), vt, pool, table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+                                     max_len=n, lse=lse)
+    # a wave adds 2^15 times to a sum, 2^-24 of it off each time, above the line and below
+    # it; the result is bf16
+    assert ((got.float().double() - value).abs() <= (2.0 ** -8 + 2.0 ** -8) * value).all()
+    few = 128 * 8 * 64
+    want = np.log((n - few) * np.exp((16 * q0 + q1) / np.sqrt(D)) + few + 1)
+    assert abs(float(lse) - want) <= 2.0 ** -9 + 2.0 ** -20
+
+
 # ---------------------------------------------------------------- weights --
 
 @pytest.mark.parametrize("H,Hkv,lens,adds", [(4, 2, [70, 5, 90, 0], [9, 0, -20, 1]), (1, 1, [0], [1]), (8, 2, [30], [300])])
