@@ -659,8 +659,9 @@ fc_status fc_paged_attention(const uint16_t* q, int64_t q_stride, const uint16_t
  * pass: what a cache is written from and attended with where a token's place in
  * it is not its position (fc_paged_byte_evict), and with rope_base 0 for the 4-bit
  * cache too.  Per head of D values y = x / sqrt(mean(x^2) + eps) * w, then the
- * pair (d, d + D/2) turns by pos[i] * rope_base^(-2d/D).  fp32 throughout, angles
- * reduced in double precision, one rounding to bf16.
+ * pair (d, d + D/2) turns by pos[i] * rope_base^(-2d/D).  fp32 throughout, heads whose
+ * squares do not fit it scaled by a power of two first; angles reduced in double
+ * precision, sines and cosines within 2^-18; one rounding to bf16.
  *
  * q [n][H][D], k [n][Hkv][D] bf16, rows q_stride and k_stride elements apart
  * (multiples of 8, at least the row's length; slices of a fused projection need

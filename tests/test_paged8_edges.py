@@ -130,6 +130,34 @@ def test_sums_of_large_values_over_the_longest_prefix(q0, q1):
     assert abs(float(lse) - want) <= 2.0 ** -9 + 2.0 ** -20
 
 
+# ------------------------------------------------------------------- norm --
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+@pytest.mark.parametrize("n", [1, 40])
+def test_norms_at_both_ends_of_the_range(n, eps):
+    """Heads whose squares, or their sum, are more than fp32 holds or less: the result is
+    what the formula gives, whatever the size of the numbers."""
+    rng = np.random.default_rng(n)
+    powers = np.array([126, 100, 66, 64, 60, 0, -40, -45, -50, -64, -70, -100, -126, -130])
+    say(f"norms at both ends n={n} eps={eps}")
+    q = torch.from_numpy(rng.uniform(0.5, 1.9, (n, len(powers), D)) * rng.choice([-1, 1], (n, len(powers), D)) *
+                         2.0 ** powers[:, None]).to(BF)
+    k = q.flip(1).clone()
+    k[..., 5::9] = 0                                # a few alone
+    k[:, :, 64:] *= 2.0 ** -20
+    w = [1 + bf16(rng, D, scale=0.3) for _ in "qk"]
+    pos = rng.integers(0, 100_000, n).astype(np.int32)
+    _norm(q, k, *w, pos, eps=eps)
+    _norm(q, k, *w, None, eps=eps, rope_base=0.0)
+    odd = q.clone()                                 # what is not finite leaves no other head
+    odd[0, 0, 3], odd[0, 1, 70], odd[0, -1, 9], odd[0, 3] = INF, -INF, float("nan"), 0
+    got = f64(fc.fc_norm_rotate(odd.cuda(), None, w[0].cuda(), None, dev(pos), eps=eps)[0])
+    rest = f64(fc.fc_norm_rotate(q.cuda(), None, w[0].cuda(), None, dev(pos), eps=eps)[0])
+    assert np.array_equal(got[1:], rest[1:]) and np.array_equal(got[0, 4:-1], rest[0, 4:-1])
+    assert np.isnan(got[0, 0, [3, 67]]).all() and np.isnan(got[0, 1, [6, 70]]).all() and np.isnan(got[0, -1]).all()
+    assert np.isnan(got[0, 3]).all() if eps == 0 else (got[0, 3] == 0).all()
+
+
 # ---------------------------------------------------------------- weights --
 
 @pytest.mark.parametrize("H,Hkv,lens,adds", [(4, 2, [70, 5, 90, 0], [9, 0, -20, 1]), (1, 1, [0], [1]), (8, 2, [30], [300])])
