@@ -1008,8 +1008,8 @@ def fc_paged_byte_read(pool: torch.Tensor, slot: torch.Tensor, out=None, stream=
         if out is None:
             out = on.empty(shape, torch.bfloat16), on.empty(shape, torch.bfloat16)
         k, v = out
-        _check("fc_paged_byte_read", lib().fc_paged_byte_read(_ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, _ptr(slot), n,
-                                                      _ptr(k), _ptr(v), on.raw()))
+        _check("fc_paged_byte_read", lib().fc_paged_byte_read(
+            _ptr(pool), n_pages, Hkv, FC_TREE_ATTN_HEAD_DIM, _ptr(slot), n, _ptr(k), _ptr(v), on.raw()))
     return k, v
 
 

@@ -186,16 +186,21 @@ struct Work {
     for (int u = 0; u < 4 * T; ++u) bits |= (uint32_t)(m[u] == 1 && j0 + 16 * (u / 4) + 4 * lg + u % 4 < n) << u;
     return bits;
   }
-  // Whether any page of this part is there.
-  __device__ __forceinline__ bool any_page(const Args& A) const {
+  // Whether query row r, of the wave's 16, may see any key of this part.
+  __device__ __forceinline__ bool sees(const Args& A, int r) const {
     const int lane = fc::lane_id();
     const int32_t* of = A.table + (int64_t)b * A.max_pages;
-    bool any = false;
-    for (int pg = pg0; pg < pg1 && !any; pg += fc::kWave) {
+    bool page = false;
+    for (int pg = pg0; pg < pg1 && !page; pg += fc::kWave) {
       const int id = pg + lane < pg1 ? of[pg + lane] : -1;
-      any = fc::ballot(id >= 0 && id < A.n_pages) != 0;
+      page = fc::ballot(id >= 0 && id < A.n_pages) != 0;
     }
-    return any;
+    int rows = 0;
+    if (tree)
+      for (int j0 = 0; j0 < n; j0 += 16) rows |= (int)allowed<1>(A, r, j0, lane >> 4);
+    rows |= __shfl_xor(rows, 16);
+    rows |= __shfl_xor(rows, 32);
+    return page || rows != 0;
   }
 };
 
@@ -505,16 +510,13 @@ __device__ __forceinline__ void take(Row& r, float& m, const float* rec) {
 // (an infinity in its query, a product past fp32).  Those are no keys beside others, but
 // alone their softmax is a NaN: such a row's maximum is the lowest number, which any
 // other key's weights leave without effect when rows are put together.  Whether it saw
-// one is looked for here, where it is rare; of the tree's rows `saw` has the lane's.
+// one is looked for here, where that is rare: kept from the loops over keys, it would
+// take registers there (48 trees of 65 rows 143 us, 141 so).
 constexpr float kLowest = -3.402823466e38f;
-template <typename Saw>
-__device__ __forceinline__ float maximum_of(const Args& A, const Work& W, const Row& r, float m, int row, Saw saw) {
+__device__ __forceinline__ float maximum_of(const Args& A, const Work& W, const Row& r, float m, int row) {
   const bool nothing = row < W.M && r.l == 0.0f;
   if (!__any(nothing)) return m;
-  int sees = saw();
-  sees |= __shfl_xor(sees, 16);
-  sees |= __shfl_xor(sees, 32);
-  sees |= W.any_page(A);
+  const bool sees = W.sees(A, row);
   return nothing && sees ? kLowest : m;
 }
 // 1 over a row's sum: 0 for a row without a key; infinite, so that its outputs of 0
@@ -683,7 +685,7 @@ __global__ void __launch_bounds__(kAloneWaves* fc::kWave, 2) k_paged8_attn_alone
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int row = kTile * i + lc;
-    m[i] = maximum_of(A, W, tile[i].row, m[i], row, [&] { return W.tree && W.allowed<T>(A, row, 0, lg) != 0; });
+    m[i] = maximum_of(A, W, tile[i].row, m[i], row);
     if (row < W.M) finish(A, W, tile[i].row, m[i], row);
   }
 }
@@ -880,7 +882,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
   else if (mine == 1) group_pages<1, kLse>(pages, s_x, here0, here1, word0, word1, tile);
   else group_pages<0, kLse>(pages, s_x, here0, here1, word0, word1, tile);
 
-  bool saw[kWaveTiles] = {false, false};  // whether the lane's rows saw any of the tree's
   if (W.tree) {
     // 64 of its rows at a time: what is read of them, and which of them each query row
     // may see, is asked for together, the next ones' before these are used
@@ -893,7 +894,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
 #pragma unroll
       for (int i = 0; i < kWaveTiles; ++i) {
         see[i] = W.allowed<kKTiles>(A, row[i], j0, lg);
-        saw[i] |= see[i] != 0;
       }
       if (tid < 2) s_bad[tid] = 0;
       __syncthreads();
@@ -913,7 +913,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
 #pragma unroll
   for (int i = 0; i < kWaveTiles; ++i) {
     whole(tile[i].row);
-    const float m = maximum_of(A, W, tile[i].row, tile[i].row.m(), row[i], [&] { return saw[i]; });
+    const float m = maximum_of(A, W, tile[i].row, tile[i].row.m(), row[i]);
     if (row[i] < W.M) finish(A, W, tile[i].row, m, row[i]);
   }
 }
@@ -1018,6 +1018,12 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   s.alone = s.tiles > kWaveTiles ? 0 : pages >= 64 || wgs <= kCus ? 8 : 4;
   const int64_t slots = s.alone == 8 ? kCus : 2 * kCus;  // workgroups at once
   int64_t each = s.alone ? s.alone : 4;
+  // As many parts as fill the card once, below 64 pages rounded down, as beginning a part
+  // and joining it cost as much as it takes over there, from 64 on up, so that the longest
+  // of different lengths are cut (32 heads on 8, lengths from an eighth of the given one:
+  // 20 trees of 65 rows over 1,000 tokens 50 us rounded down, 74 up, 20 over 2,048 87 and
+  // 99; over 8,192 244 and 232, 14 over 8,192 208 and 168; 48 single tokens over 2,048 26
+  // and 32, 25 over 8,192 54 and 55; all of one length, 20 trees over 8,192 297 and 319).
   int64_t parts = (slots + (pages < 64 ? 0 : wgs - 1)) / wgs;
   if (parts > kMostParts) parts = kMostParts;
   const int64_t fit = (pages + each - 1) / each;
