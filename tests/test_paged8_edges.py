@@ -61,6 +61,34 @@ def test_rows_whose_scores_are_all_minus_infinity(R, H, Hkv, lens, value):
     attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=table, q=q, kt=kt, max_len=max(lens))
 
 
+@pytest.mark.parametrize("R,H,Hkv,lens", [(1, 8, 2, [130, 0]), (9, 4, 1, [64, 33]), (30, 1, 1, [100]), (1, 4, 1, [3001]),
+                                          (20, 2, 1, [2500]), (65, 4, 2, [100, 0]), (65, 2, 1, [2049])],
+                         ids=lambda x: str(x).replace(" ", ""))
+@pytest.mark.parametrize("side", [1, 0])
+def test_infinities_in_queries_and_keys(R, H, Hkv, lens, side):
+    """The same with scores of +infinity alone or of both signs, in queries and in the
+    tree's keys: NaN in the rows that have or see them, nothing elsewhere."""
+    rng = np.random.default_rng(R + H + sum(lens) + side)
+    B, dim = len(lens), 7
+    pool = _one_sided(rng, 5, Hkv, dim, 1) if side else make_pool(rng, 5, Hkv)
+    q, kt = bf16(rng, B, R, H, D), bf16(rng, B, R, Hkv, D)
+    if side:
+        kt[..., dim] = kt[..., dim].abs() + 1
+    table = rng.integers(0, 5, (B, -(-max(lens) // 64))).astype(np.int32)
+    one = q.clone()
+    one[:, R // 2, H - 1, dim], one[:, 0, 0, dim] = INF, INF
+    say(f"infinities in queries R={R} H={H} lens={lens} side={side}")
+    t = trees(rng, B, R)
+    got = attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=table, q=one, kt=kt, max_len=max(lens))
+    assert np.isnan(got[0, R // 2, H - 1]).all() and np.isnan(got).any(-1).sum() <= 2 * B
+    high = kt.clone()                               # q's largest dims meet an infinity of their sign
+    q[..., dim] = q[..., dim].abs() + 0.5
+    high[:, R // 2, :, dim] = INF
+    got = attend(rng, B, R, H, Hkv, lens, t, pool=pool, table=table, q=q, kt=high, max_len=max(lens))
+    sees = t["mask"][:, :, R // 2] == 1
+    assert (np.isnan(got).all((2, 3)) == sees).all() and not np.isnan(got[~sees]).any()
+
+
 @pytest.mark.parametrize("R,H,n", [(1, 2, 300), (1, 2, 3001), (20, 1, 3001), (20, 2, 3001), (65, 2, 300), (65, 1, 2500)])
 def test_keys_of_score_minus_infinity_beside_others(R, H, n):
     """Pages, tree rows, or both whose scores are -infinity count for nothing beside keys
