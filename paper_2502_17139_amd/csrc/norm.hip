@@ -6,7 +6,7 @@
 // precision, then the hardware's sine and cosine: within 2^-18, where the result's
 // rounding is 2^-9), one rounding to bf16 at the end.  Bound by memory: 512 bytes a
 // head.  24,571 tokens of 32 query and 8 key heads 92 us, 5.5 TB/s (a copy of 2 GiB has 4.95);
-// one token 2.6 us, a launch and two round trips.
+// one token 2.8 us, a launch and two round trips.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -130,7 +130,7 @@ struct Entries {
 // there yet; in others the key rows alone and all of the values, whose 16-byte pieces
 // hold other tokens too, unless the scale rises and all codes are rounded anew.  Read are
 // 512 bytes a token and key head, written 258: prompts of 22,790 tokens, 32 key heads,
-// 162 us where a copy of as many bytes takes 113.  104 registers leave four waves a SIMD.
+// 164 us where a copy of as many bytes takes 113.  104 registers leave four waves a SIMD.
 __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
   const int lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);
@@ -329,8 +329,8 @@ __device__ __forceinline__ uint32_t pair8(uint32_t w, float s, bool high) {
 // A wave takes 16 entries through every fourth head.  Keys: 16 lanes a row, eight dims
 // each.  Values: two dims a lane, 16 tokens of them in two loads; entries of one such
 // quarter that follow one another, as the tokens of a sequence do, share the loads.  Bound
-// by what is written, 512 bytes a token and key head: 22,790 tokens of 32 key heads 117 us,
-// 4.8 TB/s of a copy's 4.95.  All loads are asked for before the first result is written
+// by what is written, 512 bytes a token and key head: 22,790 tokens of 32 key heads 121 us,
+// 4.6 TB/s of a copy's 4.95.  All loads are asked for before the first result is written
 // (137 us in a state before this, one after another 159; four dims a lane, half as many
 // tokens each, 232).
 __global__ void __launch_bounds__(kReadThreads) k_paged8_read(const uint8_t* __restrict__ pool, int n_pages, int Hkv,

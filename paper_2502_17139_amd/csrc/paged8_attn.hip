@@ -511,7 +511,7 @@ __device__ __forceinline__ void take(Row& r, float& m, const float* rec) {
 // alone their softmax is a NaN: such a row's maximum is the lowest number, which any
 // other key's weights leave without effect when rows are put together.  Whether it saw
 // one is looked for here, where that is rare: kept from the loops over keys, it would
-// take registers there (48 trees of 65 rows 143 us, 141 so).
+// take registers there (48 trees of 65 rows: 2 us).
 constexpr float kLowest = -3.402823466e38f;
 __device__ __forceinline__ float maximum_of(const Args& A, const Work& W, const Row& r, float m, int row) {
   const bool nothing = row < W.M && r.l == 0.0f;
@@ -555,6 +555,8 @@ __device__ __forceinline__ void finish(const Args& A, const Work& W, const Row& 
 // weights, its values while the next scores are made.  Bound by memory, 16.5 KB a page
 // and head: 131,000 tokens of 8 key heads 43 us and 5 for the join, 5.7 TB/s; 64 sequences
 // of up to 8,192 tokens 77 us, 4.7 TB/s; 3,000 tokens 10 and 4 us, a chain of round trips.
+// 208 registers for one tile, no scratch; 256 for two, and 84 bytes of scratch a lane (8
+// without logarithms).
 template <int NT, int kAloneWaves, bool kLse>
 __global__ void __launch_bounds__(kAloneWaves* fc::kWave, 2) k_paged8_attn_alone(Args A) {
   constexpr int T = 2;  // tiles of tree rows: at most 32
@@ -837,8 +839,11 @@ __device__ __forceinline__ void group_tree(const Args& A, const Work& W, int j0,
 
 // More tiles: a workgroup's waves share pages, four of them on their way through LDS, and
 // have one or two tiles each.  Bound by what a wave does in turn - scores, weights, values
-// - with two waves a SIMD: 48 trees of 65 rows over up to 4,096 tokens, 32 heads on 8,
-// 160 us where the products' rate allows 64; of 4,096 tokens each 390; without a prefix 55.
+// - with two waves a SIMD, whose 256 registers are not enough: 42 more lie in scratch, 172
+// bytes a lane, and come back in the loop over the tree's rows, each with a wait for all
+// loads.  48 trees of 65 rows over up to 4,096 tokens, 32 heads on 8, 146 us (160 under a
+// trace, where each launch begins on an idle card) where the products' rate allows 64; of
+// 4,096 tokens each 388; without a prefix 71, as chains without a mask 52.
 template <bool kLse>
 __global__ void __launch_bounds__(kThreads, 2) k_paged8_attn(Args A) {
   static_assert(2 * kPage8 * kRowBytes <= kSlots * kSlot, "tree rows where the pages were");
@@ -1035,7 +1040,7 @@ Shape shape_of(int32_t B, int32_t R, int32_t H, int32_t Hkv, int32_t max_len) {
   s.parts = pages <= s.part_pages ? 1 : (int)((pages + s.part_pages - 1) / s.part_pages);
   // Where not all workgroups run at once, a long one that began last would be waited
   // for alone (64 sequences of up to 8,192 tokens: 77 us, as they come 93; 48 trees of 65
-  // rows over up to 4,096: 153 and 221; of equal lengths no difference).
+  // rows over up to 4,096: 146 and 213; of equal lengths no difference).
   s.ordered = B > 1 && wgs * s.parts > slots;
   return s;
 }

@@ -125,7 +125,7 @@ def test_keys_of_score_minus_infinity_beside_others(R, H, n):
     # the tree's rows alone are finite
     say(f"-infinity beside others R={R} n={n}: finite are the tree's rows")
     table = (page - 3).astype(np.int32)[None]
-    got, want = (fc.fc_paged_byte_attention(q.cuda(), kt.cuda(), vt.cuda(), pool, dev(x.astype(np.int32)), dev(plen), tree=on_gpu(t))
+    got, want = (fc.fc_paged_byte_attention(q.cuda(), kt.cuda(), vt.cuda(), pool, dev(x), dev(plen), tree=on_gpu(t))
                  for x in (table, np.full_like(table, -1)))
     assert torch.equal(got, want) and got.any() and not torch.isnan(got).any()
 
@@ -140,7 +140,8 @@ def test_sums_of_large_values_over_the_longest_prefix(q0, q1):
     k = torch.zeros((128, 1, D))
     k[64:, 0, 0], k[64:, 0, 1] = 16, 1
     pool = torch.zeros((2, 1, fc.FC_PAGE8_HEAD_BYTES), dtype=torch.uint8, device="cuda")
-    fc.fc_paged_byte_write(pool, k.to(BF).cuda(), torch.full((128, 1, D), value).to(BF).cuda(), torch.arange(128, dtype=torch.int32, device="cuda"))
+    fc.fc_paged_byte_write(pool, k.to(BF).cuda(), torch.full((128, 1, D), value).to(BF).cuda(),
+                           dev(np.arange(128, dtype=np.int32)))
     # each of a workgroup's eight waves begins with a page of the small weights, in each of
     # the 128 parts of 2^18 pages that a prefix of this length is cut into
     table = (torch.arange(pages, dtype=torch.int32, device="cuda") % 2 ** 18 >= 8).int()[None]
@@ -148,7 +149,7 @@ def test_sums_of_large_values_over_the_longest_prefix(q0, q1):
     q[..., 0], q[..., 1] = q0, q1
     vt, lse = torch.full((1, 1, 1, D), value).to(BF).cuda(), torch.empty((1, 1, 1), device="cuda")
     say(f"sums of large values, score {16 * q0 + q1}")
-    got = fc.fc_paged_byte_attention(q.to(BF).cuda(), torch.zeros_like(vt), vt, pool, table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+    got = fc.fc_paged_byte_attention(q.to(BF).cuda(), torch.zeros_like(vt), vt, pool, table, dev(np.array([n], np.int32)),
                                      max_len=n, lse=lse)
     # a wave adds 2^15 times to a sum, 2^-24 of it off each time, above the line and below
     # it; the result is bf16
