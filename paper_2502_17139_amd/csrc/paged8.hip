@@ -66,57 +66,106 @@ __device__ __forceinline__ Scaled rescale(uint32_t top, uint32_t byte, bool fres
 // Entries as a wave looks at them, one a lane.
 struct Entries {
   const Write& A;
-  int blocks;
-  __device__ __forceinline__ explicit Entries(const Write& a) : A(a), blocks(a.n_pages * (kPage8 / kBlock8)) {}
-  __device__ __forceinline__ int block_of(int slot) const {
-    const int b = slot >> 5;
-    return b >= 0 && b < blocks ? b : -1;
-  }
+  __device__ __forceinline__ explicit Entries(const Write& a) : A(a) {}
   // Entry i's block; -1: it is skipped, or there is none.
   __device__ __forceinline__ int look(int64_t i, int& slot, int& row) const {
     const bool in = i >= 0 && i < A.n;
     slot = in ? A.slot[i] : -1;
     row = in ? (A.src ? A.src[i] : (int)i) : -1;
-    return row >= 0 && row < A.n_src ? block_of(slot) : -1;
+    return row >= 0 && row < A.n_src && (uint32_t)slot < slots() ? slot / kBlock8 : -1;
   }
-  // Which of 64 entries from i on have slots in the pool, for kStep such groups that lie
-  // `way` apart: what is skipped may be thousands of entries.
-  static constexpr int kStep = 8;
-  __device__ __forceinline__ void in_pool(int64_t i, int way, uint64_t (&m)[kStep]) const {
-    int slot[kStep];
+  // What is skipped may be thousands of entries (those behind a plan's last token), so
+  // slots are passed 16 bytes a lane, 2,048 at a time, by one comparison of their least
+  // as unsigned numbers: 65,536 entries of which the first 400 are placed 48 us, 51 in a
+  // state that did not look for more of a run behind them.  (4 bytes a lane, 512 at a time:
+  // 321; 16 bytes with a comparison for each slot: 129.)
+  static constexpr int kLoads = 8, kPiece = 4 * fc::kWave, kStep = kLoads * kPiece;
+  struct Pieces {
+    uint4 v[kLoads];
+    // The entries at (first + u * way + 4 lane) .. + 3 of [lo, hi), whole ones.
+    __device__ __forceinline__ Pieces(const int32_t* slot, int64_t first, int way, int64_t lo, int64_t hi) {
 #pragma unroll
-    for (int u = 0; u < kStep; ++u) {
-      const int64_t at = i + way * u + fc::lane_id();
-      slot[u] = at >= 0 && at < A.n ? A.slot[at] : -1;
+      for (int u = 0; u < kLoads; ++u) {
+        const int64_t at = first + u * way + 4 * fc::lane_id();
+        v[u] = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (at >= lo && at < hi) v[u] = *(const uint4*)(slot + at);
+      }
     }
+    __device__ __forceinline__ static uint32_t least(uint32_t a, uint32_t b) { return a < b ? a : b; }
+    __device__ __forceinline__ uint32_t least(int u) const { return least(least(v[u].x, v[u].y), least(v[u].z, v[u].w)); }
+    // Whether any is below `slots`.
+    __device__ __forceinline__ bool any(uint32_t slots) const {
+      uint32_t m = least(0);
 #pragma unroll
-    for (int u = 0; u < kStep; ++u) m[u] = fc::ballot(block_of(slot[u]) >= 0);
-  }
-  // The first entry from i on whose slot is in the pool, or one past the last.
+      for (int u = 1; u < kLoads; ++u) m = least(m, least(u));
+      return fc::ballot(m < slots) != 0;
+    }
+    // The first such u, then the first or last such lane's bits.
+    __device__ __forceinline__ int find(uint32_t slots, bool last, int& lane, int& bits) const {
+      int at = 0;
+#pragma unroll
+      for (int u = kLoads - 1; u >= 0; --u)
+        if (const uint64_t m = fc::ballot(least(u) < slots)) {
+          at = u;
+          lane = last ? 63 - __builtin_clzll(m) : __builtin_ctzll(m);
+          bits = __builtin_amdgcn_readlane((int)(v[u].x < slots) | (int)(v[u].y < slots) << 1 | (int)(v[u].z < slots) << 2 |
+                                               (int)(v[u].w < slots) << 3, lane);
+        }
+      return at;
+    }
+  };
+  __device__ __forceinline__ uint32_t slots() const { return (uint32_t)A.n_pages * kPage8; }
+  __device__ __forceinline__ int behind_line(int64_t i) const { return (int)((uintptr_t)(A.slot + i) >> 2) & 3; }
+  // The first entry from i on whose slot is in the pool, or one past the last; i >= 3.
   __device__ __forceinline__ int64_t next(int64_t i) const {
-    for (; i < A.n; i += kStep * fc::kWave) {
-      uint64_t m[kStep];
-      in_pool(i, fc::kWave, m);
-#pragma unroll
-      for (int u = 0; u < kStep; ++u)
-        if (m[u]) return i + fc::kWave * u + __builtin_ctzll(m[u]);
+    const int64_t end = A.n - behind_line(A.n);  // of whole pieces; up to three entries behind them
+    const int64_t mine = end + fc::lane_id();
+    const uint32_t rest = mine >= i && mine < A.n ? (uint32_t)A.slot[mine] : ~0u;
+    const int skip = behind_line(i);
+    for (int64_t x = i - skip; x < end; x += kStep) {
+      Pieces p(A.slot, x, kPiece, x, end);
+      if (x < i && fc::lane_id() == 0) {  // the first piece begins before i
+        p.v[0].x = ~0u;
+        if (skip > 1) p.v[0].y = ~0u;
+        if (skip > 2) p.v[0].z = ~0u;
+      }
+      if (!p.any(slots())) continue;
+      int lane = 0, bits = 0;
+      const int u = p.find(slots(), false, lane, bits);
+      return x + u * kPiece + 4 * lane + __builtin_ctz(bits);
     }
-    return A.n;
+    const uint64_t m = fc::ballot(rest < slots());
+    return m ? end + __builtin_ctzll(m) : A.n;
+  }
+  // The last entry before i whose slot is in the pool, or -1; i + 3 <= n.
+  __device__ __forceinline__ int64_t last(int64_t i) const {
+    const int64_t begin = -behind_line(0) & 3;  // of whole pieces; up to three entries ahead of them
+    const uint32_t rest = fc::lane_id() < begin && fc::lane_id() < i ? (uint32_t)A.slot[fc::lane_id()] : ~0u;
+    const int keep = behind_line(i);
+    for (int64_t y = i + (-keep & 3); y > begin; y -= kStep) {
+      Pieces p(A.slot, y - kPiece, -kPiece, begin, y);
+      if (y > i && fc::lane_id() == fc::kWave - 1) {  // the first piece ends behind i
+        p.v[0].w = ~0u;
+        if (keep < 3) p.v[0].z = ~0u;
+        if (keep < 2) p.v[0].y = ~0u;
+      }
+      if (!p.any(slots())) continue;
+      int lane = 0, bits = 0;
+      const int u = p.find(slots(), true, lane, bits);
+      return y - (u + 1) * kPiece + 4 * lane + 31 - __builtin_clz(bits);
+    }
+    const uint64_t m = fc::ballot(rest < slots());
+    return m ? 63 - __builtin_clzll(m) : -1;
   }
   // The block of the last entry before i that is not skipped; -1: there is none.
   __device__ __forceinline__ int block_before(int64_t i) const {
-    while (i > 0) {
-      uint64_t m[kStep];
-      in_pool(i - fc::kWave, -fc::kWave, m);
-      int u = 0;
-      while (u < kStep && !m[u]) ++u;
-      i -= fc::kWave * u;
-      if (u == kStep) continue;
+    for (i = last(i); i >= 0; i = last(i)) {
+      i -= fc::kWave - 1;
       int slot, row;
-      const int b = look(i - fc::kWave + fc::lane_id(), slot, row);
+      const int b = look(i + fc::lane_id(), slot, row);
       const uint64_t live = fc::ballot(b >= 0);
       if (live) return __builtin_amdgcn_readlane(b, 63 - __builtin_clzll(live));
-      i -= fc::kWave;
+      if (i <= 0) break;
     }
     return -1;
   }
@@ -130,7 +179,7 @@ struct Entries {
 // there yet; in others the key rows alone and all of the values, whose 16-byte pieces
 // hold other tokens too, unless the scale rises and all codes are rounded anew.  Read are
 // 512 bytes a token and key head, written 258: prompts of 22,790 tokens, 32 key heads,
-// 164 us where a copy of as many bytes takes 113.  104 registers leave four waves a SIMD.
+// 164 us where a copy of as many bytes takes 113.  112 registers leave four waves a SIMD.
 __global__ void __launch_bounds__(kWriteThreads) k_paged8_write(Write A) {
   const int lane = fc::lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / fc::kWave);

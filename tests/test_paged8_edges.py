@@ -244,7 +244,7 @@ def test_skipped_entries_inside_a_block(gap, kind):
     Hkv, n_pages = 3, 6
     say(f"skipped entries, {gap} of {kind}")
     for first in (0, 5):                                       # the block's first row is written, or not
-        for lead in (0, 1, 29, 31, 32, 40, 70):                # entries of other blocks before it
+        for lead in (0, 1, 29, 30, 31, 32, 39, 70):            # entries of other blocks before it
             rows = first + rng.permutation(32 - first)[:rng.integers(2, 33 - first)]
             if first == 0 and lead % 2:
                 rows = rows[::-1]
@@ -277,7 +277,10 @@ def test_skipped_entries_inside_a_block(gap, kind):
             k, v = bf16(rng, 100, Hkv, D), bf16(rng, 100, Hkv, D, scale=30.0)
             pool = make_pool(rng, n_pages, Hkv)
             want = o8.write(host(pool), f64(k), f64(v), slot, src)
-            fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(slot.astype(np.int32)), src=dev(src.astype(np.int32)))
+            # at every distance from a 16-byte boundary, with slots of the block ahead and behind
+            at = 4 + lead % 4
+            near = dev(np.concatenate([np.full(at, 40), slot, np.full(8, 41)]).astype(np.int32))[at:at + n]
+            fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), near, src=dev(src.astype(np.int32)))
             same_pool(pool, want, (first, lead))
 
 
@@ -300,9 +303,11 @@ def test_skipped_entries_of_whole_calls():
     fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), torch.full((100_000,), -1, dtype=torch.int32, device="cuda"))
     same_pool(pool, want)
     say("skipped entries, a hundred thousand around each of a few")
-    slot = np.full(400_000, -1)
-    slot[[7, 100_000, 200_001, 200_002, 399_999]] = [64, 70, 65, 130, 128]
-    src = rng.integers(0, B * R, len(slot))
-    want = o8.write(host(pool), f64(k), f64(v), slot, src)
-    fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), dev(slot.astype(np.int32)), src=dev(src.astype(np.int32)))
-    same_pool(pool, want)
+    for at in range(4):
+        slot = np.full(400_000 + at, -1)
+        slot[[7, 100_000, 200_001, 200_002, 399_999]] = [64, 70, 65, 130, 128]
+        near = dev(np.concatenate([np.full(at, 131), slot, np.full(8, 132)]).astype(np.int32))[at:at + len(slot)]
+        src = rng.integers(0, B * R, len(slot))
+        want = o8.write(host(pool), f64(k), f64(v), slot, src)
+        fc.fc_paged_byte_write(pool, k.cuda(), v.cuda(), near, src=dev(src.astype(np.int32)))
+        same_pool(pool, want, at)
